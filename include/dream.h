@@ -64,6 +64,7 @@ typedef enum {
 #define DREAM_MAX_TREE_WIDTH 16     /* children per node / frontier rows of one tree-expansion level */
 #define DREAM_MAX_POOL 1024         /* candidates (root included) dream_tree_finalize ranks */
 #define DREAM_MAX_VISUAL 16384  /* visual tokens per sequence handled by dream_visual_compress */
+#define DREAM_MX_GROUP 32       /* values that share a scale in a cache held in 4 bits          */
 
 /* Attention geometry shared by the three attention-shaped calls. */
 typedef struct {
@@ -325,6 +326,100 @@ int dream_project_rows(const dream_attn_desc *desc, const void *x, int32_t n_row
                        const int32_t *row_index, void *out, void *stream);
 int dream_project_rows_multi(const dream_attn_desc *desc, const dream_proj_job *jobs, int32_t n_jobs,
                              int32_t n_rows, int32_t hidden, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Rotary positions of the rows a step adds, between dream_project_rows and the calls that read them.
+ *   jobs       HOST array of n_jobs <= DREAM_MAX_ROTARY_JOBS (a step's queries and keys in one launch):
+ *              x [B, n_rows, n_heads, D] of desc->dtype (f32 or bf16); out as in dream_project_rows:
+ *              dense [B, n_rows, n_heads, D] where row_base is NULL (x itself is allowed), otherwise
+ *              cache rows row_base[b] + (row_index ? row_index[b, r] : r) of [B, n_heads, s_max, D];
+ *              a destination row outside [0, s_max) is dropped.  Jobs must not write overlapping memory.
+ *   position of row r of sequence b, the first that is given of
+ *     pos[b, r]                       pos nullable [B, n_rows] int32
+ *     pos_base[b] + depth of node r   parent nullable [B, n_rows] int32 (n_rows <= DREAM_MAX_TREE)
+ *     pos_base[b] + r
+ *   inv_freq   [rot_dim / 2] float32: angle of pair i per position, however the model scales it for long
+ *              contexts.  Angles are formed in 64 bits.
+ *   rot_dim    even, <= D: the first rot_dim values of a head turn, the others are copied
+ *   interleaved  0: pairs are (i, i + rot_dim / 2); otherwise (2i, 2i + 1)
+ *   amplitude  multiplies the turned values; 0 selects 1
+ *   y_x = amplitude (x cos a - y sin a),  y_y = amplitude (x sin a + y cos a),  a = position * inv_freq[i]
+ * Positions may be negative (turned rows are turned back by the negated positions).  head_dim even, at
+ * most 512; batch * n_rows at most 2^20.  Uses desc->batch, head_dim, dtype and, with row_base, s_max.
+ * ------------------------------------------------------------------------------------------- */
+#define DREAM_MAX_ROTARY_JOBS 4
+typedef struct dream_rotary_job {
+    const void *x;             /* device */
+    int32_t n_heads;
+    const int32_t *row_base;   /* device, nullable */
+    const int32_t *row_index;  /* device, nullable */
+    void *out;                 /* device */
+} dream_rotary_job;
+int dream_rotary_rows(const dream_attn_desc *desc, const dream_rotary_job *jobs, int32_t n_jobs,
+                      int32_t n_rows, const int32_t *pos, const int32_t *pos_base,
+                      const int32_t *parent, const float *inv_freq, int32_t rot_dim,
+                      int32_t interleaved, float amplitude, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Key/value caches held in 4 bits (0.53 bytes a value instead of 2).
+ *   codes   [B, Hkv, s_max, D / 2] bytes, 16-byte aligned: the value of even index in the low half.  A code
+ *           is a sign and three bits for 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ *   scales  [B, Hkv, s_max, D / DREAM_MX_GROUP] bytes, 8-byte aligned: 2^(byte - 127) for 32 values,
+ *           255 for NaN (whatever the codes).  A value is its code times its scale.
+ *   D in {64, 128, 256}; desc->dtype (f32 or bf16) is that of rows.
+ * dream_mx_append: rows k_rows, v_rows [B, n_rows, Hkv, D], 16-byte aligned, are rounded into the caches at
+ *   rows row_base[b] + (row_index ? row_index[b, r] : r); a destination row outside [0, s_max) is dropped,
+ *   two rows of a call must not have the same one.  The scale of 32 values is the smallest power of two s
+ *   with max|x| <= 7 s, within [2^-125, 2^125] (bytes 2 to 252); a code is the nearest value, the one with an even code where two are.
+ *   A group with a value that is not finite gets scale 255.  batch * n_rows at most 2^20.
+ * dream_mx_read: out [n_caches, B, Hkv, n_rows, D] of desc->dtype, 16-byte aligned, receives what rows row_base[b] + r
+ *   (row_base NULL: r) of the caches stand for, exactly; rows outside [0, s_max) are zeros.  A cache so
+ *   read is a k_cache of s_max = n_rows, as dream_visual_compress and dream_attention_entropy take it.
+ * dream_mx_commit: dream_kv_commit for such caches, with its arguments and its result: row
+ *   prefix_len[b] + j of codes and scales receives the old row prefix_len[b] + accept_path[b][j] for
+ *   j = 0 .. accept_len[b].  DREAM_ERR_UNSUPPORTED if min(path_stride, n_tree) * (D / 32 + 1) exceeds 2048.
+ * codes_host, scales_host are HOST arrays of n_caches DEVICE pointers (K and V of every layer), read
+ * before the call returns.
+ * ------------------------------------------------------------------------------------------- */
+int dream_mx_append(const dream_attn_desc *desc, const void *k_rows, const void *v_rows, int32_t n_rows,
+                    const int32_t *row_base, const int32_t *row_index, void *k_codes, void *k_scales,
+                    void *v_codes, void *v_scales, void *stream);
+int dream_mx_read(const dream_attn_desc *desc, void *const *codes_host, void *const *scales_host,
+                  int32_t n_caches, const int32_t *row_base, int32_t n_rows, void *out, void *stream);
+int dream_mx_commit(const dream_attn_desc *desc, void *const *codes_host, void *const *scales_host,
+                    int32_t n_caches, const int32_t *prefix_len, int32_t n_tree,
+                    const int32_t *accept_path, int32_t path_stride, const int32_t *accept_len,
+                    int32_t *prefix_len_out, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * dream_tree_verify_attn with a sliding window (layers that see a window of positions, streams that keep
+ * their first tokens), over caches of desc->dtype and over caches held in 4 bits.
+ *   window     0: every key, as dream_tree_verify_attn.  Otherwise node i, at position prefix_len[b] +
+ *              depth(i), sees a key it would see only if the key's position is less than `window` back
+ *              (a prefix row's position is its row, a tree node's prefix_len[b] + its depth) or below n_sink
+ *   n_sink     first positions that stay visible to every node; ignored without a window
+ * The other arguments and results are those of dream_tree_verify_attn (n_tree = 1 is plain decoding); a
+ * window needs `parent` beside a tree_mask, for the depths.  A node that sees nothing yields a zero row and
+ * lse = -inf.  What a node does not see does not change its row, whatever it holds: NaN and infinities too.
+ * Rows out of every node's sight are read only where they share a tile of 32 rows with others.  A value that is not finite in a row
+ * a node sees makes that channel of its row NaN or infinite.  q, caches and out 16-byte aligned,
+ * batch * n_q_heads at most 2^20, s_max at most 2^30.
+ * ------------------------------------------------------------------------------------------- */
+size_t dream_window_verify_attn_workspace(const dream_attn_desc *desc, int32_t n_tree, int64_t max_kv_len,
+                                          int32_t window, int32_t n_sink);
+int dream_window_verify_attn(const dream_attn_desc *desc, const void *q, const void *k_cache,
+                             const void *v_cache, const int32_t *prefix_len, int32_t n_tree,
+                             const int32_t *parent, const uint64_t *tree_mask, int32_t window,
+                             int32_t n_sink, int64_t max_kv_len, void *out, float *lse,
+                             void *workspace, size_t workspace_bytes, void *stream);
+size_t dream_mx_verify_attn_workspace(const dream_attn_desc *desc, int32_t n_tree, int64_t max_kv_len,
+                                      int32_t window, int32_t n_sink);
+int dream_mx_verify_attn(const dream_attn_desc *desc, const void *q, const void *k_codes,
+                         const void *k_scales, const void *v_codes, const void *v_scales,
+                         const int32_t *prefix_len, int32_t n_tree, const int32_t *parent,
+                         const uint64_t *tree_mask, int32_t window, int32_t n_sink,
+                         int64_t max_kv_len, void *out, float *lse, void *workspace,
+                         size_t workspace_bytes, void *stream);
 
 /* Host-side check of one parent array: parent_host[0] == -1 and 0 <= parent_host[i] < i.
  * Writes the maximum depth to *max_depth_out (nullable).  DREAM_OK or DREAM_ERR_INVALID_ARG. */

@@ -27,6 +27,8 @@ EXPORTED_SYMBOLS = (
     "dream_tree_expand_workspace", "dream_tree_expand_level", "dream_tree_finalize",
     "dream_attention_entropy_workspace", "dream_attention_entropy", "dream_spec_accept_workspace", "dream_spec_accept",
     "dream_project_rows", "dream_project_rows_multi", "dream_accept_path_static", "dream_accept_static_init",
+    "dream_rotary_rows", "dream_mx_append", "dream_mx_read", "dream_mx_commit", "dream_window_verify_attn_workspace",
+    "dream_window_verify_attn", "dream_mx_verify_attn_workspace", "dream_mx_verify_attn",
 )
 
 
@@ -69,7 +71,8 @@ def load() -> C.CDLL:
             getattr(lib, name)
         for name in ("dream_tree_verify_attn_workspace", "dream_draft_xattn_workspace",
                      "dream_visual_compress_workspace", "dream_accept_path_workspace", "dream_tree_expand_workspace",
-                     "dream_attention_entropy_workspace", "dream_spec_accept_workspace"):
+                     "dream_attention_entropy_workspace", "dream_spec_accept_workspace", "dream_window_verify_attn_workspace",
+                     "dream_mx_verify_attn_workspace"):
             getattr(lib, name).restype = C.c_size_t
         lib.dream_last_error.restype = C.c_char_p
         lib.dream_set_kv_splits.restype = None
@@ -246,6 +249,57 @@ def dream_project_rows_multi(desc: AttnDesc, jobs, n_rows: int, hidden: int, str
     """jobs: sequence of (x, w, n_heads, row_base, row_index, out)."""
     jobs = tuple(jobs)         # (see dream_kv_commit)
     _check(_native().dream_project_rows_multi(desc, jobs, len(jobs), n_rows, hidden, _stream(stream)))
+
+
+def dream_rotary_rows(desc: AttnDesc, jobs, n_rows: int, pos, pos_base, parent, inv_freq, rot_dim: int, interleaved: bool = False,
+                      amplitude: float = 1.0, stream=None) -> None:
+    """jobs: sequence of (x, n_heads, row_base, row_index, out)."""
+    jobs = tuple(tuple(job) for job in jobs)         # (see dream_kv_commit)
+    _check(_native().dream_rotary_rows(desc, jobs, len(jobs), n_rows, pos, pos_base, parent, inv_freq, rot_dim, int(interleaved), amplitude,
+                                       _stream(stream)))
+
+
+def dream_mx_append(desc: AttnDesc, k_rows, v_rows, n_rows: int, row_base, row_index, k_codes, k_scales, v_codes, v_scales, stream=None) -> None:
+    _check(_native().dream_mx_append(desc, k_rows, v_rows, n_rows, row_base, row_index, k_codes, k_scales, v_codes, v_scales, _stream(stream)))
+
+
+def _cache_pairs(codes, scales):
+    codes, scales = tuple(codes), tuple(scales)
+    if len(codes) != len(scales):
+        raise ValueError(f"{len(codes)} caches of codes, {len(scales)} of scales")
+    return codes, scales
+
+
+def dream_mx_read(desc: AttnDesc, codes: Sequence[torch.Tensor], scales: Sequence[torch.Tensor], row_base, n_rows: int, out, stream=None) -> None:
+    codes, scales = _cache_pairs(codes, scales)
+    _check(_native().dream_mx_read(desc, codes, scales, len(codes), row_base, n_rows, out, _stream(stream)))
+
+
+def dream_mx_commit(desc: AttnDesc, codes: Sequence[torch.Tensor], scales: Sequence[torch.Tensor], prefix_len, n_tree: int, accept_path, accept_len,
+                    prefix_len_out=None, stream=None) -> None:
+    codes, scales = _cache_pairs(codes, scales)
+    _check(_native().dream_mx_commit(desc, codes, scales, len(codes), prefix_len, n_tree, accept_path, accept_path.shape[-1], accept_len,
+                                     prefix_len_out, _stream(stream)))
+
+
+def dream_window_verify_attn_workspace(desc: AttnDesc, n_tree: int, max_kv_len: int, window: int, n_sink: int = 0) -> int:
+    return int(load().dream_window_verify_attn_workspace(C.byref(desc), C.c_int32(n_tree), C.c_int64(max_kv_len), C.c_int32(window), C.c_int32(n_sink)))
+
+
+def dream_window_verify_attn(desc: AttnDesc, q, k_cache, v_cache, prefix_len, n_tree: int, parent, tree_mask, window: int, n_sink: int,
+                             max_kv_len: int, out, lse, workspace, stream=None) -> None:
+    _check(_native().dream_window_verify_attn(desc, q, k_cache, v_cache, prefix_len, n_tree, parent, tree_mask, window, n_sink, max_kv_len, out, lse,
+                                              workspace, workspace, _stream(stream)))
+
+
+def dream_mx_verify_attn_workspace(desc: AttnDesc, n_tree: int, max_kv_len: int, window: int = 0, n_sink: int = 0) -> int:
+    return int(load().dream_mx_verify_attn_workspace(C.byref(desc), C.c_int32(n_tree), C.c_int64(max_kv_len), C.c_int32(window), C.c_int32(n_sink)))
+
+
+def dream_mx_verify_attn(desc: AttnDesc, q, k_codes, k_scales, v_codes, v_scales, prefix_len, n_tree: int, parent, tree_mask, window: int, n_sink: int,
+                         max_kv_len: int, out, lse, workspace, stream=None) -> None:
+    _check(_native().dream_mx_verify_attn(desc, q, k_codes, k_scales, v_codes, v_scales, prefix_len, n_tree, parent, tree_mask, window, n_sink,
+                                          max_kv_len, out, lse, workspace, workspace, _stream(stream)))
 
 
 def dream_spec_accept_workspace(batch: int, n_tree: int, vocab: int) -> int:

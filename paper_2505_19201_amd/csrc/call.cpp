@@ -11,6 +11,7 @@
 #include <Python.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <cstdint>
 #include <exception>
 #include <tuple>
@@ -147,12 +148,25 @@ struct Arg<void *const *> {
     }
 };
 
-// A sequence of (x, w, n_heads, row_base, row_index, out).
-template <>
-struct Arg<const dream_proj_job *> {
-    std::vector<dream_proj_job> jobs;
-    const dream_proj_job *value;
-    explicit Arg(PyObject *o)
+// A sequence of jobs, each a sequence of as many fields as the job has.
+inline int32_t number(PyObject *o) { return Arg<int32_t>(o).value; }
+inline void *pointer(PyObject *o) { return Arg<void *>(o).value; }
+inline int32_t *pointer32(PyObject *o) { return static_cast<int32_t *>(pointer(o)); }
+struct ProjFields {     // (x, w, n_heads, row_base, row_index, out)
+    static constexpr const char *what = "a job is (x, w, n_heads, row_base, row_index, out)";
+    static constexpr Py_ssize_t n = 6;
+    static dream_proj_job job(PyObject *const *f) { return {pointer(f[0]), pointer(f[1]), number(f[2]), pointer32(f[3]), pointer32(f[4]), pointer(f[5])}; }
+};
+struct RotaryFields {
+    static constexpr const char *what = "a job is (x, n_heads, row_base, row_index, out)";
+    static constexpr Py_ssize_t n = 5;
+    static dream_rotary_job job(PyObject *const *f) { return {pointer(f[0]), number(f[1]), pointer32(f[2]), pointer32(f[3]), pointer(f[4])}; }
+};
+template <class Job, class Fields>
+struct Jobs {
+    std::vector<Job> jobs;
+    const Job *value;
+    explicit Jobs(PyObject *o)
     {
         PyObject *seq = PySequence_Fast(o, "a sequence of jobs is expected");
         if (!seq)
@@ -167,13 +181,14 @@ struct Arg<const dream_proj_job *> {
                 } job = {PySequence_Tuple(PySequence_Fast_GET_ITEM(seq, i))};
                 if (!job.o)
                     throw Failed();
-                if (PyTuple_GET_SIZE(job.o) != 6) {
-                    PyErr_SetString(PyExc_ValueError, "a job is (x, w, n_heads, row_base, row_index, out)");
+                if (PyTuple_GET_SIZE(job.o) != Fields::n) {
+                    PyErr_SetString(PyExc_ValueError, Fields::what);
                     throw Failed();
                 }
-                auto pointer = [&](int k) { return Arg<void *>(PyTuple_GET_ITEM(job.o, k)).value; };
-                jobs.push_back({pointer(0), pointer(1), Arg<int32_t>(PyTuple_GET_ITEM(job.o, 2)).value, static_cast<int32_t *>(pointer(3)),
-                                static_cast<int32_t *>(pointer(4)), pointer(5)});
+                PyObject *fields[Fields::n];
+                for (Py_ssize_t k = 0; k < Fields::n; k++)
+                    fields[k] = PyTuple_GET_ITEM(job.o, k);
+                jobs.push_back(Fields::job(fields));
             }
         } catch (...) {
             Py_DECREF(seq);
@@ -183,17 +198,162 @@ struct Arg<const dream_proj_job *> {
         value = jobs.data();
     }
 };
+template <>
+struct Arg<const dream_proj_job *> : Jobs<dream_proj_job, ProjFields> {
+    using Jobs::Jobs;
+};
+template <>
+struct Arg<const dream_rotary_job *> : Jobs<dream_rotary_job, RotaryFields> {
+    using Jobs::Jobs;
+};
 
 struct WithoutGil {
     PyThreadState *state = PyEval_SaveThread();
     ~WithoutGil() { PyEval_RestoreThread(state); }
 };
 
+// What the rotary, 4-bit and window calls want of their tensors, checked before the call: the type, at least so many values, and the current device (the one the call is made on).  A
+// None is the library's to accept or refuse, and so are sizes that are not positive.
+void want(PyObject *o, const char *name, __int128 values, at::ScalarType type, at::ScalarType also)
+{
+    if (!THPVariable_Check(o))
+        return;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.is_cuda())
+        return;     // (refused where it is converted)
+    if (t.scalar_type() != type && t.scalar_type() != also) {
+        PyErr_Format(PyExc_ValueError, "%s: %s expected, not %s", name, c10::toString(type), c10::toString(t.scalar_type()));
+        throw Failed();
+    }
+    if ((__int128)t.numel() < values) {
+        PyErr_Format(PyExc_ValueError, "%s: %lld values expected, not %lld", name, (long long)values, (long long)t.numel());
+        throw Failed();
+    }
+    if (t.device() != c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice()) {
+        PyErr_Format(PyExc_ValueError, "%s: is not on the current device", name);
+        throw Failed();
+    }
+}
+void want(PyObject *o, const char *name, __int128 values, at::ScalarType type) { want(o, name, values, type, type); }
+void want_all(PyObject *seq, const char *name, __int128 values, at::ScalarType type)
+{
+    if (!PyTuple_Check(seq))
+        return;     // (the binding hands over tuples)
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(seq); i++)
+        want(PyTuple_GET_ITEM(seq, i), name, values, type);
+}
+
+using Args = PyObject *const *;
+struct Unchecked {
+    static void check(Args) {}
+};
+struct Sizes {
+    dream_attn_desc d = {};
+    at::ScalarType type;
+    __int128 b, hq, hkv, dim, row, cache;      // row: of a cache, in values
+    explicit Sizes(PyObject *o)
+    {
+        const Arg<const dream_attn_desc *> desc(o);
+        d = *desc.value;
+        type = d.dtype == DREAM_F32 ? at::kFloat : at::kBFloat16;
+        b = d.batch; hq = d.n_q_heads; hkv = d.n_kv_heads; dim = d.head_dim;
+        row = b * hkv * d.s_max;
+        cache = row * dim;
+    }
+};
+struct RotaryCheck {
+    static void check(Args a)
+    {
+        const Sizes s(a[0]);
+        const __int128 rows = s.b * number(a[3]), dim = s.dim;
+        want(a[4], "pos", rows, at::kInt);
+        want(a[5], "pos_base", s.b, at::kInt);
+        want(a[6], "parent", rows, at::kInt);
+        want(a[7], "inv_freq", number(a[8]) / 2, at::kFloat);
+        if (!PyTuple_Check(a[1]))
+            return;
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(a[1]); i++) {
+            PyObject *j = PyTuple_GET_ITEM(a[1], i);
+            if (!PyTuple_Check(j) || PyTuple_GET_SIZE(j) != RotaryFields::n)
+                continue;
+            const __int128 heads = number(PyTuple_GET_ITEM(j, 1));
+            want(PyTuple_GET_ITEM(j, 0), "x", rows * heads * dim, s.type);
+            want(PyTuple_GET_ITEM(j, 2), "row_base", s.b, at::kInt);
+            want(PyTuple_GET_ITEM(j, 3), "row_index", rows, at::kInt);
+            want(PyTuple_GET_ITEM(j, 4), "out", (PyTuple_GET_ITEM(j, 2) == Py_None ? rows : s.b * s.d.s_max) * heads * dim, s.type);
+        }
+    }
+};
+struct AppendCheck {
+    static void check(Args a)
+    {
+        const Sizes s(a[0]);
+        const __int128 rows = s.b * number(a[3]);
+        for (int i : {1, 2})
+            want(a[i], "rows", rows * s.hkv * s.dim, s.type);
+        want(a[4], "row_base", s.b, at::kInt);
+        want(a[5], "row_index", rows, at::kInt);
+        for (int i : {6, 8}) {
+            want(a[i], "codes", s.cache / 2, at::kByte);
+            want(a[i + 1], "scales", s.cache / DREAM_MX_GROUP, at::kByte);
+        }
+    }
+};
+struct ReadCheck {
+    static void check(Args a)
+    {
+        const Sizes s(a[0]);
+        want_all(a[1], "codes", s.cache / 2, at::kByte);
+        want_all(a[2], "scales", s.cache / DREAM_MX_GROUP, at::kByte);
+        want(a[4], "row_base", s.b, at::kInt);
+        want(a[6], "out", s.b * s.hkv * s.dim * number(a[5]) * number(a[3]), s.type);
+    }
+};
+struct CommitCheck {
+    static void check(Args a)
+    {
+        const Sizes s(a[0]);
+        want_all(a[1], "codes", s.cache / 2, at::kByte);
+        want_all(a[2], "scales", s.cache / DREAM_MX_GROUP, at::kByte);
+        want(a[4], "prefix_len", s.b, at::kInt);
+        want(a[6], "accept_path", s.b * number(a[7]), at::kInt);
+        want(a[8], "accept_len", s.b, at::kInt);
+        want(a[9], "prefix_len_out", s.b, at::kInt);
+    }
+};
+// MX: positions behind the caches are two further on
+template <bool MX>
+struct WindowCheck {
+    static void check(Args a)
+    {
+        const Sizes s(a[0]);
+        Args r = a + (MX ? 6 : 4);      // prefix_len, n_tree, parent, tree_mask, window, n_sink, max_kv_len, out, lse, workspace
+        const __int128 t = number(r[1]), rows = s.b * t;
+        want(a[1], "q", rows * s.hq * s.dim, s.type);
+        if (MX) {
+            for (int i : {2, 4}) {
+                want(a[i], "codes", s.cache / 2, at::kByte);
+                want(a[i + 1], "scales", s.cache / DREAM_MX_GROUP, at::kByte);
+            }
+        } else {
+            want(a[2], "k_cache", s.cache, s.type);
+            want(a[3], "v_cache", s.cache, s.type);
+        }
+        want(r[0], "prefix_len", s.b, at::kInt);
+        want(r[2], "parent", rows, at::kInt);
+        want(r[3], "tree_mask", rows * ((t + 63) / 64), at::kLong, at::kUInt64);
+        want(r[7], "out", rows * s.hq * s.dim, s.type);
+        want(r[8], "lse", rows * s.hq, at::kFloat);
+        if (THPVariable_Check(r[9]))
+            want(r[9], "workspace", 0, THPVariable_Unpack(r[9]).scalar_type());
+    }
+};
+
 // HOST: position of the host out-parameter, or -1
-template <auto F, int HOST>
+template <auto F, int HOST, class Check = Unchecked>
 struct Entry;
-template <class... A, int (*F)(A...), int HOST>
-struct Entry<F, HOST> {
+template <class... A, int (*F)(A...), int HOST, class Check>
+struct Entry<F, HOST, Check> {
     template <class T, int I>
     using ArgAt = std::conditional_t<I == (int)sizeof...(A) - 1, Stream, std::conditional_t<I == HOST, HostInt, Arg<T>>>;
     template <size_t... I>
@@ -208,6 +368,7 @@ struct Entry<F, HOST> {
         if (n != (Py_ssize_t)sizeof...(A))
             return PyErr_Format(PyExc_TypeError, "%d arguments expected, got %d", (int)sizeof...(A), (int)n);
         try {
+            Check::check(args);
             return PyLong_FromLong(run(args, std::index_sequence_for<A...>{}));
         } catch (const Failed &) {
         } catch (...) {     // torch's own errors (a sparse tensor has no bytes) and the allocator's: nothing may leave a C function
@@ -219,12 +380,16 @@ struct Entry<F, HOST> {
 
 #define ENTRY_HOST(name, host) {#name, (PyCFunction)(void (*)(void))&Entry<&name, host>::call, METH_FASTCALL, nullptr}
 #define ENTRY(name) ENTRY_HOST(name, -1)
+#define ENTRY_CHECKED(name, ...) {#name, (PyCFunction)(void (*)(void))&Entry<&name, -1, __VA_ARGS__>::call, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     ENTRY(dream_tree_verify_attn), ENTRY(dream_draft_xattn), ENTRY_HOST(dream_visual_compress, 14), ENTRY(dream_accept_path), ENTRY(dream_accept_path_static),
     ENTRY(dream_kv_commit), ENTRY(dream_project_rows), ENTRY(dream_project_rows_multi), ENTRY(dream_spec_accept), ENTRY(dream_attention_entropy),
-    ENTRY(dream_tree_expand_level), ENTRY_HOST(dream_tree_finalize, 9), {nullptr, nullptr, 0, nullptr}};
+    ENTRY(dream_tree_expand_level), ENTRY_HOST(dream_tree_finalize, 9), ENTRY_CHECKED(dream_rotary_rows, RotaryCheck),
+    ENTRY_CHECKED(dream_mx_append, AppendCheck), ENTRY_CHECKED(dream_mx_read, ReadCheck), ENTRY_CHECKED(dream_mx_commit, CommitCheck),
+    ENTRY_CHECKED(dream_window_verify_attn, WindowCheck<false>), ENTRY_CHECKED(dream_mx_verify_attn, WindowCheck<true>), {nullptr, nullptr, 0, nullptr}};
 #undef ENTRY
 #undef ENTRY_HOST
+#undef ENTRY_CHECKED
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
