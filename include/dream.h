@@ -64,6 +64,7 @@ typedef enum {
 #define DREAM_MAX_TREE_WIDTH 16     /* children per node / frontier rows of one tree-expansion level */
 #define DREAM_MAX_POOL 1024         /* candidates (root included) dream_tree_finalize ranks */
 #define DREAM_MAX_VISUAL 16384  /* visual tokens per sequence handled by dream_visual_compress */
+#define DREAM_MAX_WINDOW_ROWS ((1 << 23) - 128) /* s_max handled by the window and 4-bit attention calls */
 #define DREAM_MX_GROUP 32       /* values that share a scale in a cache held in 4 bits          */
 
 /* Attention geometry shared by the three attention-shaped calls. */
@@ -403,7 +404,7 @@ int dream_mx_commit(const dream_attn_desc *desc, void *const *codes_host, void *
  * lse = -inf.  What a node does not see does not change its row, whatever it holds: NaN and infinities too.
  * Rows out of every node's sight are read only where they share a tile of 32 rows with others.  A value that is not finite in a row
  * a node sees makes that channel of its row NaN or infinite.  q, caches and out 16-byte aligned,
- * batch * n_q_heads at most 2^20, s_max at most 2^30.
+ * batch * n_q_heads at most 2^20, s_max at most DREAM_MAX_WINDOW_ROWS.
  * ------------------------------------------------------------------------------------------- */
 size_t dream_window_verify_attn_workspace(const dream_attn_desc *desc, int32_t n_tree, int64_t max_kv_len,
                                           int32_t window, int32_t n_sink);

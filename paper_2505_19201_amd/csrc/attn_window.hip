@@ -20,6 +20,8 @@ namespace {
 constexpr int GROUP = DREAM_MX_GROUP;
 constexpr float SLACK = 8.0f;      // octaves by which a score may exceed its row's reference
 constexpr int MAX_SPLITS = 64;
+constexpr int64_t MAX_ROWS = DREAM_MAX_WINDOW_ROWS;   // a head's rows are reached by 32-bit offsets of up to 512 bytes a row
+constexpr uint32_t UNITS_Y = 32768;   // units of a grid's second dimension, by eights
 
 struct WindowArgs {
     const void *q, *k, *v;           // k, v: codes where the cache is held in 4 bits
@@ -32,8 +34,12 @@ struct WindowArgs {
     int64_t s_max;
     int32_t n_q_heads, n_kv_heads, group, n_tree, mask_words, window, n_sink;
     int32_t n_rg, n_splits, n_units; // row groups of a KV head; key splits; B * Hkv * n_splits
+    uint32_t tree_magic;             // for quick_div by n_tree
     float scale, scale_log2;
 };
+
+// x / d for x * d below 2^32: magic = ceil(2^32 / d), or 0 for d = 1
+__device__ __forceinline__ uint32_t quick_div(uint32_t x, uint32_t magic) { return magic ? __umulhi(x, magic) : x; }
 
 // Bits of the 32 keys from j0 on that lie in [from, to).
 __device__ __forceinline__ uint32_t key_bits(int j0, int from, int to)
@@ -44,30 +50,78 @@ __device__ __forceinline__ uint32_t key_bits(int j0, int from, int to)
     return (0xffffffffu >> (32 - (hi - lo))) << lo;
 }
 
-// Which tree nodes the rows see, and where their windows start; in LDS.
-struct TreeLds {
-    uint64_t mask[DREAM_MAX_TREE * (DREAM_MAX_TREE / 64)];
-    int32_t parent[DREAM_MAX_TREE], depth[DREAM_MAX_TREE];
+// Which tree nodes the rows see (bit a % 64 of word a / 64) and how deep they are; in LDS.
+struct Tree {
+    uint64_t *mask;
+    int32_t *depth;
     int32_t deepest;
 };
 
-// All threads of the workgroup; ends with a barrier.
-__device__ __forceinline__ void build_tree(TreeLds &t, const WindowArgs &a, int b, int P, int tid, int threads)
+// Takes what the window leaves out of the masks of nodes [first, T), every `step`-th; only where the window may end inside the tree.
+__device__ __forceinline__ void cut_masks(const Tree &t, const WindowArgs &a, int P, int first, int step)
+{
+    const int W = a.mask_words;
+    for (int i = first; i < a.n_tree; i += step)
+        for (int w = 0; w < W; w++) {
+            uint64_t m = t.mask[i * W + w], keep = m;
+            while (m) {
+                const int bit = __builtin_ctzll(m), n = w * 64 + bit;
+                m &= m - 1;
+                if (t.depth[i] - t.depth[n] >= a.window && P + t.depth[n] >= a.n_sink)
+                    keep &= ~(1ull << bit);
+            }
+            t.mask[i * W + w] = keep;
+        }
+}
+
+// Trees of up to 64 nodes: a wave builds its own, a node a lane, and meets nobody.  `parent`: of this lane's node (-1: none).  The paths are joined by halves: a node's mask holds its path
+// up to `up`, and takes in what `up` has found; log2 of the depth rounds.
+__device__ __forceinline__ void build_small_tree(Tree &t, const WindowArgs &a, int b, int P, int parent, int lane)
+{
+    const int T = a.n_tree;
+    uint64_t m = 1ull << lane;
+    int up = parent;
+    t.deepest = 0;
+    while (__any(up >= 0)) {
+        const int from = max(up, 0);
+        const uint64_t more = (uint64_t)(uint32_t)__shfl((int)(m >> 32), from) << 32 | (uint32_t)__shfl((int)m, from);
+        const int next = __shfl(up, from);
+        m |= up >= 0 ? more : 0ull;
+        up = up >= 0 ? next : -1;
+    }
+    const int depth = __popcll(m) - 1;
+    if (a.tree_mask) {
+        m = lane < T ? a.tree_mask[(int64_t)b * T + lane] : 0ull;
+        if (T < 64)
+            m &= (1ull << T) - 1;
+    }
+    t.mask[lane] = m;
+    if (a.window) {
+        t.depth[lane] = depth;
+        t.deepest = (int)wave_max((float)depth);
+    }
+    wave_lds_fence();
+    if (a.window && a.window < T) {
+        cut_masks(t, a, P, lane, 64);
+        wave_lds_fence();
+    }
+}
+
+// Any tree, by all threads of the workgroup; ends with a barrier.  `parent` (n_tree of them) and `deepest` are LDS.
+__device__ __forceinline__ void build_tree(Tree &t, const WindowArgs &a, int b, int P, int32_t *parent, int32_t *deepest, int tid, int threads)
 {
     const int T = a.n_tree, W = a.mask_words;
     const bool walk = !a.tree_mask || a.window;
     if (walk) {
         for (int i = tid; i < T; i += threads) {
             const int p = a.parent[(int64_t)b * T + i];
-            t.parent[i] = p < i ? p : -1;      // a walk up the tree always ends
+            parent[i] = p < i ? p : -1;        // a walk up the tree always ends
         }
         if (tid == 0)
-            t.deepest = 0;
+            *deepest = 0;
         __syncthreads();
     }
     for (int i = tid; i < T; i += threads) {
-        int depth = 0;
-        uint64_t m0 = 0;
         for (int w = 0; w < W; w++) {
             uint64_t m = 0;
             if (a.tree_mask) {
@@ -77,49 +131,32 @@ __device__ __forceinline__ void build_tree(TreeLds &t, const WindowArgs &a, int 
             } else if (i >> 6 == w) {
                 m = 1ull << (i & 63);
             }
-            if (W == 1)
-                m0 = m;
-            else
-                t.mask[i * W + w] = m;
+            t.mask[i * W + w] = m;
         }
         if (walk) {
-            for (int p = t.parent[i]; p >= 0; p = t.parent[p]) {
+            int depth = 0;
+            for (int p = parent[i]; p >= 0; p = parent[p]) {
                 depth++;
-                if (!a.tree_mask) {
-                    if (W == 1)
-                        m0 |= 1ull << p;
-                    else
-                        t.mask[i * W + (p >> 6)] |= 1ull << (p & 63);
-                }
+                if (!a.tree_mask)
+                    t.mask[i * W + (p >> 6)] |= 1ull << (p & 63);
             }
             t.depth[i] = depth;
             if (a.window)
-                atomicMax(&t.deepest, depth);
+                atomicMax(deepest, depth);
         }
-        if (W == 1)
-            t.mask[i] = m0;
     }
     __syncthreads();
-    if (a.window && a.window < T) {            // the window may end inside the tree
-        for (int i = tid; i < T; i += threads)
-            for (int w = 0; w < W; w++) {
-                uint64_t m = t.mask[i * W + w], keep = m;
-                while (m) {
-                    const int bit = __builtin_ctzll(m), n = w * 64 + bit;
-                    m &= m - 1;
-                    if (t.depth[i] - t.depth[n] >= a.window && P + t.depth[n] >= a.n_sink)
-                        keep &= ~(1ull << bit);
-                }
-                t.mask[i * W + w] = keep;
-            }
+    t.deepest = a.window ? *deepest : 0;
+    if (a.window && a.window < T) {
+        cut_masks(t, a, P, tid, threads);
         __syncthreads();
     }
 }
 
-// The keys from j0 on that node i sees, whose window starts at lo.
-__device__ __forceinline__ uint32_t visible_keys(const TreeLds &t, const WindowArgs &a, int node, int lo, int P, int j0)
+// The keys from j0 on that node i sees.  lo: where the root's window starts.
+__device__ __forceinline__ uint32_t visible_keys(const Tree &t, const WindowArgs &a, int node, int lo, int P, int j0)
 {
-    uint32_t bits = key_bits(j0, lo, P);
+    uint32_t bits = key_bits(j0, a.window ? lo + t.depth[node] : 0, P);
     if (a.window)
         bits |= key_bits(j0, 0, min(a.n_sink, P));
     const int rel = j0 - P, W = a.mask_words;
@@ -153,23 +190,47 @@ __device__ __forceinline__ Tiles tiles_of(const WindowArgs &a, int P)
     return t;
 }
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
 __device__ __forceinline__ bf16x8 from_codes(uint32_t codes, float scale)
 {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
     const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
+// The largest of eight scores; NaN where one is (v_maximum3_f32, which needs no quieting of its inputs).
+__device__ __forceinline__ float largest(f32x4 a, f32x4 b)
+{
+    auto of = [](float x, float y) { return __builtin_elementwise_maximum(x, y); };
+    return of(of(of(of(of(of(of(a[0], a[1]), a[2]), a[3]), b[0]), b[1]), b[2]), b[3]);
+}
+// not 0 where one of the two bf16 values is not finite
+__device__ __forceinline__ uint32_t strange_halves(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ u32x4 without_strange(u32x4 x)
+{
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        x[e] &= ((x[e] & 0x7f80u) == 0x7f80u ? 0u : 0xffffu) | ((x[e] & 0x7f800000u) == 0x7f800000u ? 0u : 0xffff0000u);
+    return x;
+}
 __device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// `bytes` from `base` on (the same in all lanes) as a buffer: loads behind its end return zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const uint8_t *base, uint32_t bytes)
+{
+    const uint64_t at = reinterpret_cast<uint64_t>(base);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void *>((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
 
 // What a wave has of one tile, as it came from memory.
 template <int D, bool MX>
 struct Raw;
 template <int D>
 struct Raw<D, true> {
-    static constexpr int KS = D == 256 ? 2 : 1, VP = D / 64;     // scales of a lane's K; 16-byte pieces of its V
+    static constexpr int KP = D == 256 ? 2 : 1, VP = D / 64;     // pieces of a lane's K (of 16 keys; 16 bytes, at head_dim 64 8) and 16-byte pieces of its V
     uint32_t k[2][D / 32];
-    uint8_t ks[2][KS];
+    uint8_t ks[2][KP];
     u32x4 v[VP];
     uint8_t vs[VP];
 };
@@ -179,142 +240,339 @@ struct Raw<D, false> {
     u32x4 v[D / 16];
 };
 
-template <int D, int QT, int NW, bool MX>
-struct WindowGeom {
-    static constexpr int VSTR = D + 16;                          // V row stride in LDS (values)
-    static constexpr int AREA = 32 * VSTR * 2;                   // bytes of a wave's V tile; also holds 16 rows' O at the end
-    static_assert(AREA >= 16 * D * 4, "the states of a query tile meet in the V areas");
-};
-
-template <int D, int QT, int NW, bool MX>
-__global__ __launch_bounds__(64 * NW) void window_attn_kernel(WindowArgs a)
+// First of the 8 channels of k-step ks that lane group g holds: of a 4-bit row consecutive runs of what it loads at once.
+template <int D, bool MX>
+__device__ __forceinline__ constexpr int channel_of(int ks, int g)
 {
-    using G = WindowGeom<D, QT, NW, MX>;
-    constexpr int NKS = D / 32, NDT = D / 16, VSTR = G::VSTR;
-    constexpr int ROWB = MX ? D / 2 : D * 2;                     // bytes of a row
-    __shared__ __attribute__((aligned(16))) uint8_t s_area[NW][G::AREA];
-    __shared__ TreeLds s_tree;
-    __shared__ float s_ml[NW][QT][16][2];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
-    // row groups of one share of the keys get ids that are congruent mod 8, so that they meet in one XCD's L2
-    const int unit = (int)(blockIdx.x / (8 * a.n_rg)) * 8 + (blockIdx.x & 7), rg = (blockIdx.x >> 3) % a.n_rg;
-    if (unit >= a.n_units)
-        return;
-    const int split = unit % a.n_splits, stream = unit / a.n_splits, kvh = stream % a.n_kv_heads, b = stream / a.n_kv_heads;
-    const int T = a.n_tree, rows = T * a.group;
-    const int P = (int)min((int64_t)max(a.prefix_len[b], 0), a.s_max - T);   // never past the cache, whatever the array holds
-    const Tiles tiles = tiles_of(a, P);
-    const int per = (tiles.count + a.n_splits - 1) / a.n_splits;
-    const int t0 = split * per + wave, t1 = min(tiles.count, split * per + per);
-    const int64_t head_row = (int64_t)stream * a.s_max;
-    const uint8_t *kb = static_cast<const uint8_t *>(a.k) + head_row * ROWB, *vb = static_cast<const uint8_t *>(a.v) + head_row * ROWB;
-    const uint8_t *ksb = MX ? a.k_scales + head_row * (D / GROUP) : nullptr, *vsb = MX ? a.v_scales + head_row * (D / GROUP) : nullptr;
+    return !MX ? ks * 32 + g * 8 : D == 64 ? g * 16 + ks * 8 : (ks >> 2) * 128 + g * 32 + (ks & 3) * 8;
+}
 
-    auto request = [&](Raw<D, MX> &r, int j0) {
-        const int last = (int)min((int64_t)31, a.s_max - 1 - j0);          // of a tile's rows inside the cache
-        const uint8_t *kt = kb + (int64_t)j0 * ROWB, *vt = vb + (int64_t)j0 * ROWB;
-        if constexpr (MX) {
-            const uint8_t *kst = ksb + (int64_t)j0 * (D / GROUP), *vst = vsb + (int64_t)j0 * (D / GROUP);
-#pragma unroll
-            for (int hh = 0; hh < 2; hh++) {
-                const int row = min(16 * hh + c, last);
-                if constexpr (D == 64) {
-                    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-                    const u32x2 x = *reinterpret_cast<const u32x2 *>(kt + row * ROWB + g * 8);
-                    r.k[hh][0] = x[0];
-                    r.k[hh][1] = x[1];
-                    r.ks[hh][0] = kst[row * 2 + (g >> 1)];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < D / 128; i++) {
-                        const u32x4 x = *reinterpret_cast<const u32x4 *>(kt + row * ROWB + i * 64 + g * 16);
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            r.k[hh][i * 4 + e] = x[e];
-                        r.ks[hh][i] = kst[row * (D / GROUP) + i * 4 + g];
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < D / 64; i++) {
-                const int p = lane + 64 * i, row = min(p / (D / GROUP), last), grp = p % (D / GROUP);
-                r.v[i] = *reinterpret_cast<const u32x4 *>(vt + row * ROWB + grp * 16);
-                r.vs[i] = vst[row * (D / GROUP) + grp];
-            }
-        } else {
-#pragma unroll
-            for (int hh = 0; hh < 2; hh++) {
-                const int row = min(16 * hh + c, last);
-#pragma unroll
-                for (int ks = 0; ks < NKS; ks++)
-                    r.k[hh][ks] = *reinterpret_cast<const u32x4 *>(kt + row * ROWB + ks * 64 + g * 16);
-            }
-#pragma unroll
-            for (int i = 0; i < D / 16; i++) {
-                const int p = lane + 64 * i, row = min(p / (D / 8), last);
-                r.v[i] = *reinterpret_cast<const u32x4 *>(vt + row * ROWB + p % (D / 8) * 16);
-            }
-        }
-    };
-
-    Raw<D, MX> next;
-    if (t0 < t1)
-        request(next, tiles.at(t0) * 32);
-
-    // the queries of this workgroup's rows, as the B operand; the channels in the order of the keys' pieces
-    bf16x8 qf[QT][NKS];
-    int node[QT], head[QT];
-#pragma unroll
-    for (int qt = 0; qt < QT; qt++) {
-        int f = (rg * QT + qt) * 16 + c;
-        f = f < rows ? f : 0;
-        head[qt] = kvh * a.group + f / T;
-        node[qt] = f % T;
-        const uint16_t *qp = static_cast<const uint16_t *>(a.q) + (((int64_t)b * T + node[qt]) * a.n_q_heads + head[qt]) * D;
-#pragma unroll
-        for (int ks = 0; ks < NKS; ks++) {
-            const int ch = !MX ? ks * 32 + g * 8 : D == 64 ? g * 16 + ks * 8 : (ks >> 2) * 128 + g * 32 + (ks & 3) * 8;
-            qf[qt][ks] = *reinterpret_cast<const bf16x8 *>(qp + ch);
-        }
-    }
-    build_tree(s_tree, a, b, P, tid, 64 * NW);
-    const int lo_min = a.window ? P - a.window + 1 : 0, lo_max = a.window ? lo_min + s_tree.deepest : 0;      // windows' starts, root and deepest node
-
+// The state of a query tile: O^T (a lane owns query row c = lane % 16 and channels 16 dt + 4 (lane / 16) + r), the reference of its scores in octaves and the lane's share of the sum.
+template <int QT, int NDT>
+struct RowState {
     f32x4 o[QT][NDT];
     float m[QT], l[QT];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-    for (int qt = 0; qt < QT; qt++) {
-        m[qt] = -INFINITY;
-        l[qt] = 0.0f;
+        for (int qt = 0; qt < QT; qt++) {
+            m[qt] = -INFINITY;
+            l[qt] = 0.0f;
 #pragma unroll
-        for (int dt = 0; dt < NDT; dt++)
-            o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int dt = 0; dt < NDT; dt++)
+                o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
     }
-    uint16_t *area = reinterpret_cast<uint16_t *>(s_area[wave]);
-    const uint16_t *turned = area + (g * 4 + (c >> 2)) * VSTR + (c & 3) * 4;      // what this lane reads transposed
-    auto read_v = [&](int dt) {
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(turned + dt * 16));
-        const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(turned + dt * 16 + 16 * VSTR));
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+};
+
+// Online softmax of a tile of 32 keys: a lane owns query row c and keys 4 g + r of both halves.  `vis` (of this lane's eight keys: bits 0 to 3 and 16 to 19) counts where the tile is not `whole`.
+// The scores are left as they are, and what the two kinds of tile do apart stands apart: values that either way may have written are copied on both.
+// Probabilities are rounded to bf16, half a step of 2^-8 each, as the matrix instruction takes them; sums stay float32.
+template <int QT, int NDT>
+__device__ __forceinline__ void softmax_tile(const f32x4 (&s)[2][QT], RowState<QT, NDT> &st, bool whole, const uint32_t (&vis)[QT], float scale_log2, bf16x8 (&pf)[QT])
+{
+    auto seen = [&](int qt, int e) { return (vis[qt] >> ((e >> 2) * 16 + (e & 3)) & 1u) != 0u; };
+    float top[QT];
+    if (whole) {
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++)
+            top[qt] = largest(s[0][qt], s[1][qt]) * scale_log2;
+    } else {
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++) {
+            f32x4 x[2];
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+                x[e >> 2][e & 3] = seen(qt, e) ? s[e >> 2][qt][e & 3] * scale_log2 : -INFINITY;
+            top[qt] = largest(x[0], x[1]);
+        }
+    }
+    bool raise = false;
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++)
+        raise = raise || top[qt] > st.m[qt] + SLACK;
+    if (__any(raise)) {
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++) {
+            float x = fmaxf(top[qt], __shfl_xor(top[qt], 16));
+            x = fmaxf(x, __shfl_xor(x, 32));
+            if (x > st.m[qt] + SLACK) {
+                const float f = __builtin_amdgcn_exp2f(st.m[qt] - x);       // 0 where nothing was seen before
+                st.m[qt] = x;
+                st.l[qt] *= f;
+#pragma unroll
+                for (int dt = 0; dt < NDT; dt++)
+                    st.o[qt][dt] *= f;
+            }
+        }
+    }
+    float sum[QT];
+    if (whole) {
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++) {
+            sum[qt] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][qt][e & 3], scale_log2, -st.m[qt]));
+                sum[qt] += p;
+                pf[qt][e] = (__bf16)p;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++) {
+            const float ref = st.m[qt] == -INFINITY ? 0.0f : st.m[qt];
+            sum[qt] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][qt][e & 3], scale_log2, -ref)), p = seen(qt, e) ? x : 0.0f;
+                sum[qt] += p;
+                pf[qt][e] = (__bf16)p;
+            }
+        }
+    }
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++)
+        st.l[qt] += sum[qt];
+}
+
+// V^T for channels 16 dt .. +15 of a 32-key tile [32][VSTR] in LDS, as the A operand whose keys are in the order in which a lane holds its probabilities.
+template <int VSTR>
+__device__ __forceinline__ bf16x8 read_turned(const uint16_t *tile, int dt, int c, int g)
+{
+    const uint16_t *at = tile + (g * 4 + (c >> 2)) * VSTR + (c & 3) * 4 + dt * 16;
+    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
+    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(at + 16 * VSTR));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// O^T += V^T P^T
+template <int QT, int NDT, int VSTR>
+__device__ __forceinline__ void add_values(const uint16_t *tile, const bf16x8 (&pf)[QT], RowState<QT, NDT> &st, int c, int g)
+{
+#pragma unroll
+    for (int dt = 0; dt < NDT; dt++) {
+        const bf16x8 vf = read_turned<VSTR>(tile, dt, c, g);
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++)
+            st.o[qt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt], st.o[qt][dt], 0, 0, 0);
+    }
+}
+
+// Of a tile [32][VSTR] that holds ones in the places of values that are not finite: how many of them the keys in `vis` have, per channel; what counts any is NaN.
+template <int QT, int NDT, int VSTR>
+__device__ __forceinline__ void mark_strange(const uint16_t *tile, int qt, uint32_t vis, RowState<QT, NDT> &st, int c, int g)
+{
+    bf16x8 seen;
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        seen[e] = (__bf16)(float)(vis >> ((e >> 2) * 16 + (e & 3)) & 1u);
+#pragma unroll
+    for (int dt = 0; dt < NDT; dt++) {
+        const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(read_turned<VSTR>(tile, dt, c, g), seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+        for (int r = 0; r < 4; r++)
+            st.o[qt][dt][r] = n[r] > 0.0f ? __builtin_nanf("") : st.o[qt][dt][r];
+    }
+}
+// ones in the places of values that are not finite
+__device__ __forceinline__ u32x4 strange_places(u32x4 x)
+{
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+        x[e] = ((x[e] & 0x7f80u) == 0x7f80u ? 0x3f80u : 0u) | ((x[e] & 0x7f800000u) == 0x7f800000u ? 0x3f800000u : 0u);
+    return x;
+}
+
+template <int D, int QT, int NW, bool MX>
+struct WindowGeom {
+    static constexpr int VSTR = D + 16;                          // V row stride in LDS (values): four consecutive rows land 8 banks apart
+    static constexpr int TILE = 32 * VSTR * 2, STATE = QT * 16 * D * 4;
+    static constexpr int AREA = TILE > STATE ? TILE : STATE;     // bytes of a wave's LDS: its V tile, at the end its O
+    // tiles on their way to a wave beside the one it works on.  4-bit tiles are small: with two, waves waited for memory as long as they worked
+    static constexpr int DEPTH = MX ? 2 : 1;
+    // waves of a SIMD that the registers have to leave room for: O, the queries, the scores and the tiles as they come from memory
+    static constexpr int WAVES = MX ? (D == 64 ? (QT == 1 ? 4 : QT == 2 ? 3 : 2) : D == 128 ? (QT == 1 ? 3 : 2) : 2) : D == 64 ? (QT == 1 ? 4 : 3) : D == 128 ? 2 : 1;
+};
+
+// What stands ahead of a launch's first loads comes as plain arguments, the 14 dwords that are in scalar registers when a wave starts.
+template <int D, int QT, int NW, bool MX>
+__global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void window_attn_kernel(const uint8_t *k, const uint8_t *v, const uint8_t *k_scales, const uint8_t *v_scales,
+                                                                                                const int32_t *prefix_len, uint32_t s_max, uint32_t heads_splits, uint32_t heads_magic,
+                                                                                                uint32_t tree_windowed, WindowArgs a)
+{
+    using G = WindowGeom<D, QT, NW, MX>;
+    constexpr int NKS = D / 32, NDT = D / 16, VSTR = G::VSTR, DEPTH = G::DEPTH;
+    constexpr int ROWB = MX ? D / 2 : D * 2, SCB = D / GROUP;    // bytes of a row, and of its scales
+    __shared__ __attribute__((aligned(16))) uint8_t s_area[NW][G::AREA];
+    __shared__ uint64_t s_mask[DREAM_MAX_TREE * 4];              // (up to 64 nodes: 64 words a wave)
+    __shared__ int32_t s_depth[512], s_parent[DREAM_MAX_TREE], s_deepest;
+    __shared__ float s_ml[NW][QT][2][16];
+    static_assert(NW <= 8, "the waves' own trees");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    // row groups of one share of the keys have ids that are congruent mod 8, so that they meet in one XCD's L2
+    const uint32_t unit = (blockIdx.z * UNITS_Y + blockIdx.y) * 8 + (blockIdx.x & 7), rg = blockIdx.x >> 3;
+    const uint32_t n_heads = heads_splits & 0xffff, n_splits = heads_splits >> 16;
+    if (unit >= (uint32_t)a.n_units)
+        return;
+    const uint32_t stream = n_splits == 1 ? unit : unit / n_splits, split = unit - stream * n_splits;
+    const uint32_t b = heads_magic ? __umulhi(stream, heads_magic) : stream / n_heads, kvh = stream - b * n_heads;
+    const int T = tree_windowed & 0x7fffffff;
+    const bool windowed = tree_windowed >> 31;
+    const int64_t head_row = (int64_t)stream * s_max;
+    k += head_row * ROWB;
+    v += head_row * ROWB;
+    k_scales += head_row * SCB;
+    v_scales += head_row * SCB;
+
+    // The pieces of a tile that this lane loads: K's as the matrix instruction has them, V's in the order of memory.  Every call has as many loads, so that what waits for one tile never
+    // waits for another: behind the last live row, and for a tile that is not this workgroup's, they return zeros and go nowhere (the descriptors' bounds).  One descriptor a tensor
+    // for the whole range: a scalar instruction costs a wave as long as ten vector lanes' work (a wave's scalar instructions issue every 10 clocks, its vector ones every 6).
+    constexpr int VPR = ROWB / 16, VPL = 32 * VPR / 64;          // pieces of a V row; of a lane's share of a tile
+    const int vrow = lane / VPR, vcol = lane % VPR;              // (and rows 64 / VPR apart)
+    struct Range {
+        __amdgpu_buffer_rsrc_t k, v, ks, vs;
+    };
+    auto range_of = [&](uint32_t rows) __attribute__((always_inline)) {
+        Range r;
+        r.k = buffer_of(k, rows * ROWB);
+        r.v = buffer_of(v, rows * ROWB);
+        if (MX) {
+            r.ks = buffer_of(k_scales, rows * SCB);
+            r.vs = buffer_of(v_scales, rows * SCB);
+        }
+        return r;
+    };
+    const uint32_t k_at = c * ROWB + g * (MX && D == 64 ? 8 : 16), ks_at = c * SCB + (D == 64 ? g >> 1 : g);
+    auto request_k = [&](Raw<D, MX> &r, const Range &from, uint32_t tile) __attribute__((always_inline)) {
+        const uint32_t at = k_at + tile * (32 * ROWB);
+#pragma unroll
+        for (int hh = 0; hh < 2; hh++) {
+            if constexpr (!MX) {
+#pragma unroll
+                for (int ks = 0; ks < NKS; ks++)
+                    r.k[hh][ks] = __builtin_amdgcn_raw_buffer_load_b128(from.k, at + hh * 16 * ROWB + ks * 64, 0, 0);
+            } else if constexpr (D == 64) {
+                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from.k, at + hh * 16 * ROWB, 0, 0);
+                r.k[hh][0] = x[0];
+                r.k[hh][1] = x[1];
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 128; i++) {
+                    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from.k, at + hh * 16 * ROWB + i * 64, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        r.k[hh][i * 4 + e] = x[e];
+                }
+            }
+        }
+        if constexpr (MX) {
+            const uint32_t sat = ks_at + tile * (32 * SCB);
+#pragma unroll
+            for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                for (int i = 0; i < Raw<D, MX>::KP; i++)
+                    r.ks[hh][i] = __builtin_amdgcn_raw_buffer_load_b8(from.ks, sat + hh * 16 * SCB + i * 4, 0, 0);
+        }
+    };
+    auto request_v = [&](Raw<D, MX> &r, const Range &from, uint32_t tile) __attribute__((always_inline)) {
+        const uint32_t at = lane * 16 + tile * (32 * ROWB);
+#pragma unroll
+        for (int i = 0; i < VPL; i++)
+            r.v[i] = __builtin_amdgcn_raw_buffer_load_b128(from.v, at + i * 1024, 0, 0);
+        if constexpr (MX) {
+            const uint32_t sat = lane + tile * (32 * SCB);
+#pragma unroll
+            for (int i = 0; i < VPL; i++)
+                r.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(from.vs, sat + i * 64, 0, 0);
+        }
     };
 
-    for (int t = t0; t < t1; t += NW) {
-        const Raw<D, MX> raw = next;
-        const int j0 = tiles.at(t) * 32;
-        if (t + NW < t1)
-            request(next, tiles.at(t + NW) * 32);
-        // every row sees every key of this tile, as it does but at the ends (a negative scale goes the general way)
-        const bool whole = j0 + 32 <= P && (j0 >= lo_max || j0 + 32 <= a.n_sink) && a.scale_log2 >= 0.0f;
+    Raw<D, MX> raw[DEPTH];
+    const bool early = n_splits == 1 && !windowed;               // the first tiles are known without the prefix length
+    if (early) {
+        const Range all = range_of(s_max);
+#pragma unroll
+        for (int i = 0; i < DEPTH; i++) {
+            const uint32_t tile = min((uint32_t)(wave + i * NW), (s_max + 31) / 32);
+            request_k(raw[i], all, tile);
+            request_v(raw[i], all, tile);
+        }
+    }
+    int parent = -1;
+    if (T <= 64 && lane < T && (!a.tree_mask || windowed)) {
+        parent = a.parent[(int64_t)b * T + lane];
+        parent = parent < lane ? parent : -1;                    // a path up the tree always ends
+    }
+    const int P = min(max(prefix_len[b], 0), (int)s_max - T);    // never past the cache, whatever the array holds
+    const Tiles tiles = tiles_of(a, P);
+    const int per = n_splits == 1 ? tiles.count : (tiles.count + n_splits - 1) / n_splits;
+    const int t0 = split * per + wave, t1 = min(tiles.count, (int)(split * per) + per);
+    const Range live = range_of(P + T);
+    const uint32_t no_tile = (P + T + 31) / 32;                  // behind the live rows
+    auto tile_of = [&](int t) __attribute__((always_inline)) { return t < t1 ? (uint32_t)tiles.at(t) : no_tile; };
+    if (!early) {
+#pragma unroll
+        for (int i = 0; i < DEPTH; i++) {
+            const uint32_t tile = tile_of(t0 + i * NW);
+            request_k(raw[i], live, tile);
+            request_v(raw[i], live, tile);
+        }
+    }
 
+    // the queries of this workgroup's rows: row f of a KV head is node f % T of its head f / T
+    const uint32_t rows = T * a.group;
+    bf16x8 qf[QT][NKS];
+    int node[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        uint32_t f = (rg * QT + qt) * 16 + c;
+        f = f < rows ? f : 0;
+        const uint32_t head = quick_div(f, a.tree_magic);
+        node[qt] = f - head * T;
+        const uint16_t *qp = static_cast<const uint16_t *>(a.q) + (((int64_t)b * T + node[qt]) * a.n_q_heads + kvh * a.group + head) * D;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ks++)
+            qf[qt][ks] = *reinterpret_cast<const bf16x8 *>(qp + channel_of<D, MX>(ks, g));
+    }
+    Tree tree = {s_mask, s_depth, 0};
+    if (T <= 64) {
+        tree.mask += wave * 64;
+        tree.depth += wave * 64;
+        build_small_tree(tree, a, b, P, parent, lane);
+    } else {
+        build_tree(tree, a, b, P, s_parent, &s_deepest, tid, 64 * NW);
+    }
+    const int lo_min = windowed ? P - a.window + 1 : 0, lo_max = windowed ? lo_min + tree.deepest : 0;      // windows' starts, root and deepest node
+    // tiles [w0, w1) of the list are seen whole by every row (a negative scale goes the general way)
+    const int w0 = max(tiles.sinks, tiles.sinks + (lo_max + 31) / 32 - tiles.first), w1 = a.scale_log2 >= 0.0f ? tiles.sinks + P / 32 - tiles.first : 0;
+
+    RowState<QT, NDT> st;
+    st.clear();
+    uint16_t *area = reinterpret_cast<uint16_t *>(s_area[wave]);
+    // (the queries are waited for here: in the loop it would be for every load since)
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++)
+#pragma unroll
+        for (int ks = 0; ks < NKS; ks++)
+            asm volatile("" : "+v"(qf[qt][ks]));
+    bool poisoned = false;
+    // One tile, the t-th of the list, from `raw`, which then receives the one DEPTH further on of this wave.
+    auto step = [&](Raw<D, MX> &raw, int t) __attribute__((always_inline)) {
+        const bool whole = t >= w0 && t < w1;
+        const int j0 = tiles.at(t) * 32;
+        const uint32_t next = tile_of(t + DEPTH * NW);
         // ---- S^T = K Q^T
         f32x4 s[2][QT];
 #pragma unroll
-        for (int hh = 0; hh < 2; hh++) {
+        for (int hh = 0; hh < 2; hh++)
 #pragma unroll
             for (int qt = 0; qt < QT; qt++)
                 s[hh][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int ks = 0; ks < NKS; ks++) {
+        for (int ks = 0; ks < NKS; ks++) {
+#pragma unroll
+            for (int hh = 0; hh < 2; hh++) {
                 bf16x8 kf;
                 if constexpr (MX)
                     kf = from_codes(raw.k[hh][ks], scale_value(raw.ks[hh][D == 256 ? ks >> 2 : 0]));
@@ -325,224 +583,403 @@ __global__ __launch_bounds__(64 * NW) void window_attn_kernel(WindowArgs a)
                     s[hh][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[qt][ks], s[hh][qt], 0, 0, 0);
             }
         }
+        request_k(raw, live, next);
 
-        // ---- V to LDS, as bf16.  Where not every row sees every key: rows that nobody may read are zeros, and so is, for now, what is not finite (0 * NaN is no zero)
-        bool odd = false;
-        auto dead = [&](int row) {
-            const int j = j0 + row;
-            return j >= P + T || (j < lo_min && j >= a.n_sink);
-        };
+        // ---- V to LDS, as bf16.  Where not every row sees every key, zeros stand for what is not finite (0 * NaN is no zero); what that does to the rows that see it comes behind the loop
         if constexpr (MX) {
+            const uint32_t last = whole ? 255u : 252u;
 #pragma unroll
-            for (int i = 0; i < D / 64; i++) {
-                const int p = lane + 64 * i, row = p / (D / GROUP), grp = p % (D / GROUP);
-                uint32_t byte = raw.vs[i];
-                if (!whole) {
-                    byte = dead(row) ? 0u : byte;
-                    odd = odd || byte > 252u;
-                    byte = byte > 252u ? 0u : byte;
-                }
-                const float scale = scale_value(byte);
+            for (int i = 0; i < VPL; i++) {
+                uint16_t *to = area + (vrow + i * (64 / VPR)) * VSTR + vcol * 32;
+                const uint32_t byte = raw.vs[i];
+                poisoned = poisoned || byte > last;
+                const float scale = scale_value(byte > last ? 0u : byte);
 #pragma unroll
                 for (int e = 0; e < 4; e++)
-                    *reinterpret_cast<bf16x8 *>(area + row * VSTR + grp * 32 + e * 8) = from_codes(raw.v[i][e], scale);
+                    *reinterpret_cast<bf16x8 *>(to + e * 8) = from_codes(raw.v[i][e], scale);
             }
         } else {
+            if (!whole) {
+                uint32_t found = 0;
 #pragma unroll
-            for (int i = 0; i < D / 16; i++) {
-                const int p = lane + 64 * i, row = p / (D / 8);
-                u32x4 x = raw.v[i];
-                if (!whole) {
-                    const bool none = dead(row);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const bool lo = (x[e] & 0x7f80u) == 0x7f80u, hi = (x[e] & 0x7f800000u) == 0x7f800000u;
-                        odd = odd || (!none && (lo || hi));
-                        x[e] = none ? 0u : x[e] & ((lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u));
-                    }
+                for (int i = 0; i < VPL; i++) {
+                    found |= (strange_halves(raw.v[i][0]) | strange_halves(raw.v[i][1])) | (strange_halves(raw.v[i][2]) | strange_halves(raw.v[i][3]));
+                    raw.v[i] = without_strange(raw.v[i]);
                 }
-                *reinterpret_cast<u32x4 *>(area + row * VSTR + p % (D / 8) * 8) = x;
+                poisoned = poisoned || found != 0u;
             }
+#pragma unroll
+            for (int i = 0; i < VPL; i++)
+                *reinterpret_cast<u32x4 *>(area + (vrow + i * (64 / VPR)) * VSTR + vcol * 8) = raw.v[i];
         }
+        request_v(raw, live, next);
 
-        // ---- online softmax; a lane owns query row c and keys g * 4 + r of both halves
-        uint32_t vis[QT];
-        float top[QT];
-        float mult = a.scale_log2;
-        if (whole) {
+        uint32_t vis[QT] = {};
+        if (!whole) {
 #pragma unroll
-            for (int qt = 0; qt < QT; qt++) {
-                float x = s[0][qt][0];
-#pragma unroll
-                for (int e = 1; e < 8; e++)
-                    x = fmaxf(x, s[e >> 2][qt][e & 3]);
-                top[qt] = x * a.scale_log2;
-                vis[qt] = 0xffffffffu;
-            }
-        } else {
-            mult = 1.0f;
-#pragma unroll
-            for (int qt = 0; qt < QT; qt++) {
-                const int lo = a.window ? lo_min + s_tree.depth[node[qt]] : 0;
-                vis[qt] = visible_keys(s_tree, a, node[qt], lo, P, j0) >> (g * 4);
-                float x = -INFINITY;
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const float y = vis[qt] >> ((e >> 2) * 16 + (e & 3)) & 1u ? s[e >> 2][qt][e & 3] * a.scale_log2 : -INFINITY;
-                    s[e >> 2][qt][e & 3] = y;
-                    x = fmaxf(x, y);
-                }
-                top[qt] = x;
-            }
-        }
-        bool raise = false;
-#pragma unroll
-        for (int qt = 0; qt < QT; qt++)
-            raise = raise || top[qt] > m[qt] + SLACK;
-        if (__any(raise)) {
-#pragma unroll
-            for (int qt = 0; qt < QT; qt++) {
-                float x = fmaxf(top[qt], __shfl_xor(top[qt], 16));
-                x = fmaxf(x, __shfl_xor(x, 32));
-                if (x > m[qt] + SLACK) {
-                    const float f = __builtin_amdgcn_exp2f(m[qt] - x);       // 0 where nothing was seen before
-                    m[qt] = x;
-                    l[qt] *= f;
-#pragma unroll
-                    for (int dt = 0; dt < NDT; dt++)
-                        o[qt][dt] *= f;
-                }
-            }
+            for (int qt = 0; qt < QT; qt++)
+                vis[qt] = visible_keys(tree, a, node[qt], lo_min, P, j0) >> (g * 4);
         }
         bf16x8 pf[QT];
-#pragma unroll
-        for (int qt = 0; qt < QT; qt++) {
-            const float neg = m[qt] == -INFINITY ? 0.0f : -m[qt];
-            float sum = 0.0f;
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][qt][e & 3], mult, neg));
-                sum += p;
-                pf[qt][e] = (__bf16)p;       // (probabilities of a tile are rounded to bf16, half a step of 2^-8 each, as the matrix instruction takes them; sums stay float32)
-            }
-            l[qt] += sum;
-        }
+        softmax_tile(s, st, whole, vis, a.scale_log2, pf);
+        wave_lds_fence();
+        add_values<QT, NDT, VSTR>(area, pf, st, c, g);
+        wave_lds_fence();
+    };
+    // (no way out between two steps: the loads in flight at the loop's head have to be the same on every way there)
+    int t = t0;
+    for (; t + (DEPTH - 1) * NW < t1; t += DEPTH * NW) {
+        step(raw[0], t);
+        if (DEPTH > 1)
+            step(raw[DEPTH - 1], t + NW);
+    }
+    if (DEPTH > 1 && t < t1)
+        step(raw[0], t);
 
-        // ---- O^T += V^T P^T
-        wave_lds_fence();
-#pragma unroll
-        for (int dt = 0; dt < NDT; dt++) {
-            const bf16x8 vf = read_v(dt);
-#pragma unroll
-            for (int qt = 0; qt < QT; qt++)
-                o[qt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt], o[qt][dt], 0, 0, 0);
-        }
-        wave_lds_fence();
-        if (!whole && __any(odd)) {
-            // Values that are not finite, in a tile that some row does not see all of: ones in their places and ones for the keys a row sees count them, and what
-            // counts any is NaN.
+    if (__any(poisoned)) {
+        // Tiles that some row does not see all of, again: ones in the places of values that are not finite, and ones for the keys a row sees, count them, and what counts
+        // any is NaN.
 #pragma unroll 1
-            for (int i = 0; i < (MX ? D / 64 : D / 16); i++) {
-                const int p = lane + 64 * i, row = p / (MX ? D / GROUP : D / 8);
-                const int64_t at = min((int64_t)j0 + row, a.s_max - 1);
-                if constexpr (MX) {
-                    const int grp = p % (D / GROUP);
-                    const bool bad = !dead(row) && vsb[at * (D / GROUP) + grp] > 252;
-                    const u32x4 x = u32x4{1u, 1u, 1u, 1u} * (bad ? 0x3f803f80u : 0u);
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        *reinterpret_cast<u32x4 *>(area + row * VSTR + grp * 32 + e * 8) = x;
-                } else {
-                    u32x4 x = *reinterpret_cast<const u32x4 *>(vb + at * ROWB + p % (D / 8) * 16);
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        x[e] = dead(row) ? 0u : ((x[e] & 0x7f80u) == 0x7f80u ? 0x3f80u : 0u) | ((x[e] & 0x7f800000u) == 0x7f800000u ? 0x3f800000u : 0u);
-                    *reinterpret_cast<u32x4 *>(area + row * VSTR + p % (D / 8) * 8) = x;
-                }
+        for (int t = t0; t < t1; t += NW) {
+            if (t >= w0 && t < w1)
+                continue;
+            const int j0 = tiles.at(t) * 32;
+#pragma unroll 1
+            for (int p = lane; p < 32 * D / 8; p += 64) {
+                const int row = p / (D / 8), piece = p % (D / 8), j = j0 + row;
+                const bool none = j >= P + T || (j < lo_min && j >= a.n_sink);
+                const int64_t at = none ? j0 : j;
+                u32x4 x;
+                if constexpr (MX)
+                    x = __builtin_bit_cast(u32x4, from_codes(*reinterpret_cast<const uint32_t *>(v + at * ROWB + piece * 4), scale_value(v_scales[at * SCB + piece / 4])));
+                else
+                    x = *reinterpret_cast<const u32x4 *>(v + at * ROWB + piece * 16);
+                *reinterpret_cast<u32x4 *>(area + row * VSTR + piece * 8) = none ? u32x4{0u, 0u, 0u, 0u} : strange_places(x);
             }
             wave_lds_fence();
 #pragma unroll
             for (int qt = 0; qt < QT; qt++)
-#pragma unroll
-                for (int e = 0; e < 8; e++)
-                    pf[qt][e] = (__bf16)(float)(vis[qt] >> ((e >> 2) * 16 + (e & 3)) & 1u);
-#pragma unroll
-            for (int dt = 0; dt < NDT; dt++) {
-                const bf16x8 vf = read_v(dt);
-#pragma unroll
-                for (int qt = 0; qt < QT; qt++) {
-                    const f32x4 n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                    for (int r = 0; r < 4; r++)
-                        o[qt][dt][r] = n[r] > 0.0f ? __builtin_nanf("") : o[qt][dt][r];
-                }
-            }
+                mark_strange<QT, NDT, VSTR>(area, qt, visible_keys(tree, a, node[qt], lo_min, P, j0) >> (g * 4), st, c, g);
             wave_lds_fence();
         }
     }
 
-    // ---- the waves' states meet, one query tile after the other, in wave order
+    // ---- the waves' states meet in LDS, in wave order
+    f32x4 *mine = reinterpret_cast<f32x4 *>(s_area[wave]);
+    wave_lds_fence();
 #pragma unroll
     for (int qt = 0; qt < QT; qt++) {
-        l[qt] += __shfl_xor(l[qt], 16);
-        l[qt] += __shfl_xor(l[qt], 32);
+        float l = st.l[qt];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
         if (g == 0) {
-            s_ml[wave][qt][c][0] = m[qt];
-            s_ml[wave][qt][c][1] = l[qt];
+            s_ml[wave][qt][0][c] = st.m[qt];
+            s_ml[wave][qt][1][c] = l;
         }
-    }
 #pragma unroll
-    for (int qt = 0; qt < QT; qt++) {
-        __syncthreads();
+        for (int dt = 0; dt < NDT; dt++)
+            mine[(qt * NDT + dt) * 64 + lane] = st.o[qt][dt];
+    }
+    __syncthreads();
+    // a thread takes 8 channels of a row at a time, 16 rows side by side
+#pragma unroll
+    for (int i = 0; i < (QT * 2 * D + 64 * NW - 1) / (64 * NW); i++) {
+        const int item = i * 64 * NW + tid;
+        if (QT * 2 * D % (64 * NW) && item >= QT * 2 * D)
+            break;
+        const int qt = item / (2 * D), ch = item / 16 % (D / 8);
+        const uint32_t f = (rg * QT + qt) * 16 + c;
         float mt = -INFINITY, lt = 0.0f;
 #pragma unroll
         for (int w = 0; w < NW; w++)
-            mt = fmaxf(mt, s_ml[w][qt][c][0]);
+            mt = fmaxf(mt, s_ml[w][qt][0][c]);
         const float ref = mt == -INFINITY ? 0.0f : mt;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
+        const int from = qt * NDT * 64 + (ch >> 1) * 64 + (ch & 1) * 32 + c;
 #pragma unroll
-        for (int w = 0; w < NW; w++)
-            lt += s_ml[w][qt][c][1] * __builtin_amdgcn_exp2f(s_ml[w][qt][c][0] - ref);
-        const float f = __builtin_amdgcn_exp2f(m[qt] - ref);
-        f32x4 *mine = reinterpret_cast<f32x4 *>(s_area[wave]);
-#pragma unroll
-        for (int dt = 0; dt < NDT; dt++)
-            mine[dt * 64 + lane] = o[qt][dt] * f;
-        __syncthreads();
-        // a thread takes 8 channels of row c
-        const int fr = (rg * QT + qt) * 16 + c;
-        for (int k = tid >> 4; k < D / 8; k += 4 * NW) {
-            f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = {0.f, 0.f, 0.f, 0.f};
-            const int from = (k >> 1) * 64 + (k & 1) * 32 + c;
-#pragma unroll
-            for (int w = 0; w < NW; w++) {
-                const f32x4 *src = reinterpret_cast<const f32x4 *>(s_area[w]);
-                x += src[from];
-                y += src[from + 16];
+        for (int w = 0; w < NW; w++) {
+            const float wgt = __builtin_amdgcn_exp2f(s_ml[w][qt][0][c] - ref);
+            const f32x4 *src = reinterpret_cast<const f32x4 *>(s_area[w]);
+            lt += s_ml[w][qt][1][c] * wgt;
+            x += src[from] * wgt;
+            y += src[from + 16] * wgt;
+        }
+        if (f >= rows)
+            continue;
+        if (n_splits > 1) {
+            const int64_t slot = (((int64_t)unit * a.n_rg + rg) * QT + qt) * 16 + c;
+            f32x4 *dst = reinterpret_cast<f32x4 *>(a.part + slot * D + ch * 8);
+            dst[0] = x;
+            dst[1] = y;
+            if (ch == 0) {
+                a.part_ml[slot * 2] = mt;
+                a.part_ml[slot * 2 + 1] = lt;
             }
-            if (fr < rows) {
-                if (a.n_splits > 1) {
-                    const int64_t slot = (((int64_t)unit * a.n_rg + rg) * QT + qt) * 16 + c;
-                    f32x4 *dst = reinterpret_cast<f32x4 *>(a.part + slot * D + k * 8);
-                    dst[0] = x;
-                    dst[1] = y;
-                    if (k == 0) {
-                        a.part_ml[slot * 2] = mt;
-                        a.part_ml[slot * 2 + 1] = lt;
-                    }
-                } else {
-                    const float inv = lt != 0.0f ? 1.0f / lt : 0.0f;
-                    bf16x8 r;
+        } else {
+            const float inv = lt != 0.0f ? 1.0f / lt : 0.0f;
+            bf16x8 r;
 #pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        r[e] = (__bf16)(x[e] * inv);
-                        r[4 + e] = (__bf16)(y[e] * inv);
+            for (int e = 0; e < 4; e++) {
+                r[e] = (__bf16)(x[e] * inv);
+                r[4 + e] = (__bf16)(y[e] * inv);
+            }
+            const uint32_t head = quick_div(f, a.tree_magic), n = f - head * T, hq = kvh * a.group + head;
+            *reinterpret_cast<bf16x8 *>(static_cast<uint16_t *>(a.out) + (((int64_t)b * T + n) * a.n_q_heads + hq) * D + ch * 8) = r;
+            if (a.lse && ch == 0)
+                a.lse[((int64_t)b * a.n_q_heads + hq) * T + n] = lt != 0.0f ? (mt + log2f(lt)) * 0.6931471805599453f : -INFINITY;
+        }
+    }
+}
+
+// All rows of a KV head in one workgroup, or as many as its eight waves hold.  What a CU can pull, 64 KB in flight, bounds a kernel whose workgroups for 16 rows each read the same keys, and so
+// does what it takes to turn 4 bits into 16: here a tile of 32 keys is read once, lies in LDS as bf16 and serves every wave's QT query tiles.  Two stages: while the waves work on one, the next
+// tile goes from registers to the other, and the one after that is on its way; one barrier a tile.  The keys are shared out over workgroups (splits), whose states window_merge_kernel joins.
+template <int D, int QT, bool MX>
+struct SharedGeom {
+    static constexpr int NW = 8, THREADS = 512;
+    static constexpr int KSTR = D + 8, VSTR = D + 16;            // row strides in LDS (values): 16-byte reads of K rows and transposing ones of V meet in no bank
+    static constexpr int STAGE = 32 * (KSTR + VSTR);             // values
+    static constexpr int PIECE = MX ? D / 8 : 8;                 // values a thread loads at once
+    static constexpr int PER_ROW = D / PIECE;                    // pieces of a row
+};
+
+template <int D, int QT, bool MX>
+__global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k, const uint8_t *v, const uint8_t *k_scales, const uint8_t *v_scales, const int32_t *prefix_len,
+                                                               uint32_t s_max, uint32_t heads_splits, uint32_t heads_magic, uint32_t tree_windowed, WindowArgs a)
+{
+    using G = SharedGeom<D, QT, MX>;
+    constexpr int NKS = D / 32, NDT = D / 16, KSTR = G::KSTR, VSTR = G::VSTR, PIECE = G::PIECE, PER_ROW = G::PER_ROW;
+    constexpr int ROWB = MX ? D / 2 : D * 2, SCB = D / GROUP;
+    constexpr int N = 32 * PER_ROW / G::THREADS > 0 ? 32 * PER_ROW / G::THREADS : 1;      // pieces of K of a thread, and of V; with fewer than threads, the threads share K and V out
+    constexpr bool HALVES = 32 * PER_ROW < G::THREADS;
+    static_assert(HALVES ? 64 * PER_ROW == G::THREADS : 32 * PER_ROW % G::THREADS == 0, "pieces");
+    __shared__ __attribute__((aligned(16))) uint16_t s_stage[2][G::STAGE];
+    __shared__ uint64_t s_mask[DREAM_MAX_TREE * 4];
+    __shared__ int32_t s_depth[DREAM_MAX_TREE], s_parent[DREAM_MAX_TREE], s_deepest, s_strange[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const uint32_t unit = (blockIdx.z * UNITS_Y + blockIdx.y) * 8 + (blockIdx.x & 7), rg = blockIdx.x >> 3;
+    const uint32_t n_heads = heads_splits & 0xffff, n_splits = heads_splits >> 16;
+    if (unit >= (uint32_t)a.n_units)
+        return;
+    const uint32_t stream = n_splits == 1 ? unit : unit / n_splits, split = unit - stream * n_splits;
+    const uint32_t b = heads_magic ? __umulhi(stream, heads_magic) : stream / n_heads, kvh = stream - b * n_heads;
+    const int T = tree_windowed & 0x7fffffff;
+    const bool windowed = tree_windowed >> 31;
+    const int64_t head_row = (int64_t)stream * s_max;
+    k += head_row * ROWB;
+    v += head_row * ROWB;
+    k_scales += head_row * SCB;
+    v_scales += head_row * SCB;
+    if (tid < 2)
+        s_strange[tid] = -1;
+
+    const int P = min(max(prefix_len[b], 0), (int)s_max - T);
+    const Tiles tiles = tiles_of(a, P);
+    const int per = n_splits == 1 ? tiles.count : (tiles.count + n_splits - 1) / n_splits;
+    const int t0 = split * per, t1 = min(tiles.count, t0 + per);
+
+    // a thread's pieces of a tile; loads of rows that are not there return zeros (see window_attn_kernel)
+    const bool second = HALVES && tid >= G::THREADS / 2;         // this thread takes V
+    const int ptid = HALVES ? tid % (G::THREADS / 2) : tid;
+    constexpr int BYTES = MX ? PIECE / 2 : 16;
+    struct Part {
+        u32x4 x[N];
+        uint8_t scale[N];
+    };
+    Part part[HALVES ? 1 : 2];
+    // (a wave's threads all take K or all take V)
+    const bool wave_second = HALVES && wave >= G::NW / 2;
+    const auto first_rows = buffer_of(wave_second ? v : k, (P + T) * ROWB), second_rows = buffer_of(v, (P + T) * ROWB);
+    const auto first_scales = buffer_of(wave_second ? v_scales : k_scales, (P + T) * SCB), second_scales = buffer_of(v_scales, (P + T) * SCB);
+    const uint32_t no_tile = (P + T + 31) / 32;                  // behind the live rows
+    auto request = [&](int t) __attribute__((always_inline)) {
+        const uint32_t tile = t < t1 ? (uint32_t)tiles.at(t) : no_tile;
+        const uint32_t at = ptid * BYTES + tile * (32 * ROWB), scale_at = ptid * PIECE / GROUP + tile * (32 * SCB);
+#pragma unroll
+        for (int half = 0; half < (HALVES ? 1 : 2); half++) {
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const auto rows_at = half ? second_rows : first_rows;
+                const int more = i * G::THREADS;
+                if constexpr (BYTES == 16) {
+                    part[half].x[i] = __builtin_amdgcn_raw_buffer_load_b128(rows_at, at + more * BYTES, 0, 0);
+                } else if constexpr (BYTES == 8) {
+                    const auto y = __builtin_amdgcn_raw_buffer_load_b64(rows_at, at + more * BYTES, 0, 0);
+                    part[half].x[i][0] = y[0];
+                    part[half].x[i][1] = y[1];
+                } else {
+                    part[half].x[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rows_at, at + more * BYTES, 0, 0);
+                }
+                if constexpr (MX)
+                    part[half].scale[i] = __builtin_amdgcn_raw_buffer_load_b8(half ? second_scales : first_scales, scale_at + more * PIECE / GROUP, 0, 0);
+            }
+        }
+    };
+    // tiles [w0, w1) are seen whole by every row; lo_min: where the root's window starts
+    int w0 = 0, w1 = 0, lo_min = 0;
+    auto deliver = [&](int t) __attribute__((always_inline)) {
+        uint16_t *stage = s_stage[(t - t0) & 1];
+        const bool whole = t >= w0 && t < w1;
+        bool strange = false;
+#pragma unroll
+        for (int half = 0; half < (HALVES ? 1 : 2); half++) {
+            const bool of_v = HALVES ? second : half == 1;
+            uint16_t *tile = stage + (of_v ? 32 * KSTR : 0);
+#pragma unroll
+            for (int i = 0; i < N; i++) {
+                const int p = ptid + i * G::THREADS, row = p / PER_ROW, col = p % PER_ROW * PIECE;
+                uint16_t *to = tile + row * (of_v ? VSTR : KSTR) + col;
+#pragma unroll
+                for (int e = 0; e < PIECE / 8; e++) {
+                    u32x4 x;
+                    if constexpr (MX)
+                        x = __builtin_bit_cast(u32x4, from_codes(part[half].x[i][e], scale_value(part[half].scale[i])));
+                    else
+                        x = part[half].x[i];
+                    if (of_v && !whole) {        // (0 * NaN is no zero: see window_attn_kernel)
+                        strange = strange || ((strange_halves(x[0]) | strange_halves(x[1])) | (strange_halves(x[2]) | strange_halves(x[3]))) != 0u;
+                        x = without_strange(x);
                     }
-                    const int hq = kvh * a.group + fr / T, n = fr % T;
-                    *reinterpret_cast<bf16x8 *>(static_cast<uint16_t *>(a.out) + (((int64_t)b * T + n) * a.n_q_heads + hq) * D + k * 8) = r;
-                    if (a.lse && k == 0)
-                        a.lse[((int64_t)b * a.n_q_heads + hq) * T + n] = lt != 0.0f ? (mt + log2f(lt)) * 0.6931471805599453f : -INFINITY;
+                    *reinterpret_cast<u32x4 *>(to + e * 8) = x;
                 }
             }
+        }
+        if (!whole && __any(strange) && lane == 0)
+            s_strange[(t - t0) & 1] = t;
+    };
+
+    request(t0);
+    const uint32_t rows = T * a.group;
+    bf16x8 qf[QT][NKS];
+    int node[QT];
+    const bool idle = ((rg * G::NW + wave) * QT) * 16 >= rows;   // (a wave without rows only brings keys)
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        uint32_t f = ((rg * G::NW + wave) * QT + qt) * 16 + c;
+        f = f < rows ? f : 0;
+        const uint32_t head = quick_div(f, a.tree_magic);
+        node[qt] = f - head * T;
+        const uint16_t *qp = static_cast<const uint16_t *>(a.q) + (((int64_t)b * T + node[qt]) * a.n_q_heads + kvh * a.group + head) * D;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ks++)
+            qf[qt][ks] = *reinterpret_cast<const bf16x8 *>(qp + ks * 32 + g * 8);
+    }
+    Tree tree = {s_mask, s_depth, 0};
+    build_tree(tree, a, b, P, s_parent, &s_deepest, tid, G::THREADS);
+    if (windowed)
+        lo_min = P - a.window + 1;
+    w0 = max(tiles.sinks, tiles.sinks + ((windowed ? lo_min + tree.deepest : 0) + 31) / 32 - tiles.first);
+    w1 = a.scale_log2 >= 0.0f ? tiles.sinks + P / 32 - tiles.first : 0;
+    RowState<QT, NDT> st;
+    st.clear();
+    if (t0 < t1)
+        deliver(t0);
+    request(t0 + 1);
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++)
+#pragma unroll
+        for (int ks = 0; ks < NKS; ks++)
+            asm volatile("" : "+v"(qf[qt][ks]));
+    __syncthreads();
+    bool poisoned = false;
+    for (int t = t0; t < t1; t++) {
+        const uint16_t *stage = s_stage[(t - t0) & 1];
+        if (t + 1 < t1)
+            deliver(t + 1);
+        request(t + 2);
+        const bool whole = t >= w0 && t < w1;
+        const int j0 = tiles.at(t) * 32;
+        poisoned = poisoned || (!whole && s_strange[(t - t0) & 1] == t);
+        if (!idle) {
+            f32x4 s[2][QT];
+#pragma unroll
+            for (int hh = 0; hh < 2; hh++)
+#pragma unroll
+                for (int qt = 0; qt < QT; qt++)
+                    s[hh][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < NKS; ks++)
+#pragma unroll
+                for (int hh = 0; hh < 2; hh++) {
+                    const bf16x8 kf = *reinterpret_cast<const bf16x8 *>(stage + (16 * hh + c) * KSTR + ks * 32 + g * 8);
+#pragma unroll
+                    for (int qt = 0; qt < QT; qt++)
+                        s[hh][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[qt][ks], s[hh][qt], 0, 0, 0);
+                }
+            uint32_t vis[QT] = {};
+            if (!whole) {
+#pragma unroll
+                for (int qt = 0; qt < QT; qt++)
+                    vis[qt] = visible_keys(tree, a, node[qt], lo_min, P, j0) >> (g * 4);
+            }
+            bf16x8 pf[QT];
+            softmax_tile(s, st, whole, vis, a.scale_log2, pf);
+            add_values<QT, NDT, VSTR>(stage + 32 * KSTR, pf, st, c, g);
+        }
+        __syncthreads();
+    }
+    if (poisoned) {      // (the same for all waves) see window_attn_kernel
+        uint16_t *tile = s_stage[0];
+#pragma unroll 1
+        for (int t = t0; t < t1; t++) {
+            if (t >= w0 && t < w1)
+                continue;
+            const int j0 = tiles.at(t) * 32;
+#pragma unroll 1
+            for (int p = tid; p < 32 * D / 8; p += G::THREADS) {
+                const int row = p / (D / 8), piece = p % (D / 8), j = j0 + row;
+                const bool none = j >= P + T || (j < lo_min && j >= a.n_sink);
+                const int64_t at = none ? j0 : j;
+                u32x4 x;
+                if constexpr (MX)
+                    x = __builtin_bit_cast(u32x4, from_codes(*reinterpret_cast<const uint32_t *>(v + at * ROWB + piece * 4), scale_value(v_scales[at * SCB + piece / 4])));
+                else
+                    x = *reinterpret_cast<const u32x4 *>(v + at * ROWB + piece * 16);
+                *reinterpret_cast<u32x4 *>(tile + row * VSTR + piece * 8) = none ? u32x4{0u, 0u, 0u, 0u} : strange_places(x);
+            }
+            __syncthreads();
+            if (!idle) {
+#pragma unroll
+                for (int qt = 0; qt < QT; qt++)
+                    mark_strange<QT, NDT, VSTR>(tile, qt, visible_keys(tree, a, node[qt], lo_min, P, j0) >> (g * 4), st, c, g);
+            }
+            __syncthreads();
+        }
+    }
+    if (idle)
+        return;
+    // ---- a lane has 4 adjacent channels of a row in every 16
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        float l = st.l[qt];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        const uint32_t f = ((rg * G::NW + wave) * QT + qt) * 16 + c;
+        if (f >= rows)
+            continue;
+        if (n_splits > 1) {
+            const int64_t slot = ((((int64_t)unit * a.n_rg + rg) * G::NW + wave) * QT + qt) * 16 + c;
+#pragma unroll
+            for (int dt = 0; dt < NDT; dt++)
+                *reinterpret_cast<f32x4 *>(a.part + slot * D + dt * 16 + g * 4) = st.o[qt][dt];
+            if (g == 0) {
+                a.part_ml[slot * 2] = st.m[qt];
+                a.part_ml[slot * 2 + 1] = l;
+            }
+        } else {
+            const float inv = l != 0.0f ? 1.0f / l : 0.0f;
+            const uint32_t head = quick_div(f, a.tree_magic), n = f - head * T, hq = kvh * a.group + head;
+            uint16_t *to = static_cast<uint16_t *>(a.out) + (((int64_t)b * T + n) * a.n_q_heads + hq) * D + g * 4;
+#pragma unroll
+            for (int dt = 0; dt < NDT; dt++) {
+                bf16x4 r;
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    r[e] = (__bf16)(st.o[qt][dt][e] * inv);
+                *reinterpret_cast<bf16x4 *>(to + dt * 16) = r;
+            }
+            if (a.lse && g == 0)
+                a.lse[((int64_t)b * a.n_q_heads + hq) * T + n] = l != 0.0f ? (st.m[qt] + log2f(l)) * 0.6931471805599453f : -INFINITY;
         }
     }
 }
@@ -560,17 +997,36 @@ __global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a, int row
     if (stream * n >= a.n_units)
         return;
     const int64_t slot = stream * n * rows_per_unit + f;
-    float m = -INFINITY;
-    for (int s = 0; s < n; s++)
-        m = fmaxf(m, a.part_ml[(slot + (int64_t)s * rows_per_unit) * 2]);
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f;
+    // eight splits' loads at a time (behind the last: the first again, weighted with nothing)
+    float m = -INFINITY, l = 0.0f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < n; s++) {
-        const int64_t i = slot + (int64_t)s * rows_per_unit;
-        const float w = __builtin_amdgcn_exp2f(a.part_ml[i * 2] - ref);
-        l += w * a.part_ml[i * 2 + 1];
-        o += *reinterpret_cast<const f32x4 *>(a.part + i * D + lane * 4) * w;
+    for (int s0 = 0; s0 < n; s0 += 8) {
+        float mm[8], ll[8];
+        f32x4 oo[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            const int64_t i = slot + (int64_t)(s0 + j < n ? s0 + j : 0) * rows_per_unit;
+            mm[j] = a.part_ml[i * 2];
+            ll[j] = a.part_ml[i * 2 + 1];
+            oo[j] = *reinterpret_cast<const f32x4 *>(a.part + i * D + lane * 4);
+        }
+        float top = m;
+#pragma unroll
+        for (int j = 0; j < 8; j++) {
+            mm[j] = s0 + j < n ? mm[j] : -INFINITY;
+            top = fmaxf(top, mm[j]);
+        }
+        const float ref = top == -INFINITY ? 0.0f : top, old = __builtin_amdgcn_exp2f(m - ref);
+        l *= old;
+        o *= old;
+        m = top;
+#pragma unroll
+        for (int j = 0; j < 8; j++)
+            if (s0 + j < n) {
+                const float w = __builtin_amdgcn_exp2f(mm[j] - ref);
+                l += w * ll[j];
+                o += oo[j] * w;
+            }
     }
     const float inv = l != 0.0f ? 1.0f / l : 0.0f;
     const int kvh = (int)(stream % a.n_kv_heads), hq = kvh * a.group + f / a.n_tree, node = f % a.n_tree;
@@ -590,7 +1046,8 @@ template <int D, bool MX>
 __global__ __launch_bounds__(256) void window_f32_kernel(WindowArgs a)
 {
     constexpr int LPK = D / 4, KPW = 64 / LPK, U = 4, PASS = 4 * KPW * U;
-    __shared__ TreeLds s_tree;
+    __shared__ uint64_t s_mask[DREAM_MAX_TREE * 4];
+    __shared__ int32_t s_depth[DREAM_MAX_TREE], s_parent[DREAM_MAX_TREE], s_deepest;
     __shared__ __attribute__((aligned(16))) float s_o[4][D];
     __shared__ float s_m[4], s_l[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane % LPK;
@@ -598,8 +1055,9 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WindowArgs a)
     const int P = (int)min((int64_t)max(a.prefix_len[b], 0), a.s_max - T);
     const int64_t head_row = ((int64_t)b * a.n_kv_heads + hq / a.group) * a.s_max;
     const f32x4 q = reinterpret_cast<const f32x4 *>(static_cast<const float *>(a.q) + (((int64_t)b * T + node) * a.n_q_heads + hq) * D)[col];
-    build_tree(s_tree, a, b, P, tid, 256);
-    const int lo = a.window ? max(0, P - a.window + 1 + s_tree.depth[node]) : 0, start = min(lo, P);
+    Tree tree = {s_mask, s_depth, 0};
+    build_tree(tree, a, b, P, s_parent, &s_deepest, tid, 256);
+    const int lo = a.window ? max(0, P - a.window + 1 + tree.depth[node]) : 0, start = min(lo, P);
     const int sinks = a.window ? min(a.n_sink, start) : 0, count = sinks + P + T - start;
     auto value = [&](const void *x, const uint8_t *scales, int64_t row) {
         if constexpr (MX) {
@@ -621,7 +1079,7 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WindowArgs a)
         for (int u = 0; u < U; u++) {
             const int i = i0 + (u * 4 + wave) * KPW + lane / LPK;
             const int ii = min(i, count - 1), j = ii < sinks ? ii : ii - sinks + start, rel = j - P;
-            see[u] = i < count && (rel < 0 || (s_tree.mask[node * a.mask_words + (rel >> 6)] >> (rel & 63) & 1ull));
+            see[u] = i < count && (rel < 0 || (tree.mask[node * a.mask_words + (rel >> 6)] >> (rel & 63) & 1ull));
             kr[u] = value(a.k, a.k_scales, head_row + j);
             vr[u] = value(a.v, a.v_scales, head_row + j);
         }
@@ -682,54 +1140,154 @@ __global__ __launch_bounds__(256) void window_f32_kernel(WindowArgs a)
 // host side
 // ------------------------------------------------------------------------------------------------
 struct WindowPlan {
+    bool shared;                   // window_shared_kernel
     int qt, nw, n_rg, n_splits;
-    int64_t n_units, slots;
-    size_t off_ml, total;
+    int64_t n_units, slots;        // (stream, split) pairs; rows of parts of O
+    size_t off_ml;
 };
 
-void make_plan(const dream_attn_desc *d, int n_tree, int64_t max_kv_len, int window, int n_sink, WindowPlan *p)
+// Which kernel a call takes, and into how many parts its keys are split, is what is estimated to take the shortest.  Where one workgroup is on a CU a wave's steps cost what one takes to come
+// through; where many are, what the CU can issue; whichever is more:
+//     us = base + per_group * groups + steps * max(latency, issue * groups)  [+ many_nodes]  [+ 2.3 + 0.11 * splits + 1e-6 * head_dim * rows of parts, for the join]
+// with groups the workgroups (of four waves) a CU gets, steps those of a wave.  The constants are fitted to times of every kernel with every split from 1 to 64 in powers of two over 7 head
+// layouts x batches of 1, 4, 16, 64 x trees of 1, 16, 60, 250 x 40 to 40000 keys, 528 shapes of 4-bit and 516 of 16-bit caches.  Over these the choice takes 2.5 % and 2.0 % longer than the
+// fastest in the geometric mean, 14 % and 12 % at the 95th percentile.  Without the shared kernel the fastest would take 6 % (4-bit) and 34 % (16-bit) longer, without several query tiles to a
+// wave 2 % and 1 %, without the eight-wave form 2 % with 4-bit caches; with 16-bit ones it brought 0.2 % and is left out, as is the shared kernel over 4-bit caches at head_dim 64 (0.1 %).
+struct Steps {
+    float base, per_group, latency, latency_tile, issue, issue_tile, many_nodes;      // window_attn_kernel; .._tile: for each query tile of a wave
+    float s_base, s_per_group, s_latency, s_issue, s_many_nodes;                      // window_shared_kernel
+};
+
+constexpr Steps STEPS[2][3] = {{{3.5f, 0.55f, 0.35f, 0.20f, 0.74f, 0.00f, 2.1f, 4.4f, 0.35f, 0.72f, 0.56f, 9.9f},
+                                {2.7f, 1.1f, 0.35f, 0.20f, 0.88f, 0.71f, 2.0f, 5.1f, 1.3f, 0.78f, 0.69f, 4.8f},
+                                {0.52f, 5.0f, 0.35f, 0.20f, 2.4f, 0.62f, 2.0f, 1.5f, 8.0f, 1.3f, 1.3f, 2.3f}},
+                               {{3.6f, 0.61f, 0.23f, 0.19f, 0.13f, 0.15f, 3.2f, 0.f, 0.f, 0.f, 0.f, 0.f},
+                                {2.9f, 1.3f, 0.47f, 0.22f, 0.42f, 0.13f, 6.3f, 4.3f, 2.1f, 0.80f, 0.57f, 6.2f},
+                                {4.0f, 1.4f, 0.35f, 0.20f, 1.1f, 0.31f, 4.6f, 4.3f, 5.5f, 0.43f, 1.5f, 3.1f}}};
+
+// query tiles a wave of window_attn_kernel may have, and those of window_shared_kernel's (0: there is none)
+constexpr int most_tiles(int D, bool mx) { return D == 64 ? (mx ? 4 : 2) : D == 128 && mx ? 2 : 1; }
+constexpr int shared_tiles(int D, bool mx) { return D == 64 ? (mx ? 0 : 2) : 1; }
+
+struct Choice {
+    bool shared;
+    int qt, nw;
+};
+
+// All a call may take, the overrides obeyed.  each(choice, groups of rows, most splits)
+template <class F>
+void every_choice(const dream_attn_desc *d, bool mx, int tiles, int64_t steps, F each)
 {
+    const int most = most_tiles(d->head_dim, mx), in_shared = shared_tiles(d->head_dim, mx);
+    const int waves = tile_waves_override(), asked = q_tiles_override(), forced = asked <= 0 ? 0 : asked < 2 || most < 2 ? 1 : asked < 4 || most < 4 ? 2 : 4;
     const int64_t streams = (int64_t)d->batch * d->n_kv_heads;
-    const int tiles = ceil_div((int64_t)d->n_q_heads / d->n_kv_heads * n_tree, 16);
+    auto offer = [&](const Choice &c) {
+        const int64_t groups = ceil_div(tiles, c.qt * (c.shared ? c.nw : 1));
+        int64_t splits = (c.shared ? 512 : 2048) / (streams * groups);       // parts beyond these only cost the join
+        splits = splits > steps ? steps : splits;
+        each(c, (int)groups, (int)(splits < 1 ? 1 : splits > MAX_SPLITS ? MAX_SPLITS : splits));
+    };
+    const bool eight = waves == 8, four = waves == 4;
+    for (int qt = 1; qt <= most; qt *= 2) {
+        if (forced ? qt != forced : qt > 1 && qt / 2 >= tiles)
+            continue;
+        const bool has_eight = mx && qt == 1;
+        if (!eight || (forced && !has_eight))
+            offer({false, qt, 4});
+        if (has_eight && !four && !(eight && !forced && in_shared))
+            offer({false, qt, 8});
+    }
+    if (in_shared && !four && !forced)
+        offer({true, in_shared, 8});
+}
+
+void shape_of(const dream_attn_desc *d, int n_tree, int64_t max_kv_len, int window, int n_sink, int *tiles, int64_t *steps)
+{
     int64_t keys = max_kv_len;
     if (window && (int64_t)window + n_tree + n_sink + 64 < keys)
         keys = (int64_t)window + n_tree + n_sink + 64;
-    const int64_t steps = ceil_div(keys, 32);
-    const int most = d->head_dim == 256 ? 2 : 4;
-    p->nw = 4;
-    p->qt = 1;
-    while (p->qt < most && p->qt < tiles)
-        p->qt *= 2;
-    while (p->qt > 1 && streams * ceil_div(tiles, p->qt) < 256)
-        p->qt /= 2;
-    p->n_rg = ceil_div(tiles, p->qt);
-    const int64_t wgs = streams * p->n_rg;
-    int64_t splits = wgs >= 256 ? 1 : 512 / wgs;
-    if (splits > steps / (2 * p->nw))
-        splits = steps / (2 * p->nw);
-    p->n_splits = (int)(splits < 1 ? 1 : splits > MAX_SPLITS ? MAX_SPLITS : splits);
+    *tiles = ceil_div((int64_t)d->n_q_heads / d->n_kv_heads * n_tree, 16);
+    *steps = ceil_div(keys, 32);
+}
+
+int64_t slots_of(const dream_attn_desc *d, const Choice &c, int groups, int splits)
+{
+    return (int64_t)d->batch * d->n_kv_heads * splits * groups * (c.shared ? c.nw : 1) * c.qt * 16;
+}
+
+size_t bytes_of(const dream_attn_desc *d, int64_t slots, int splits)
+{
+    if (splits == 1 || d->dtype != DREAM_BF16)
+        return DREAM_WORKSPACE_MIN_BYTES;
+    return align_up((size_t)slots * d->head_dim * 4, 256) + align_up((size_t)slots * 8, 256);
+}
+
+void make_plan(const dream_attn_desc *d, bool mx, int n_tree, int64_t max_kv_len, int window, int n_sink, WindowPlan *p)
+{
+    int tiles;
+    int64_t steps;
+    shape_of(d, n_tree, max_kv_len, window, n_sink, &tiles, &steps);
+    const int64_t streams = (int64_t)d->batch * d->n_kv_heads;
+    const Steps &s = STEPS[mx][d->head_dim == 64 ? 0 : d->head_dim == 128 ? 1 : 2];
+    float least = INFINITY;
+    *p = {};
+    every_choice(d, mx, tiles, steps, [&](const Choice &c, int groups, int most) {
+        const int forced = kv_splits_override() > MAX_SPLITS ? MAX_SPLITS : kv_splits_override();
+        for (int splits = forced ? forced : 1; splits <= (forced ? forced : most); splits *= 2) {
+            const int64_t slots = slots_of(d, c, groups, splits);
+            const float load = (float)((streams * groups * splits + 255) / 256) * (c.shared ? 1.0f : c.nw * 0.25f);
+            const float n = (float)((steps + splits - 1) / splits);
+            float us;
+            if (c.shared)
+                us = s.s_base + s.s_per_group * load + n * fmaxf(s.s_latency, s.s_issue * load) + (n_tree > 64 ? s.s_many_nodes : 0.0f);
+            else
+                us = s.base + s.per_group * load + (n_tree > 64 ? s.many_nodes : 0.0f) +
+                     (float)(((int64_t)n + c.nw - 1) / c.nw) * fmaxf(s.latency + s.latency_tile * c.qt, (s.issue + s.issue_tile * c.qt) * load);
+            if (splits > 1)
+                us += 2.3f + 0.11f * splits + 1e-6f * d->head_dim * slots;
+            if (us < least) {
+                least = us;
+                p->shared = c.shared;
+                p->qt = c.qt; p->nw = c.nw; p->n_rg = groups; p->n_splits = splits;
+                p->slots = slots;
+            }
+        }
+    });
     p->n_units = streams * p->n_splits;
-    p->slots = p->n_units * p->n_rg * p->qt * 16;
-    p->off_ml = 0;
-    p->total = DREAM_WORKSPACE_MIN_BYTES;
-    if (p->n_splits > 1 && d->dtype == DREAM_BF16) {
-        p->off_ml = align_up((size_t)p->slots * d->head_dim * 4, 256);
-        p->total = p->off_ml + align_up((size_t)p->slots * 8, 256);
-    }
+    p->off_ml = align_up((size_t)p->slots * d->head_dim * 4, 256);
 }
 
 template <int D, bool MX>
-int launch(const WindowArgs &a, const WindowPlan &p, hipStream_t st)
+auto kernel_of(const WindowPlan &p)
 {
-    constexpr int MOST = D == 256 ? 2 : 4;
-    auto *kernel = p.qt == 1 ? &window_attn_kernel<D, 1, 4, MX> : p.qt == 2 ? &window_attn_kernel<D, 2, 4, MX> : &window_attn_kernel<D, MOST, 4, MX>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((p.n_units + 7) / 8 * 8 * p.n_rg)), dim3(64 * p.nw), 0, st, a);
+    constexpr int MOST = most_tiles(D, MX), TWO = MOST < 2 ? MOST : 2, SHARED = shared_tiles(D, MX);
+    if constexpr (SHARED > 0)
+        if (p.shared)
+            return &window_shared_kernel<D, SHARED, MX>;
+    if constexpr (MX)
+        if (p.nw == 8)
+            return &window_attn_kernel<D, 1, 8, MX>;
+    return p.qt == 1 ? &window_attn_kernel<D, 1, 4, MX> : p.qt == 2 ? &window_attn_kernel<D, TWO, 4, MX> : &window_attn_kernel<D, MOST, 4, MX>;
+}
+
+uint32_t magic_of(uint32_t d) { return d == 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d); }
+
+template <int D, bool MX>
+int launch(WindowArgs &a, const WindowPlan &p, hipStream_t st)
+{
+    auto *kernel = kernel_of<D, MX>(p);
+    const int64_t eights = (p.n_units + 7) / 8;
+    const dim3 grid(8 * p.n_rg, (unsigned)(eights < UNITS_Y ? eights : UNITS_Y), (unsigned)((eights + UNITS_Y - 1) / UNITS_Y));
+    // (streams times heads below 2^32, or the kernel divides)
+    const uint32_t heads = a.n_kv_heads, magic = heads == 1 ? 0 : heads <= 4096 ? magic_of(heads) : 0;
+    hipLaunchKernelGGL(kernel, grid, dim3(p.shared ? 512 : 64 * p.nw), 0, st, static_cast<const uint8_t *>(a.k), static_cast<const uint8_t *>(a.v), a.k_scales, a.v_scales, a.prefix_len,
+                       (uint32_t)a.s_max, heads | (uint32_t)p.n_splits << 16, magic, (uint32_t)a.n_tree | (a.window ? 1u << 31 : 0u), a);
     if (int rc = check_launch("window_attn_kernel"))
         return rc;
     if (p.n_splits == 1)
         return DREAM_OK;
     const int64_t rows = p.n_units / p.n_splits * a.n_tree * a.group;
-    hipLaunchKernelGGL(window_merge_kernel<D>, dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, st, a, p.n_rg * p.qt * 16);
+    hipLaunchKernelGGL(window_merge_kernel<D>, dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, st, a, p.n_rg * (p.shared ? 8 : 1) * p.qt * 16);
     return check_launch("window_merge_kernel");
 }
 
@@ -745,9 +1303,27 @@ int check_desc(const dream_attn_desc *d, const char *who)
         return fail(DREAM_ERR_UNSUPPORTED, "%s: head_dim %d not in {64,128,256}", who, d->head_dim);
     if (d->dtype != DREAM_F32 && d->dtype != DREAM_BF16)
         return fail(DREAM_ERR_INVALID_ARG, "%s: unknown dtype %d", who, d->dtype);
-    if (d->batch > 65535 || d->n_q_heads > 65535 || (int64_t)d->batch * d->n_q_heads > (1 << 20) || d->s_max > (1 << 30))
-        return fail(DREAM_ERR_UNSUPPORTED, "%s: batch and n_q_heads are limited to 65535, their product to 2^20, s_max to 2^30", who);
+    if (d->batch > 65535 || d->n_q_heads > 65535 || (int64_t)d->batch * d->n_q_heads > (1 << 20) || d->s_max > MAX_ROWS)
+        return fail(DREAM_ERR_UNSUPPORTED, "%s: batch and n_q_heads are limited to 65535, their product to 2^20, s_max to %lld", who, (long long)MAX_ROWS);
     return DREAM_OK;
+}
+
+size_t workspace_for(const dream_attn_desc *d, bool mx, int n_tree, int64_t max_kv_len, int window, int n_sink)
+{
+    if (!d || d->batch < 1 || d->n_kv_heads < 1 || d->n_q_heads < 1 || d->n_q_heads % d->n_kv_heads || d->head_dim < 1 || n_tree < 1 || max_kv_len < 1 ||
+        window < 0 || n_sink < 0)
+        return DREAM_WORKSPACE_MIN_BYTES;
+    // what the most splits of any choice need, so that it never falls as max_kv_len rises
+    int tiles;
+    int64_t steps;
+    shape_of(d, n_tree, max_kv_len, window, n_sink, &tiles, &steps);
+    size_t total = DREAM_WORKSPACE_MIN_BYTES;
+    every_choice(d, mx, tiles, steps, [&](const Choice &c, int groups, int most) {
+        const int splits = kv_splits_override() ? (kv_splits_override() > MAX_SPLITS ? MAX_SPLITS : kv_splits_override()) : most;
+        const size_t bytes = bytes_of(d, slots_of(d, c, groups, splits), splits);
+        total = bytes > total ? bytes : total;
+    });
+    return total;
 }
 
 int run(const char *who, const dream_attn_desc *d, bool mx, WindowArgs &a, int64_t max_kv_len, void *ws, size_t ws_bytes, void *stream)
@@ -769,14 +1345,16 @@ int run(const char *who, const dream_attn_desc *d, bool mx, WindowArgs &a, int64
     if (mx && ((reinterpret_cast<uintptr_t>(a.k_scales) | reinterpret_cast<uintptr_t>(a.v_scales)) & 7))
         return fail(DREAM_ERR_INVALID_ARG, "%s: scales must be 8-byte aligned", who);
     WindowPlan p;
-    make_plan(d, a.n_tree, max_kv_len, a.window, a.n_sink, &p);
-    if (!ws || ws_bytes < p.total || (reinterpret_cast<uintptr_t>(ws) & 15))
-        return fail(DREAM_ERR_WORKSPACE, "%s: 16-byte aligned workspace of %zu bytes, %zu needed", who, ws_bytes, p.total);
+    make_plan(d, mx, a.n_tree, max_kv_len, a.window, a.n_sink, &p);
+    const size_t needed = workspace_for(d, mx, a.n_tree, max_kv_len, a.window, a.n_sink);
+    if (!ws || ws_bytes < needed || (reinterpret_cast<uintptr_t>(ws) & 15))
+        return fail(DREAM_ERR_WORKSPACE, "%s: 16-byte aligned workspace of %zu bytes, %zu needed", who, ws_bytes, needed);
     a.part = static_cast<float *>(ws);
     a.part_ml = reinterpret_cast<float *>(static_cast<char *>(ws) + p.off_ml);
     a.s_max = d->s_max;
     a.n_q_heads = d->n_q_heads; a.n_kv_heads = d->n_kv_heads; a.group = d->n_q_heads / d->n_kv_heads;
     a.mask_words = ceil_div(a.n_tree, 64);
+    a.tree_magic = magic_of(a.n_tree);
     a.n_rg = p.n_rg; a.n_splits = p.n_splits; a.n_units = (int32_t)p.n_units;
     a.scale = d->scale != 0.0f ? d->scale : 1.0f / sqrtf((float)d->head_dim);
     a.scale_log2 = a.scale * 1.4426950408889634f;
@@ -794,28 +1372,18 @@ int run(const char *who, const dream_attn_desc *d, bool mx, WindowArgs &a, int64
     return d->head_dim == 64 ? launch<64, false>(a, p, st) : d->head_dim == 128 ? launch<128, false>(a, p, st) : launch<256, false>(a, p, st);
 }
 
-size_t workspace_for(const dream_attn_desc *d, int n_tree, int64_t max_kv_len, int window, int n_sink)
-{
-    if (!d || d->batch < 1 || d->n_kv_heads < 1 || d->n_q_heads < 1 || d->n_q_heads % d->n_kv_heads || d->head_dim < 1 || n_tree < 1 || max_kv_len < 1 ||
-        window < 0 || n_sink < 0)
-        return DREAM_WORKSPACE_MIN_BYTES;
-    WindowPlan p;
-    make_plan(d, n_tree, max_kv_len, window, n_sink, &p);
-    return p.total;
-}
-
 }  // namespace
 
 extern "C" {
 
 size_t dream_window_verify_attn_workspace(const dream_attn_desc *desc, int32_t n_tree, int64_t max_kv_len, int32_t window, int32_t n_sink)
 {
-    return workspace_for(desc, n_tree, max_kv_len, window, n_sink);
+    return workspace_for(desc, false, n_tree, max_kv_len, window, n_sink);
 }
 
 size_t dream_mx_verify_attn_workspace(const dream_attn_desc *desc, int32_t n_tree, int64_t max_kv_len, int32_t window, int32_t n_sink)
 {
-    return workspace_for(desc, n_tree, max_kv_len, window, n_sink);
+    return workspace_for(desc, true, n_tree, max_kv_len, window, n_sink);
 }
 
 int dream_window_verify_attn(const dream_attn_desc *desc, const void *q, const void *k_cache, const void *v_cache, const int32_t *prefix_len,
