@@ -38,9 +38,6 @@ struct WindowArgs {
     float scale, scale_log2;
 };
 
-// x / d for x * d below 2^32: magic = ceil(2^32 / d), or 0 for d = 1
-__device__ __forceinline__ uint32_t quick_div(uint32_t x, uint32_t magic) { return magic ? __umulhi(x, magic) : x; }
-
 // Bits of the 32 keys from j0 on that lie in [from, to).
 __device__ __forceinline__ uint32_t key_bits(int j0, int from, int to)
 {
@@ -1269,8 +1266,6 @@ auto kernel_of(const WindowPlan &p)
             return &window_attn_kernel<D, 1, 8, MX>;
     return p.qt == 1 ? &window_attn_kernel<D, 1, 4, MX> : p.qt == 2 ? &window_attn_kernel<D, TWO, 4, MX> : &window_attn_kernel<D, MOST, 4, MX>;
 }
-
-uint32_t magic_of(uint32_t d) { return d == 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d); }
 
 template <int D, bool MX>
 int launch(WindowArgs &a, const WindowPlan &p, hipStream_t st)

@@ -31,6 +31,7 @@ struct RotaryArgs {
     const float *inv_freq;
     int64_t s_max;
     int32_t n_rows, head_dim, rot, pieces;   // pieces of a head
+    uint32_t rows_magic, pieces_magic;       // for quick_div; 0: divide
     float amplitude;
 };
 
@@ -87,19 +88,19 @@ template <class T, bool PAIRED, int N>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a)
 {
     __shared__ float2 s_turn[MAX_DIM / 2];
-    __shared__ int32_t s_par[DREAM_MAX_TREE];
     const int tid = threadIdx.x;
-    const int b = blockIdx.x / a.n_rows, r = blockIdx.x - b * a.n_rows;
+    const int b = a.rows_magic ? quick_div(blockIdx.x, a.rows_magic) : blockIdx.x / a.n_rows, r = blockIdx.x - b * a.n_rows;
     const int D = a.head_dim, rot = a.rot, half = rot / 2, pieces = a.pieces;
     const int turned = (PAIRED ? rot : half) / N;     // pieces of a head that turn; the others are copied
     const int total = a.job[DREAM_MAX_ROTARY_JOBS - 1].end;
+    const int stride = gridDim.y * 256;
     Piece<T, N> x[BATCH], y[BATCH];
     T *dst[BATCH];
     int at[BATCH];                                    // piece of its head
     auto request = [&](int first) {
 #pragma unroll
         for (int u = 0; u < BATCH; u++) {
-            const int idx = first + u * 256 + tid;
+            const int idx = first + u * stride + tid;
             dst[u] = nullptr;
             at[u] = 0;
             if (idx < total) {
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a)
                         index = a.job[i].row_index;
                         heads = a.job[i].n_heads;
                     }
-                const int h = (idx - start) / pieces, it = idx - start - h * pieces;
+                const int h = a.pieces_magic ? quick_div(idx - start, a.pieces_magic) : (idx - start) / pieces, it = idx - start - h * pieces;
                 const int c = PAIRED || it < turned ? it * N : it * N + half;     // first channel
                 const int64_t dense = ((int64_t)blockIdx.x * heads + h) * D;
                 int64_t to = dense;
@@ -141,35 +142,44 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a)
             }
         }
     };
-    request(0);
-    if (a.parent && !a.pos) {
-        if (tid < a.n_rows) {
-            const int p = a.parent[(int64_t)b * a.n_rows + tid];
-            s_par[tid] = p < tid ? p : -1;            // a walk up the tree always ends
-        }
-        __syncthreads();
+    // all that the position needs is requested before anything is waited for
+    const bool walk = a.parent && !a.pos;
+    int32_t par[DREAM_MAX_TREE / 64];                 // every wave holds the tree, lane l nodes l, 64 + l, ...
+#pragma unroll
+    for (int i = 0; i < DREAM_MAX_TREE / 64; i++) {
+        const int node = i * 64 + (tid & 63);
+        par[i] = walk && node < a.n_rows ? a.parent[(int64_t)b * a.n_rows + node] : -1;
     }
-    int64_t pos;
-    if (a.pos) {
-        pos = a.pos[blockIdx.x];
-    } else {
-        int step = r;
-        if (a.parent) {
-            step = 0;
-            for (int p = s_par[r]; p >= 0; p = s_par[p])
-                step++;
+    const int32_t start = a.pos ? a.pos[blockIdx.x] : a.pos_base[b];
+    const float freq = a.inv_freq[tid < half ? tid : 0];
+    request(blockIdx.y * 256);
+    int64_t pos = start;
+    if (walk) {
+        int p = r;
+        for (int step = 0;; step++) {
+            int32_t up = par[0];
+#pragma unroll
+            for (int i = 1; i < DREAM_MAX_TREE / 64; i++)
+                up = p >> 6 == i ? par[i] : up;
+            up = __builtin_amdgcn_readlane(up, p & 63);
+            if (up < 0 || up >= p) {                  // (a parent behind its node is none: a walk up the tree always ends)
+                pos += step;
+                break;
+            }
+            p = up;
         }
-        pos = (int64_t)a.pos_base[b] + step;
+    } else if (!a.pos) {
+        pos += r;
     }
     if (tid < half) {
-        const double turns = (double)pos * (double)a.inv_freq[tid] * 0.15915494309189533577;
+        const double turns = (double)pos * (double)freq * 0.15915494309189533577;
         float s, c;
         sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
         s_turn[tid] = make_float2(c * a.amplitude, s * a.amplitude);
     }
     __syncthreads();
-    for (int first = 0; first < total; first += 256 * BATCH) {
-        if (first)
+    for (int first = blockIdx.y * 256; first < total; first += stride * BATCH) {
+        if (first >= stride)
             request(first);
 #pragma unroll
         for (int u = 0; u < BATCH; u++) {
@@ -205,7 +215,8 @@ int launch(const RotaryArgs &a, bool paired, bool wide, int64_t rows, hipStream_
 {
     constexpr int N = 16 / sizeof(T);
     auto *kernel = paired ? (wide ? &rotary_kernel<T, true, N> : &rotary_kernel<T, true, 2>) : wide ? &rotary_kernel<T, false, N> : &rotary_kernel<T, false, 1>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)rows), dim3(256), 0, st, a);
+    const int64_t parts = 1024 / rows, most = (a.job[DREAM_MAX_ROTARY_JOBS - 1].end + 255) / 256;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)rows, (unsigned)(parts < 1 ? 1 : parts < most ? parts : most)), dim3(256), 0, st, a);
     return check_launch("rotary_kernel");
 }
 
@@ -269,6 +280,8 @@ int dream_rotary_rows(const dream_attn_desc *desc, const dream_rotary_job *jobs,
     a.s_max = desc->s_max; a.n_rows = n_rows; a.head_dim = desc->head_dim; a.rot = rot_dim;
     a.amplitude = amplitude != 0.0f ? amplitude : 1.0f;
     const int64_t rows = (int64_t)desc->batch * n_rows;
+    a.rows_magic = rows * n_rows < 1ll << 32 ? magic_of(n_rows) : 0;
+    a.pieces_magic = end * a.pieces < 1ll << 32 ? magic_of(a.pieces) : 0;
     return desc->dtype == DREAM_F32 ? launch<float>(a, interleaved != 0, wide, rows, as_stream(stream))
                                     : launch<uint16_t>(a, interleaved != 0, wide, rows, as_stream(stream));
 }
