@@ -386,8 +386,6 @@ struct WindowGeom {
     static constexpr int VSTR = D + 16;                          // V row stride in LDS (values): four consecutive rows land 8 banks apart
     static constexpr int TILE = 32 * VSTR * 2, STATE = QT * 16 * D * 4;
     static constexpr int AREA = TILE > STATE ? TILE : STATE;     // bytes of a wave's LDS: its V tile, at the end its O
-    // tiles on their way to a wave beside the one it works on.  4-bit tiles are small: with two, waves waited for memory as long as they worked
-    static constexpr int DEPTH = MX ? 2 : 1;
     // waves of a SIMD that the registers have to leave room for: O, the queries, the scores and the tiles as they come from memory
     static constexpr int WAVES = MX ? (D == 64 ? (QT == 1 ? 4 : QT == 2 ? 3 : 2) : D == 128 ? (QT == 1 ? 3 : 2) : 2) : D == 64 ? (QT == 1 ? 4 : 3) : D == 128 ? 2 : 1;
 };
@@ -399,7 +397,7 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
                                                                                                 uint32_t tree_windowed, WindowArgs a)
 {
     using G = WindowGeom<D, QT, NW, MX>;
-    constexpr int NKS = D / 32, NDT = D / 16, VSTR = G::VSTR, DEPTH = G::DEPTH;
+    constexpr int NKS = D / 32, NDT = D / 16, VSTR = G::VSTR;
     constexpr int ROWB = MX ? D / 2 : D * 2, SCB = D / GROUP;    // bytes of a row, and of its scales
     __shared__ __attribute__((aligned(16))) uint8_t s_area[NW][G::AREA];
     __shared__ uint64_t s_mask[DREAM_MAX_TREE * 4];              // (up to 64 nodes: 64 words a wave)
@@ -485,16 +483,13 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
         }
     };
 
-    Raw<D, MX> raw[DEPTH];
+    Raw<D, MX> raw;
     const bool early = n_splits == 1 && !windowed;               // the first tiles are known without the prefix length
     if (early) {
         const Range all = range_of(s_max);
-#pragma unroll
-        for (int i = 0; i < DEPTH; i++) {
-            const uint32_t tile = min((uint32_t)(wave + i * NW), (s_max + 31) / 32);
-            request_k(raw[i], all, tile);
-            request_v(raw[i], all, tile);
-        }
+        const uint32_t tile = min((uint32_t)(wave), (s_max + 31) / 32);
+        request_k(raw, all, tile);
+        request_v(raw, all, tile);
     }
     int parent = -1;
     if (T <= 64 && lane < T && (!a.tree_mask || windowed)) {
@@ -509,12 +504,9 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
     const uint32_t no_tile = (P + T + 31) / 32;                  // behind the live rows
     auto tile_of = [&](int t) __attribute__((always_inline)) { return t < t1 ? (uint32_t)tiles.at(t) : no_tile; };
     if (!early) {
-#pragma unroll
-        for (int i = 0; i < DEPTH; i++) {
-            const uint32_t tile = tile_of(t0 + i * NW);
-            request_k(raw[i], live, tile);
-            request_v(raw[i], live, tile);
-        }
+        const uint32_t tile = tile_of(t0);
+        request_k(raw, live, tile);
+        request_v(raw, live, tile);
     }
 
     // the queries of this workgroup's rows: row f of a KV head is node f % T of its head f / T
@@ -554,11 +546,10 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
         for (int ks = 0; ks < NKS; ks++)
             asm volatile("" : "+v"(qf[qt][ks]));
     bool poisoned = false;
-    // One tile, the t-th of the list, from `raw`, which then receives the one DEPTH further on of this wave.
-    auto step = [&](Raw<D, MX> &raw, int t) __attribute__((always_inline)) {
-        const bool whole = t >= w0 && t < w1;
-        const int j0 = tiles.at(t) * 32;
-        const uint32_t next = tile_of(t + DEPTH * NW);
+    // One tile, the t-th of the list; `raw` then receives the wave's next.
+    auto step = [&](auto seen, int t) __attribute__((always_inline)) {
+        constexpr bool whole = decltype(seen)::value;
+        const uint32_t next = tile_of(t + NW);
         // ---- S^T = K Q^T
         f32x4 s[2][QT];
 #pragma unroll
@@ -615,7 +606,7 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
         if (!whole) {
 #pragma unroll
             for (int qt = 0; qt < QT; qt++)
-                vis[qt] = visible_keys(tree, a, node[qt], lo_min, P, j0) >> (g * 4);
+                vis[qt] = visible_keys(tree, a, node[qt], lo_min, P, tiles.at(t) * 32) >> (g * 4);
         }
         bf16x8 pf[QT];
         softmax_tile(s, st, whole, vis, a.scale_log2, pf);
@@ -623,15 +614,14 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
         add_values<QT, NDT, VSTR>(area, pf, st, c, g);
         wave_lds_fence();
     };
-    // (no way out between two steps: the loads in flight at the loop's head have to be the same on every way there)
-    int t = t0;
-    for (; t + (DEPTH - 1) * NW < t1; t += DEPTH * NW) {
-        step(raw[0], t);
-        if (DEPTH > 1)
-            step(raw[DEPTH - 1], t + NW);
+    // Tiles that every row sees whole in straight code of their own: one step is some 200 instructions that a wave issues one by one, and flags and branches were a quarter of them.
+    const int w2 = min(w1, t1);
+    for (int t = t0; t < t1; t += NW) {
+        for (; t >= w0 && t < w2; t += NW)
+            step(std::true_type(), t);
+        if (t < t1)
+            step(std::false_type(), t);
     }
-    if (DEPTH > 1 && t < t1)
-        step(raw[0], t);
 
     if (__any(poisoned)) {
         // Tiles that some row does not see all of, again: ones in the places of values that are not finite, and ones for the keys a row sees, count them, and what counts
