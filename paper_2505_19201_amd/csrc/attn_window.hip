@@ -34,7 +34,7 @@ struct WindowArgs {
     int64_t s_max;
     int32_t n_q_heads, n_kv_heads, group, n_tree, mask_words, window, n_sink;
     int32_t n_rg, n_splits, n_units; // row groups of a KV head; key splits; B * Hkv * n_splits
-    uint32_t tree_magic;             // for quick_div by n_tree
+    uint32_t tree_magic, splits_magic; // for quick_div by n_tree, by n_splits
     float scale, scale_log2;
 };
 
@@ -71,36 +71,45 @@ __device__ __forceinline__ void cut_masks(const Tree &t, const WindowArgs &a, in
         }
 }
 
-// Trees of up to 64 nodes: a wave builds its own, a node a lane, and meets nobody.  `parent`: of this lane's node (-1: none).  The paths are joined by halves: a node's mask holds its path
-// up to `up`, and takes in what `up` has found; log2 of the depth rounds.
-__device__ __forceinline__ void build_small_tree(Tree &t, const WindowArgs &a, int b, int P, int parent, int lane)
+// Trees of up to 64 nodes: every wave has its own in registers, lane l node l's mask and depth, and meets nobody.  `parent`: of this lane's node (-1: none).  The paths are joined by halves:
+// a node's mask holds its path up to `up`, and takes in what `up` has found; log2 of the depth rounds.
+struct SmallTree {
+    uint64_t mask;
+    int depth, deepest;
+};
+__device__ __forceinline__ SmallTree small_tree(const WindowArgs &a, bool windowed, int b, int T, int parent, int lane)
 {
-    const int T = a.n_tree;
-    uint64_t m = 1ull << lane;
+    SmallTree t = {1ull << lane, 0, 0};
     int up = parent;
-    t.deepest = 0;
     while (__any(up >= 0)) {
         const int from = max(up, 0);
-        const uint64_t more = (uint64_t)(uint32_t)__shfl((int)(m >> 32), from) << 32 | (uint32_t)__shfl((int)m, from);
+        const uint64_t more = (uint64_t)(uint32_t)__shfl((int)(t.mask >> 32), from) << 32 | (uint32_t)__shfl((int)t.mask, from);
         const int next = __shfl(up, from);
-        m |= up >= 0 ? more : 0ull;
+        t.mask |= up >= 0 ? more : 0ull;
         up = up >= 0 ? next : -1;
     }
-    const int depth = __popcll(m) - 1;
+    if (windowed) {
+        t.depth = __popcll(t.mask) - 1;
+        t.deepest = (int)wave_max((float)t.depth);
+    }
     if (a.tree_mask) {
-        m = lane < T ? a.tree_mask[(int64_t)b * T + lane] : 0ull;
+        t.mask = lane < T ? a.tree_mask[(int64_t)b * T + lane] : 0ull;
         if (T < 64)
-            m &= (1ull << T) - 1;
+            t.mask &= (1ull << T) - 1;
     }
-    t.mask[lane] = m;
-    if (a.window) {
-        t.depth[lane] = depth;
-        t.deepest = (int)wave_max((float)depth);
-    }
+    return t;
+}
+// Takes what the window leaves out of the masks; only where it may end inside the tree.  `depths`: 64 words of LDS.
+__device__ __forceinline__ void cut_small_masks(SmallTree &t, const WindowArgs &a, int P, int32_t *depths, int lane)
+{
+    depths[lane] = t.depth;
     wave_lds_fence();
-    if (a.window && a.window < T) {
-        cut_masks(t, a, P, lane, 64);
-        wave_lds_fence();
+    uint64_t m = t.mask;
+    while (m) {
+        const int bit = __builtin_ctzll(m), depth = depths[bit];
+        m &= m - 1;
+        if (t.depth - depth >= a.window && P + depth >= a.n_sink)
+            t.mask &= ~(1ull << bit);
     }
 }
 
@@ -150,12 +159,20 @@ __device__ __forceinline__ void build_tree(Tree &t, const WindowArgs &a, int b, 
     }
 }
 
-// The keys from j0 on that node i sees.  lo: where the root's window starts.
+// The keys of the prefix from j0 on that a node of this depth sees.  lo: where the root's window starts.
+__device__ __forceinline__ uint32_t visible_prefix(const WindowArgs &a, int depth, int lo, int P, int j0)
+{
+    return a.window ? key_bits(j0, lo + depth, P) | key_bits(j0, 0, min(a.n_sink, P)) : key_bits(j0, 0, P);
+}
+// And of the tree, as its mask has them: one word, or those of a large tree in LDS.
+__device__ __forceinline__ uint32_t visible_nodes(uint64_t mask, int P, int j0)
+{
+    const int rel = j0 - P;
+    return rel <= -32 || rel >= 64 ? 0u : rel <= 0 ? (uint32_t)(mask << -rel) : (uint32_t)(mask >> rel);
+}
 __device__ __forceinline__ uint32_t visible_keys(const Tree &t, const WindowArgs &a, int node, int lo, int P, int j0)
 {
-    uint32_t bits = key_bits(j0, a.window ? lo + t.depth[node] : 0, P);
-    if (a.window)
-        bits |= key_bits(j0, 0, min(a.n_sink, P));
+    uint32_t bits = visible_prefix(a, a.window ? t.depth[node] : 0, lo, P, j0);
     const int rel = j0 - P, W = a.mask_words;
     if (rel > -32 && rel < a.n_tree) {
         const uint64_t *m = t.mask + node * W;
@@ -265,23 +282,22 @@ struct RowState {
 // Online softmax of a tile of 32 keys: a lane owns query row c and keys 4 g + r of both halves.  `vis` (of this lane's eight keys: bits 0 to 3 and 16 to 19) counts where the tile is not `whole`.
 // The scores are left as they are, and what the two kinds of tile do apart stands apart: values that either way may have written are copied on both.
 // Probabilities are rounded to bf16, half a step of 2^-8 each, as the matrix instruction takes them; sums stay float32.
-template <int QT, int NDT>
-__device__ __forceinline__ void softmax_tile(const f32x4 (&s)[2][QT], RowState<QT, NDT> &st, bool whole, const uint32_t (&vis)[QT], float scale_log2, bf16x8 (&pf)[QT])
+template <bool WHOLE, int QT, int NDT>
+__device__ __forceinline__ void softmax_tile(f32x4 (&s)[2][QT], RowState<QT, NDT> &st, const uint32_t (&vis)[QT], float scale_log2, bf16x8 (&pf)[QT])
 {
     auto seen = [&](int qt, int e) { return (vis[qt] >> ((e >> 2) * 16 + (e & 3)) & 1u) != 0u; };
     float top[QT];
-    if (whole) {
+    if constexpr (WHOLE) {
 #pragma unroll
         for (int qt = 0; qt < QT; qt++)
             top[qt] = largest(s[0][qt], s[1][qt]) * scale_log2;
     } else {
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
-            f32x4 x[2];
 #pragma unroll
             for (int e = 0; e < 8; e++)
-                x[e >> 2][e & 3] = seen(qt, e) ? s[e >> 2][qt][e & 3] * scale_log2 : -INFINITY;
-            top[qt] = largest(x[0], x[1]);
+                s[e >> 2][qt][e & 3] = seen(qt, e) ? s[e >> 2][qt][e & 3] * scale_log2 : -INFINITY;
+            top[qt] = largest(s[0][qt], s[1][qt]);
         }
     }
     bool raise = false;
@@ -304,7 +320,7 @@ __device__ __forceinline__ void softmax_tile(const f32x4 (&s)[2][QT], RowState<Q
         }
     }
     float sum[QT];
-    if (whole) {
+    if constexpr (WHOLE) {
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
             sum[qt] = 0.0f;
@@ -322,7 +338,7 @@ __device__ __forceinline__ void softmax_tile(const f32x4 (&s)[2][QT], RowState<Q
             sum[qt] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][qt][e & 3], scale_log2, -ref)), p = seen(qt, e) ? x : 0.0f;
+                const float p = __builtin_amdgcn_exp2f(s[e >> 2][qt][e & 3] - ref);
                 sum[qt] += p;
                 pf[qt][e] = (__bf16)p;
             }
@@ -394,26 +410,26 @@ struct WindowGeom {
 template <int D, int QT, int NW, bool MX>
 __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void window_attn_kernel(const uint8_t *k, const uint8_t *v, const uint8_t *k_scales, const uint8_t *v_scales,
                                                                                                 const int32_t *prefix_len, uint32_t s_max, uint32_t heads_splits, uint32_t heads_magic,
-                                                                                                uint32_t tree_windowed, WindowArgs a)
+                                                                                                uint32_t tree_units, WindowArgs a)
 {
     using G = WindowGeom<D, QT, NW, MX>;
     constexpr int NKS = D / 32, NDT = D / 16, VSTR = G::VSTR;
     constexpr int ROWB = MX ? D / 2 : D * 2, SCB = D / GROUP;    // bytes of a row, and of its scales
     __shared__ __attribute__((aligned(16))) uint8_t s_area[NW][G::AREA];
-    __shared__ uint64_t s_mask[DREAM_MAX_TREE * 4];              // (up to 64 nodes: 64 words a wave)
-    __shared__ int32_t s_depth[512], s_parent[DREAM_MAX_TREE], s_deepest;
+    __shared__ uint64_t s_mask[DREAM_MAX_TREE * 4];              // of more than 64 nodes
+    __shared__ int32_t s_depth[DREAM_MAX_TREE], s_parent[DREAM_MAX_TREE], s_deepest;
     __shared__ float s_ml[NW][QT][2][16];
-    static_assert(NW <= 8, "the waves' own trees");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     // row groups of one share of the keys have ids that are congruent mod 8, so that they meet in one XCD's L2
     const uint32_t unit = (blockIdx.z * UNITS_Y + blockIdx.y) * 8 + (blockIdx.x & 7), rg = blockIdx.x >> 3;
     const uint32_t n_heads = heads_splits & 0xffff, n_splits = heads_splits >> 16;
-    if (unit >= (uint32_t)a.n_units)
+    const int T = tree_units & 0x1ff;
+    const bool windowed = tree_units & 0x200;
+    if (unit >= (n_splits == 1 ? tree_units >> 10 : (uint32_t)a.n_units))
         return;
-    const uint32_t stream = n_splits == 1 ? unit : unit / n_splits, split = unit - stream * n_splits;
+    const uint32_t stream = n_splits == 1 ? unit : quick_div(unit, a.splits_magic), split = unit - stream * n_splits;
     const uint32_t b = heads_magic ? __umulhi(stream, heads_magic) : stream / n_heads, kvh = stream - b * n_heads;
-    const int T = tree_windowed & 0x7fffffff;
-    const bool windowed = tree_windowed >> 31;
+    const int prefix = prefix_len[b];
     const int64_t head_row = (int64_t)stream * s_max;
     k += head_row * ROWB;
     v += head_row * ROWB;
@@ -483,27 +499,37 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
         }
     };
 
-    Raw<D, MX> raw;
-    const bool early = n_splits == 1 && !windowed;               // the first tiles are known without the prefix length
-    if (early) {
-        const Range all = range_of(s_max);
-        const uint32_t tile = min((uint32_t)(wave), (s_max + 31) / 32);
-        request_k(raw, all, tile);
-        request_v(raw, all, tile);
-    }
+    // What a wave waits for one after the other is most of a short call: the arguments, the prefix length, the tree, the queries, the first tile.  So all are requested as soon as their
+    // addresses are known, and the tree, which needs the parents only, is built meanwhile.
     int parent = -1;
     if (T <= 64 && lane < T && (!a.tree_mask || windowed)) {
         parent = a.parent[(int64_t)b * T + lane];
         parent = parent < lane ? parent : -1;                    // a path up the tree always ends
     }
-    const int P = min(max(prefix_len[b], 0), (int)s_max - T);    // never past the cache, whatever the array holds
-    const Tiles tiles = tiles_of(a, P);
-    const int per = n_splits == 1 ? tiles.count : (tiles.count + n_splits - 1) / n_splits;
-    const int t0 = split * per + wave, t1 = min(tiles.count, (int)(split * per) + per);
-    const Range live = range_of(P + T);
-    const uint32_t no_tile = (P + T + 31) / 32;                  // behind the live rows
+    Raw<D, MX> raw;
+    const bool early = n_splits == 1 && !windowed;               // the first tile is known without the prefix length
+    if (early) {
+        const Range all = range_of(s_max);
+        const uint32_t tile = min((uint32_t)wave, (s_max + 31) / 32);
+        request_k(raw, all, tile);
+        request_v(raw, all, tile);
+    }
+    int P, t0, t1;
+    Tiles tiles;
+    Range live;
+    uint32_t no_tile;                                            // behind the live rows
     auto tile_of = [&](int t) __attribute__((always_inline)) { return t < t1 ? (uint32_t)tiles.at(t) : no_tile; };
+    auto find_tiles = [&]() __attribute__((always_inline)) {
+        P = min(max(prefix, 0), (int)s_max - T);                 // never past the cache, whatever the array holds
+        tiles = tiles_of(a, P);
+        const int per = n_splits == 1 ? tiles.count : quick_div(tiles.count + n_splits - 1, a.splits_magic);
+        t0 = split * per + wave;
+        t1 = min(tiles.count, (int)(split * per) + per);
+        live = range_of(P + T);
+        no_tile = (P + T + 31) / 32;
+    };
     if (!early) {
+        find_tiles();
         const uint32_t tile = tile_of(t0);
         request_k(raw, live, tile);
         request_v(raw, live, tile);
@@ -524,13 +550,22 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
         for (int ks = 0; ks < NKS; ks++)
             qf[qt][ks] = *reinterpret_cast<const bf16x8 *>(qp + channel_of<D, MX>(ks, g));
     }
-    Tree tree = {s_mask, s_depth, 0};
-    if (T <= 64) {
-        tree.mask += wave * 64;
-        tree.depth += wave * 64;
-        build_small_tree(tree, a, b, P, parent, lane);
-    } else {
+    SmallTree small = {0, 0, 0};
+    if (T <= 64)
+        small = small_tree(a, windowed, b, T, parent, lane);
+    if (early)
+        find_tiles();
+    Tree tree = {s_mask, s_depth, small.deepest};
+    if (T > 64)
         build_tree(tree, a, b, P, s_parent, &s_deepest, tid, 64 * NW);
+    else if (windowed && a.window < T)
+        cut_small_masks(small, a, P, reinterpret_cast<int32_t *>(s_area[wave]), lane);
+    uint64_t mask[QT];
+    int depth[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        mask[qt] = (uint64_t)(uint32_t)__shfl((int)(small.mask >> 32), node[qt]) << 32 | (uint32_t)__shfl((int)small.mask, node[qt]);
+        depth[qt] = windowed ? __shfl(small.depth, node[qt]) : 0;
     }
     const int lo_min = windowed ? P - a.window + 1 : 0, lo_max = windowed ? lo_min + tree.deepest : 0;      // windows' starts, root and deepest node
     // tiles [w0, w1) of the list are seen whole by every row (a negative scale goes the general way)
@@ -545,6 +580,9 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
 #pragma unroll
         for (int ks = 0; ks < NKS; ks++)
             asm volatile("" : "+v"(qf[qt][ks]));
+    auto visible = [&](int qt, int j0) __attribute__((always_inline)) {
+        return T <= 64 ? visible_prefix(a, depth[qt], lo_min, P, j0) | visible_nodes(mask[qt], P, j0) : visible_keys(tree, a, node[qt], lo_min, P, j0);
+    };
     bool poisoned = false;
     // One tile, the t-th of the list; `raw` then receives the wave's next.
     auto step = [&](auto seen, int t) __attribute__((always_inline)) {
@@ -606,10 +644,10 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
         if (!whole) {
 #pragma unroll
             for (int qt = 0; qt < QT; qt++)
-                vis[qt] = visible_keys(tree, a, node[qt], lo_min, P, tiles.at(t) * 32) >> (g * 4);
+                vis[qt] = visible(qt, tiles.at(t) * 32) >> (g * 4);
         }
         bf16x8 pf[QT];
-        softmax_tile(s, st, whole, vis, a.scale_log2, pf);
+        softmax_tile<whole>(s, st, vis, a.scale_log2, pf);
         wave_lds_fence();
         add_values<QT, NDT, VSTR>(area, pf, st, c, g);
         wave_lds_fence();
@@ -646,7 +684,7 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
             wave_lds_fence();
 #pragma unroll
             for (int qt = 0; qt < QT; qt++)
-                mark_strange<QT, NDT, VSTR>(area, qt, visible_keys(tree, a, node[qt], lo_min, P, j0) >> (g * 4), st, c, g);
+                mark_strange<QT, NDT, VSTR>(area, qt, visible(qt, j0) >> (g * 4), st, c, g);
             wave_lds_fence();
         }
     }
@@ -732,7 +770,7 @@ struct SharedGeom {
 
 template <int D, int QT, bool MX>
 __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k, const uint8_t *v, const uint8_t *k_scales, const uint8_t *v_scales, const int32_t *prefix_len,
-                                                               uint32_t s_max, uint32_t heads_splits, uint32_t heads_magic, uint32_t tree_windowed, WindowArgs a)
+                                                               uint32_t s_max, uint32_t heads_splits, uint32_t heads_magic, uint32_t tree_units, WindowArgs a)
 {
     using G = SharedGeom<D, QT, MX>;
     constexpr int NKS = D / 32, NDT = D / 16, KSTR = G::KSTR, VSTR = G::VSTR, PIECE = G::PIECE, PER_ROW = G::PER_ROW;
@@ -748,10 +786,10 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
     const uint32_t n_heads = heads_splits & 0xffff, n_splits = heads_splits >> 16;
     if (unit >= (uint32_t)a.n_units)
         return;
-    const uint32_t stream = n_splits == 1 ? unit : unit / n_splits, split = unit - stream * n_splits;
+    const uint32_t stream = n_splits == 1 ? unit : quick_div(unit, a.splits_magic), split = unit - stream * n_splits;
     const uint32_t b = heads_magic ? __umulhi(stream, heads_magic) : stream / n_heads, kvh = stream - b * n_heads;
-    const int T = tree_windowed & 0x7fffffff;
-    const bool windowed = tree_windowed >> 31;
+    const int T = tree_units & 0x1ff;
+    const bool windowed = tree_units & 0x200;
     const int64_t head_row = (int64_t)stream * s_max;
     k += head_row * ROWB;
     v += head_row * ROWB;
@@ -900,7 +938,10 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
                     vis[qt] = visible_keys(tree, a, node[qt], lo_min, P, j0) >> (g * 4);
             }
             bf16x8 pf[QT];
-            softmax_tile(s, st, whole, vis, a.scale_log2, pf);
+            if (whole)
+                softmax_tile<true>(s, st, vis, a.scale_log2, pf);
+            else
+                softmax_tile<false>(s, st, vis, a.scale_log2, pf);
             add_values<QT, NDT, VSTR>(stage + 32 * KSTR, pf, st, c, g);
         }
         __syncthreads();
@@ -1197,6 +1238,13 @@ void shape_of(const dream_attn_desc *d, int n_tree, int64_t max_kv_len, int wind
     *steps = ceil_div(keys, 32);
 }
 
+// (with more streams a unit's number times the splits passes 32 bits)
+int forced_splits(int64_t streams)
+{
+    const int asked = kv_splits_override();
+    return asked <= 0 ? 0 : streams > 65536 ? 1 : asked > MAX_SPLITS ? MAX_SPLITS : asked;
+}
+
 int64_t slots_of(const dream_attn_desc *d, const Choice &c, int groups, int splits)
 {
     return (int64_t)d->batch * d->n_kv_heads * splits * groups * (c.shared ? c.nw : 1) * c.qt * 16;
@@ -1219,7 +1267,7 @@ void make_plan(const dream_attn_desc *d, bool mx, int n_tree, int64_t max_kv_len
     float least = INFINITY;
     *p = {};
     every_choice(d, mx, tiles, steps, [&](const Choice &c, int groups, int most) {
-        const int forced = kv_splits_override() > MAX_SPLITS ? MAX_SPLITS : kv_splits_override();
+        const int forced = forced_splits(streams);
         for (int splits = forced ? forced : 1; splits <= (forced ? forced : most); splits *= 2) {
             const int64_t slots = slots_of(d, c, groups, splits);
             const float load = (float)((streams * groups * splits + 255) / 256) * (c.shared ? 1.0f : c.nw * 0.25f);
@@ -1266,7 +1314,7 @@ int launch(WindowArgs &a, const WindowPlan &p, hipStream_t st)
     // (streams times heads below 2^32, or the kernel divides)
     const uint32_t heads = a.n_kv_heads, magic = heads == 1 ? 0 : heads <= 4096 ? magic_of(heads) : 0;
     hipLaunchKernelGGL(kernel, grid, dim3(p.shared ? 512 : 64 * p.nw), 0, st, static_cast<const uint8_t *>(a.k), static_cast<const uint8_t *>(a.v), a.k_scales, a.v_scales, a.prefix_len,
-                       (uint32_t)a.s_max, heads | (uint32_t)p.n_splits << 16, magic, (uint32_t)a.n_tree | (a.window ? 1u << 31 : 0u), a);
+                       (uint32_t)a.s_max, heads | (uint32_t)p.n_splits << 16, magic, (uint32_t)a.n_tree | (a.window ? 0x200u : 0u) | (p.n_splits == 1 ? (uint32_t)p.n_units << 10 : 0u), a);
     if (int rc = check_launch("window_attn_kernel"))
         return rc;
     if (p.n_splits == 1)
@@ -1304,7 +1352,7 @@ size_t workspace_for(const dream_attn_desc *d, bool mx, int n_tree, int64_t max_
     shape_of(d, n_tree, max_kv_len, window, n_sink, &tiles, &steps);
     size_t total = DREAM_WORKSPACE_MIN_BYTES;
     every_choice(d, mx, tiles, steps, [&](const Choice &c, int groups, int most) {
-        const int splits = kv_splits_override() ? (kv_splits_override() > MAX_SPLITS ? MAX_SPLITS : kv_splits_override()) : most;
+        const int forced = forced_splits((int64_t)d->batch * d->n_kv_heads), splits = forced ? forced : most;
         const size_t bytes = bytes_of(d, slots_of(d, c, groups, splits), splits);
         total = bytes > total ? bytes : total;
     });
@@ -1340,6 +1388,7 @@ int run(const char *who, const dream_attn_desc *d, bool mx, WindowArgs &a, int64
     a.n_q_heads = d->n_q_heads; a.n_kv_heads = d->n_kv_heads; a.group = d->n_q_heads / d->n_kv_heads;
     a.mask_words = ceil_div(a.n_tree, 64);
     a.tree_magic = magic_of(a.n_tree);
+    a.splits_magic = magic_of(p.n_splits);
     a.n_rg = p.n_rg; a.n_splits = p.n_splits; a.n_units = (int32_t)p.n_units;
     a.scale = d->scale != 0.0f ? d->scale : 1.0f / sqrtf((float)d->head_dim);
     a.scale_log2 = a.scale * 1.4426950408889634f;
