@@ -404,7 +404,7 @@ int dream_mx_commit(const dream_attn_desc *desc, void *const *codes_host, void *
  * lse = -inf.  What a node does not see does not change its row, whatever it holds: NaN and infinities too.
  * Rows out of every node's sight are read only where they share a tile of 32 rows with others.  A value that is not finite in a row
  * a node sees makes that channel of its row NaN or infinite.  q, caches and out 16-byte aligned,
- * batch * n_q_heads at most 2^20, s_max at most DREAM_MAX_WINDOW_ROWS.
+ * n_q_heads at most 4096, batch * n_q_heads at most 2^20, s_max at most DREAM_MAX_WINDOW_ROWS.
  * ------------------------------------------------------------------------------------------- */
 size_t dream_window_verify_attn_workspace(const dream_attn_desc *desc, int32_t n_tree, int64_t max_kv_len,
                                           int32_t window, int32_t n_sink);

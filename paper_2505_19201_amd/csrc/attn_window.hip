@@ -34,9 +34,12 @@ struct WindowArgs {
     int64_t s_max;
     int32_t n_q_heads, n_kv_heads, group, n_tree, mask_words, window, n_sink;
     int32_t n_rg, n_splits, n_units; // row groups of a KV head; key splits; B * Hkv * n_splits
-    uint32_t tree_magic, splits_magic; // for quick_div by n_tree, by n_splits
+    uint32_t tree_magic;             // for quick_div by n_tree
     float scale, scale_log2;
 };
+
+// A value that every lane of a wave wants and this launch does not write, by the scalar unit: a vector load would be waited for before anything that follows it.
+__device__ __forceinline__ int scalar_load(const int32_t *p) { return *(const __attribute__((address_space(4))) int32_t *)(uintptr_t)p; }
 
 // Bits of the 32 keys from j0 on that lie in [from, to).
 __device__ __forceinline__ uint32_t key_bits(int j0, int from, int to)
@@ -422,14 +425,14 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     // row groups of one share of the keys have ids that are congruent mod 8, so that they meet in one XCD's L2
     const uint32_t unit = (blockIdx.z * UNITS_Y + blockIdx.y) * 8 + (blockIdx.x & 7), rg = blockIdx.x >> 3;
-    const uint32_t n_heads = heads_splits & 0xffff, n_splits = heads_splits >> 16;
+    const uint32_t n_heads = heads_splits & 0xffff, lg_splits = heads_splits >> 16, n_splits = 1u << lg_splits;
     const int T = tree_units & 0x1ff;
     const bool windowed = tree_units & 0x200;
-    if (unit >= (n_splits == 1 ? tree_units >> 10 : (uint32_t)a.n_units))
+    if (unit >= tree_units >> 10)
         return;
-    const uint32_t stream = n_splits == 1 ? unit : quick_div(unit, a.splits_magic), split = unit - stream * n_splits;
-    const uint32_t b = heads_magic ? __umulhi(stream, heads_magic) : stream / n_heads, kvh = stream - b * n_heads;
-    const int prefix = prefix_len[b];
+    const uint32_t stream = unit >> lg_splits, split = unit & (n_splits - 1);
+    const uint32_t b = quick_div(stream, heads_magic), kvh = stream - b * n_heads;
+    const int prefix = scalar_load(prefix_len + b);
     const int64_t head_row = (int64_t)stream * s_max;
     k += head_row * ROWB;
     v += head_row * ROWB;
@@ -501,11 +504,10 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
 
     // What a wave waits for one after the other is most of a short call: the arguments, the prefix length, the tree, the queries, the first tile.  So all are requested as soon as their
     // addresses are known, and the tree, which needs the parents only, is built meanwhile.
-    int parent = -1;
-    if (T <= 64 && lane < T && (!a.tree_mask || windowed)) {
-        parent = a.parent[(int64_t)b * T + lane];
-        parent = parent < lane ? parent : -1;                    // a path up the tree always ends
-    }
+    const bool walk = T <= 64 && (!a.tree_mask || windowed);
+    int parent = 0;
+    if (walk)
+        parent = a.parent[(int64_t)b * T + min(lane, T - 1)];
     Raw<D, MX> raw;
     const bool early = n_splits == 1 && !windowed;               // the first tile is known without the prefix length
     if (early) {
@@ -522,7 +524,7 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
     auto find_tiles = [&]() __attribute__((always_inline)) {
         P = min(max(prefix, 0), (int)s_max - T);                 // never past the cache, whatever the array holds
         tiles = tiles_of(a, P);
-        const int per = n_splits == 1 ? tiles.count : quick_div(tiles.count + n_splits - 1, a.splits_magic);
+        const int per = n_splits == 1 ? tiles.count : (tiles.count + n_splits - 1) >> lg_splits;
         t0 = split * per + wave;
         t1 = min(tiles.count, (int)(split * per) + per);
         live = range_of(P + T);
@@ -552,7 +554,7 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
     }
     SmallTree small = {0, 0, 0};
     if (T <= 64)
-        small = small_tree(a, windowed, b, T, parent, lane);
+        small = small_tree(a, windowed, b, T, walk && lane < T && parent < lane ? parent : -1, lane);      // (a path up the tree always ends)
     if (early)
         find_tiles();
     Tree tree = {s_mask, s_depth, small.deepest};
@@ -783,11 +785,11 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
     __shared__ int32_t s_depth[DREAM_MAX_TREE], s_parent[DREAM_MAX_TREE], s_deepest, s_strange[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     const uint32_t unit = (blockIdx.z * UNITS_Y + blockIdx.y) * 8 + (blockIdx.x & 7), rg = blockIdx.x >> 3;
-    const uint32_t n_heads = heads_splits & 0xffff, n_splits = heads_splits >> 16;
-    if (unit >= (uint32_t)a.n_units)
+    const uint32_t n_heads = heads_splits & 0xffff, lg_splits = heads_splits >> 16, n_splits = 1u << lg_splits;
+    if (unit >= tree_units >> 10)
         return;
-    const uint32_t stream = n_splits == 1 ? unit : quick_div(unit, a.splits_magic), split = unit - stream * n_splits;
-    const uint32_t b = heads_magic ? __umulhi(stream, heads_magic) : stream / n_heads, kvh = stream - b * n_heads;
+    const uint32_t stream = unit >> lg_splits, split = unit & (n_splits - 1);
+    const uint32_t b = quick_div(stream, heads_magic), kvh = stream - b * n_heads;
     const int T = tree_units & 0x1ff;
     const bool windowed = tree_units & 0x200;
     const int64_t head_row = (int64_t)stream * s_max;
@@ -800,7 +802,7 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
 
     const int P = min(max(prefix_len[b], 0), (int)s_max - T);
     const Tiles tiles = tiles_of(a, P);
-    const int per = n_splits == 1 ? tiles.count : (tiles.count + n_splits - 1) / n_splits;
+    const int per = n_splits == 1 ? tiles.count : (tiles.count + n_splits - 1) >> lg_splits;
     const int t0 = split * per, t1 = min(tiles.count, t0 + per);
 
     // a thread's pieces of a tile; loads of rows that are not there return zeros (see window_attn_kernel)
@@ -1238,11 +1240,13 @@ void shape_of(const dream_attn_desc *d, int n_tree, int64_t max_kv_len, int wind
     *steps = ceil_div(keys, 32);
 }
 
-// (with more streams a unit's number times the splits passes 32 bits)
+// a power of two, like what the choice takes (a shift divides by it), and units below 2^22 (the launch's arguments)
 int forced_splits(int64_t streams)
 {
-    const int asked = kv_splits_override();
-    return asked <= 0 ? 0 : streams > 65536 ? 1 : asked > MAX_SPLITS ? MAX_SPLITS : asked;
+    int n = kv_splits_override() > MAX_SPLITS ? MAX_SPLITS : kv_splits_override();
+    while (n > 1 && ((n & (n - 1)) || streams * n >= 1 << 22))
+        n--;
+    return n < 0 ? 0 : n;
 }
 
 int64_t slots_of(const dream_attn_desc *d, const Choice &c, int groups, int splits)
@@ -1311,10 +1315,9 @@ int launch(WindowArgs &a, const WindowPlan &p, hipStream_t st)
     auto *kernel = kernel_of<D, MX>(p);
     const int64_t eights = (p.n_units + 7) / 8;
     const dim3 grid(8 * p.n_rg, (unsigned)(eights < UNITS_Y ? eights : UNITS_Y), (unsigned)((eights + UNITS_Y - 1) / UNITS_Y));
-    // (streams times heads below 2^32, or the kernel divides)
-    const uint32_t heads = a.n_kv_heads, magic = heads == 1 ? 0 : heads <= 4096 ? magic_of(heads) : 0;
     hipLaunchKernelGGL(kernel, grid, dim3(p.shared ? 512 : 64 * p.nw), 0, st, static_cast<const uint8_t *>(a.k), static_cast<const uint8_t *>(a.v), a.k_scales, a.v_scales, a.prefix_len,
-                       (uint32_t)a.s_max, heads | (uint32_t)p.n_splits << 16, magic, (uint32_t)a.n_tree | (a.window ? 0x200u : 0u) | (p.n_splits == 1 ? (uint32_t)p.n_units << 10 : 0u), a);
+                       (uint32_t)a.s_max, (uint32_t)a.n_kv_heads | (uint32_t)__builtin_ctz(p.n_splits) << 16, magic_of(a.n_kv_heads),
+                       (uint32_t)a.n_tree | (a.window ? 0x200u : 0u) | (uint32_t)p.n_units << 10, a);
     if (int rc = check_launch("window_attn_kernel"))
         return rc;
     if (p.n_splits == 1)
@@ -1336,8 +1339,8 @@ int check_desc(const dream_attn_desc *d, const char *who)
         return fail(DREAM_ERR_UNSUPPORTED, "%s: head_dim %d not in {64,128,256}", who, d->head_dim);
     if (d->dtype != DREAM_F32 && d->dtype != DREAM_BF16)
         return fail(DREAM_ERR_INVALID_ARG, "%s: unknown dtype %d", who, d->dtype);
-    if (d->batch > 65535 || d->n_q_heads > 65535 || (int64_t)d->batch * d->n_q_heads > (1 << 20) || d->s_max > MAX_ROWS)
-        return fail(DREAM_ERR_UNSUPPORTED, "%s: batch and n_q_heads are limited to 65535, their product to 2^20, s_max to %lld", who, (long long)MAX_ROWS);
+    if (d->batch > 65535 || d->n_q_heads > 4096 || (int64_t)d->batch * d->n_q_heads > (1 << 20) || d->s_max > MAX_ROWS)
+        return fail(DREAM_ERR_UNSUPPORTED, "%s: batch is limited to 65535, n_q_heads to 4096, their product to 2^20, s_max to %lld", who, (long long)MAX_ROWS);
     return DREAM_OK;
 }
 
@@ -1388,7 +1391,6 @@ int run(const char *who, const dream_attn_desc *d, bool mx, WindowArgs &a, int64
     a.n_q_heads = d->n_q_heads; a.n_kv_heads = d->n_kv_heads; a.group = d->n_q_heads / d->n_kv_heads;
     a.mask_words = ceil_div(a.n_tree, 64);
     a.tree_magic = magic_of(a.n_tree);
-    a.splits_magic = magic_of(p.n_splits);
     a.n_rg = p.n_rg; a.n_splits = p.n_splits; a.n_units = (int32_t)p.n_units;
     a.scale = d->scale != 0.0f ? d->scale : 1.0f / sqrtf((float)d->head_dim);
     a.scale_log2 = a.scale * 1.4426950408889634f;
