@@ -800,7 +800,11 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
     if (tid < 2)
         s_strange[tid] = -1;
 
-    const int P = min(max(prefix_len[b], 0), (int)s_max - T);
+    const bool walk = T <= 64 && (!a.tree_mask || windowed);
+    int parent = 0;
+    if (walk)
+        parent = a.parent[(int64_t)b * T + min(lane, T - 1)];
+    const int P = min(max(scalar_load(prefix_len + b), 0), (int)s_max - T);
     const Tiles tiles = tiles_of(a, P);
     const int per = n_splits == 1 ? tiles.count : (tiles.count + n_splits - 1) >> lg_splits;
     const int t0 = split * per, t1 = min(tiles.count, t0 + per);
@@ -813,13 +817,15 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
         u32x4 x[N];
         uint8_t scale[N];
     };
-    Part part[HALVES ? 1 : 2];
+    struct Pieces {
+        Part part[HALVES ? 1 : 2];
+    } even, odd;                                                 // of the tiles at even and at odd distances from t0
     // (a wave's threads all take K or all take V)
     const bool wave_second = HALVES && wave >= G::NW / 2;
     const auto first_rows = buffer_of(wave_second ? v : k, (P + T) * ROWB), second_rows = buffer_of(v, (P + T) * ROWB);
     const auto first_scales = buffer_of(wave_second ? v_scales : k_scales, (P + T) * SCB), second_scales = buffer_of(v_scales, (P + T) * SCB);
     const uint32_t no_tile = (P + T + 31) / 32;                  // behind the live rows
-    auto request = [&](int t) __attribute__((always_inline)) {
+    auto request = [&](Pieces &of, int t) __attribute__((always_inline)) {
         const uint32_t tile = t < t1 ? (uint32_t)tiles.at(t) : no_tile;
         const uint32_t at = ptid * BYTES + tile * (32 * ROWB), scale_at = ptid * PIECE / GROUP + tile * (32 * SCB);
 #pragma unroll
@@ -829,22 +835,22 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
                 const auto rows_at = half ? second_rows : first_rows;
                 const int more = i * G::THREADS;
                 if constexpr (BYTES == 16) {
-                    part[half].x[i] = __builtin_amdgcn_raw_buffer_load_b128(rows_at, at + more * BYTES, 0, 0);
+                    of.part[half].x[i] = __builtin_amdgcn_raw_buffer_load_b128(rows_at, at + more * BYTES, 0, 0);
                 } else if constexpr (BYTES == 8) {
                     const auto y = __builtin_amdgcn_raw_buffer_load_b64(rows_at, at + more * BYTES, 0, 0);
-                    part[half].x[i][0] = y[0];
-                    part[half].x[i][1] = y[1];
+                    of.part[half].x[i][0] = y[0];
+                    of.part[half].x[i][1] = y[1];
                 } else {
-                    part[half].x[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rows_at, at + more * BYTES, 0, 0);
+                    of.part[half].x[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rows_at, at + more * BYTES, 0, 0);
                 }
                 if constexpr (MX)
-                    part[half].scale[i] = __builtin_amdgcn_raw_buffer_load_b8(half ? second_scales : first_scales, scale_at + more * PIECE / GROUP, 0, 0);
+                    of.part[half].scale[i] = __builtin_amdgcn_raw_buffer_load_b8(half ? second_scales : first_scales, scale_at + more * PIECE / GROUP, 0, 0);
             }
         }
     };
     // tiles [w0, w1) are seen whole by every row; lo_min: where the root's window starts
     int w0 = 0, w1 = 0, lo_min = 0;
-    auto deliver = [&](int t) __attribute__((always_inline)) {
+    auto deliver = [&](const Pieces &of, int t) __attribute__((always_inline)) {
         uint16_t *stage = s_stage[(t - t0) & 1];
         const bool whole = t >= w0 && t < w1;
         bool strange = false;
@@ -860,9 +866,9 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
                 for (int e = 0; e < PIECE / 8; e++) {
                     u32x4 x;
                     if constexpr (MX)
-                        x = __builtin_bit_cast(u32x4, from_codes(part[half].x[i][e], scale_value(part[half].scale[i])));
+                        x = __builtin_bit_cast(u32x4, from_codes(of.part[half].x[i][e], scale_value(of.part[half].scale[i])));
                     else
-                        x = part[half].x[i];
+                        x = of.part[half].x[i];
                     if (of_v && !whole) {        // (0 * NaN is no zero: see window_attn_kernel)
                         strange = strange || ((strange_halves(x[0]) | strange_halves(x[1])) | (strange_halves(x[2]) | strange_halves(x[3]))) != 0u;
                         x = without_strange(x);
@@ -875,7 +881,8 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
             s_strange[(t - t0) & 1] = t;
     };
 
-    request(t0);
+    request(even, t0);
+    request(odd, t0 + 1);
     const uint32_t rows = T * a.group;
     bf16x8 qf[QT][NKS];
     int node[QT];
@@ -891,8 +898,24 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
         for (int ks = 0; ks < NKS; ks++)
             qf[qt][ks] = *reinterpret_cast<const bf16x8 *>(qp + ks * 32 + g * 8);
     }
+    SmallTree small = {0, 0, 0};
     Tree tree = {s_mask, s_depth, 0};
-    build_tree(tree, a, b, P, s_parent, &s_deepest, tid, G::THREADS);
+    if (T <= 64) {
+        small = small_tree(a, windowed, b, T, walk && lane < T && parent < lane ? parent : -1, lane);      // (a path up the tree always ends)
+        tree.deepest = small.deepest;
+        if (windowed && a.window < T)
+            cut_small_masks(small, a, P, reinterpret_cast<int32_t *>(s_stage[1]) + wave * 64, lane);
+        __syncthreads();                                         // (s_strange, and s_stage[1] again)
+    } else {
+        build_tree(tree, a, b, P, s_parent, &s_deepest, tid, G::THREADS);
+    }
+    uint64_t mask[QT];
+    int depth[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        mask[qt] = (uint64_t)(uint32_t)__shfl((int)(small.mask >> 32), node[qt]) << 32 | (uint32_t)__shfl((int)small.mask, node[qt]);
+        depth[qt] = windowed ? __shfl(small.depth, node[qt]) : 0;
+    }
     if (windowed)
         lo_min = P - a.window + 1;
     w0 = max(tiles.sinks, tiles.sinks + ((windowed ? lo_min + tree.deepest : 0) + 31) / 32 - tiles.first);
@@ -900,20 +923,23 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
     RowState<QT, NDT> st;
     st.clear();
     if (t0 < t1)
-        deliver(t0);
-    request(t0 + 1);
+        deliver(even, t0);
+    request(even, t0 + 2);
 #pragma unroll
     for (int qt = 0; qt < QT; qt++)
 #pragma unroll
         for (int ks = 0; ks < NKS; ks++)
             asm volatile("" : "+v"(qf[qt][ks]));
     __syncthreads();
+    auto visible = [&](int qt, int j0) __attribute__((always_inline)) {
+        return T <= 64 ? visible_prefix(a, depth[qt], lo_min, P, j0) | visible_nodes(mask[qt], P, j0) : visible_keys(tree, a, node[qt], lo_min, P, j0);
+    };
     bool poisoned = false;
-    for (int t = t0; t < t1; t++) {
+    auto step = [&](Pieces &next, int t) __attribute__((always_inline)) {
         const uint16_t *stage = s_stage[(t - t0) & 1];
         if (t + 1 < t1)
-            deliver(t + 1);
-        request(t + 2);
+            deliver(next, t + 1);
+        request(next, t + 3);
         const bool whole = t >= w0 && t < w1;
         const int j0 = tiles.at(t) * 32;
         poisoned = poisoned || (!whole && s_strange[(t - t0) & 1] == t);
@@ -937,7 +963,7 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
             if (!whole) {
 #pragma unroll
                 for (int qt = 0; qt < QT; qt++)
-                    vis[qt] = visible_keys(tree, a, node[qt], lo_min, P, j0) >> (g * 4);
+                    vis[qt] = visible(qt, j0) >> (g * 4);
             }
             bf16x8 pf[QT];
             if (whole)
@@ -947,7 +973,15 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
             add_values<QT, NDT, VSTR>(stage + 32 * KSTR, pf, st, c, g);
         }
         __syncthreads();
+    };
+    // (no way out between two steps: the loads in flight at the loop's head have to be the same on every way there)
+    int t = t0;
+    for (; t + 1 < t1; t += 2) {
+        step(odd, t);
+        step(even, t + 1);
     }
+    if (t < t1)
+        step(odd, t);
     if (poisoned) {      // (the same for all waves) see window_attn_kernel
         uint16_t *tile = s_stage[0];
 #pragma unroll 1
@@ -971,7 +1005,7 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
             if (!idle) {
 #pragma unroll
                 for (int qt = 0; qt < QT; qt++)
-                    mark_strange<QT, NDT, VSTR>(tile, qt, visible_keys(tree, a, node[qt], lo_min, P, j0) >> (g * 4), st, c, g);
+                    mark_strange<QT, NDT, VSTR>(tile, qt, visible(qt, j0) >> (g * 4), st, c, g);
             }
             __syncthreads();
         }
