@@ -34,7 +34,7 @@ struct WindowArgs {
     int64_t s_max;
     int32_t n_q_heads, n_kv_heads, group, n_tree, mask_words, window, n_sink;
     int32_t n_rg, n_splits, n_units; // row groups of a KV head; key splits; B * Hkv * n_splits
-    uint32_t tree_magic;             // for quick_div by n_tree
+    uint32_t tree_magic, heads_magic; // for quick_div by n_tree, by n_kv_heads
     float scale, scale_log2;
 };
 
@@ -1054,13 +1054,11 @@ __global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a, int row
 {
     constexpr int LPR = D / 4;
     const int rows = a.n_tree * a.group, n = a.n_splits;
-    const int64_t at = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+    const uint32_t stream = blockIdx.z * UNITS_Y + blockIdx.y, f = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
     const int lane = threadIdx.x % LPR;
-    const int64_t stream = at / rows;
-    const int f = (int)(at - stream * rows);
-    if (stream * n >= a.n_units)
+    if (stream * n >= (uint32_t)a.n_units || f >= (uint32_t)rows)
         return;
-    const int64_t slot = stream * n * rows_per_unit + f;
+    const int64_t slot = (int64_t)stream * n * rows_per_unit + f;
     // eight splits' loads at a time (behind the last: the first again, weighted with nothing)
     float m = -INFINITY, l = 0.0f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -1093,15 +1091,14 @@ __global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a, int row
             }
     }
     const float inv = l != 0.0f ? 1.0f / l : 0.0f;
-    const int kvh = (int)(stream % a.n_kv_heads), hq = kvh * a.group + f / a.n_tree, node = f % a.n_tree;
-    const int64_t b = stream / a.n_kv_heads;
+    const uint32_t b = quick_div(stream, a.heads_magic), head = quick_div(f, a.tree_magic), node = f - head * a.n_tree, hq = (stream - b * a.n_kv_heads) * a.group + head;
     bf16x4 r;
 #pragma unroll
     for (int e = 0; e < 4; e++)
         r[e] = (__bf16)(o[e] * inv);
-    *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(a.out) + ((b * a.n_tree + node) * a.n_q_heads + hq) * D + lane * 4) = r;
+    *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(a.out) + (((int64_t)b * a.n_tree + node) * a.n_q_heads + hq) * D + lane * 4) = r;
     if (a.lse && lane == 0)
-        a.lse[(b * a.n_q_heads + hq) * a.n_tree + node] = l != 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        a.lse[((int64_t)b * a.n_q_heads + hq) * a.n_tree + node] = l != 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
 // float32 queries and rows (the small configuration): one workgroup of 4 waves per (node, head, sequence), D / 4 lanes a key, each with 4 channels; every wave keeps a state
@@ -1356,8 +1353,9 @@ int launch(WindowArgs &a, const WindowPlan &p, hipStream_t st)
         return rc;
     if (p.n_splits == 1)
         return DREAM_OK;
-    const int64_t rows = p.n_units / p.n_splits * a.n_tree * a.group;
-    hipLaunchKernelGGL(window_merge_kernel<D>, dim3((unsigned)((rows + 1024 / D - 1) / (1024 / D))), dim3(256), 0, st, a, p.n_rg * (p.shared ? 8 : 1) * p.qt * 16);
+    const int64_t streams = p.n_units / p.n_splits, rows = (int64_t)a.n_tree * a.group, at_once = 1024 / D;
+    const dim3 merge((unsigned)((rows + at_once - 1) / at_once), (unsigned)(streams < UNITS_Y ? streams : UNITS_Y), (unsigned)((streams + UNITS_Y - 1) / UNITS_Y));
+    hipLaunchKernelGGL(window_merge_kernel<D>, merge, dim3(256), 0, st, a, p.n_rg * (p.shared ? 8 : 1) * p.qt * 16);
     return check_launch("window_merge_kernel");
 }
 
@@ -1425,6 +1423,7 @@ int run(const char *who, const dream_attn_desc *d, bool mx, WindowArgs &a, int64
     a.n_q_heads = d->n_q_heads; a.n_kv_heads = d->n_kv_heads; a.group = d->n_q_heads / d->n_kv_heads;
     a.mask_words = ceil_div(a.n_tree, 64);
     a.tree_magic = magic_of(a.n_tree);
+    a.heads_magic = magic_of(a.n_kv_heads);
     a.n_rg = p.n_rg; a.n_splits = p.n_splits; a.n_units = (int32_t)p.n_units;
     a.scale = d->scale != 0.0f ? d->scale : 1.0f / sqrtf((float)d->head_dim);
     a.scale_log2 = a.scale * 1.4426950408889634f;
