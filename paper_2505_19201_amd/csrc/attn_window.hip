@@ -400,6 +400,17 @@ __device__ __forceinline__ u32x4 strange_places(u32x4 x)
     return x;
 }
 
+// Workgroup ids that are congruent mod 8 run on one XCD.  Row groups of one unit (a stream's share of the keys) meet in one XCD's L2, or, where there are so few units that XCDs would stay
+// without, in that of 2, 4 or 8.
+struct Place {
+    uint32_t unit, rg;
+};
+__device__ __forceinline__ Place place_of(uint32_t heads_splits)
+{
+    const uint32_t lg = heads_splits >> 24, part = (blockIdx.z * UNITS_Y + blockIdx.y) * 8 + (blockIdx.x & 7);
+    return {part >> lg, (blockIdx.x >> 3) << lg | (part & ((1u << lg) - 1))};
+}
+
 template <int D, int QT, int NW, bool MX>
 struct WindowGeom {
     static constexpr int VSTR = D + 16;                          // V row stride in LDS (values): four consecutive rows land 8 banks apart
@@ -423,9 +434,8 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
     __shared__ int32_t s_depth[DREAM_MAX_TREE], s_parent[DREAM_MAX_TREE], s_deepest;
     __shared__ float s_ml[NW][QT][2][16];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
-    // row groups of one share of the keys have ids that are congruent mod 8, so that they meet in one XCD's L2
-    const uint32_t unit = (blockIdx.z * UNITS_Y + blockIdx.y) * 8 + (blockIdx.x & 7), rg = blockIdx.x >> 3;
-    const uint32_t n_heads = heads_splits & 0xffff, lg_splits = heads_splits >> 16, n_splits = 1u << lg_splits;
+    const Place place = place_of(heads_splits);
+    const uint32_t unit = place.unit, rg = place.rg, n_heads = heads_splits & 0xffff, lg_splits = heads_splits >> 16 & 0xff, n_splits = 1u << lg_splits;
     const int T = tree_units & 0x1ff;
     const bool windowed = tree_units & 0x200;
     if (unit >= tree_units >> 10)
@@ -539,6 +549,8 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
 
     // the queries of this workgroup's rows: row f of a KV head is node f % T of its head f / T
     const uint32_t rows = T * a.group;
+    if (rg * QT * 16 >= rows)
+        return;
     bf16x8 qf[QT][NKS];
     int node[QT];
 #pragma unroll
@@ -784,8 +796,8 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
     __shared__ uint64_t s_mask[DREAM_MAX_TREE * 4];
     __shared__ int32_t s_depth[DREAM_MAX_TREE], s_parent[DREAM_MAX_TREE], s_deepest, s_strange[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
-    const uint32_t unit = (blockIdx.z * UNITS_Y + blockIdx.y) * 8 + (blockIdx.x & 7), rg = blockIdx.x >> 3;
-    const uint32_t n_heads = heads_splits & 0xffff, lg_splits = heads_splits >> 16, n_splits = 1u << lg_splits;
+    const Place place = place_of(heads_splits);
+    const uint32_t unit = place.unit, rg = place.rg, n_heads = heads_splits & 0xffff, lg_splits = heads_splits >> 16 & 0xff, n_splits = 1u << lg_splits;
     if (unit >= tree_units >> 10)
         return;
     const uint32_t stream = unit >> lg_splits, split = unit & (n_splits - 1);
@@ -884,6 +896,8 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
     request(even, t0);
     request(odd, t0 + 1);
     const uint32_t rows = T * a.group;
+    if (rg * G::NW * QT * 16 >= rows)
+        return;
     bf16x8 qf[QT][NKS];
     int node[QT];
     const bool idle = ((rg * G::NW + wave) * QT) * 16 >= rows;   // (a wave without rows only brings keys)
@@ -1344,10 +1358,14 @@ template <int D, bool MX>
 int launch(WindowArgs &a, const WindowPlan &p, hipStream_t st)
 {
     auto *kernel = kernel_of<D, MX>(p);
-    const int64_t eights = (p.n_units + 7) / 8;
-    const dim3 grid(8 * p.n_rg, (unsigned)(eights < UNITS_Y ? eights : UNITS_Y), (unsigned)((eights + UNITS_Y - 1) / UNITS_Y));
+    // the fewest XCDs to a unit with which the busiest one has at most a fifth more than its share (2 KV heads, 125 row groups each: 104 us on two XCDs, 36 on eight)
+    int lg = 0;
+    while (lg < 3 && 2 << lg <= p.n_rg && 5 * 8 * (((p.n_units << lg) + 7) / 8) > 6 * (p.n_units << lg))
+        lg++;
+    const int64_t eights = ((p.n_units << lg) + 7) / 8;
+    const dim3 grid(8 * ((p.n_rg + (1 << lg) - 1) >> lg), (unsigned)(eights < UNITS_Y ? eights : UNITS_Y), (unsigned)((eights + UNITS_Y - 1) / UNITS_Y));
     hipLaunchKernelGGL(kernel, grid, dim3(p.shared ? 512 : 64 * p.nw), 0, st, static_cast<const uint8_t *>(a.k), static_cast<const uint8_t *>(a.v), a.k_scales, a.v_scales, a.prefix_len,
-                       (uint32_t)a.s_max, (uint32_t)a.n_kv_heads | (uint32_t)__builtin_ctz(p.n_splits) << 16, magic_of(a.n_kv_heads),
+                       (uint32_t)a.s_max, (uint32_t)a.n_kv_heads | (uint32_t)__builtin_ctz(p.n_splits) << 16 | (uint32_t)lg << 24, magic_of(a.n_kv_heads),
                        (uint32_t)a.n_tree | (a.window ? 0x200u : 0u) | (uint32_t)p.n_units << 10, a);
     if (int rc = check_launch("window_attn_kernel"))
         return rc;
