@@ -1224,21 +1224,22 @@ struct WindowPlan {
 // Which kernel a call takes, and into how many parts its keys are split, is what is estimated to take the shortest.  Where one workgroup is on a CU a wave's steps cost what one takes to come
 // through; where many are, what the CU can issue; whichever is more:
 //     us = base + per_group * groups + steps * max(latency, issue * groups)  [+ many_nodes]  [+ 2.3 + 0.11 * splits + 1e-6 * head_dim * rows of parts, for the join]
-// with groups the workgroups (of four waves) a CU gets, steps those of a wave.  The constants are fitted to times of every kernel with every split from 1 to 64 in powers of two over 7 head
-// layouts x batches of 1, 4, 16, 64 x trees of 1, 16, 60, 250 x 40 to 40000 keys, 528 shapes of 4-bit and 516 of 16-bit caches.  Over these the choice takes 2.5 % and 2.0 % longer than the
-// fastest in the geometric mean, 14 % and 12 % at the 95th percentile.  Without the shared kernel the fastest would take 6 % (4-bit) and 34 % (16-bit) longer, without several query tiles to a
-// wave 2 % and 1 %, without the eight-wave form 2 % with 4-bit caches; with 16-bit ones it brought 0.2 % and is left out, as is the shared kernel over 4-bit caches at head_dim 64 (0.1 %).
+// with groups the workgroups (of four waves) a CU gets, steps those of a wave.  The constants are those with which the choice is best over measured times of every kernel with every split from
+// 1 to 64 in powers of two, over 7 head layouts x batches of 1, 4, 16, 64 x trees of 1, 16, 60, 250 x 40 to 40000 keys, 528 shapes of 4-bit and 516 of 16-bit caches: 0.8 % and 0.5 % behind
+// the fastest in the geometric mean, 5 % and 3 % at the 95th percentile, 34 % at most.  What the forms are
+// worth there (4-bit, 16-bit): the fastest would take 4 % and 30 % longer without the shared kernel, 5 % and 1.5 % without several query tiles to a wave, 33 % and 57 % without splits, and
+// 1 % without the eight-wave form over 4-bit caches; over 16-bit ones that brought 0.2 % and is left out, as is the shared kernel over 4-bit caches at head_dim 64 (0.1 %).
 struct Steps {
     float base, per_group, latency, latency_tile, issue, issue_tile, many_nodes;      // window_attn_kernel; .._tile: for each query tile of a wave
     float s_base, s_per_group, s_latency, s_issue, s_many_nodes;                      // window_shared_kernel
 };
 
-constexpr Steps STEPS[2][3] = {{{3.5f, 0.55f, 0.35f, 0.20f, 0.74f, 0.00f, 2.1f, 4.4f, 0.35f, 0.72f, 0.56f, 9.9f},
-                                {2.7f, 1.1f, 0.35f, 0.20f, 0.88f, 0.71f, 2.0f, 5.1f, 1.3f, 0.78f, 0.69f, 4.8f},
-                                {0.52f, 5.0f, 0.35f, 0.20f, 2.4f, 0.62f, 2.0f, 1.5f, 8.0f, 1.3f, 1.3f, 2.3f}},
-                               {{3.6f, 0.61f, 0.23f, 0.19f, 0.13f, 0.15f, 3.2f, 0.f, 0.f, 0.f, 0.f, 0.f},
-                                {2.9f, 1.3f, 0.47f, 0.22f, 0.42f, 0.13f, 6.3f, 4.3f, 2.1f, 0.80f, 0.57f, 6.2f},
-                                {4.0f, 1.4f, 0.35f, 0.20f, 1.1f, 0.31f, 4.6f, 4.3f, 5.5f, 0.43f, 1.5f, 3.1f}}};
+constexpr Steps STEPS[2][3] = {{{3.9f, 0.66f, 0.48f, 0.11f, 0.65f, 0.00f, 3.1f, 1.1f, 4.3f, 0.72f, 0.82f, 4.8f},
+                                {2.6f, 0.63f, 0.35f, 0.33f, 1.3f, 0.42f, 0.0f, 1.3f, 3.7f, 0.62f, 0.71f, 7.1f},
+                                {0.54f, 5.1f, 0.35f, 0.20f, 2.3f, 0.59f, 2.9f, 0.03f, 8.7f, 1.4f, 1.4f, 2.2f}},
+                               {{2.7f, 0.56f, 0.37f, 0.11f, 0.093f, 0.099f, 2.1f, 0.f, 0.f, 0.f, 0.f, 0.f},
+                                {3.3f, 2.1f, 0.24f, 0.25f, 0.15f, 0.22f, 1.6f, 2.4f, 3.0f, 0.012f, 1.0f, 4.2f},
+                                {5.1f, 0.87f, 1.1f, 0.097f, 0.85f, 0.14f, 2.4f, 3.0f, 4.2f, 0.51f, 1.1f, 3.5f}}};
 
 // query tiles a wave of window_attn_kernel may have, and those of window_shared_kernel's (0: there is none)
 constexpr int most_tiles(int D, bool mx) { return D == 64 ? (mx ? 4 : 2) : D == 128 && mx ? 2 : 1; }
