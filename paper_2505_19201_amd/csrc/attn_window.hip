@@ -9,7 +9,18 @@
 //   S^T = K Q^T   v_mfma_f32_16x16x32_bf16 with the keys as A operand.  The order of the channels is free as long as both operands agree, so a lane takes what it can load at
 //                 once: of a 4-bit row 16 bytes, the 32 channels of one scale, which go from memory through v_cvt_scalef32_pk_bf16_fp4 (exact: code times power of two) straight into the operand.
 //   O^T += V^T P^T   the scores' registers, as bf16, are the B operand; V needs turning, so a wave writes its rows (as bf16) to LDS that is its own and reads them transposed.
-// A row of 4 bits is turned into bf16 once for all QT tiles of a wave.
+// A row of 4 bits is turned into bf16 once for all QT tiles of a wave.  (The matrix instruction that takes 4-bit operands beside 8-bit ones, with the queries as two parts, drops what lies 2^13
+// below its largest product; the scores would be off by more than the rounding of bf16 rows allows.)
+//
+// What bounds it: a wave issues a vector instruction every 6 clocks alone and every 3.5 to 5.5 beside a second one, a scalar one every 10; a step over 32 keys is some 200 to 340 of them
+// (head_dim 128, one query tile: 1500 clocks), and before the first lie the arguments, the prefix length, the tree and the first tile from memory, 4200 clocks.  Measured, one call of a
+// graph, against 5.2 TB/s for a large copy and 1390 TFLOP/s for a large matrix product:
+//   4-bit   B 1, 32 heads of 128, 60 nodes, 704 keys     7.6 us    (read and written: 4.3 MB, 0.8 us; a kernel that does nothing 1.6 us)
+//           B 8, 32 heads on 8, 128, 60 nodes, 1283     19.7 us    (8.1 GFLOP, 5.8 us)
+//           B 32, 32 heads of 64, 60 nodes, 1600        46.1 us    (131 MB, 25 us; 26 GFLOP, 19 us)
+//           B 4, 32 heads on 8, 128, 1 node, 32700      30.3 us    (122 MB, 24 us)
+//   16-bit  B 4, 8 heads on 4, 256, 33 nodes, window 1024 of 1283    22.5 us    (36 MB, 7.0 us; parts of 8 splits, written and read: 17 MB, 3.3 us)
+//           B 1, 32 heads of 128, 1 node, window 1020 and 4 first tokens    10.8 us    (17 MB, 3.3 us; two launches)
 #include <type_traits>
 #include "common.h"
 
@@ -420,6 +431,8 @@ struct WindowGeom {
     static constexpr int WAVES = MX ? (D == 64 ? (QT == 1 ? 4 : QT == 2 ? 3 : 2) : D == 128 ? (QT == 1 ? 3 : 2) : 2) : D == 64 ? (QT == 1 ? 4 : 3) : D == 128 ? 2 : 1;
 };
 
+// Key tiles shared out over NW waves: few rows read the same keys, so what counts is that many waves have a tile each on its way.  Each wave asks for its next tile as soon as a tile's
+// registers are free (two, three or four tiles ahead brought nothing: code that is unrolled for them costs what waiting less wins; lines touched two steps ahead, into the L2, neither).
 // What stands ahead of a launch's first loads comes as plain arguments, the 14 dwords that are in scalar registers when a wave starts.
 template <int D, int QT, int NW, bool MX>
 __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void window_attn_kernel(const uint8_t *k, const uint8_t *v, const uint8_t *k_scales, const uint8_t *v_scales,
@@ -772,7 +785,7 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
 
 // All rows of a KV head in one workgroup, or as many as its eight waves hold.  What a CU can pull, 64 KB in flight, bounds a kernel whose workgroups for 16 rows each read the same keys, and so
 // does what it takes to turn 4 bits into 16: here a tile of 32 keys is read once, lies in LDS as bf16 and serves every wave's QT query tiles.  Two stages: while the waves work on one, the next
-// tile goes from registers to the other, and the one after that is on its way; one barrier a tile.  The keys are shared out over workgroups (splits), whose states window_merge_kernel joins.
+// tile goes from registers to the other, and the two after that are on their way (one: 24.2 us, two: 22.6, at B 4, 8 heads on 4 of 256, 33 nodes, 1024 keys); one barrier a tile.  The keys are shared out over workgroups (splits), whose states window_merge_kernel joins.
 template <int D, int QT, bool MX>
 struct SharedGeom {
     static constexpr int NW = 8, THREADS = 512;
@@ -1062,7 +1075,8 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
     }
 }
 
-// The states of a row's key splits, in their order.  D / 4 lanes a row.
+// The states of a row's key splits, in their order.  D / 4 lanes a row.  What other XCDs wrote comes from memory: 2.2 to 5 us with the launch.  (A row's splits over several waves that meet in
+// LDS took longer: 5.6 instead of 4.7 us for 1056 rows of 256 with 8 splits, 2.6 instead of 2.2 for 32 rows of 128.)
 template <int D>
 __global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a, int rows_per_unit)
 {

@@ -8,7 +8,7 @@
 //
 // All three calls only move bytes.  Append: a lane takes 16 bytes of a row; the lanes that share a scale are neighbours (4 for bf16, 8 for float32) and find their
 // maximum by moves between registers.  A workgroup takes consecutive rows of one head, whose codes and scales are consecutive in the cache.
-// Roofline: HBM; for the rows of a tree the launch.
+// Roofline: HBM, 531 MB in 101 us (5.2 TB/s, what a large copy reaches); for the rows of a tree the launch: 33 rows of 4 heads of 256 in 2.2 us, a kernel that does nothing 1.6.
 #include <type_traits>
 #include "common.h"
 
