@@ -366,7 +366,8 @@ int dream_rotary_rows(const dream_attn_desc *desc, const dream_rotary_job *jobs,
  *   codes   [B, Hkv, s_max, D / 2] bytes, 16-byte aligned: the value of even index in the low half.  A code
  *           is a sign and three bits for 0, 0.5, 1, 1.5, 2, 3, 4, 6.
  *   scales  [B, Hkv, s_max, D / DREAM_MX_GROUP] bytes, 8-byte aligned: 2^(byte - 127) for 32 values,
- *           255 for NaN (whatever the codes).  A value is its code times its scale.
+ *           255 for NaN (whatever the codes).  A value is its code times its scale.  Bytes 0, 1, 253 and 254
+ *           (values that bf16 does not hold as normal numbers) must not stand in rows that are read or seen.
  *   D in {64, 128, 256}; desc->dtype (f32 or bf16) is that of rows.
  * dream_mx_append: rows k_rows, v_rows [B, n_rows, Hkv, D], 16-byte aligned, are rounded into the caches at
  *   rows row_base[b] + (row_index ? row_index[b, r] : r); a destination row outside [0, s_max) is dropped,

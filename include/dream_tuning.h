@@ -24,7 +24,7 @@ void dream_set_q_tiles(int32_t q_tiles);
 /* Waves per workgroup of the shared-tile kernel: 4 = never one of the 8-wave forms, 8 = one wherever it exists (bf16, unsplit
  * key range: one workgroup per KV head at head_dim >= 128 with 5 query tiles or more, two key groups at head_dim <= 128),
  * 0 = automatic.
- * The calls with a window or over a 4-bit cache obey all three: splits up to 64; query tiles of a wave of the kernel without
+ * The calls with a window or over a 4-bit cache obey all three: splits as the power of two at or below, up to 64; query tiles of a wave of the kernel without
  * shared tiles (as many as it has at that head_dim); 4 = that kernel with 4 waves, 8 = the kernel with shared tiles where it
  * exists, and with dream_set_q_tiles(1) the other one's eight-wave form where that exists. */
 void dream_set_tile_waves(int32_t waves);

@@ -1287,7 +1287,7 @@ void every_choice(const dream_attn_desc *d, bool mx, int tiles, int64_t steps, F
         if (has_eight && !four && !(eight && !forced && in_shared))
             offer({false, qt, 8});
     }
-    if (in_shared && !four && !forced)
+    if (in_shared && !four && !forced && (eight || tiles > 2))       // (fewer tiles leave most of its waves idle: never measured, never taken)
         offer({true, in_shared, 8});
 }
 
