@@ -254,7 +254,7 @@ def dream_project_rows_multi(desc: AttnDesc, jobs, n_rows: int, hidden: int, str
 def dream_rotary_rows(desc: AttnDesc, jobs, n_rows: int, pos, pos_base, parent, inv_freq, rot_dim: int, interleaved: bool = False,
                       amplitude: float = 1.0, stream=None) -> None:
     """jobs: sequence of (x, n_heads, row_base, row_index, out)."""
-    jobs = tuple(tuple(job) for job in jobs)         # (see dream_kv_commit)
+    jobs = tuple(map(tuple, jobs))         # (see dream_kv_commit)
     _check(_native().dream_rotary_rows(desc, jobs, len(jobs), n_rows, pos, pos_base, parent, inv_freq, rot_dim, int(interleaved), amplitude,
                                        _stream(stream)))
 

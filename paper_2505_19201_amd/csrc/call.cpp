@@ -214,6 +214,7 @@ struct WithoutGil {
 
 // What the rotary, 4-bit and window calls want of their tensors, checked before the call: the type, at least so many values, and the current device (the one the call is made on).  A
 // None is the library's to accept or refuse, and so are sizes that are not positive.
+thread_local c10::DeviceIndex current_device = -1;      // of this call; -1: not asked for yet (Sizes)
 void want(PyObject *o, const char *name, __int128 values, at::ScalarType type, at::ScalarType also)
 {
     if (!THPVariable_Check(o))
@@ -229,7 +230,9 @@ void want(PyObject *o, const char *name, __int128 values, at::ScalarType type, a
         PyErr_Format(PyExc_ValueError, "%s: %lld values expected, not %lld", name, (long long)values, (long long)t.numel());
         throw Failed();
     }
-    if (t.device() != c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice()) {
+    if (current_device < 0)
+        current_device = c10::impl::VirtualGuardImpl(c10::DeviceType::CUDA).getDevice().index();
+    if (t.device().index() != current_device) {
         PyErr_Format(PyExc_ValueError, "%s: is not on the current device", name);
         throw Failed();
     }
@@ -255,6 +258,7 @@ struct Sizes {
     {
         const Arg<const dream_attn_desc *> desc(o);
         d = *desc.value;
+        current_device = -1;
         type = d.dtype == DREAM_F32 ? at::kFloat : at::kBFloat16;
         b = d.batch; hq = d.n_q_heads; hkv = d.n_kv_heads; dim = d.head_dim;
         row = b * hkv * d.s_max;
