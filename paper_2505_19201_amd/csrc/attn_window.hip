@@ -528,6 +528,8 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
     // What a wave waits for one after the other is most of a short call: the arguments, the prefix length, the tree, the queries, the first tile.  So all are requested as soon as their
     // addresses are known, and the tree, which needs the parents only, is built meanwhile.
     const bool walk = T <= 64 && (!a.tree_mask || windowed);
+    // (requested together, not where each is used: every trip to memory that is waited for here is 600 clocks)
+    asm volatile("" ::"s"(prefix), "s"(a.q), "s"(a.tree_magic), "s"(a.group), "s"(a.n_q_heads), "s"(a.scale_log2));
     int parent = 0;
     if (walk)
         parent = a.parent[(int64_t)b * T + min(lane, T - 1)];
