@@ -132,9 +132,10 @@ __global__ __launch_bounds__(256) void mx_read_kernel(ReadArgs a)
     reinterpret_cast<u32x4 *>(a.out)[row * PER_ROW + piece] = v;
 }
 
-// dream_mx_commit: the codes and scales of the accepted path's rows become the next rows of the prefix, in place.  One workgroup per (head, sequence, cache): what is to move, a few
-// hundred bytes to a few KB, is in registers before anything is written.  A row is D / 32 pieces of 16 bytes of codes and one piece of D / 32 bytes of scales.
-constexpr int MOVES = 8;            // pieces a thread holds: 2048 a workgroup
+// dream_mx_commit: the codes and scales of the accepted path's rows become the next rows of the prefix, in place.  A head of a sequence in a cache is moved by one wave, or, where the longest
+// path has more pieces than four for each of its lanes, by a workgroup: what is to move, a few hundred bytes to a few KB, is in registers before anything is written.  A row is D / 32 pieces of
+// 16 bytes of codes and one piece of D / 32 bytes of scales.  (16 caches of 8 sequences of 32 heads of 64, paths of up to 7 rows: 4.8 us, with a workgroup a head 17.9.)
+constexpr int WAVE_MOVES = 4, GROUP_MOVES = 8;            // pieces a lane holds
 
 struct CommitArgs {
     uint8_t *codes[MAX_CACHES], *scales[MAX_CACHES];
@@ -144,12 +145,16 @@ struct CommitArgs {
     int32_t n_heads, n_tree, path_stride, first_cache;
 };
 
-template <int D>
+// LANES: 64 or 256 to a head
+template <int D, int LANES>
 __global__ __launch_bounds__(256) void mx_commit_kernel(CommitArgs a)
 {
+    constexpr int MOVES = LANES == 64 ? WAVE_MOVES : GROUP_MOVES;
     constexpr int CPR = D / GROUP, PPR = CPR + 1;
     using Scales = std::conditional_t<D == 64, uint16_t, std::conditional_t<D == 128, uint32_t, uint64_t>>;
-    const int h = blockIdx.x, b = blockIdx.y, ci = blockIdx.z, tid = threadIdx.x;
+    const int h = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, b = blockIdx.y, ci = blockIdx.z, tid = threadIdx.x % LANES;
+    if (h >= a.n_heads)
+        return;
     const int32_t *path = a.path + (int64_t)b * a.path_stride;
     const int P = (int)min((int64_t)max(a.prefix_len[b], 0), a.s_max - a.n_tree);
     const int n = min(max(a.accept_len[b], 0), min(a.path_stride, a.n_tree) - 1);
@@ -163,7 +168,7 @@ __global__ __launch_bounds__(256) void mx_commit_kernel(CommitArgs a)
     Scales s[MOVES];
 #pragma unroll
     for (int i = 0; i < MOVES; i++) {
-        const int idx = tid + i * 256;
+        const int idx = tid + i * LANES;
         if (idx < total) {
             const int j = idx / PPR, c = idx % PPR;
             const int node = min(max(path[j], 0), a.n_tree - 1);
@@ -174,10 +179,11 @@ __global__ __launch_bounds__(256) void mx_commit_kernel(CommitArgs a)
         }
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();   // every source of this head is in a register
+    if (LANES > 64)
+        __syncthreads();   // every source of this head is in a register
 #pragma unroll
     for (int i = 0; i < MOVES; i++) {
-        const int idx = tid + i * 256;
+        const int idx = tid + i * LANES;
         if (idx < total) {
             const int j = idx / PPR, c = idx % PPR;
             if (c < CPR)
@@ -210,6 +216,8 @@ bool unaligned(const void *codes, const void *scales)
 
 template <class T>
 auto append_kernel(int d) { return d == 64 ? &mx_append_kernel<T, 64> : d == 128 ? &mx_append_kernel<T, 128> : &mx_append_kernel<T, 256>; }
+template <int LANES>
+auto commit_kernel(int d) { return d == 64 ? &mx_commit_kernel<64, LANES> : d == 128 ? &mx_commit_kernel<128, LANES> : &mx_commit_kernel<256, LANES>; }
 template <class T>
 auto read_kernel(int d) { return d == 64 ? &mx_read_kernel<T, 64> : d == 128 ? &mx_read_kernel<T, 128> : &mx_read_kernel<T, 256>; }
 
@@ -303,7 +311,8 @@ int dream_mx_commit(const dream_attn_desc *desc, void *const *codes_host, void *
     if (prefix_len_out == prefix_len)
         return fail(DREAM_ERR_INVALID_ARG, "%s: prefix_len_out must not alias prefix_len", who);
     const int64_t max_rows = path_stride < n_tree ? path_stride : n_tree;
-    if (max_rows * (desc->head_dim / GROUP + 1) > 256 * MOVES)
+    const int64_t pieces = max_rows * (desc->head_dim / GROUP + 1);
+    if (pieces > 256 * GROUP_MOVES)
         return fail(DREAM_ERR_UNSUPPORTED, "%s: a path of %lld rows is longer than a workgroup moves", who, (long long)max_rows);
     for (int32_t i = 0; i < n_caches; i++) {
         if (!codes_host[i] || !scales_host[i])
@@ -320,8 +329,9 @@ int dream_mx_commit(const dream_attn_desc *desc, void *const *codes_host, void *
         }
         a.prefix_len = prefix_len; a.path = accept_path; a.accept_len = accept_len; a.prefix_len_out = prefix_len_out;
         a.s_max = desc->s_max; a.n_heads = desc->n_kv_heads; a.n_tree = n_tree; a.path_stride = path_stride; a.first_cache = first;
-        auto *kernel = desc->head_dim == 64 ? &mx_commit_kernel<64> : desc->head_dim == 128 ? &mx_commit_kernel<128> : &mx_commit_kernel<256>;
-        hipLaunchKernelGGL(kernel, dim3(desc->n_kv_heads, desc->batch, m), dim3(256), 0, as_stream(stream), a);
+        const bool wave = pieces <= 64 * WAVE_MOVES;
+        auto *kernel = wave ? commit_kernel<64>(desc->head_dim) : commit_kernel<256>(desc->head_dim);
+        hipLaunchKernelGGL(kernel, dim3(wave ? (desc->n_kv_heads + 3) / 4 : desc->n_kv_heads, desc->batch, m), dim3(256), 0, as_stream(stream), a);
         if (int rc = check_launch("mx_commit_kernel"))
             return rc;
     }
