@@ -827,11 +827,13 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
     if (tid < 2)
         s_strange[tid] = -1;
 
+    const int prefix = scalar_load(prefix_len + b);
     const bool walk = T <= 64 && (!a.tree_mask || windowed);
+    asm volatile("" ::"s"(prefix), "s"(a.q), "s"(a.tree_magic), "s"(a.group), "s"(a.n_q_heads), "s"(a.scale_log2));      // (requested together: see window_attn_kernel)
     int parent = 0;
     if (walk)
         parent = a.parent[(int64_t)b * T + min(lane, T - 1)];
-    const int P = min(max(scalar_load(prefix_len + b), 0), (int)s_max - T);
+    const int P = min(max(prefix, 0), (int)s_max - T);
     const Tiles tiles = tiles_of(a, P);
     const int per = n_splits == 1 ? tiles.count : (tiles.count + n_splits - 1) >> lg_splits;
     const int t0 = split * per, t1 = min(tiles.count, t0 + per);
