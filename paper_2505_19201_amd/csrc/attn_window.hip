@@ -21,6 +21,7 @@
 //           B 4, 32 heads on 8, 128, 1 node, 32700      30.3 us    (122 MB, 24 us)
 //   16-bit  B 4, 8 heads on 4, 256, 33 nodes, window 1024 of 1283    22.5 us    (36 MB, 7.0 us; parts of 8 splits, written and read: 17 MB, 3.3 us)
 //           B 1, 32 heads of 128, 1 node, window 1020 and 4 first tokens    10.8 us    (17 MB, 3.3 us; two launches)
+#include <cfloat>
 #include <type_traits>
 #include "common.h"
 
@@ -337,10 +338,11 @@ __device__ __forceinline__ void softmax_tile(f32x4 (&s)[2][QT], RowState<QT, NDT
     if constexpr (WHOLE) {
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
+            const float ref = fmaxf(st.m[qt], -FLT_MAX);      // where all scores so far are -inf, their weight is 0 and not exp(-inf + inf)
             sum[qt] = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][qt][e & 3], scale_log2, -st.m[qt]));
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e >> 2][qt][e & 3], scale_log2, -ref));
                 sum[qt] += p;
                 pf[qt][e] = (__bf16)p;
             }
