@@ -24,6 +24,7 @@
 #include <cfloat>
 #include <type_traits>
 #include "common.h"
+#include "quick_div.h"
 
 using namespace dream;
 

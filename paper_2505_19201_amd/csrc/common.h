@@ -43,10 +43,6 @@ typedef unsigned int u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
-// x / d for x * d below 2^32 by one multiplication (a division is some 20 instructions): magic_of(d), 0 for d = 1
-inline uint32_t magic_of(uint32_t d) { return d == 1 ? 0u : (uint32_t)(((1ull << 32) + d - 1) / d); }
-__device__ __forceinline__ uint32_t quick_div(uint32_t x, uint32_t magic) { return magic ? __umulhi(x, magic) : x; }
-
 __device__ __forceinline__ float bf16_bits_to_float(uint16_t b) { return __uint_as_float(((uint32_t)b) << 16); }
 
 // LDS traffic inside one wave needs no barrier, only program order.

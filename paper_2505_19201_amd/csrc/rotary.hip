@@ -11,6 +11,7 @@
 // 64 heads of 128 in 3.7 us (with one workgroup a row 4.3; a kernel that does nothing 1.6), 0.4 us of them the walk up the tree.
 #include <type_traits>
 #include "common.h"
+#include "quick_div.h"
 
 using namespace dream;
 
