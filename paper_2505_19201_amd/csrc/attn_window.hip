@@ -25,6 +25,7 @@
 #include <type_traits>
 #include "common.h"
 #include "quick_div.h"
+#include "window_maps.h"
 
 using namespace dream;
 
@@ -33,7 +34,6 @@ namespace {
 constexpr int GROUP = DREAM_MX_GROUP;
 constexpr float SLACK = 8.0f;      // octaves by which a score may exceed its row's reference
 constexpr int MAX_SPLITS = 64;
-constexpr int64_t MAX_ROWS = DREAM_MAX_WINDOW_ROWS;   // a head's rows are reached by 32-bit offsets of up to 512 bytes a row
 constexpr uint32_t UNITS_Y = 32768;   // units of a grid's second dimension, by eights
 
 struct WindowArgs {
@@ -205,21 +205,6 @@ __device__ __forceinline__ uint32_t visible_keys(const Tree &t, const WindowArgs
     return bits;
 }
 
-// The key tiles of a sequence, in the order they are taken: those of the sinks, then those from the root's window on.
-struct Tiles {
-    int sinks, first, count;
-    __device__ __forceinline__ int at(int i) const { return i < sinks ? i : i - sinks + first; }
-};
-__device__ __forceinline__ Tiles tiles_of(const WindowArgs &a, int P)
-{
-    Tiles t;
-    const int start = a.window ? max(0, P - a.window + 1) : 0;
-    t.sinks = a.window ? (min(a.n_sink, start) + 31) / 32 : 0;
-    t.first = max(start / 32, t.sinks);
-    t.count = t.sinks + (P + a.n_tree + 31) / 32 - t.first;
-    return t;
-}
-
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ bf16x8 from_codes(uint32_t codes, float scale)
@@ -258,7 +243,7 @@ template <int D, bool MX>
 struct Raw;
 template <int D>
 struct Raw<D, true> {
-    static constexpr int KP = D == 256 ? 2 : 1, VP = D / 64;     // pieces of a lane's K (of 16 keys; 16 bytes, at head_dim 64 8) and 16-byte pieces of its V
+    static constexpr int KP = WaveLoads<D, true>::K_PIECES, VP = WaveLoads<D, true>::V_PIECES;
     uint32_t k[2][D / 32];
     uint8_t ks[2][KP];
     u32x4 v[VP];
@@ -269,13 +254,6 @@ struct Raw<D, false> {
     u32x4 k[2][D / 32];
     u32x4 v[D / 16];
 };
-
-// First of the 8 channels of k-step ks that lane group g holds: of a 4-bit row consecutive runs of what it loads at once.
-template <int D, bool MX>
-__device__ __forceinline__ constexpr int channel_of(int ks, int g)
-{
-    return !MX ? ks * 32 + g * 8 : D == 64 ? g * 16 + ks * 8 : (ks >> 2) * 128 + g * 32 + (ks & 3) * 8;
-}
 
 // The state of a query tile: O^T (a lane owns query row c = lane % 16 and channels 16 dt + 4 (lane / 16) + r), the reference of its scores in octaves and the lane's share of the sum.
 template <int QT, int NDT>
@@ -444,7 +422,8 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
 {
     using G = WindowGeom<D, QT, NW, MX>;
     constexpr int NKS = D / 32, NDT = D / 16, VSTR = G::VSTR;
-    constexpr int ROWB = MX ? D / 2 : D * 2, SCB = D / GROUP;    // bytes of a row, and of its scales
+    using Loads = WaveLoads<D, MX>;
+    constexpr int ROWB = Loads::ROW, SCB = Loads::SCALES;        // bytes of a row, and of its scales
     __shared__ __attribute__((aligned(16))) uint8_t s_area[NW][G::AREA];
     __shared__ uint64_t s_mask[DREAM_MAX_TREE * 4];              // of more than 64 nodes
     __shared__ int32_t s_depth[DREAM_MAX_TREE], s_parent[DREAM_MAX_TREE], s_deepest;
@@ -468,8 +447,8 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
     // The pieces of a tile that this lane loads: K's as the matrix instruction has them, V's in the order of memory.  Every call has as many loads, so that what waits for one tile never
     // waits for another: behind the last live row, and for a tile that is not this workgroup's, they return zeros and go nowhere (the descriptors' bounds).  One descriptor a tensor
     // for the whole range: a scalar instruction costs a wave as long as ten vector lanes' work (a wave's scalar instructions issue every 10 clocks, its vector ones every 6).
-    constexpr int VPR = ROWB / 16, VPL = 32 * VPR / 64;          // pieces of a V row; of a lane's share of a tile
-    const int vrow = lane / VPR, vcol = lane % VPR;              // (and rows 64 / VPR apart)
+    constexpr int VPL = Loads::V_PIECES;
+    const int vrow = Loads::v_row(lane, 0), vcol = Loads::v_column(lane);
     struct Range {
         __amdgpu_buffer_rsrc_t k, v, ks, vs;
     };
@@ -483,23 +462,23 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
         }
         return r;
     };
-    const uint32_t k_at = c * ROWB + g * (MX && D == 64 ? 8 : 16), ks_at = c * SCB + (D == 64 ? g >> 1 : g);
+    const uint32_t k_at = Loads::k(c, g), ks_at = Loads::k_scale(c, g);
     auto request_k = [&](Raw<D, MX> &r, const Range &from, uint32_t tile) __attribute__((always_inline)) {
-        const uint32_t at = k_at + tile * (32 * ROWB);
+        const uint32_t at = k_at + tile * (TILE * ROWB);
 #pragma unroll
         for (int hh = 0; hh < 2; hh++) {
             if constexpr (!MX) {
 #pragma unroll
                 for (int ks = 0; ks < NKS; ks++)
-                    r.k[hh][ks] = __builtin_amdgcn_raw_buffer_load_b128(from.k, at + hh * 16 * ROWB + ks * 64, 0, 0);
+                    r.k[hh][ks] = __builtin_amdgcn_raw_buffer_load_b128(from.k, at + Loads::k_further(hh, ks), 0, 0);
             } else if constexpr (D == 64) {
-                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from.k, at + hh * 16 * ROWB, 0, 0);
+                const auto x = __builtin_amdgcn_raw_buffer_load_b64(from.k, at + Loads::k_further(hh, 0), 0, 0);
                 r.k[hh][0] = x[0];
                 r.k[hh][1] = x[1];
             } else {
 #pragma unroll
-                for (int i = 0; i < D / 128; i++) {
-                    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from.k, at + hh * 16 * ROWB + i * 64, 0, 0);
+                for (int i = 0; i < Loads::K_PIECES; i++) {
+                    const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(from.k, at + Loads::k_further(hh, i), 0, 0);
 #pragma unroll
                     for (int e = 0; e < 4; e++)
                         r.k[hh][i * 4 + e] = x[e];
@@ -507,24 +486,24 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
             }
         }
         if constexpr (MX) {
-            const uint32_t sat = ks_at + tile * (32 * SCB);
+            const uint32_t sat = ks_at + tile * (TILE * SCB);
 #pragma unroll
             for (int hh = 0; hh < 2; hh++)
 #pragma unroll
                 for (int i = 0; i < Raw<D, MX>::KP; i++)
-                    r.ks[hh][i] = __builtin_amdgcn_raw_buffer_load_b8(from.ks, sat + hh * 16 * SCB + i * 4, 0, 0);
+                    r.ks[hh][i] = __builtin_amdgcn_raw_buffer_load_b8(from.ks, sat + Loads::k_scale_further(hh, i), 0, 0);
         }
     };
     auto request_v = [&](Raw<D, MX> &r, const Range &from, uint32_t tile) __attribute__((always_inline)) {
-        const uint32_t at = lane * 16 + tile * (32 * ROWB);
+        const uint32_t at = Loads::v(lane) + tile * (TILE * ROWB);
 #pragma unroll
         for (int i = 0; i < VPL; i++)
-            r.v[i] = __builtin_amdgcn_raw_buffer_load_b128(from.v, at + i * 1024, 0, 0);
+            r.v[i] = __builtin_amdgcn_raw_buffer_load_b128(from.v, at + Loads::v_further(i), 0, 0);
         if constexpr (MX) {
-            const uint32_t sat = lane + tile * (32 * SCB);
+            const uint32_t sat = Loads::v_scale(lane) + tile * (TILE * SCB);
 #pragma unroll
             for (int i = 0; i < VPL; i++)
-                r.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(from.vs, sat + i * 64, 0, 0);
+                r.vs[i] = __builtin_amdgcn_raw_buffer_load_b8(from.vs, sat + Loads::v_scale_further(i), 0, 0);
         }
     };
 
@@ -540,7 +519,7 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
     const bool early = n_splits == 1 && !windowed;               // the first tile is known without the prefix length
     if (early) {
         const Range all = range_of(s_max);
-        const uint32_t tile = min((uint32_t)wave, (s_max + 31) / 32);
+        const uint32_t tile = early_tile(wave, s_max);
         request_k(raw, all, tile);
         request_v(raw, all, tile);
     }
@@ -550,13 +529,13 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
     uint32_t no_tile;                                            // behind the live rows
     auto tile_of = [&](int t) __attribute__((always_inline)) { return t < t1 ? (uint32_t)tiles.at(t) : no_tile; };
     auto find_tiles = [&]() __attribute__((always_inline)) {
-        P = min(max(prefix, 0), (int)s_max - T);                 // never past the cache, whatever the array holds
+        P = prefix_rows(prefix, s_max, T);
         tiles = tiles_of(a, P);
-        const int per = n_splits == 1 ? tiles.count : (tiles.count + n_splits - 1) >> lg_splits;
+        const int per = tiles_per_split(tiles.count, lg_splits);
         t0 = split * per + wave;
-        t1 = min(tiles.count, (int)(split * per) + per);
+        t1 = split_end(tiles.count, split, per);
         live = range_of(P + T);
-        no_tile = (P + T + 31) / 32;
+        no_tile = tile_behind(P + T);
     };
     if (!early) {
         find_tiles();
@@ -648,7 +627,7 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
             const uint32_t last = whole ? 255u : 252u;
 #pragma unroll
             for (int i = 0; i < VPL; i++) {
-                uint16_t *to = area + (vrow + i * (64 / VPR)) * VSTR + vcol * 32;
+                uint16_t *to = area + (vrow + Loads::v_row(0, i)) * VSTR + vcol * Loads::V_VALUES;
                 const uint32_t byte = raw.vs[i];
                 poisoned = poisoned || byte > last;
                 const float scale = scale_value(byte > last ? 0u : byte);
@@ -668,7 +647,7 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
             }
 #pragma unroll
             for (int i = 0; i < VPL; i++)
-                *reinterpret_cast<u32x4 *>(area + (vrow + i * (64 / VPR)) * VSTR + vcol * 8) = raw.v[i];
+                *reinterpret_cast<u32x4 *>(area + (vrow + Loads::v_row(0, i)) * VSTR + vcol * Loads::V_VALUES) = raw.v[i];
         }
         request_v(raw, live, next);
 
@@ -793,11 +772,9 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
 // tile goes from registers to the other, and the two after that are on their way (one: 24.2 us, two: 22.6, at B 4, 8 heads on 4 of 256, 33 nodes, 1024 keys); one barrier a tile.  The keys are shared out over workgroups (splits), whose states window_merge_kernel joins.
 template <int D, int QT, bool MX>
 struct SharedGeom {
-    static constexpr int NW = 8, THREADS = 512;
+    static constexpr int NW = 8, THREADS = GroupLoads<D, MX>::THREADS;
     static constexpr int KSTR = D + 8, VSTR = D + 16;            // row strides in LDS (values): 16-byte reads of K rows and transposing ones of V meet in no bank
     static constexpr int STAGE = 32 * (KSTR + VSTR);             // values
-    static constexpr int PIECE = MX ? D / 8 : 8;                 // values a thread loads at once
-    static constexpr int PER_ROW = D / PIECE;                    // pieces of a row
 };
 
 template <int D, int QT, bool MX>
@@ -805,11 +782,10 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
                                                                uint32_t s_max, uint32_t heads_splits, uint32_t heads_magic, uint32_t tree_units, WindowArgs a)
 {
     using G = SharedGeom<D, QT, MX>;
-    constexpr int NKS = D / 32, NDT = D / 16, KSTR = G::KSTR, VSTR = G::VSTR, PIECE = G::PIECE, PER_ROW = G::PER_ROW;
-    constexpr int ROWB = MX ? D / 2 : D * 2, SCB = D / GROUP;
-    constexpr int N = 32 * PER_ROW / G::THREADS > 0 ? 32 * PER_ROW / G::THREADS : 1;      // pieces of K of a thread, and of V; with fewer than threads, the threads share K and V out
-    constexpr bool HALVES = 32 * PER_ROW < G::THREADS;
-    static_assert(HALVES ? 64 * PER_ROW == G::THREADS : 32 * PER_ROW % G::THREADS == 0, "pieces");
+    using Loads = GroupLoads<D, MX>;
+    constexpr int NKS = D / 32, NDT = D / 16, KSTR = G::KSTR, VSTR = G::VSTR;
+    constexpr int ROWB = Loads::ROW, SCB = Loads::SCALES, N = Loads::PIECES;
+    constexpr bool HALVES = Loads::HALVES;
     __shared__ __attribute__((aligned(16))) uint16_t s_stage[2][G::STAGE];
     __shared__ uint64_t s_mask[DREAM_MAX_TREE * 4];
     __shared__ int32_t s_depth[DREAM_MAX_TREE], s_parent[DREAM_MAX_TREE], s_deepest, s_strange[2];
@@ -836,15 +812,15 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
     int parent = 0;
     if (walk)
         parent = a.parent[(int64_t)b * T + min(lane, T - 1)];
-    const int P = min(max(prefix, 0), (int)s_max - T);
+    const int P = prefix_rows(prefix, s_max, T);
     const Tiles tiles = tiles_of(a, P);
-    const int per = n_splits == 1 ? tiles.count : (tiles.count + n_splits - 1) >> lg_splits;
-    const int t0 = split * per, t1 = min(tiles.count, t0 + per);
+    const int per = tiles_per_split(tiles.count, lg_splits);
+    const int t0 = split * per, t1 = split_end(tiles.count, split, per);
 
     // a thread's pieces of a tile; loads of rows that are not there return zeros (see window_attn_kernel)
-    const bool second = HALVES && tid >= G::THREADS / 2;         // this thread takes V
-    const int ptid = HALVES ? tid % (G::THREADS / 2) : tid;
-    constexpr int BYTES = MX ? PIECE / 2 : 16;
+    const bool second = Loads::takes_v(tid);
+    const int ptid = Loads::thread(tid);
+    constexpr int BYTES = Loads::WIDTH;
     struct Part {
         u32x4 x[N];
         uint8_t scale[N];
@@ -856,27 +832,26 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
     const bool wave_second = HALVES && wave >= G::NW / 2;
     const auto first_rows = buffer_of(wave_second ? v : k, (P + T) * ROWB), second_rows = buffer_of(v, (P + T) * ROWB);
     const auto first_scales = buffer_of(wave_second ? v_scales : k_scales, (P + T) * SCB), second_scales = buffer_of(v_scales, (P + T) * SCB);
-    const uint32_t no_tile = (P + T + 31) / 32;                  // behind the live rows
+    const uint32_t no_tile = tile_behind(P + T);
     auto request = [&](Pieces &of, int t) __attribute__((always_inline)) {
         const uint32_t tile = t < t1 ? (uint32_t)tiles.at(t) : no_tile;
-        const uint32_t at = ptid * BYTES + tile * (32 * ROWB), scale_at = ptid * PIECE / GROUP + tile * (32 * SCB);
+        const uint32_t at = Loads::at(ptid) + tile * (TILE * ROWB), scale_at = Loads::scale(ptid) + tile * (TILE * SCB);
 #pragma unroll
         for (int half = 0; half < (HALVES ? 1 : 2); half++) {
 #pragma unroll
             for (int i = 0; i < N; i++) {
                 const auto rows_at = half ? second_rows : first_rows;
-                const int more = i * G::THREADS;
                 if constexpr (BYTES == 16) {
-                    of.part[half].x[i] = __builtin_amdgcn_raw_buffer_load_b128(rows_at, at + more * BYTES, 0, 0);
+                    of.part[half].x[i] = __builtin_amdgcn_raw_buffer_load_b128(rows_at, at + Loads::further(i), 0, 0);
                 } else if constexpr (BYTES == 8) {
-                    const auto y = __builtin_amdgcn_raw_buffer_load_b64(rows_at, at + more * BYTES, 0, 0);
+                    const auto y = __builtin_amdgcn_raw_buffer_load_b64(rows_at, at + Loads::further(i), 0, 0);
                     of.part[half].x[i][0] = y[0];
                     of.part[half].x[i][1] = y[1];
                 } else {
-                    of.part[half].x[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rows_at, at + more * BYTES, 0, 0);
+                    of.part[half].x[i][0] = __builtin_amdgcn_raw_buffer_load_b32(rows_at, at + Loads::further(i), 0, 0);
                 }
                 if constexpr (MX)
-                    of.part[half].scale[i] = __builtin_amdgcn_raw_buffer_load_b8(half ? second_scales : first_scales, scale_at + more * PIECE / GROUP, 0, 0);
+                    of.part[half].scale[i] = __builtin_amdgcn_raw_buffer_load_b8(half ? second_scales : first_scales, scale_at + Loads::scale_further(i), 0, 0);
             }
         }
     };
@@ -892,10 +867,9 @@ __global__ __launch_bounds__(512, 2) void window_shared_kernel(const uint8_t *k,
             uint16_t *tile = stage + (of_v ? 32 * KSTR : 0);
 #pragma unroll
             for (int i = 0; i < N; i++) {
-                const int p = ptid + i * G::THREADS, row = p / PER_ROW, col = p % PER_ROW * PIECE;
-                uint16_t *to = tile + row * (of_v ? VSTR : KSTR) + col;
+                uint16_t *to = tile + Loads::row(ptid, i) * (of_v ? VSTR : KSTR) + Loads::channel(ptid, i);
 #pragma unroll
-                for (int e = 0; e < PIECE / 8; e++) {
+                for (int e = 0; e < Loads::PIECE / 8; e++) {
                     u32x4 x;
                     if constexpr (MX)
                         x = __builtin_bit_cast(u32x4, from_codes(of.part[half].x[i][e], scale_value(of.part[half].scale[i])));
