@@ -403,7 +403,8 @@ int dream_mx_commit(const dream_attn_desc *desc, void *const *codes_host, void *
  * The other arguments and results are those of dream_tree_verify_attn (n_tree = 1 is plain decoding); a
  * window needs `parent` beside a tree_mask, for the depths.  A node that sees nothing yields a zero row and
  * lse = -inf.  What a node does not see does not change its row, whatever it holds: NaN and infinities too.
- * Rows out of every node's sight are read only where they share a tile of 32 rows with others.  A value of v_cache that is not
+ * Rows out of every node's sight are read only where they share a tile of 32 rows with others, and without a window also among the
+ * first 256 of a head, which may be asked for before the prefix length is known.  A value of v_cache that is not
  * finite in a row a node sees makes that channel of its row NaN or infinite.  A key whose score is -inf has weight 0 (a node with no
  * other yields a zero row and lse = -inf), any other score that is not finite makes the row NaN.  q, caches and out 16-byte aligned,
  * n_q_heads at most 4096, batch * n_q_heads at most 2^20, s_max at most DREAM_MAX_WINDOW_ROWS.
