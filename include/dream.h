@@ -66,6 +66,7 @@ typedef enum {
 #define DREAM_MAX_VISUAL 16384  /* visual tokens per sequence handled by dream_visual_compress */
 #define DREAM_MAX_WINDOW_ROWS ((1 << 23) - 128) /* s_max handled by the window and 4-bit attention calls */
 #define DREAM_MX_GROUP 32       /* values that share a scale in a cache held in 4 bits          */
+#define DREAM_MAX_MX_BATCH 32767 /* sequences of the calls that append to, read or commit such caches */
 
 /* Attention geometry shared by the three attention-shaped calls. */
 typedef struct {
@@ -346,7 +347,7 @@ int dream_project_rows_multi(const dream_attn_desc *desc, const dream_proj_job *
  *   amplitude  multiplies the turned values; 0 selects 1
  *   y_x = amplitude (x cos a - y sin a),  y_y = amplitude (x sin a + y cos a),  a = position * inv_freq[i]
  * Positions may be negative (turned rows are turned back by the negated positions).  head_dim even, at
- * most 512; batch * n_rows at most 2^20.  Uses desc->batch, head_dim, dtype and, with row_base, s_max.
+ * most 512; n_heads at most 65535, batch * n_rows at most 2^20.  Uses desc->batch, head_dim, dtype and, with row_base, s_max.
  * ------------------------------------------------------------------------------------------- */
 #define DREAM_MAX_ROTARY_JOBS 4
 typedef struct dream_rotary_job {
@@ -368,14 +369,15 @@ int dream_rotary_rows(const dream_attn_desc *desc, const dream_rotary_job *jobs,
  *   scales  [B, Hkv, s_max, D / DREAM_MX_GROUP] bytes, 8-byte aligned: 2^(byte - 127) for 32 values,
  *           255 for NaN (whatever the codes).  A value is its code times its scale.  Bytes 0, 1, 253 and 254
  *           (values that bf16 does not hold as normal numbers) must not stand in rows that are read or seen.
- *   D in {64, 128, 256}; desc->dtype (f32 or bf16) is that of rows.
+ *   D in {64, 128, 256}; desc->dtype (f32 or bf16) is that of rows.  These three calls take up to DREAM_MAX_MX_BATCH
+ *   sequences, n_kv_heads up to 65535; larger batches in parts (caches and rows of a part are contiguous).
  * dream_mx_append: rows k_rows, v_rows [B, n_rows, Hkv, D], 16-byte aligned, are rounded into the caches at
  *   rows row_base[b] + (row_index ? row_index[b, r] : r); a destination row outside [0, s_max) is dropped,
  *   two rows of a call must not have the same one.  The scale of 32 values is the smallest power of two s
  *   with max|x| <= 7 s, within [2^-125, 2^125] (bytes 2 to 252); a code is the nearest value, the one with an even code where two are.
  *   A group with a value that is not finite gets scale 255.  batch * n_rows at most 2^20.
  * dream_mx_read: out [n_caches, B, Hkv, n_rows, D] of desc->dtype, 16-byte aligned, receives what rows row_base[b] + r
- *   (row_base NULL: r) of the caches stand for, exactly; rows outside [0, s_max) are zeros.  A cache so
+ *   (row_base NULL: r) of the caches stand for, exactly; rows outside [0, s_max) are zeros.  n_rows at most s_max and 2^24.  A cache so
  *   read is a k_cache of s_max = n_rows, as dream_visual_compress and dream_attention_entropy take it.
  * dream_mx_commit: dream_kv_commit for such caches, with its arguments and its result: row
  *   prefix_len[b] + j of codes and scales receives the old row prefix_len[b] + accept_path[b][j] for
@@ -399,7 +401,8 @@ int dream_mx_commit(const dream_attn_desc *desc, void *const *codes_host, void *
  *   window     0: every key, as dream_tree_verify_attn.  Otherwise node i, at position prefix_len[b] +
  *              depth(i), sees a key it would see only if the key's position is less than `window` back
  *              (a prefix row's position is its row, a tree node's prefix_len[b] + its depth) or below n_sink
- *   n_sink     first positions that stay visible to every node; ignored without a window
+ *   n_sink     first positions that stay visible to every node; ignored without a window.  Both at most 2^30 (a window
+ *              of s_max or more leaves nothing out)
  * The other arguments and results are those of dream_tree_verify_attn (n_tree = 1 is plain decoding); a
  * window needs `parent` beside a tree_mask, for the depths.  A node that sees nothing yields a zero row and
  * lse = -inf.  What a node does not see does not change its row, whatever it holds: NaN and infinities too.
@@ -407,7 +410,7 @@ int dream_mx_commit(const dream_attn_desc *desc, void *const *codes_host, void *
  * first 256 of a head, which may be asked for before the prefix length is known.  A value of v_cache that is not
  * finite in a row a node sees makes that channel of its row NaN or infinite.  A key whose score is -inf has weight 0 (a node with no
  * other yields a zero row and lse = -inf), any other score that is not finite makes the row NaN.  q, caches and out 16-byte aligned,
- * n_q_heads at most 4096, batch * n_q_heads at most 2^20, s_max at most DREAM_MAX_WINDOW_ROWS.
+ * batch at most 65535, n_q_heads at most 4096, their product at most 2^20, s_max at most DREAM_MAX_WINDOW_ROWS.
  * ------------------------------------------------------------------------------------------- */
 size_t dream_window_verify_attn_workspace(const dream_attn_desc *desc, int32_t n_tree, int64_t max_kv_len,
                                           int32_t window, int32_t n_sink);

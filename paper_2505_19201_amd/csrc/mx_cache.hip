@@ -204,8 +204,8 @@ int check_cache(const char *who, const dream_attn_desc *d)
         return fail(DREAM_ERR_INVALID_ARG, "%s: unknown dtype %d", who, d->dtype);
     if (d->head_dim != 64 && d->head_dim != 128 && d->head_dim != 256)
         return fail(DREAM_ERR_UNSUPPORTED, "%s: head_dim %d not in {64,128,256}", who, d->head_dim);
-    if (d->batch > 32767 || d->n_kv_heads > 65535)
-        return fail(DREAM_ERR_UNSUPPORTED, "%s: batch is limited to 32767, n_kv_heads to 65535", who);
+    if (d->batch > DREAM_MAX_MX_BATCH || d->n_kv_heads > 65535)      // (append's grid has K and V of a sequence in one dimension)
+        return fail(DREAM_ERR_UNSUPPORTED, "%s: batch is limited to %d, n_kv_heads to 65535", who, DREAM_MAX_MX_BATCH);
     return DREAM_OK;
 }
 
