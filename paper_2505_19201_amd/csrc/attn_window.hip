@@ -13,14 +13,15 @@
 // below its largest product; the scores would be off by more than the rounding of bf16 rows allows.)
 //
 // What bounds it: a wave issues a vector instruction every 6 clocks alone and every 3.5 to 5.5 beside a second one, a scalar one every 10; a step over 32 keys is some 200 to 340 of them
-// (head_dim 128, one query tile: 1500 clocks), and before the first lie the arguments, the prefix length, the tree and the first tile from memory, 4200 clocks.  Measured, one call of a
-// graph, against 5.2 TB/s for a large copy and 1390 TFLOP/s for a large matrix product:
-//   4-bit   B 1, 32 heads of 128, 60 nodes, 704 keys     7.6 us    (read and written: 4.3 MB, 0.8 us; a kernel that does nothing 1.6 us)
-//           B 8, 32 heads on 8, 128, 60 nodes, 1283     19.7 us    (8.1 GFLOP, 5.8 us)
-//           B 32, 32 heads of 64, 60 nodes, 1600        46.1 us    (131 MB, 25 us; 26 GFLOP, 19 us)
-//           B 4, 32 heads on 8, 128, 1 node, 32700      30.3 us    (122 MB, 24 us)
-//   16-bit  B 4, 8 heads on 4, 256, 33 nodes, window 1024 of 1283    22.5 us    (36 MB, 7.0 us; parts of 8 splits, written and read: 17 MB, 3.3 us)
-//           B 1, 32 heads of 128, 1 node, window 1020 and 4 first tokens    10.8 us    (17 MB, 3.3 us; two launches)
+// (head_dim 128, one query tile: 1500 clocks), and before the first lie the arguments, the prefix length, the tree and the first tile from memory, 4200 clocks.  Where many waves share a SIMD
+// that is issue (of a SIMD's time 89 % at B 32, 74 % at B 8); a lone wave waits, step after step, for its own chain of conversions, products, maximum and LDS.  Measured, one call of a
+// graph (medians; a few percent from one run to the next), against 5.2 TB/s for a large copy and 1390 TFLOP/s for a large matrix product:
+//   4-bit   B 1, 32 heads of 128, 60 nodes, 704 keys     7.6 us    (read and written: 4.3 MB, 0.8 us; a kernel that does nothing 1.6 us; issue 44 %: 128 workgroups, six steps a wave)
+//           B 8, 32 heads on 8, 128, 60 nodes, 1283     19.6 us    (8.1 GFLOP, 5.8 us)
+//           B 32, 32 heads of 64, 60 nodes, 1600        46 to 49 us    (131 MB, 25 us; 26 GFLOP, 19 us)
+//           B 4, 32 heads on 8, 128, 1 node, 32700      30.4 us    (122 MB, 24 us)
+//   16-bit  B 4, 16 heads on 8, 256, 33 nodes, window 1024 of 1283    22.9 us    (36 MB, 7.0 us; the states of 8 splits are 17 MB, written and then read: 6.7 us)
+//           B 1, 32 heads of 128, 1 node, window 1020 and 4 first tokens    10.9 us    (17 MB, 3.3 us; two launches)
 #include <cfloat>
 #include <type_traits>
 #include "common.h"
@@ -769,7 +770,7 @@ __global__ __launch_bounds__(64 * NW, (WindowGeom<D, QT, NW, MX>::WAVES)) void w
 
 // All rows of a KV head in one workgroup, or as many as its eight waves hold.  What a CU can pull, 64 KB in flight, bounds a kernel whose workgroups for 16 rows each read the same keys, and so
 // does what it takes to turn 4 bits into 16: here a tile of 32 keys is read once, lies in LDS as bf16 and serves every wave's QT query tiles.  Two stages: while the waves work on one, the next
-// tile goes from registers to the other, and the two after that are on their way (one: 24.2 us, two: 22.6, at B 4, 8 heads on 4 of 256, 33 nodes, 1024 keys); one barrier a tile.  The keys are shared out over workgroups (splits), whose states window_merge_kernel joins.
+// tile goes from registers to the other, and the two after that are on their way (one: 24.2 us, two: 22.6 to 22.9, at B 4, 16 heads on 8 of 256, 33 nodes, 1024 keys); one barrier a tile.  The keys are shared out over workgroups (splits), whose states window_merge_kernel joins.
 template <int D, int QT, bool MX>
 struct SharedGeom {
     static constexpr int NW = 8, THREADS = GroupLoads<D, MX>::THREADS;
@@ -1111,7 +1112,9 @@ __global__ __launch_bounds__(256) void window_merge_kernel(WindowArgs a, int row
 }
 
 // float32 queries and rows (the small configuration): one workgroup of 4 waves per (node, head, sequence), D / 4 lanes a key, each with 4 channels; every wave keeps a state
-// of its own keys and they meet in LDS.  Only keys that the node's window reaches are read.
+// of its own keys and they meet in LDS.  Only keys that the node's window reaches are read, but every node reads its own: there for its precision and for small shapes, not for long ones.
+// 4 heads on 2 of 64, 21 nodes, 121 keys: 5.3 us (4-bit 5.4; the launch and one round of loads).  32 heads of 128, 60 nodes, 764 keys: 80 us (4-bit 82), where the 25 MB read once would take 5;
+// one token with a window of 1024: 44 us, 32 workgroups.
 template <int D, bool MX>
 __global__ __launch_bounds__(256) void window_f32_kernel(WindowArgs a)
 {
@@ -1220,9 +1223,9 @@ struct WindowPlan {
 // through; where many are, what the CU can issue; whichever is more:
 //     us = base + per_group * groups + steps * max(latency, issue * groups)  [+ many_nodes]  [+ 2.3 + 0.11 * splits + 1e-6 * head_dim * rows of parts, for the join]
 // with groups the workgroups (of four waves) a CU gets, steps those of a wave.  The constants are those with which the choice is best over measured times of every kernel with every split from
-// 1 to 64 in powers of two, over 7 head layouts x batches of 1, 4, 16, 64 x trees of 1, 16, 60, 250 x 40 to 40000 keys, 528 shapes of 4-bit and 516 of 16-bit caches: 0.8 % and 0.5 % behind
-// the fastest in the geometric mean, 5 % and 3 % at the 95th percentile, 34 % at most.  What the forms are
-// worth there (4-bit, 16-bit): the fastest would take 4 % and 30 % longer without the shared kernel, 5 % and 1.5 % without several query tiles to a wave, 33 % and 57 % without splits, and
+// 1 to 64 in powers of two, over 7 head layouts x batches of 1, 4, 16, 64 x trees of 1, 16, 60, 250 x 40 to 40000 keys, 528 shapes of 4-bit and 515 of 16-bit caches: 0.8 % and 0.6 % behind
+// the fastest in the geometric mean, 5 % and 3 % at the 95th percentile, 34 % at most.  These are the data that it was fitted to, without a window; over 144 shapes each with windows of 500 to 4096
+// keys, measured afterwards, 1.7 % and 1.3 %, 9 % and 7 %, 17 % at most.  What the forms are worth without one (4-bit, 16-bit): the fastest would take 4 % and 30 % longer without the shared kernel, 5 % and 1.5 % without several query tiles to a wave, 33 % and 57 % without splits, and
 // 1 % without the eight-wave form over 4-bit caches; over 16-bit ones that brought 0.2 % and is left out, as is the shared kernel over 4-bit caches at head_dim 64 (0.1 %).
 struct Steps {
     float base, per_group, latency, latency_tile, issue, issue_tile, many_nodes;      // window_attn_kernel; .._tile: for each query tile of a wave

@@ -135,6 +135,8 @@ __global__ __launch_bounds__(256) void mx_read_kernel(ReadArgs a)
 // dream_mx_commit: the codes and scales of the accepted path's rows become the next rows of the prefix, in place.  A head of a sequence in a cache is moved by one wave, or, where the longest
 // path has more pieces than four for each of its lanes, by a workgroup: what is to move, a few hundred bytes to a few KB, is in registers before anything is written.  A row is D / 32 pieces of
 // 16 bytes of codes and one piece of D / 32 bytes of scales.  (16 caches of 8 sequences of 32 heads of 64, paths of up to 7 rows: 4.8 us, with a workgroup a head 17.9.)
+// Bound by trips to memory, one after the other: the arguments, the lengths, the path, the rows; a path of four rows is 12 pieces of 16 bytes, so four of five lanes have none.  The bytes, about
+// 1 MB each way, would take 0.4 us.  It runs once a round behind all layers' attention, 0.2 us a layer, which is why it was left so.
 constexpr int WAVE_MOVES = 4, GROUP_MOVES = 8;            // pieces a lane holds
 
 struct CommitArgs {
