@@ -335,7 +335,9 @@ int dream_project_rows_multi(const dream_attn_desc *desc, const dream_proj_job *
  *              x [B, n_rows, n_heads, D] of desc->dtype (f32 or bf16); out as in dream_project_rows:
  *              dense [B, n_rows, n_heads, D] where row_base is NULL (x itself is allowed), otherwise
  *              cache rows row_base[b] + (row_index ? row_index[b, r] : r) of [B, n_heads, s_max, D];
- *              a destination row outside [0, s_max) is dropped.  Jobs must not write overlapping memory.
+ *              a destination row outside [0, s_max) is dropped.  Jobs must not write overlapping memory, nor
+ *              what another job reads; a dense out that overlaps a job's x (other than its own, whole) or another
+ *              dense out is refused.
  *   position of row r of sequence b, the first that is given of
  *     pos[b, r]                       pos nullable [B, n_rows] int32
  *     pos_base[b] + depth of node r   parent nullable [B, n_rows] int32 (n_rows <= DREAM_MAX_TREE)

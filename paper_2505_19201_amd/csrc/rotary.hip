@@ -266,6 +266,17 @@ int dream_rotary_rows(const dream_attn_desc *desc, const dream_rotary_job *jobs,
             return fail(DREAM_ERR_INVALID_ARG, "%s: job %d writes a cache over its own rows", who, j);
         wide = wide && !((reinterpret_cast<uintptr_t>(jb.x) | reinterpret_cast<uintptr_t>(jb.out)) & 15);
     }
+    // a launch's workgroups come in any order: what one writes none may read, but its own rows in place
+    const int64_t values = (int64_t)desc->batch * n_rows * desc->head_dim * size;
+    auto overlap = [&](const void *p, const dream_rotary_job &of_p, const void *q, const dream_rotary_job &of_q) {
+        const uintptr_t a0 = reinterpret_cast<uintptr_t>(p), b0 = reinterpret_cast<uintptr_t>(q);
+        return a0 < b0 + of_q.n_heads * values && b0 < a0 + of_p.n_heads * values;
+    };
+    for (int j = 0; j < n_jobs; j++)
+        for (int i = 0; i < n_jobs && !jobs[j].row_base; i++)
+            if ((!(i == j && jobs[j].x == jobs[j].out) && overlap(jobs[j].out, jobs[j], jobs[i].x, jobs[i])) ||
+                (i < j && !jobs[i].row_base && overlap(jobs[j].out, jobs[j], jobs[i].out, jobs[i])))
+                return fail(DREAM_ERR_INVALID_ARG, "%s: out of job %d overlaps a tensor of job %d", who, j, i);
     const int step = wide ? n : interleaved ? 2 : 1;
     a.pieces = interleaved ? desc->head_dim / step : half / step + (desc->head_dim - rot_dim) / step;
     int64_t end = 0;
