@@ -7,7 +7,7 @@
 // One workgroup per row, or where there are few rows several: the angles of a row are the same for all its heads, so they are formed once, by rot_dim / 2 threads, and lie in LDS; the
 // row's first pieces are requested ahead of that, and every wave holds the tree in registers.  A thread then takes 16 bytes of a head (in the half layout with the 16 bytes rot_dim / 2 further
 // on), whatever job the head belongs to: one launch serves the queries and the keys.  Sizes that 16-byte pieces do not divide, and unaligned tensors, go pair by pair.
-// Roofline: HBM for prompts (rows read and written once): 210 MB in 40.9 us, 5.1 TB/s, what a large copy reaches.  For a tree the launch and the chain parents, angles, rows: 60 rows of
+// Roofline: HBM for prompts (rows read and written once): 210 MB in 40 to 41 us, 5.2 TB/s, what a large copy reaches.  For a tree the launch and the chain parents, angles, rows: 60 rows of
 // 64 heads of 128 in 3.7 us (with one workgroup a row 4.3; a kernel that does nothing 1.6), 0.4 us of them the walk up the tree.
 #include <type_traits>
 #include "common.h"
