@@ -430,6 +430,108 @@ int dream_mx_verify_attn(const dream_attn_desc *desc, const void *q, const void 
                          int64_t max_kv_len, void *out, float *lse, void *workspace,
                          size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Key/value caches held in pages.  The sequences of a batch take pages from one pool, so that a cache grows by what
+ * it holds and sequences with the same prefix can hold its pages once.
+ *   a pool      [n_pages, Hkv, page_size, D] of desc->dtype (one for K and one for V in every layer), 16-byte aligned
+ *   page_table  [B, max_pages] int32: row j of sequence b stands in row j % page_size of page page_table[b, j / page_size]
+ * page_size is 16, 32, 64, 128 or 256; max_pages * page_size is at most DREAM_MAX_WINDOW_ROWS, batch at most 65535,
+ * n_q_heads and n_kv_heads at most 4096, D in {64, 128, 256}.  desc->s_max is not looked at: max_pages * page_size stands in its place.
+ * An entry of the table outside [0, n_pages) is never followed: what would be written there is dropped, and in the
+ * place of what would be read there some other page is.  Entries behind the last live page are not looked at, except that their
+ * pages may be read where they share a tile of 64 rows with live ones (results do not depend on them).  Rows that a call writes must stand in pages that no other sequence
+ * of the call writes to; a shared prefix that ends inside a page needs a copy of that page for every sequence
+ * but one.
+ *
+ * dream_paged_append: the rows a step (or a prompt) adds, turned by their positions on the way.
+ *   q, k, v     [B, n_rows, Hq, D] nullable, [B, n_rows, Hkv, D] of desc->dtype
+ *   row r of sequence b goes to cache row row_base[b] + (row_index ? row_index[b, r] : r) of k_pages, v_pages; one outside
+ *   [0, max_pages * page_size) is dropped, two rows of a call must not have the same one
+ *   n_live      nullable [B] int32: of sequence b only rows r < n_live[b] exist, the others are padding (nothing is read or written for them)
+ *   pos, pos_base, parent, inv_freq, rot_dim, interleaved, amplitude   as in dream_rotary_rows, for k and q; where
+ *               neither pos nor pos_base is given, row_base is the base.  inv_freq nullable: nothing turns (q is
+ *               then copied, and rot_dim, interleaved and amplitude are ignored)
+ *   q_out       [B, n_rows, Hq, D], given iff q is; q itself is allowed.  batch * n_rows at most 2^20, tensors 16-byte aligned.
+ *               No other output may overlap an input or another output; q_out that does is refused
+ *
+ * dream_paged_commit: dream_kv_commit for pools, with its arguments and its result: row prefix_len[b] + j receives the old row
+ *   prefix_len[b] + accept_path[b][j] for j = 0 .. accept_len[b], in every pool of pools_host (HOST array of n_pools DEVICE
+ *   pointers).  DREAM_ERR_UNSUPPORTED if min(path_stride, n_tree) rows exceed 64 KB.
+ *
+ * dream_paged_verify_attn: dream_tree_verify_attn over pages (n_tree = 1 is plain decoding), where a prefix that sequences
+ *   share is read once for all of them.
+ *   n_groups     0: nothing is shared.  Otherwise group g is the sequences group_start[g] .. group_start[g + 1] - 1 ([n_groups + 1] int32,
+ *                ascending, from 0 to B), and positions below shared_len[g] ([n_groups] int32) of all of them are those of its
+ *                first sequence: its entries of the page table are followed, those of the others not looked at.  A sequence
+ *                sees shared positions below its own prefix length only.  n_groups at most B
+ *   max_shared_len, max_kv_len   host-known upper bounds of shared_len and of prefix_len + n_tree; only used to choose the launch shape
+ *   A node that sees nothing yields a zero row and lse = -inf.  What a node does not see does not change its row, whatever it holds:
+ *   NaN and infinities too.  Values and scores that are not finite: as in dream_window_verify_attn.  batch * n_q_heads at most 2^20, q and out 16-byte aligned.
+ *
+ * dream_page_bounds: of every page that rows from_len[b] .. to_len[b] - 1 (from_len NULL: 0) lie in, the largest and the
+ *   smallest of its keys' values in every channel, over the page's rows below to_len[b]:
+ *   bounds       [n_pages, Hkv, 2, D] of desc->dtype, 16-byte aligned: largest, then smallest.  A channel with a value that is not finite gets +inf
+ *                and -inf.  Other pages' bounds keep their content
+ *   max_new      host-known upper bound of to_len - from_len; only used to choose the launch shape
+ *
+ * dream_page_select: which pages of its prefix each node is to see, for every KV head, by an upper bound of its scores there.
+ *   With the queries of the Hq / Hkv heads of a KV head held as whole numbers c = rint(q / 2^f), f in [-100, 122] the least
+ *   exponent at which none exceeds 127 (one for all the heads and channels), and the bounds of a page as u = ceil(largest / 2^e),
+ *   w = floor(smallest / 2^e), e likewise (one for all the channels),
+ *     score = 2^e float32(sum over channels and heads of (c > 0 ? c u : c w))
+ *   in whole numbers, rounded once to float32: the same pages every time, on any machine.  (q finite; a page with a
+ *   bound that is not has score +inf.)  Of the pages that hold the prefix rows a node sees the first n_first, the last n_last, and the n_best
+ *   of highest score in between; equal scores toward the lower page.
+ *   page_nodes   [B, Hkv, max_pages, W] uint64, W = ceil(n_tree / 64): bit (i % 64) of word i / 64 of a page is set iff node i sees
+ *                it; all of it is written
+ *   max_kv_len   host-known upper bound of prefix_len + n_tree: prefix rows behind max_kv_len - n_tree are taken as not there.  Hq / Hkv at most 64
+ * dream_sparse_verify_attn: dream_paged_verify_attn where node i sees of the prefix only the rows of pages whose bit in
+ *   page_nodes is set for it (as dream_page_select writes it, or the caller's own), and the tree as ever.  Pages that no node of a sequence
+ *   sees are not read.
+ *   max_pages_seen   about how many pages a node sees; only used to choose the launch shape, 0 if unknown
+ * ------------------------------------------------------------------------------------------- */
+typedef struct {
+    int32_t page_size;  /* rows of a page: 16, 32, 64, 128 or 256                              */
+    int32_t n_pages;    /* pages of a pool                                                     */
+    int32_t max_pages;  /* entries of a sequence's row of the page table                       */
+} dream_page_desc;
+int dream_paged_append(const dream_attn_desc *desc, const dream_page_desc *pages, const int32_t *page_table,
+                       const void *q, const void *k, const void *v, int32_t n_rows, const int32_t *row_base,
+                       const int32_t *row_index, const int32_t *n_live, const int32_t *pos,
+                       const int32_t *pos_base, const int32_t *parent, const float *inv_freq, int32_t rot_dim,
+                       int32_t interleaved, float amplitude, void *q_out, void *k_pages, void *v_pages,
+                       void *stream);
+int dream_paged_commit(const dream_attn_desc *desc, const dream_page_desc *pages, const int32_t *page_table,
+                       void *const *pools_host, int32_t n_pools, const int32_t *prefix_len, int32_t n_tree,
+                       const int32_t *accept_path, int32_t path_stride, const int32_t *accept_len,
+                       int32_t *prefix_len_out, void *stream);
+size_t dream_paged_verify_attn_workspace(const dream_attn_desc *desc, const dream_page_desc *pages,
+                                         int32_t n_tree, int64_t max_kv_len, int32_t n_groups,
+                                         int64_t max_shared_len);
+int dream_paged_verify_attn(const dream_attn_desc *desc, const dream_page_desc *pages, const void *q,
+                            const void *k_pages, const void *v_pages, const int32_t *page_table,
+                            const int32_t *prefix_len, int32_t n_tree, const int32_t *parent,
+                            const uint64_t *tree_mask, int32_t n_groups, const int32_t *group_start,
+                            const int32_t *shared_len, int64_t max_shared_len, int64_t max_kv_len, void *out,
+                            float *lse, void *workspace, size_t workspace_bytes, void *stream);
+int dream_page_bounds(const dream_attn_desc *desc, const dream_page_desc *pages, const int32_t *page_table,
+                      const void *k_pages, const int32_t *from_len, const int32_t *to_len, int64_t max_new,
+                      void *bounds, void *stream);
+size_t dream_page_select_workspace(const dream_attn_desc *desc, const dream_page_desc *pages, int32_t n_tree,
+                                   int64_t max_kv_len);
+int dream_page_select(const dream_attn_desc *desc, const dream_page_desc *pages, const int32_t *page_table,
+                      const void *q, const void *bounds, const int32_t *prefix_len, int32_t n_tree,
+                      int32_t n_first, int32_t n_last, int32_t n_best, int64_t max_kv_len,
+                      uint64_t *page_nodes, void *workspace, size_t workspace_bytes, void *stream);
+size_t dream_sparse_verify_attn_workspace(const dream_attn_desc *desc, const dream_page_desc *pages,
+                                          int32_t n_tree, int64_t max_kv_len, int32_t max_pages_seen);
+int dream_sparse_verify_attn(const dream_attn_desc *desc, const dream_page_desc *pages, const void *q,
+                             const void *k_pages, const void *v_pages, const int32_t *page_table,
+                             const uint64_t *page_nodes, const int32_t *prefix_len, int32_t n_tree,
+                             const int32_t *parent, const uint64_t *tree_mask, int64_t max_kv_len,
+                             int32_t max_pages_seen, void *out, float *lse, void *workspace,
+                             size_t workspace_bytes, void *stream);
+
 /* Host-side check of one parent array: parent_host[0] == -1 and 0 <= parent_host[i] < i.
  * Writes the maximum depth to *max_depth_out (nullable).  DREAM_OK or DREAM_ERR_INVALID_ARG. */
 int dream_tree_validate_host(const int32_t *parent_host, int32_t n_tree, int32_t *max_depth_out);

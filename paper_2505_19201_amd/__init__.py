@@ -16,5 +16,7 @@ from .binding import (  # noqa: F401
     dream_attention_entropy_workspace, dream_attention_entropy, dream_spec_accept_workspace, dream_spec_accept, dream_project_rows, dream_project_rows_multi,
     dream_rotary_rows, dream_mx_append, dream_mx_read, dream_mx_commit, dream_window_verify_attn_workspace, dream_window_verify_attn,
     dream_mx_verify_attn_workspace, dream_mx_verify_attn,
+    PageDesc, page_desc, dream_paged_append, dream_paged_commit, dream_paged_verify_attn_workspace, dream_paged_verify_attn, dream_page_bounds,
+    dream_page_select_workspace, dream_page_select, dream_sparse_verify_attn_workspace, dream_sparse_verify_attn,
     alloc_workspace, to_device, EXPORTED_SYMBOLS,
 )

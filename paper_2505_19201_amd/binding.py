@@ -29,6 +29,8 @@ EXPORTED_SYMBOLS = (
     "dream_project_rows", "dream_project_rows_multi", "dream_accept_path_static", "dream_accept_static_init",
     "dream_rotary_rows", "dream_mx_append", "dream_mx_read", "dream_mx_commit", "dream_window_verify_attn_workspace",
     "dream_window_verify_attn", "dream_mx_verify_attn_workspace", "dream_mx_verify_attn",
+    "dream_paged_append", "dream_paged_commit", "dream_paged_verify_attn_workspace", "dream_paged_verify_attn", "dream_page_bounds",
+    "dream_page_select_workspace", "dream_page_select", "dream_sparse_verify_attn_workspace", "dream_sparse_verify_attn",
 )
 
 
@@ -52,6 +54,14 @@ def attn_desc(batch: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype:
     return AttnDesc(batch, n_q_heads, n_kv_heads, head_dim, dtype, scale, s_max)
 
 
+class PageDesc(C.Structure):
+    _fields_ = [("page_size", C.c_int32), ("n_pages", C.c_int32), ("max_pages", C.c_int32)]
+
+
+def page_desc(page_size: int, n_pages: int, max_pages: int) -> PageDesc:
+    return PageDesc(page_size, n_pages, max_pages)
+
+
 _lib: Optional[C.CDLL] = None
 
 
@@ -72,7 +82,8 @@ def load() -> C.CDLL:
         for name in ("dream_tree_verify_attn_workspace", "dream_draft_xattn_workspace",
                      "dream_visual_compress_workspace", "dream_accept_path_workspace", "dream_tree_expand_workspace",
                      "dream_attention_entropy_workspace", "dream_spec_accept_workspace", "dream_window_verify_attn_workspace",
-                     "dream_mx_verify_attn_workspace"):
+                     "dream_mx_verify_attn_workspace", "dream_paged_verify_attn_workspace", "dream_page_select_workspace",
+                     "dream_sparse_verify_attn_workspace"):
             getattr(lib, name).restype = C.c_size_t
         lib.dream_last_error.restype = C.c_char_p
         lib.dream_set_kv_splits.restype = None
@@ -300,6 +311,54 @@ def dream_mx_verify_attn(desc: AttnDesc, q, k_codes, k_scales, v_codes, v_scales
                          max_kv_len: int, out, lse, workspace, stream=None) -> None:
     _check(_native().dream_mx_verify_attn(desc, q, k_codes, k_scales, v_codes, v_scales, prefix_len, n_tree, parent, tree_mask, window, n_sink,
                                           max_kv_len, out, lse, workspace, workspace, _stream(stream)))
+
+
+def dream_paged_append(desc: AttnDesc, pages: PageDesc, page_table, q, k, v, n_rows: int, row_base, row_index, n_live, pos, pos_base, parent, inv_freq,
+                       rot_dim: int, interleaved: bool, amplitude: float, q_out, k_pages, v_pages, stream=None) -> None:
+    _check(_native().dream_paged_append(desc, pages, page_table, q, k, v, n_rows, row_base, row_index, n_live, pos, pos_base, parent, inv_freq, rot_dim,
+                                        int(interleaved), amplitude, q_out, k_pages, v_pages, _stream(stream)))
+
+
+def dream_paged_commit(desc: AttnDesc, pages: PageDesc, page_table, pools: Sequence[torch.Tensor], prefix_len, n_tree: int, accept_path, accept_len,
+                       prefix_len_out=None, stream=None) -> None:
+    pools = tuple(pools)       # (see dream_kv_commit)
+    _check(_native().dream_paged_commit(desc, pages, page_table, pools, len(pools), prefix_len, n_tree, accept_path, accept_path.shape[-1], accept_len,
+                                        prefix_len_out, _stream(stream)))
+
+
+def dream_paged_verify_attn_workspace(desc: AttnDesc, pages: PageDesc, n_tree: int, max_kv_len: int, n_groups: int = 0, max_shared_len: int = 0) -> int:
+    return int(load().dream_paged_verify_attn_workspace(C.byref(desc), C.byref(pages), C.c_int32(n_tree), C.c_int64(max_kv_len), C.c_int32(n_groups),
+                                                        C.c_int64(max_shared_len)))
+
+
+def dream_paged_verify_attn(desc: AttnDesc, pages: PageDesc, q, k_pages, v_pages, page_table, prefix_len, n_tree: int, parent, tree_mask, n_groups: int,
+                            group_start, shared_len, max_shared_len: int, max_kv_len: int, out, lse, workspace, stream=None) -> None:
+    _check(_native().dream_paged_verify_attn(desc, pages, q, k_pages, v_pages, page_table, prefix_len, n_tree, parent, tree_mask, n_groups, group_start,
+                                             shared_len, max_shared_len, max_kv_len, out, lse, workspace, workspace, _stream(stream)))
+
+
+def dream_page_bounds(desc: AttnDesc, pages: PageDesc, page_table, k_pages, from_len, to_len, max_new: int, bounds, stream=None) -> None:
+    _check(_native().dream_page_bounds(desc, pages, page_table, k_pages, from_len, to_len, max_new, bounds, _stream(stream)))
+
+
+def dream_page_select_workspace(desc: AttnDesc, pages: PageDesc, n_tree: int, max_kv_len: int) -> int:
+    return int(load().dream_page_select_workspace(C.byref(desc), C.byref(pages), C.c_int32(n_tree), C.c_int64(max_kv_len)))
+
+
+def dream_page_select(desc: AttnDesc, pages: PageDesc, page_table, q, bounds, prefix_len, n_tree: int, n_first: int, n_last: int, n_best: int,
+                      max_kv_len: int, page_nodes, workspace, stream=None) -> None:
+    _check(_native().dream_page_select(desc, pages, page_table, q, bounds, prefix_len, n_tree, n_first, n_last, n_best, max_kv_len, page_nodes, workspace,
+                                       workspace, _stream(stream)))
+
+
+def dream_sparse_verify_attn_workspace(desc: AttnDesc, pages: PageDesc, n_tree: int, max_kv_len: int, max_pages_seen: int = 0) -> int:
+    return int(load().dream_sparse_verify_attn_workspace(C.byref(desc), C.byref(pages), C.c_int32(n_tree), C.c_int64(max_kv_len), C.c_int32(max_pages_seen)))
+
+
+def dream_sparse_verify_attn(desc: AttnDesc, pages: PageDesc, q, k_pages, v_pages, page_table, page_nodes, prefix_len, n_tree: int, parent, tree_mask,
+                             max_kv_len: int, max_pages_seen: int, out, lse, workspace, stream=None) -> None:
+    _check(_native().dream_sparse_verify_attn(desc, pages, q, k_pages, v_pages, page_table, page_nodes, prefix_len, n_tree, parent, tree_mask, max_kv_len,
+                                              max_pages_seen, out, lse, workspace, workspace, _stream(stream)))
 
 
 def dream_spec_accept_workspace(batch: int, n_tree: int, vocab: int) -> int:

@@ -4,7 +4,7 @@
 //
 // Every wrapper follows from the entry point's own signature (one template).  A pointer is a device pointer: it takes a contiguous
 // tensor on the GPU or None, and nothing else, so that host memory never reaches a kernel as one.  The exceptions have types of
-// their own: the descriptor (a ctypes structure), host out-parameters (ENTRY_HOST names their position) and the stream (always the
+// their own: the descriptors (ctypes structures), host out-parameters (ENTRY_HOST names their position) and the stream (always the
 // last argument, a raw handle).  An array of pointers takes a sequence of tensors, the projection jobs a sequence of sequences; size_t
 // takes an integer or a tensor (its bytes); the rest are numbers.
 #define PY_SSIZE_T_CLEAN
@@ -105,6 +105,10 @@ struct HostObject {
 };
 template <>
 struct Arg<const dream_attn_desc *> : HostObject<dream_attn_desc> {
+    explicit Arg(PyObject *o) : HostObject(o, false) {}
+};
+template <>
+struct Arg<const dream_page_desc *> : HostObject<dream_page_desc> {
     explicit Arg(PyObject *o) : HostObject(o, false) {}
 };
 struct HostInt : HostObject<int32_t> {
@@ -212,7 +216,7 @@ struct WithoutGil {
     ~WithoutGil() { PyEval_RestoreThread(state); }
 };
 
-// What the rotary, 4-bit and window calls want of their tensors, checked before the call: the type, at least so many values, and the current device (the one the call is made on).  A
+// What the rotary, 4-bit, window and paged calls want of their tensors, checked before the call: the type, at least so many values, and the current device (the one the call is made on).  A
 // None is the library's to accept or refuse, and so are sizes that are not positive.
 thread_local c10::DeviceIndex current_device = -1;      // of this call; -1: not asked for yet (Sizes)
 void want(PyObject *o, const char *name, __int128 values, at::ScalarType type, at::ScalarType also)
@@ -353,6 +357,105 @@ struct WindowCheck {
     }
 };
 
+// Caches held in pages
+struct PagedSizes : Sizes {
+    dream_page_desc p = {};
+    __int128 table, pool;
+    explicit PagedSizes(Args a) : Sizes(a[0])
+    {
+        const Arg<const dream_page_desc *> pages(a[1]);
+        p = *pages.value;
+        table = b * p.max_pages;
+        pool = (__int128)p.n_pages * hkv * p.page_size * dim;
+    }
+};
+struct PagedAppendCheck {
+    static void check(Args a)
+    {
+        const PagedSizes s(a);
+        const __int128 rows = s.b * number(a[6]);
+        want(a[2], "page_table", s.table, at::kInt);
+        want(a[3], "q", rows * s.hq * s.dim, s.type);
+        want(a[4], "k", rows * s.hkv * s.dim, s.type);
+        want(a[5], "v", rows * s.hkv * s.dim, s.type);
+        want(a[7], "row_base", s.b, at::kInt);
+        want(a[8], "row_index", rows, at::kInt);
+        want(a[9], "n_live", s.b, at::kInt);
+        want(a[10], "pos", rows, at::kInt);
+        want(a[11], "pos_base", s.b, at::kInt);
+        want(a[12], "parent", rows, at::kInt);
+        want(a[13], "inv_freq", number(a[14]) / 2, at::kFloat);
+        want(a[17], "q_out", rows * s.hq * s.dim, s.type);
+        want(a[18], "k_pages", s.pool, s.type);
+        want(a[19], "v_pages", s.pool, s.type);
+    }
+};
+struct PagedCommitCheck {
+    static void check(Args a)
+    {
+        const PagedSizes s(a);
+        want(a[2], "page_table", s.table, at::kInt);
+        want_all(a[3], "pools", s.pool, s.type);
+        want(a[5], "prefix_len", s.b, at::kInt);
+        want(a[7], "accept_path", s.b * number(a[8]), at::kInt);
+        want(a[9], "accept_len", s.b, at::kInt);
+        want(a[10], "prefix_len_out", s.b, at::kInt);
+    }
+};
+// SPARSE: over selected pages
+template <bool SPARSE>
+struct PagedAttnCheck {
+    static void check(Args a)
+    {
+        const PagedSizes s(a);
+        Args r = a + (SPARSE ? 7 : 6), e = a + (SPARSE ? 13 : 15);      // prefix_len, n_tree, parent, tree_mask; out, lse, workspace
+        const __int128 t = number(r[1]), rows = s.b * t, words = (t + 63) / 64;
+        want(a[2], "q", rows * s.hq * s.dim, s.type);
+        want(a[3], "k_pages", s.pool, s.type);
+        want(a[4], "v_pages", s.pool, s.type);
+        want(a[5], "page_table", s.table, at::kInt);
+        if (SPARSE) {
+            want(a[6], "page_nodes", s.table * s.hkv * words, at::kLong, at::kUInt64);
+        } else {
+            const __int128 groups = number(a[10]);
+            want(a[11], "group_start", groups + 1, at::kInt);
+            want(a[12], "shared_len", groups, at::kInt);
+        }
+        want(r[0], "prefix_len", s.b, at::kInt);
+        want(r[2], "parent", rows, at::kInt);
+        want(r[3], "tree_mask", rows * words, at::kLong, at::kUInt64);
+        want(e[0], "out", rows * s.hq * s.dim, s.type);
+        want(e[1], "lse", rows * s.hq, at::kFloat);
+        if (THPVariable_Check(e[2]))
+            want(e[2], "workspace", 0, THPVariable_Unpack(e[2]).scalar_type());
+    }
+};
+struct PageBoundsCheck {
+    static void check(Args a)
+    {
+        const PagedSizes s(a);
+        want(a[2], "page_table", s.table, at::kInt);
+        want(a[3], "k_pages", s.pool, s.type);
+        want(a[4], "from_len", s.b, at::kInt);
+        want(a[5], "to_len", s.b, at::kInt);
+        want(a[7], "bounds", (__int128)s.p.n_pages * s.hkv * 2 * s.dim, s.type);
+    }
+};
+struct PageSelectCheck {
+    static void check(Args a)
+    {
+        const PagedSizes s(a);
+        const __int128 t = number(a[6]);
+        want(a[2], "page_table", s.table, at::kInt);
+        want(a[3], "q", s.b * t * s.hq * s.dim, s.type);
+        want(a[4], "bounds", (__int128)s.p.n_pages * s.hkv * 2 * s.dim, s.type);
+        want(a[5], "prefix_len", s.b, at::kInt);
+        want(a[11], "page_nodes", s.table * s.hkv * ((t + 63) / 64), at::kLong, at::kUInt64);
+        if (THPVariable_Check(a[12]))
+            want(a[12], "workspace", 0, THPVariable_Unpack(a[12]).scalar_type());
+    }
+};
+
 // HOST: position of the host out-parameter, or -1
 template <auto F, int HOST, class Check = Unchecked>
 struct Entry;
@@ -390,7 +493,9 @@ PyMethodDef methods[] = {
     ENTRY(dream_kv_commit), ENTRY(dream_project_rows), ENTRY(dream_project_rows_multi), ENTRY(dream_spec_accept), ENTRY(dream_attention_entropy),
     ENTRY(dream_tree_expand_level), ENTRY_HOST(dream_tree_finalize, 9), ENTRY_CHECKED(dream_rotary_rows, RotaryCheck),
     ENTRY_CHECKED(dream_mx_append, AppendCheck), ENTRY_CHECKED(dream_mx_read, ReadCheck), ENTRY_CHECKED(dream_mx_commit, CommitCheck),
-    ENTRY_CHECKED(dream_window_verify_attn, WindowCheck<false>), ENTRY_CHECKED(dream_mx_verify_attn, WindowCheck<true>), {nullptr, nullptr, 0, nullptr}};
+    ENTRY_CHECKED(dream_window_verify_attn, WindowCheck<false>), ENTRY_CHECKED(dream_mx_verify_attn, WindowCheck<true>),
+    ENTRY_CHECKED(dream_paged_append, PagedAppendCheck), ENTRY_CHECKED(dream_paged_commit, PagedCommitCheck), ENTRY_CHECKED(dream_paged_verify_attn, PagedAttnCheck<false>),
+    ENTRY_CHECKED(dream_page_bounds, PageBoundsCheck), ENTRY_CHECKED(dream_page_select, PageSelectCheck), ENTRY_CHECKED(dream_sparse_verify_attn, PagedAttnCheck<true>), {nullptr, nullptr, 0, nullptr}};
 #undef ENTRY
 #undef ENTRY_HOST
 #undef ENTRY_CHECKED
