@@ -24,8 +24,11 @@ using namespace dream;
 namespace {
 
 constexpr float SLACK = 8.0f;             // octaves a score may exceed its row's reference by before that is raised
-constexpr int DENSE_LIST = 512;           // pages a workgroup's list holds where all are taken
 
+// One of a launch's two kinds of workgroups: those of the shared positions, and those of what is a sequence's own.
+struct Part {
+    int32_t blocks, streams, row_groups, splits, slot;      // workgroups; units of a sequence or all groups, KV head and split; workgroups of a unit; its first slot
+};
 struct PagedAttnArgs {
     const unsigned char *q, *k, *v;
     const int32_t *table, *prefix_len, *parent, *group_start, *shared_len;
@@ -35,38 +38,34 @@ struct PagedAttnArgs {
     float2 *part_ml;
     int64_t all_rows;                     // rows of a slot of part_o
     int32_t batch, n_tree, words, hq, hkv, group, rows;      // rows: query rows of a sequence and KV head
-    int32_t lg_page, n_pages, max_pages, n_groups;
-    int32_t shared, splits, slot, n_slots, shared_slots, streams, row_groups, list_size;      // of this launch: are these the shared positions; its slots
+    int32_t lg_page, n_pages, max_pages, n_groups, n_slots, shared_slots, list_size;
     float scale_log2;
+    Part shared, own;
 };
 
 // What a workgroup does.
 struct Unit {
-    int b, kvh, split, row0, n_rows;      // the sequence whose pages are read; rows are numbered through the sequences from b on
-    int lo, hi, P;                        // positions [lo, hi), of which those from P on are the tree's
+    bool shared;
+    int b, kvh, split, splits, slot, row0, n_rows;      // the sequence whose pages are read; its slot; rows are numbered through the sequences from b on
+    int lo, hi, P;                                      // positions [lo, hi), of which those from P on are the tree's
 };
 
 __device__ __forceinline__ int clamped_prefix(const PagedAttnArgs &a, int p) { return min(max(p, 0), (a.max_pages << a.lg_page) - a.n_tree); }
 
-// The group that sequence b is in: its first sequence, and how many positions it shares; no group: b and 0.
-__device__ __forceinline__ void group_of(const PagedAttnArgs &a, int b, int lane, int &first, int &shared)
+// How many positions sequence b shares; -1 outside every group.
+__device__ __forceinline__ int shared_by(const PagedAttnArgs &a, int b, int lane)
 {
-    first = b;
-    shared = -1;
     for (int g0 = 0; g0 < a.n_groups; g0 += 64) {
         const int g = min(g0 + lane, a.n_groups - 1);
         const int s = a.group_start[g], e = a.group_start[g + 1], n = a.shared_len[g];
         const uint64_t mine = __ballot(s <= b && b < e);
-        if (mine) {
-            const int l = __builtin_ctzll(mine);
-            first = min(max(__builtin_amdgcn_readlane(s, l), 0), b);
-            shared = min(max(__builtin_amdgcn_readlane(n, l), 0), a.max_pages << a.lg_page);
-            return;
-        }
+        if (mine)
+            return min(max(__builtin_amdgcn_readlane(n, __builtin_ctzll(mine)), 0), a.max_pages << a.lg_page);
     }
+    return -1;
 }
 
-// The group whose query rows the t-th tile of `cap` rows of all groups has.  first, n (sequences), shared, row0; n = 0: there is no such tile.
+// The group whose query rows the t-th tile of `cap` rows of all groups has: its first sequence, sequences, shared positions, and the tile's first row; n = 0: there is no such tile.
 __device__ __forceinline__ void group_of_tile(const PagedAttnArgs &a, int t, int cap, int lane, int &first, int &n, int &shared, int &row0)
 {
     n = 0;
@@ -99,109 +98,86 @@ __device__ __forceinline__ void group_of_tile(const PagedAttnArgs &a, int t, int
     }
 }
 
-// Workgroup ids that are congruent mod 8 run on one XCD: row groups that read the same keys meet in one L2.
-__device__ __forceinline__ bool unit_of(const PagedAttnArgs &a, int cap, int lane, Unit &u)
+// Workgroup ids that are congruent mod 8 run on one XCD: row groups that read the same keys meet in one L2.  What needs no load; false: there is no such unit.
+__device__ __forceinline__ bool unit_at(const PagedAttnArgs &a, int cap, Unit &u, int &rg)
 {
-    const uint32_t at = blockIdx.x >> 3, rg = at % (uint32_t)a.row_groups, stream = at / (uint32_t)a.row_groups * 8 + (blockIdx.x & 7);
-    if (stream >= (uint32_t)a.streams)
-        return false;
-    u.split = stream % (uint32_t)a.splits;
-    const uint32_t head = stream / (uint32_t)a.splits;
-    u.kvh = head % (uint32_t)a.hkv;
-    if (a.shared) {
+    const uint32_t block = blockIdx.x;
+    u.shared = block < (uint32_t)a.shared.blocks;
+    const uint32_t row_groups = u.shared ? a.shared.row_groups : a.own.row_groups, streams = u.shared ? a.shared.streams : a.own.streams;
+    u.splits = u.shared ? a.shared.splits : a.own.splits;
+    const uint32_t at = (block - (u.shared ? 0 : a.shared.blocks)) >> 3, slot = at / row_groups, stream = slot * 8 + (block & 7);
+    rg = at - slot * row_groups;
+    const uint32_t head = stream / (uint32_t)u.splits;
+    u.split = stream - head * u.splits;
+    u.slot = (u.shared ? a.shared.slot : a.own.slot) + u.split;
+    const uint32_t b = head / (uint32_t)a.hkv;      // (shared: 0)
+    u.kvh = head - b * a.hkv;
+    u.b = b;
+    u.row0 = rg * cap;
+    u.n_rows = a.rows;
+    u.lo = 0;
+    return stream < streams;
+}
+// And what does: the prefix length (asked for by the caller), the groups
+__device__ __forceinline__ bool unit_of(const PagedAttnArgs &a, int cap, int lane, int rg, int prefix, Unit &u)
+{
+    if (u.shared) {
         int n, shared;
         group_of_tile(a, rg, cap, lane, u.b, n, shared, u.row0);
         u.n_rows = n * a.rows;
-        u.lo = 0;
         u.hi = u.P = shared;
         return n > 0;
     }
-    u.b = head / (uint32_t)a.hkv;
-    u.row0 = rg * cap;
-    u.n_rows = a.rows;
-    u.P = clamped_prefix(a, uniform_load(a.prefix_len + u.b));
+    u.P = clamped_prefix(a, prefix);
     u.hi = u.P + a.n_tree;
-    u.lo = 0;
-    if (a.n_groups) {
-        int first, shared;
-        group_of(a, u.b, lane, first, shared);
-        u.lo = min(max(shared, 0), u.P);
-    }
+    if (a.n_groups)
+        u.lo = min(max(shared_by(a, u.b, lane), 0), u.P);
     return true;
 }
 
-// ---- the list of pages -----------------------------------------------------------------------------------------------
-constexpr uint32_t TREE_PAGE = 1u << 31;      // of an entry of s_logical: the tree's rows in it are meant
+// ---- selected pages --------------------------------------------------------------------------------------------------
+constexpr int SPARSE_LIST = 1024;              // entries of a list (trees of up to 64 nodes; others half of that)
+constexpr uint32_t TREE_PAGE = 1u << 31;      // of an entry of `logical`: the tree's rows in it are meant, otherwise the prefix's
 
-// Batch after batch of the pages that this split takes.  Positions along the list: x counts rows of its pages from `base` on; tiles of KEYS rows start at multiples of KEYS.
-template <int KEYS, int THREADS, bool SPARSE>
+// The pages of a sequence that some node of the workgroup's rows sees, and those of the tree: of them, by their rank, every splits-th, in LDS, from the `skip`-th of these on.  Rows of the list are numbered through its pages.
+template <int THREADS>
 struct PageList {
-    static constexpr int TILE = KEYS, SCAN = 4 * THREADS;      // SCAN: pages looked at in a batch, where they are selected
+    static constexpr int EACH = THREADS == 512 ? 2 : 4, SCAN = EACH * THREADS;      // pages looked at at a time: by a thread; by all
     int32_t *phys;
     uint32_t *logical;
     uint64_t *word;
-    int32_t *counts;
-    int n, base, first;             // entries; x of the first one; its place in the sequence (dense)
-    int tile, tile_end;             // of the batch
-    int next_page, end_page, all_first, all_end, rank, scanned;
+    int n, all;                     // entries; this split's pages
 
-    __device__ __forceinline__ void start(const PagedAttnArgs &a, const Unit &u, unsigned char *smem)
+    // By all threads; starts and ends with a barrier.
+    __device__ __forceinline__ void build(const PagedAttnArgs &a, const Unit &u, int cap, int tid, unsigned char *smem, int skip)
     {
         phys = reinterpret_cast<int32_t *>(smem);
         logical = reinterpret_cast<uint32_t *>(smem + 4 * a.list_size);
         word = reinterpret_cast<uint64_t *>(smem + 8 * a.list_size);
-        counts = reinterpret_cast<int32_t *>(smem + 8 * a.list_size + (SPARSE ? 8 * a.words * a.list_size : 0));
-        rewind(a, u);
-    }
-    __device__ __forceinline__ void rewind(const PagedAttnArgs &a, const Unit &u)
-    {
-        if constexpr (SPARSE) {
-            rank = scanned = 0;
-        } else {
-            const int t0 = u.lo / KEYS, t1 = u.hi > u.lo ? (u.hi + KEYS - 1) / KEYS : t0;
-            const int per = (t1 - t0 + a.splits - 1) / a.splits;
-            all_first = min(t0 + u.split * per, t1);
-            all_end = min(all_first + per, t1);
-            next_page = (all_first * KEYS) >> a.lg_page;
-            end_page = all_end > all_first ? min((int)(((int64_t)all_end * KEYS + (1 << a.lg_page) - 1) >> a.lg_page), a.max_pages) : next_page;
-        }
-    }
-    // The next batch, by all threads; false: there is none.  Starts and ends with a barrier.
-    __device__ __forceinline__ bool next(const PagedAttnArgs &a, const Unit &u, int tid)
-    {
+        int32_t *counts = reinterpret_cast<int32_t *>(smem + (8 + 8 * a.words) * a.list_size);
+        const int in_prefix = (u.P + (1 << a.lg_page) - 1) >> a.lg_page, tree_page = u.P >> a.lg_page;
+        const int total = in_prefix + ((u.hi - 1) >> a.lg_page) - tree_page + 1;
         const int32_t *table = a.table + (int64_t)u.b * a.max_pages;
-        if constexpr (!SPARSE) {
-            if (next_page >= end_page)
-                return false;
+        const int lane = tid & 63, wave = tid >> 6;
+        const uint64_t *nodes = a.nodes + ((int64_t)u.b * a.hkv + u.kvh) * a.max_pages * a.words;
+        const int node0 = (uint32_t)u.row0 / (uint32_t)a.group, node1 = (uint32_t)(min(u.row0 + cap, u.n_rows) - 1) / (uint32_t)a.group;
+        auto ours = [&](int w) {      // of word w
+            const int lo = max(node0 - 64 * w, 0), hi = min(node1 - 64 * w, 63);
+            return lo > hi ? 0ull : ~0ull >> (63 - hi) & ~0ull << lo;
+        };
+        auto upto = [&](int r) { return r > u.split ? (int)((uint32_t)(r - u.split + u.splits - 1) / (uint32_t)u.splits) : 0; };      // this split's among the first r
+        int rank = 0;
+        for (int scanned = 0; scanned < total; scanned += SCAN) {
             __syncthreads();
-            n = min(end_page - next_page, a.list_size);
-            for (int i = tid; i < n; i += THREADS)
-                phys[i] = min(max(table[next_page + i], 0), a.n_pages - 1);
-            first = next_page;
-            base = first << a.lg_page;
-            tile = max(all_first, base / KEYS);
-            next_page += n;
-            tile_end = next_page >= end_page ? all_end : min(all_end, (next_page << a.lg_page) / KEYS);
-            __syncthreads();
-            return true;
-        } else {
-            const int in_prefix = (u.P + (1 << a.lg_page) - 1) >> a.lg_page, tree_page = u.P >> a.lg_page;
-            const int total = in_prefix + ((u.hi - 1) >> a.lg_page) - tree_page + 1;
-            if (scanned >= total)
-                return false;
-            __syncthreads();
-            const int lane = tid & 63, wave = tid >> 6;
-            const uint64_t *nodes = a.nodes + ((int64_t)u.b * a.hkv + u.kvh) * a.max_pages * a.words;
-            const uint64_t last = a.n_tree & 63 ? (1ull << (a.n_tree & 63)) - 1 : ~0ull;
             int taken = 0;
             uint32_t mine = 0;
-            const int v0 = scanned + tid * 4;
+            const int v0 = scanned + tid * EACH;
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
+            for (int i = 0; i < EACH; i++) {
                 bool in = v0 + i >= in_prefix && v0 + i < total;
                 if (v0 + i < in_prefix)
                     for (int w = 0; w < a.words; w++)
-                        in = in || (nodes[(int64_t)(v0 + i) * a.words + w] & (w == a.words - 1 ? last : ~0ull)) != 0ull;
+                        in = in || (nodes[(int64_t)(v0 + i) * a.words + w] & ours(w)) != 0ull;
                 mine |= (uint32_t)in << i;
                 taken += in;
             }
@@ -214,22 +190,19 @@ struct PageList {
             if (lane == 63)
                 counts[wave] = sum;
             __syncthreads();
-            int before = rank, all = 0;
+            int r = rank + sum - taken;
 #pragma unroll
             for (int w = 0; w < THREADS / 64; w++) {
                 const int x = counts[w];
-                before += w < wave ? x : 0;
-                all += x;
+                r += w < wave ? x : 0;
+                rank += x;
             }
-            auto upto = [&](int r) { return r > u.split ? (r - u.split + a.splits - 1) / a.splits : 0; };      // this split's among the first r
-            const int skipped = upto(rank);
-            int r = before + sum - taken;
-            for (int i = 0; i < 4; i++) {
+            for (int i = 0; i < EACH; i++) {
                 if (!(mine >> i & 1))
                     continue;
-                if (r % a.splits == u.split) {
-                    const int at = upto(r) - skipped, v = v0 + i;
-                    const int page = v < in_prefix ? v : tree_page + v - in_prefix;
+                const int at = upto(r) - skip;
+                if ((uint32_t)r % (uint32_t)u.splits == (uint32_t)u.split && at >= 0 && at < a.list_size) {
+                    const int v = v0 + i, page = v < in_prefix ? v : tree_page + v - in_prefix;
                     phys[at] = min(max(table[page], 0), a.n_pages - 1);
                     logical[at] = (uint32_t)page | (v < in_prefix ? 0u : TREE_PAGE);
                     for (int w = 0; w < a.words; w++)
@@ -237,43 +210,32 @@ struct PageList {
                 }
                 r++;
             }
-            rank = __builtin_amdgcn_readfirstlane(rank + all);
-            n = __builtin_amdgcn_readfirstlane(upto(rank) - skipped);
-            scanned += SCAN;
-            base = first = 0;
-            tile = 0;
-            tile_end = ((n << a.lg_page) + KEYS - 1) / KEYS;
-            __syncthreads();
-            return true;
         }
+        all = __builtin_amdgcn_readfirstlane(upto(rank));
+        n = min(max(all - skip, 0), a.list_size);
+        __syncthreads();
     }
-    static size_t bytes(int list_size, int words) { return (size_t)list_size * (8 + (SPARSE ? 8 * words : 0)) + 64; }
+    static size_t bytes(int list_size, int words) { return (size_t)list_size * (8 + 8 * words) + 64; }
 };
 
-// Where 16 rows of the list stand (all of it the same in every lane).
+// Where 16 rows stand that are taken together (the same in every lane).
 struct Chunk {
-    int entry, at;                  // of the list; row in the page
+    int entry;                      // of the list
     int pos;                        // position of the first row
-    bool live, tree, prefix;        // the list has it; the rows that are meant: the tree's, the prefix's
+    bool live, tree, prefix;        // there are such rows; those that are meant: the tree's, the prefix's
 };
-template <bool SPARSE, class List>
-__device__ __forceinline__ Chunk chunk_at(const PagedAttnArgs &a, const List &list, int x)
+// Row x of a list
+template <class List>
+__device__ __forceinline__ Chunk listed_chunk(const PagedAttnArgs &a, const List &list, int x)
 {
     Chunk c;
-    x -= list.base;
     const int e = x >> a.lg_page;
     c.live = e < list.n;
     c.entry = min(e, list.n - 1);
-    c.at = x & ((1 << a.lg_page) - 1);
-    if constexpr (SPARSE) {
-        const uint32_t l = __builtin_amdgcn_readfirstlane((int)list.logical[c.entry]);
-        c.tree = l >> 31;
-        c.prefix = !c.tree;
-        c.pos = (int)((l & ~TREE_PAGE) << a.lg_page) + c.at;
-    } else {
-        c.tree = c.prefix = true;
-        c.pos = ((list.first + e) << a.lg_page) + c.at;
-    }
+    const uint32_t l = __builtin_amdgcn_readfirstlane((int)list.logical[c.entry]);
+    c.tree = l >> 31;
+    c.prefix = !c.tree;
+    c.pos = (int)((l & ~TREE_PAGE) << a.lg_page) + (x & ((1 << a.lg_page) - 1));
     return c;
 }
 
@@ -287,7 +249,7 @@ __device__ __forceinline__ Row row_at(const PagedAttnArgs &a, const Unit &u, int
     Row w;
     w.b = u.b;
     w.r = j;
-    if (a.shared) {
+    if (u.shared) {
         const int s = (uint32_t)j / (uint32_t)a.rows;
         w.b += s;
         w.r = j - s * a.rows;
@@ -297,9 +259,9 @@ __device__ __forceinline__ Row row_at(const PagedAttnArgs &a, const Unit &u, int
     return w;
 }
 __device__ __forceinline__ int64_t row_of_q(const PagedAttnArgs &a, const Row &w) { return ((int64_t)w.b * a.n_tree + w.node) * a.hq + w.head; }
-__device__ __forceinline__ int64_t row_of_part(const PagedAttnArgs &a, const Unit &u, const Row &w) { return (int64_t)(a.slot + u.split) * a.all_rows + ((int64_t)w.b * a.hkv + u.kvh) * a.rows + w.r; }
+__device__ __forceinline__ int64_t row_of_part(const PagedAttnArgs &a, const Unit &u, const Row &w) { return (int64_t)u.slot * a.all_rows + ((int64_t)w.b * a.hkv + u.kvh) * a.rows + w.r; }
 // Prefix positions below this are the row's
-__device__ __forceinline__ int row_limit(const PagedAttnArgs &a, const Unit &u, const Row &w) { return a.shared ? min(u.hi, clamped_prefix(a, a.prefix_len[w.b])) : u.P; }
+__device__ __forceinline__ int row_limit(const PagedAttnArgs &a, const Unit &u, const Row &w) { return u.shared ? min(u.hi, clamped_prefix(a, a.prefix_len[w.b])) : u.P; }
 
 __device__ __forceinline__ void put_ml(const PagedAttnArgs &a, const Unit &u, const Row &w, float m, float l)
 {
@@ -314,7 +276,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y)
     return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
 }
 
-// Which nodes of the tree each of the workgroup's rows sees, `words` words a row; by all threads, ends with a barrier.  parents: n_tree words of LDS.
+// Which nodes of the tree each of the workgroup's rows sees, `words` words a row in LDS; by all threads, ends with a barrier.  parents: n_tree words of LDS.
 __device__ __forceinline__ void build_masks(const PagedAttnArgs &a, const Unit &u, uint64_t *masks, int32_t *parents, int cap, int tid, int threads)
 {
     if (!a.tree_mask) {
@@ -323,7 +285,12 @@ __device__ __forceinline__ void build_masks(const PagedAttnArgs &a, const Unit &
         __syncthreads();
     }
     const uint64_t last = a.n_tree & 63 ? (1ull << (a.n_tree & 63)) - 1 : ~0ull;
-    for (int j = tid; j < min(cap, u.n_rows - u.row0); j += threads) {
+    for (int j = tid; j < cap; j += threads) {
+        if (u.row0 + j >= u.n_rows) {      // (no such row: it sees no node, so that its sums stay finite)
+            for (int w = 0; w < a.words; w++)
+                masks[j * a.words + w] = 0ull;
+            continue;
+        }
         const int node = (uint32_t)(u.row0 + j) / (uint32_t)a.group;
         if (a.tree_mask) {
             for (int w = 0; w < a.words; w++)
@@ -342,30 +309,62 @@ __device__ __forceinline__ void build_masks(const PagedAttnArgs &a, const Unit &
     }
     __syncthreads();
 }
-// Of the nodes n0 .. n0 + 3 (n0 may be negative) those that a row's mask has, as four bits
-__device__ __forceinline__ uint32_t four_nodes(const PagedAttnArgs &a, const uint64_t *mask, int n0)
+// Trees of up to 64 nodes: lane l gets node l's mask.  parent: of this lane's node.  The paths are joined by halves: a node's mask holds its path in front of `up`, and takes in what `up` has found.
+__device__ __forceinline__ uint64_t small_tree(int lane, int n_tree, int parent)
+{
+    uint32_t lo = lane < 32 ? 1u << lane : 0u, hi = lane < 32 ? 0u : 1u << (lane - 32);
+    int up = lane < n_tree && parent < lane ? parent : -1;      // (a parent that does not precede its node is none)
+    while (__any(up >= 0)) {
+        const int from = max(up, 0);
+        const uint32_t l = __shfl(lo, from), h = __shfl(hi, from);
+        const int next = __shfl(up, from);
+        if (up >= 0) {
+            lo |= l;
+            hi |= h;
+            up = next;
+        }
+    }
+    return (uint64_t)hi << 32 | lo;
+}
+// Of the nodes n0 .. n0 + 3 (n0 may be negative) those that a row's mask has, as four bits: the mask of a small tree, or that in LDS
+__device__ __forceinline__ uint32_t four_nodes(const PagedAttnArgs &a, uint64_t small, const uint64_t *mask, int n0)
 {
     if (n0 <= -4 || n0 >= a.n_tree)
         return 0u;
-    if (n0 < 0)
-        return (uint32_t)(mask[0] << -n0) & 15u;
-    const int w = n0 >> 6, s = n0 & 63;
-    uint64_t x = mask[w] >> s;
-    if (s > 60 && w + 1 < a.words)
-        x |= mask[w + 1] << (64 - s);
-    return (uint32_t)x & 15u;
+    if (a.words > 1) {
+        if (n0 < 0)
+            return (uint32_t)(mask[0] << -n0) & 15u;
+        const int w = n0 >> 6, s = n0 & 63;
+        uint64_t x = mask[w] >> s;
+        if (s > 60 && w + 1 < a.words)
+            x |= mask[w + 1] << (64 - s);
+        return (uint32_t)x & 15u;
+    }
+    return (uint32_t)(n0 < 0 ? small << -n0 : small >> n0) & 15u;
 }
 
 // ---- row by row ------------------------------------------------------------------------------------------------------
-// The workgroup's rows, one to a wave at a time: a lane takes a key's whole product, then D / 64 channels of the weighted sum.  Only rows that the node sees are read.
-// s_q: D floats for each wave.
-template <class T, int D, int THREADS, bool SPARSE, class List>
-__device__ void attend_rows_singly(const PagedAttnArgs &a, const Unit &u, List &list, const uint64_t *masks, float *s_q, int cap)
+// LDS of attend_rows_singly: queries, masks, parents, the list
+template <int D, int THREADS>
+constexpr int single_masks() { return THREADS / 64 * D * 4; }
+template <int D, int THREADS>
+int single_bytes(int cap, int words) { return single_masks<D, THREADS>() + cap * words * 8 + DREAM_MAX_TREE * 4; }
+
+// The workgroup's rows, one to a wave at a time: a lane takes a key's whole product, then D / 64 channels of the weighted sum.  Only rows that the node sees are read.  Where the keys are shared
+// out, a workgroup has every splits-th run of `run` keys from the tile of `tile` keys on that holds the first.
+template <class T, int D, int THREADS, bool SPARSE>
+__device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const Unit &u, int cap, int tile, int run, unsigned char *smem)
 {
     constexpr int NW = THREADS / 64, CH = D / 64, N = 16 / sizeof(T);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int count = min(cap, u.n_rows - u.row0), ps_mask = (1 << a.lg_page) - 1;
-    float *q = s_q + wave * D;
+    float *q = reinterpret_cast<float *>(smem) + wave * D;
+    uint64_t *masks = reinterpret_cast<uint64_t *>(smem + single_masks<D, THREADS>());
+    int32_t *parents = reinterpret_cast<int32_t *>(masks + cap * a.words);
+    PageList<THREADS> list;
+    const int32_t *table = a.table + (int64_t)u.b * a.max_pages;
+    if (!u.shared)
+        build_masks(a, u, masks, parents, cap, tid, THREADS);
     for (int j0 = 0; j0 < count; j0 += NW) {
         const bool mine = j0 + wave < count;
         const int j = min(j0 + wave, count - 1);
@@ -378,62 +377,75 @@ __device__ void attend_rows_singly(const PagedAttnArgs &a, const Unit &u, List &
             else
                 q[i] = bf16_bits_to_float(*p);
         }
+        wave_lds_fence();
         float m = -INFINITY, l = 0.0f, o[CH];
 #pragma unroll
         for (int i = 0; i < CH; i++)
             o[i] = 0.0f;
-        list.rewind(a, u);
-        while (list.next(a, u, tid)) {
-            const int end = min(SPARSE ? list.n << a.lg_page : list.base + (list.n << a.lg_page), list.tile_end * List::TILE);
-            for (int x0 = list.tile * List::TILE; x0 < end; x0 += 64) {
-                const int x = x0 + lane - list.base, e = min(x >> a.lg_page, list.n - 1), at = x & ps_mask;
-                int pos;
-                bool sees = x0 + lane < end;
-                const uint32_t entry = SPARSE ? list.logical[e] : 0u;
-                pos = (SPARSE ? (int)((entry & ~TREE_PAGE) << a.lg_page) : (list.first + e) << a.lg_page) + at;
-                const bool in_prefix = pos >= u.lo && pos < limit && (!SPARSE || (!(entry >> 31) && (list.word[e * a.words + (w.node >> 6)] >> (w.node & 63) & 1)));
-                const int node = pos - u.P;
-                const bool in_tree = !a.shared && node >= 0 && node < a.n_tree && (!SPARSE || entry >> 31) && (masks[j * a.words + (node >> 6)] >> (node & 63) & 1);
-                sees = sees && (in_prefix || in_tree);
-                float s = -INFINITY;
-                const int64_t row = ((((int64_t)list.phys[e] * a.hkv + u.kvh) << a.lg_page) + at) * D;
-                if (sees) {
-                    const T *k = reinterpret_cast<const T *>(a.k) + row;
-                    float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                    for (int i = 0; i < D; i += N) {
-                        const u32x4 raw = *reinterpret_cast<const u32x4 *>(k + i);
+        // 64 keys: this lane's row of the page and where it stands; `kind`: which of them are meant (1: the prefix's, 2: the tree's)
+        auto keys = [&](bool there, int page, int pos, int kind, const uint64_t *word) {
+            const int node = pos - u.P;
+            const bool in_prefix = (kind & 1) && pos >= u.lo && pos < limit && (!SPARSE || (word[w.node >> 6] >> (w.node & 63) & 1));
+            const bool in_tree = (kind & 2) && !u.shared && node >= 0 && node < a.n_tree && (masks[j * a.words + (node >> 6)] >> (node & 63) & 1);
+            const bool sees = there && (in_prefix || in_tree);
+            float s = -INFINITY;
+            const int64_t row = ((((int64_t)page * a.hkv + u.kvh) << a.lg_page) + (pos & ps_mask)) * D;
+            if (sees) {
+                const T *k = reinterpret_cast<const T *>(a.k) + row;
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                for (int i = 0; i < D; i += N) {
+                    const u32x4 raw = *reinterpret_cast<const u32x4 *>(k + i);
 #pragma unroll
-                        for (int d = 0; d < 4; d++) {
-                            if constexpr (std::is_same_v<T, float>) {
-                                sum[d] = __builtin_fmaf(__uint_as_float(raw[d]), q[i + d], sum[d]);
-                            } else {
-                                sum[d] = __builtin_fmaf(__uint_as_float(raw[d] << 16), q[i + 2 * d], sum[d]);
-                                sum[d] = __builtin_fmaf(__uint_as_float(raw[d] & 0xffff0000u), q[i + 2 * d + 1], sum[d]);
-                            }
+                    for (int d = 0; d < 4; d++) {
+                        if constexpr (std::is_same_v<T, float>) {
+                            sum[d] = __builtin_fmaf(__uint_as_float(raw[d]), q[i + d], sum[d]);
+                        } else {
+                            sum[d] = __builtin_fmaf(__uint_as_float(raw[d] << 16), q[i + 2 * d], sum[d]);
+                            sum[d] = __builtin_fmaf(__uint_as_float(raw[d] & 0xffff0000u), q[i + 2 * d + 1], sum[d]);
                         }
                     }
-                    s = ((sum[0] + sum[1]) + (sum[2] + sum[3])) * a.scale_log2;
                 }
-                const float top = fmaxf(m, wave_max(s));
-                const float f = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top), ref = fmaxf(top, -FLT_MAX);
-                m = top;
-                const float p = sees ? __builtin_amdgcn_exp2f(s - ref) : 0.0f;
-                l = l * f + p;
+                s = ((sum[0] + sum[1]) + (sum[2] + sum[3])) * a.scale_log2;
+            }
+            const float top = fmaxf(m, wave_max(s));
+            const float f = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top), ref = fmaxf(top, -FLT_MAX);
+            m = top;
+            const float p = sees ? __builtin_amdgcn_exp2f(s - ref) : 0.0f;
+            l = l * f + p;
 #pragma unroll
-                for (int i = 0; i < CH; i++)
-                    o[i] *= f;
-                for (uint64_t left = __ballot(sees); left; left &= left - 1) {
-                    const int key = __builtin_ctzll(left);
-                    const float pk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(p), key));
-                    const int64_t of = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(row >> 32), key) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)row, key));
-                    const T *v = reinterpret_cast<const T *>(a.v) + of + lane * CH;
+            for (int i = 0; i < CH; i++)
+                o[i] *= f;
+            for (uint64_t left = __ballot(sees && s != -INFINITY); left; left &= left - 1) {      // (a key of weight 0 through a score of -inf adds nothing, whatever its values)
+                const int key = __builtin_ctzll(left);
+                const float pk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(p), key));
+                const int64_t of = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(row >> 32), key) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)row, key));
+                const T *v = reinterpret_cast<const T *>(a.v) + of + lane * CH;
 #pragma unroll
-                    for (int i = 0; i < CH; i++) {
-                        if constexpr (std::is_same_v<T, float>)
-                            o[i] = __builtin_fmaf(pk, v[i], o[i]);
-                        else
-                            o[i] = __builtin_fmaf(pk, bf16_bits_to_float(v[i]), o[i]);
-                    }
+                for (int i = 0; i < CH; i++) {
+                    if constexpr (std::is_same_v<T, float>)
+                        o[i] = __builtin_fmaf(pk, v[i], o[i]);
+                    else
+                        o[i] = __builtin_fmaf(pk, bf16_bits_to_float(v[i]), o[i]);
+                }
+            }
+        };
+        if constexpr (SPARSE) {
+            int skip = 0;
+            do {
+                list.build(a, u, cap, tid, reinterpret_cast<unsigned char *>(parents + DREAM_MAX_TREE), skip);
+                for (int x0 = 0; x0 < list.n << a.lg_page; x0 += 64) {
+                    const int e = min((x0 + lane) >> a.lg_page, list.n - 1);
+                    const uint32_t entry = list.logical[e];
+                    keys(x0 + lane < list.n << a.lg_page, list.phys[e], (int)((entry & ~TREE_PAGE) << a.lg_page) + ((x0 + lane) & ps_mask), entry >> 31 ? 2 : 1, list.word + e * a.words);
+                }
+                skip += a.list_size;
+            } while (skip < list.all);
+        } else {
+            for (int start = u.lo / tile * tile + u.split * run; start < u.hi; start += u.splits * run) {
+                const int end = min(start + run, u.hi);
+                for (int x0 = start; x0 < end; x0 += 64) {
+                    const int pos = x0 + lane;
+                    keys(pos < end, min(max(table[min(pos, u.hi - 1) >> a.lg_page], 0), a.n_pages - 1), pos, 3, nullptr);
                 }
             }
         }
@@ -456,220 +468,165 @@ __device__ void attend_rows_singly(const PagedAttnArgs &a, const Unit &u, List &
 }
 
 // float32: there for its precision and for small shapes.
-constexpr int SINGLE_ROWS = 4;
+constexpr int SINGLE_ROWS = 4, SINGLE_RUN = 64;
 template <int D, bool SPARSE>
 __global__ __launch_bounds__(256) void paged_f32_kernel(PagedAttnArgs a)
 {
-    using List = PageList<64, 256, SPARSE>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    float *s_q = reinterpret_cast<float *>(smem);
-    uint64_t *masks = reinterpret_cast<uint64_t *>(smem + 4 * D * 4);
-    int32_t *parents = reinterpret_cast<int32_t *>(masks + SINGLE_ROWS * a.words);
     Unit u;
-    if (!unit_of(a, SINGLE_ROWS, threadIdx.x & 63, u))
+    int rg;
+    if (!unit_at(a, SINGLE_ROWS, u, rg))
         return;
-    if (!a.shared)
-        build_masks(a, u, masks, parents, SINGLE_ROWS, threadIdx.x, 256);
-    List list;
-    list.start(a, u, smem + 4 * D * 4 + SINGLE_ROWS * a.words * 8 + DREAM_MAX_TREE * 4);
-    attend_rows_singly<float, D, 256, SPARSE>(a, u, list, masks, s_q, SINGLE_ROWS);
+    const int prefix = u.shared ? 0 : uniform_load(a.prefix_len + u.b);
+    if (unit_of(a, SINGLE_ROWS, threadIdx.x & 63, rg, prefix, u))
+        attend_rows_singly<float, D, 256, SPARSE>(a, u, SINGLE_ROWS, SINGLE_RUN, SINGLE_RUN, smem);
 }
 
 // ---- bf16 ------------------------------------------------------------------------------------------------------------
-template <int D, int QT, int WR, int WK>
-struct PagedGeom {
-    static constexpr int NW = WR * WK, THREADS = 64 * NW, CAP = 16 * QT * WR;
-    static constexpr int ROW = 2 * D, KEYS = WR == 1 || D == 256 ? 32 : 64, TILE = KEYS * ROW, STAGE = 2 * TILE;
-    static constexpr int NS = WR == 1 ? 2 : 3;
-    static constexpr int LOADS = TILE / 1024 / WR;                          // of a wave, a tile and K or V
-    static constexpr int STAGES = WK * NS * STAGE;
-    static constexpr int JOIN = WR == 1 ? WK * 16 * QT * (D + 4) * 4 : 0;   // the waves' sums meet here
-    static constexpr int MASKS = STAGES > JOIN ? STAGES : JOIN;
-    static_assert(LOADS * 1024 * WR == TILE, "loads");
-    static int masks(int words) { return CAP * words * 8; }
-    static int small(int words) { return masks(words) + DREAM_MAX_TREE * 4 + NW * 8 + WK * 16 * QT * 8; }      // masks, parents, flags, (m, l) of the waves
-};
-
 template <int N>
 __device__ __forceinline__ void wait_loads()
 {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
-
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+// The same value, from which the compiler forms nothing ahead of the loop it stands in: the addresses of a step are a few instructions, and all of them kept are more registers than there are.
+__device__ __forceinline__ int here(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+__device__ __forceinline__ int here_scalar(int x)
+{
+    x = __builtin_amdgcn_readfirstlane(x);
+    asm volatile("" : "+s"(x));
+    return x;
+}
 __device__ __forceinline__ float largest(f32x4 a) { return fmaxf(fmaxf(fmaxf(a[0], a[1]), a[2]), a[3]); }
 
-template <int D, int QT, int WR, int WK, bool SPARSE>
-__global__ __launch_bounds__(64 * WR * WK) void paged_attn_kernel(PagedAttnArgs a)
-{
-    using G = PagedGeom<D, QT, WR, WK>;
-    constexpr int ROW = G::ROW, KEYS = G::KEYS, NKS = D / 32, NDT = D / 16, LPR = ROW / 16, RPI = 1024 / ROW, NS = G::NS;
-    using List = PageList<KEYS, G::THREADS, SPARSE>;
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wr = wave % WR, wk = wave / WR;
-    const int c = lane & 15, g = lane >> 4;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
-    uint64_t *masks = reinterpret_cast<uint64_t *>(smem + G::MASKS);
-    int32_t *parents = reinterpret_cast<int32_t *>(smem + G::MASKS + G::CAP * a.words * 8);
-    int32_t *flags = parents + DREAM_MAX_TREE;
-    float2 *s_ml = reinterpret_cast<float2 *>(flags + 2 * G::NW);
-    unsigned char *list_at = reinterpret_cast<unsigned char *>(s_ml + WK * 16 * QT);
-
-    Unit u;
-    if (!unit_of(a, G::CAP, lane, u))
-        return;
-    List list;
-    list.start(a, u, list_at);
-
-    // ---- query fragments: lane (c, g) has row c's channels 8 g .. of every 32
+// The query rows of a wave, QT tiles of 16, and their sums.  Lane (c, g) = (lane % 16, lane / 16) has of row c: of the queries the channels 8 g .. of every 32; of O^T the channels
+// 16 dt + 4 g + r; and scores of the keys 4 g + r of every 16.
+template <int D, int QT, bool SPARSE>
+struct QueryRows {
+    static constexpr int ROW = 2 * D, NKS = D / 32, NDT = D / 16;
     bf16x8 qf[QT][NKS];
-    int limit[QT], node[QT];
-    int whole = 0x7fffffff;                       // prefix positions below it are everyone's
-#pragma unroll
-    for (int qt = 0; qt < QT; qt++) {
-        const Row w = row_at(a, u, min(u.row0 + (wr * QT + qt) * 16 + c, u.n_rows - 1));
-        const unsigned char *q = a.q + row_of_q(a, w) * ROW + g * 16;
-#pragma unroll
-        for (int ks = 0; ks < NKS; ks++)
-            qf[qt][ks] = *reinterpret_cast<const bf16x8 *>(q + ks * 64);
-        limit[qt] = row_limit(a, u, w);
-        node[qt] = w.node;
-        whole = min(whole, limit[qt]);
-    }
-    if (a.shared) {
-#pragma unroll
-        for (int s = 1; s < 16; s *= 2)
-            whole = min(whole, __shfl_xor(whole, s));
-        whole = __builtin_amdgcn_readfirstlane(whole);
-    } else {
-        whole = u.P;
-        build_masks(a, u, masks, parents, G::CAP, tid, G::THREADS);
-    }
-
     f32x4 o[QT][NDT];
     float m[QT], l[QT];
-#pragma unroll
-    for (int qt = 0; qt < QT; qt++) {
-        m[qt] = -INFINITY;
-        l[qt] = 0.0f;
-#pragma unroll
-        for (int dt = 0; dt < NDT; dt++)
-            o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    const int foff = fragment_k<ROW>(c, g), voff = fragment_v<ROW>(c, g);
-    const int krow = lane / LPR, kl = piece_k<ROW>(lane), vl = piece_v<ROW>(lane);
-    const float scale_log2 = a.scale_log2;
+    int limit[QT], node[QT];
+    uint64_t small[QT];                           // what a row sees of a tree of up to 64 nodes
+    const uint64_t *large;                        // of a larger one: in LDS, row c's of tile 0
+    int whole;                                    // prefix positions below it are everyone's
 
-    auto stage_at = [&](int i) { return (wk * NS + i % NS) * G::STAGE; };
-    // The wave's share of tile t: 16-row pieces that its load instructions lie in, each within a page
-    auto issue = [&](int t, int at) {
+    __device__ __forceinline__ void load(const PagedAttnArgs &a, const Unit &u, int first, int c, int g)
+    {
 #pragma unroll
-        for (int i = 0; i < G::LOADS; i++) {
-            const int j = wr * G::LOADS + i;
-            const Chunk ch = chunk_at<SPARSE>(a, list, t * KEYS + (j * RPI & ~15));
-            const int page = __builtin_amdgcn_readfirstlane(list.phys[ch.entry]);
-            const int64_t from = ((((int64_t)page * a.hkv + u.kvh) << a.lg_page) + ch.at + (j * RPI & 15)) * ROW;
-            lds_load16(a.k + from, (uint32_t)(krow * ROW + (kl ^ swizzle_k<ROW>(j))), lds0 + at + j * 1024);
-            lds_load16(a.v + from, (uint32_t)(krow * ROW + (vl ^ swizzle_v<ROW>(j))), lds0 + at + G::TILE + j * 1024);
-        }
-    };
-    auto plain = [&](const Chunk &ch) { return ch.live && ch.prefix && ch.pos >= u.lo && ch.pos + 16 <= whole; };      // all its rows are everyone's (or everyone's whose page it is)
-    // Zeros over the values of rows that are nobody's, by the wave that loaded them
-    auto clear_dead = [&](int t, int at) {
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < G::LOADS; i++) {
-            const int j = wr * G::LOADS + i;
-            const Chunk ch = chunk_at<SPARSE>(a, list, t * KEYS + (j * RPI & ~15));
-            if (plain(ch))
-                continue;
-            const int pos = ch.pos + (j * RPI & 15) + krow;
-            const bool seen = ch.live && ((ch.prefix && pos >= u.lo && pos < u.P) || (ch.tree && pos >= u.P && pos < u.hi));
-            if (!seen)
-                *reinterpret_cast<u32x4 *>(smem + at + G::TILE + j * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
-            any = true;
-        }
-        if (any)
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    };
-
-    // 32 keys from row `sub` * 32 of the tile at `at` on
-    auto compute = [&](int t, int at, int sub) {
-        Chunk ch[2];
-        bool straight = true;
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            ch[h] = chunk_at<SPARSE>(a, list, t * KEYS + sub * 32 + h * 16);
-            straight = straight && plain(ch[h]);
-        }
-        bool in[2][QT];                           // selected pages: is the lane's node one of theirs
-        if constexpr (SPARSE) {
-            bool any = !straight;
-#pragma unroll
-            for (int h = 0; h < 2; h++)
-#pragma unroll
-                for (int qt = 0; qt < QT; qt++) {
-                    in[h][qt] = list.word[ch[h].entry * a.words + (node[qt] >> 6)] >> (node[qt] & 63) & 1;
-                    any = any || in[h][qt];
-                }
-            if (!__any(any))
-                return;
-        }
-        const unsigned char *kt = smem + at + sub * 32 * ROW, *vt = smem + at + G::TILE + sub * 32 * ROW;
-        f32x4 s[2][QT];
-        {
-            bf16x8 kf[NKS][2];
+        for (int qt = 0; qt < QT; qt++) {
+            const Row w = row_at(a, u, min(first + qt * 16 + c, u.n_rows - 1));
+            const unsigned char *q = a.q + row_of_q(a, w) * ROW + g * 16;
 #pragma unroll
             for (int ks = 0; ks < NKS; ks++)
+                qf[qt][ks] = *reinterpret_cast<const bf16x8 *>(q + ks * 64);
+            node[qt] = w.node;
+            limit[qt] = u.shared ? a.prefix_len[w.b] : 0;
+            m[qt] = -INFINITY;
+            l[qt] = 0.0f;
 #pragma unroll
-                for (int h = 0; h < 2; h++)
-                    kf[ks][h] = *reinterpret_cast<const bf16x8 *>(kt + h * 16 * ROW + at_key_step(foff, ks));
+            for (int dt = 0; dt < NDT; dt++)
+                o[qt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+    // parent: of the lane's node of a small tree; tid, threads, masks, parents: for a large one
+    __device__ __forceinline__ void see(const PagedAttnArgs &a, const Unit &u, int first, int cap, int parent, int c, int tid, int threads, uint64_t *masks, int32_t *parents, int in_group)
+    {
+        whole = u.P;
+        if (u.shared) {
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++) {
+                limit[qt] = min(u.hi, clamped_prefix(a, limit[qt]));
+                whole = min(whole, limit[qt]);
+                small[qt] = 0ull;
+            }
+#pragma unroll
+            for (int s = 1; s < 16; s *= 2)
+                whole = min(whole, __shfl_xor(whole, s));
+            whole = __builtin_amdgcn_readfirstlane(whole);
+            return;
+        }
+        const uint64_t tree = a.words > 1 || a.tree_mask ? 0ull : small_tree(tid & 63, a.n_tree, parent);
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++) {
+            limit[qt] = u.P;
+            small[qt] = 0ull;
+            if (a.words > 1)
+                continue;
+            if (a.tree_mask)
+                small[qt] = a.tree_mask[(int64_t)u.b * a.n_tree + node[qt]] & (a.n_tree & 63 ? (1ull << (a.n_tree & 63)) - 1 : ~0ull);
+            else
+                small[qt] = (uint64_t)(uint32_t)__shfl((int)(tree >> 32), node[qt]) << 32 | (uint32_t)__shfl((int)tree, node[qt]);
+            if (first + qt * 16 + c >= u.n_rows)
+                small[qt] = 0ull;
+        }
+        if (a.words > 1) {
+            build_masks(a, u, masks, parents, cap, tid, threads);
+            large = masks + (in_group + c) * a.words;
+        }
+    }
+
+    // S^T = K Q^T of 32 keys
+    __device__ __forceinline__ void scores(const unsigned char *kt, int foff, f32x4 (&s)[2][QT]) const
+    {
+        bf16x8 kf[NKS][2];
+#pragma unroll
+        for (int ks = 0; ks < NKS; ks++)
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+                kf[ks][h] = *reinterpret_cast<const bf16x8 *>(kt + h * 16 * ROW + at_key_step(foff, ks));
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++)
+                s[h][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < NKS; ks++)
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
                 for (int qt = 0; qt < QT; qt++)
-                    s[h][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < NKS; ks++)
-#pragma unroll
-                for (int h = 0; h < 2; h++)
-#pragma unroll
-                    for (int qt = 0; qt < QT; qt++)
-                        s[h][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks][h], qf[qt][ks], s[h][qt], 0, 0, 0);
-        }
-        // ---- online softmax: a lane owns query row c and keys 4 g + r of both halves
+                    s[h][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks][h], qf[qt][ks], s[h][qt], 0, 0, 0);
+    }
+    // All rows of the chunk are everyone's (or everyone's whose page it is)
+    __device__ __forceinline__ bool plain(const Unit &u, const Chunk &c) const { return c.live && c.prefix && c.pos >= u.lo && c.pos + 16 <= whole; }
+
+    // Online softmax of 32 keys; bit h * QT + qt of `in`: does the row see chunk h's page (selected pages).  WHOLE: all rows of both chunks are everyone's (or everyone's whose page it is).
+    // (Two functions with a raise of the reference each: values that either kind of tile may have written are copied on both.)
+    template <bool WHOLE>
+    __device__ __forceinline__ void softmax(const PagedAttnArgs &a, const Unit &u, const Chunk (&ch)[2], uint32_t in, int g, f32x4 (&s)[2][QT], bf16x8 (&pf)[QT])
+    {
+        const float scale_log2 = a.scale_log2;
         float top[QT];
-        straight = straight && scale_log2 >= 0.0f;
-        if (straight) {
 #pragma unroll
-            for (int qt = 0; qt < QT; qt++) {
-                if constexpr (SPARSE) {
-                    const float x = in[0][qt] ? largest(s[0][qt]) : -INFINITY, y = in[1][qt] ? largest(s[1][qt]) : -INFINITY;
-                    top[qt] = fmaxf(x, y) * scale_log2;
-                } else {
-                    top[qt] = fmaxf(largest(s[0][qt]), largest(s[1][qt])) * scale_log2;
-                }
-            }
-        } else {
-#pragma unroll
-            for (int qt = 0; qt < QT; qt++) {
-                top[qt] = -INFINITY;
+        for (int qt = 0; qt < QT; qt++) {
+            if constexpr (WHOLE && SPARSE) {
+                const float x = in >> qt & 1u ? largest(s[0][qt]) : -INFINITY, y = in >> (QT + qt) & 1u ? largest(s[1][qt]) : -INFINITY;
+                top[qt] = fmaxf(x, y) * scale_log2;
+            } else if constexpr (WHOLE) {
+                top[qt] = fmaxf(largest(s[0][qt]), largest(s[1][qt])) * scale_log2;
+            } else {
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     const int pos = ch[h].pos + 4 * g;
                     uint32_t vis = 0u;
-                    if (ch[h].live && ch[h].prefix && (!SPARSE || in[h][qt])) {
+                    if (ch[h].live && ch[h].prefix && (!SPARSE || (in >> (h * QT + qt) & 1u))) {
 #pragma unroll
                         for (int r = 0; r < 4; r++)
                             vis |= (uint32_t)(pos + r >= u.lo && pos + r < limit[qt]) << r;
                     }
-                    if (ch[h].live && ch[h].tree && !a.shared)
-                        vis |= four_nodes(a, masks + ((wr * QT + qt) * 16 + c) * a.words, pos - u.P);
+                    if (ch[h].live && ch[h].tree && !u.shared)
+                        vis |= four_nodes(a, small[qt], large + qt * 16 * a.words, pos - u.P);
 #pragma unroll
-                    for (int r = 0; r < 4; r++) {
+                    for (int r = 0; r < 4; r++)
                         s[h][qt][r] = vis >> r & 1u ? s[h][qt][r] * scale_log2 : -INFINITY;
-                        top[qt] = fmaxf(top[qt], s[h][qt][r]);
-                    }
                 }
+                top[qt] = fmaxf(largest(s[0][qt]), largest(s[1][qt]));
             }
         }
         bool raise = false;
@@ -681,43 +638,37 @@ __global__ __launch_bounds__(64 * WR * WK) void paged_attn_kernel(PagedAttnArgs 
             for (int qt = 0; qt < QT; qt++) {
                 float x = fmaxf(top[qt], __shfl_xor(top[qt], 16));
                 x = fmaxf(x, __shfl_xor(x, 32));
-                if (x > m[qt] + SLACK) {
-                    const float f = __builtin_amdgcn_exp2f(m[qt] - x);       // 0 where nothing was seen before
-                    m[qt] = x;
-                    l[qt] *= f;
+                // (no branch of its own: sums that lanes may or may not have changed would be held twice)
+                const bool up = x > m[qt] + SLACK;
+                const float f = up ? __builtin_amdgcn_exp2f(m[qt] - x) : 1.0f;       // 0 where nothing was seen before
+                m[qt] = up ? x : m[qt];
+                l[qt] *= f;
 #pragma unroll
-                    for (int dt = 0; dt < NDT; dt++)
-                        o[qt][dt] *= f;
-                }
+                for (int dt = 0; dt < NDT; dt++)
+                    o[qt][dt] *= f;
             }
         }
-        bf16x8 pf[QT];
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
             const float ref = fmaxf(m[qt], -FLT_MAX);      // where all scores so far are -inf, their weight is 0 and not exp(-inf + inf)
             float sum = 0.0f;
-            if (straight) {
 #pragma unroll
-                for (int h = 0; h < 2; h++) {
-                    const float mult = SPARSE && !in[h][qt] ? 0.0f : scale_log2, less = SPARSE && !in[h][qt] ? -INFINITY : -ref;
+            for (int h = 0; h < 2; h++) {
+                const bool out = WHOLE && SPARSE && !(in >> (h * QT + qt) & 1u);
+                const float mult = out ? 0.0f : WHOLE ? scale_log2 : 1.0f, less = out ? -INFINITY : -ref;
 #pragma unroll
-                    for (int r = 0; r < 4; r++) {
-                        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][qt][r], mult, less));
-                        sum += p;
-                        pf[qt][h * 4 + r] = (__bf16)p;      // rounded as the matrix instruction takes it, half a step of 2^-8; the sum stays float32
-                    }
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const float p = __builtin_amdgcn_exp2f(s[e >> 2][qt][e & 3] - ref);
+                for (int r = 0; r < 4; r++) {
+                    const float p = __builtin_amdgcn_exp2f(WHOLE ? __builtin_fmaf(s[h][qt][r], mult, less) : s[h][qt][r] + less);
                     sum += p;
-                    pf[qt][e] = (__bf16)p;
+                    pf[qt][h * 4 + r] = (__bf16)p;      // rounded as the matrix instruction takes it, half a step of 2^-8; the sum stays float32
                 }
             }
             l[qt] += sum;
         }
-        // ---- O^T += V^T P^T
+    }
+    // O^T += V^T P^T
+    __device__ __forceinline__ void add_values(const unsigned char *vt, int voff, const bf16x8 (&pf)[QT])
+    {
 #pragma unroll
         for (int dt = 0; dt < NDT; dt++) {
             const unsigned char *vp = vt + at_column_tile(voff, dt);
@@ -728,135 +679,449 @@ __global__ __launch_bounds__(64 * WR * WK) void paged_attn_kernel(PagedAttnArgs 
             for (int qt = 0; qt < QT; qt++)
                 o[qt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt], o[qt][dt], 0, 0, 0);
         }
-    };
+    }
+    // The rows' sums over all four g; true where one is not finite
+    __device__ __forceinline__ bool finish()
+    {
+        float strange = 0.0f;
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++) {
+            l[qt] += __shfl_xor(l[qt], 16);
+            l[qt] += __shfl_xor(l[qt], 32);
+            strange = __builtin_fmaf(l[qt], 0.0f, strange);
+#pragma unroll
+            for (int dt = 0; dt < NDT; dt++)
+#pragma unroll
+                for (int r = 0; r < 4; r++)
+                    strange = __builtin_fmaf(o[qt][dt][r], 0.0f, strange);
+        }
+        return __any(strange != 0.0f);      // (0 * inf and 0 * NaN are NaN)
+    }
+    // Of the pages of two chunks, which the rows see; false where none does
+    template <class List>
+    __device__ __forceinline__ bool seen_by(const PagedAttnArgs &a, const List &list, const Chunk (&ch)[2], bool straight, uint32_t &in) const
+    {
+        in = 0u;
+        if constexpr (SPARSE) {
+#pragma unroll
+            for (int h = 0; h < 2; h++)
+#pragma unroll
+                for (int qt = 0; qt < QT; qt++)
+                    in |= (uint32_t)(list.word[ch[h].entry * a.words + (node[qt] >> 6)] >> (node[qt] & 63) & 1) << (h * QT + qt);
+            return !straight || __any(in != 0u);
+        }
+        return true;
+    }
+};
 
-    while (list.next(a, u, tid)) {
-        const int first = list.tile + wk, steps = max(0, (list.tile_end - first + WK - 1) / WK);
-        constexpr int AHEAD = WR == 1 ? NS : NS - 1;
+// The page of this lane's tile of a run of 64 (tile first + lane * stride; `further`: rows into it)
+__device__ __forceinline__ int page_of_tile(const PagedAttnArgs &a, int b, int row)
+{
+    const int32_t *table = a.table + (int64_t)b * a.max_pages;
+    return min(max(table[min(row >> a.lg_page, a.max_pages - 1)], 0), a.n_pages - 1);
+}
+
+// Takes a workgroup's rows again, where a sum is not finite.  Not part of the kernels' code: it would have registers of its own beside theirs.
+template <int D, int THREADS, bool SPARSE>
+__device__ __noinline__ void attend_again(const __attribute__((address_space(4))) PagedAttnArgs *kernel_args, int cap, int tile, int run, unsigned char *smem)
+{
+    const PagedAttnArgs &a = *(const PagedAttnArgs *)kernel_args;
+    Unit u;
+    int rg;
+    if (!unit_at(a, cap, u, rg))
+        return;
+    const int prefix = u.shared ? 0 : uniform_load(a.prefix_len + u.b);
+    if (unit_of(a, cap, threadIdx.x & 63, rg, prefix, u))
+        attend_rows_singly<uint16_t, D, THREADS, SPARSE>(a, u, cap, tile, run, smem);
+}
+
+template <int D, int QT, int NW>
+struct KeysGeom {
+    static constexpr int THREADS = 64 * NW, CAP = 16 * QT, ROW = 2 * D, TILE = 32 * ROW, LOADS = TILE / 1024;
+    static constexpr int STAGES = NW * 2 * TILE, JOIN = NW * CAP * (D + 4) * 4, MAIN = STAGES > JOIN ? STAGES : JOIN;
+    static int bytes(int words) { return MAIN + NW * CAP * 8 + NW * 8 + (words > 1 ? CAP * words * 8 + DREAM_MAX_TREE * 4 : 0); }
+};
+
+// Few rows: the waves take the key tiles in turn, each for all of the rows, and never meet until the end.  A wave asks for its next keys as soon as a tile's scores are there, and for its next
+// values as soon as they are added up.
+template <int D, int QT, int NW, bool SPARSE>
+__global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
+{
+    using G = KeysGeom<D, QT, NW>;
+    constexpr int ROW = G::ROW, LPR = ROW / 16, RPI = 1024 / ROW, HALF = G::LOADS / 2;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
+    float2 *s_ml = reinterpret_cast<float2 *>(smem + G::MAIN);
+    int32_t *flags = reinterpret_cast<int32_t *>(s_ml + NW * G::CAP);
+    uint64_t *masks = reinterpret_cast<uint64_t *>(flags + 2 * NW);
+    int32_t *parents = reinterpret_cast<int32_t *>(masks + G::CAP * a.words);
+
+    Unit u;
+    int rg;
+    if (!unit_at(a, G::CAP, u, rg))
+        return;
+    // what needs no load is asked for first: of an own part the pages of the wave's tiles, the prefix length, the tree, the queries
+    const int prefix = u.shared ? 0 : uniform_load(a.prefix_len + u.b);
+    const int stride = u.splits * NW, mine = u.split * NW + wave;
+    int pages[2] = {0, 0};
+    auto ask_pages = [&](int first) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; i++)
-            if (i < steps)
-                issue(first + i * WK, stage_at(i));
-        for (int i = 0; i < steps; i++) {
-            const int t = first + i * WK, at = stage_at(i);
-            if (i + AHEAD <= steps)
-                wait_loads<(AHEAD - 1) * 2 * G::LOADS>();
-            else
-                wait_loads<0>();
-            clear_dead(t, at);
-            if constexpr (WR > 1) {
-                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the tile is there, and all have done with the stage that is loaded next
-                if (i + AHEAD < steps)
-                    issue(t + AHEAD * WK, stage_at(i + AHEAD));
-            }
+        for (int h = 0; h < 2; h++)
+            pages[h] = page_of_tile(a, u.b, (first + lane * stride) * 32 + h * 16);
+    };
+    if (!SPARSE && !a.n_groups)
+        ask_pages(mine);
+    int parent = -1;
+    if (!u.shared && a.words == 1 && !a.tree_mask)
+        parent = a.parent[(int64_t)u.b * a.n_tree + min(lane, a.n_tree - 1)];
+    if (!unit_of(a, G::CAP, lane, rg, prefix, u))
+        return;
+    PageList<G::THREADS> list;
+    if constexpr (SPARSE)
+        list.build(a, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (a.words > 1 ? G::CAP * a.words + DREAM_MAX_TREE / 2 : 0)), 0);
+    QueryRows<D, QT, SPARSE> rows;
+    rows.load(a, u, u.row0, c, g);
+    const int tile0 = u.lo / 32;
+    if (!SPARSE && a.n_groups)
+        ask_pages(tile0 + mine);
+
+    const int foff = fragment_k<ROW>(c, g), voff = fragment_v<ROW>(c, g);
+    const int krow = lane / LPR, k_lane = krow * ROW + piece_k<ROW>(lane), v_lane = krow * ROW + piece_v<ROW>(lane);
+    const int stage = wave * 2 * G::TILE;
+    auto chunk = [&](int i, int h) -> Chunk {
+        if constexpr (SPARSE) {
+            return listed_chunk(a, list, (wave + i * NW) * 32 + h * 16);
+        } else {
+            const int pos = (tile0 + mine + i * stride) * 32 + h * 16;
+            return Chunk{0, pos, pos < u.hi, true, true};
+        }
+    };
+    auto place = [&](int i, int h) {              // of the chunk's rows, in bytes
+        int page, at;
+        if constexpr (SPARSE) {
+            const int x = (wave + i * NW) * 32 + h * 16;
+            page = __builtin_amdgcn_readfirstlane(list.phys[min(x >> a.lg_page, list.n - 1)]);
+            at = x;
+        } else {
+            page = __builtin_amdgcn_readlane(pages[h], i & 63);
+            at = (tile0 + mine + i * stride) * 32 + h * 16;
+        }
+        return ((((int64_t)page * a.hkv + u.kvh) << a.lg_page) + (at & ((1 << a.lg_page) - 1))) * ROW;
+    };
+    auto ask_k = [&](int i) {
+        if (!SPARSE && (i & 63) == 0 && i)
+            ask_pages(tile0 + mine + i * stride);
 #pragma unroll
-            for (int sub = 0; sub < KEYS / 32; sub++)
-                compute(t, at, sub);
-            if constexpr (WR == 1) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if (i + AHEAD < steps)
-                    issue(t + AHEAD * WK, at);
+        for (int h = 0; h < 2; h++) {
+            const unsigned char *from = a.k + place(i, h);
+            const int at = here(k_lane);
+            const uint32_t to = here_scalar(lds0 + stage);
+#pragma unroll
+            for (int j = 0; j < HALF; j++)
+                lds_load16(from + j * 1024, (uint32_t)(at ^ swizzle_k<ROW>(h * HALF + j)), to + (h * HALF + j) * 1024);
+        }
+    };
+    auto ask_v = [&](int i) {
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const unsigned char *from = a.v + place(i, h);
+            const int at = here(v_lane);
+            const uint32_t to = here_scalar(lds0 + stage + G::TILE);
+#pragma unroll
+            for (int j = 0; j < HALF; j++)
+                lds_load16(from + j * 1024, (uint32_t)(at ^ swizzle_v<ROW>(h * HALF + j)), to + (h * HALF + j) * 1024);
+        }
+    };
+    // Zeros over the values of rows that are nobody's
+    auto clear_dead = [&](const Chunk (&ch)[2]) {
+        const int vat = here_scalar(stage + G::TILE);
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            if (rows.plain(u, ch[h]))
+                continue;
+#pragma unroll 1
+            for (int j = 0; j < HALF; j++) {
+                const int pos = ch[h].pos + j * RPI + krow;
+                if (!(ch[h].live && ((ch[h].prefix && pos >= u.lo && pos < u.P) || (ch[h].tree && pos >= u.P && pos < u.hi))))
+                    *reinterpret_cast<u32x4 *>(smem + vat + (h * HALF + j) * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
             }
         }
+        wait_lds();
+    };
+    auto take = [&](int steps) {
+        for (int i = 0; i < steps; i++) {
+            Chunk ch[2] = {chunk(i, 0), chunk(i, 1)};
+            const bool straight = rows.plain(u, ch[0]) && rows.plain(u, ch[1]);
+            uint32_t in;
+            rows.seen_by(a, list, ch, straight, in);
+            f32x4 s[2][QT];
+            bf16x8 pf[QT];
+            wait_loads<G::LOADS>();
+            rows.scores(smem + stage, here(foff), s);
+            wait_lds();
+            if (i + 1 < steps)
+                ask_k(i + 1);
+            if (straight && a.scale_log2 >= 0.0f)
+                rows.template softmax<true>(a, u, ch, in, g, s, pf);
+            else
+                rows.template softmax<false>(a, u, ch, in, g, s, pf);
+            if (i + 1 < steps)
+                wait_loads<G::LOADS>();
+            else
+                wait_loads<0>();
+            if (!straight)
+                clear_dead(ch);
+            rows.add_values(smem + stage + G::TILE, here(voff), pf);
+            wait_lds();
+            if (i + 1 < steps)
+                ask_v(i + 1);
+        }
+    };
+    const int steps = SPARSE ? (((list.n << a.lg_page) + 31) / 32 - wave + NW - 1) / NW : u.hi > u.lo ? ((u.hi + 31) / 32 - tile0 - mine + stride - 1) / stride : 0;
+    if (steps > 0) {
+        ask_k(0);
+        ask_v(0);
     }
+    rows.see(a, u, u.row0, G::CAP, parent, c, tid, G::THREADS, masks, parents, 0);
+    take(steps);
 
-    // ---- the end: sums that are not finite have the rows taken again
-    float strange = 0.0f;
-#pragma unroll
-    for (int qt = 0; qt < QT; qt++) {
-        l[qt] += __shfl_xor(l[qt], 16);
-        l[qt] += __shfl_xor(l[qt], 32);
-        strange = __builtin_fmaf(l[qt], 0.0f, strange);
-#pragma unroll
-        for (int dt = 0; dt < NDT; dt++)
-#pragma unroll
-            for (int r = 0; r < 4; r++)
-                strange = __builtin_fmaf(o[qt][dt][r], 0.0f, strange);
-    }
-    const bool mine = __any(strange != 0.0f);      // (0 * inf and 0 * NaN are NaN)
+    // ---- the waves' sums
+    const bool strange = rows.finish() || (SPARSE && list.all > list.n);      // (a list longer than what it was planned for: row by row)
     if (lane == 0)
-        flags[wave] = mine;
-    if constexpr (WR == 1) {
-        if (g == 0)
+        flags[wave] = strange;
+    if (g == 0)
 #pragma unroll
-            for (int qt = 0; qt < QT; qt++)
-                s_ml[wk * 16 * QT + qt * 16 + c] = make_float2(m[qt], l[qt]);
-    }
+        for (int qt = 0; qt < QT; qt++)
+            s_ml[wave * G::CAP + qt * 16 + c] = make_float2(rows.m[qt], rows.l[qt]);
     __syncthreads();
     int again = 0;
 #pragma unroll
-    for (int w = 0; w < G::NW; w++)
+    for (int w = 0; w < NW; w++)
         again |= flags[w];
     if (again) {
-        attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(a, u, list, masks, reinterpret_cast<float *>(smem), G::CAP);
+        attend_again<D, G::THREADS, SPARSE>((const __attribute__((address_space(4))) PagedAttnArgs *)__builtin_amdgcn_kernarg_segment_ptr(), G::CAP, 32, 32 * NW, smem);
         return;
     }
-    if constexpr (WR == 1) {
-        constexpr int STR = D + 4;
-        float *join = reinterpret_cast<float *>(smem);
+    constexpr int STR = D + 4;
+    float *join = reinterpret_cast<float *>(smem);
 #pragma unroll
-        for (int qt = 0; qt < QT; qt++) {
-            float most = -INFINITY;
+    for (int qt = 0; qt < QT; qt++) {
+        float most = -INFINITY;
 #pragma unroll
-            for (int w = 0; w < WK; w++)
-                most = fmaxf(most, s_ml[w * 16 * QT + qt * 16 + c].x);
-            const float f = m[qt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[qt] - most);
-            float *row = join + ((wk * QT + qt) * 16 + c) * STR + 4 * g;
+        for (int w = 0; w < NW; w++)
+            most = fmaxf(most, s_ml[w * G::CAP + qt * 16 + c].x);
+        const float f = rows.m[qt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(rows.m[qt] - most);
+        float *row = join + ((wave * QT + qt) * 16 + c) * STR + 4 * g;
 #pragma unroll
-            for (int dt = 0; dt < NDT; dt++)
-                *reinterpret_cast<f32x4 *>(row + dt * 16) = o[qt][dt] * f;
+        for (int dt = 0; dt < D / 16; dt++)
+            *reinterpret_cast<f32x4 *>(row + dt * 16) = rows.o[qt][dt] * f;
+    }
+    __syncthreads();
+    const int count = min(G::CAP, u.n_rows - u.row0);
+    for (int i = tid; i < count * (D / 4); i += G::THREADS) {
+        const int j = i / (D / 4), ch = i % (D / 4);
+        const Row w = row_at(a, u, u.row0 + j);
+        float most = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int x = 0; x < NW; x++)
+            most = fmaxf(most, s_ml[x * G::CAP + j].x);
+        f32x4 all = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < NW; x++) {
+            const float2 ml = s_ml[x * G::CAP + j];
+            sum += ml.x == -INFINITY ? 0.0f : ml.y * __builtin_amdgcn_exp2f(ml.x - most);
+            all += *reinterpret_cast<const f32x4 *>(join + (x * G::CAP + j) * STR + ch * 4);
         }
-        __syncthreads();
-        const int count = min(G::CAP, u.n_rows - u.row0);
-        for (int i = tid; i < count * (D / 4); i += G::THREADS) {
-            const int j = i / (D / 4), ch = i % (D / 4);
-            const Row w = row_at(a, u, u.row0 + j);
-            float most = -INFINITY, sum = 0.0f;
-#pragma unroll
-            for (int x = 0; x < WK; x++)
-                most = fmaxf(most, s_ml[x * 16 * QT + j].x);
-            f32x4 all = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int x = 0; x < WK; x++) {
-                const float2 ml = s_ml[x * 16 * QT + j];
-                sum += ml.x == -INFINITY ? 0.0f : ml.y * __builtin_amdgcn_exp2f(ml.x - most);
-                all += *reinterpret_cast<const f32x4 *>(join + (x * 16 * QT + j) * STR + ch * 4);
-            }
-            if (ch == 0)
-                put_ml(a, u, w, most, sum);
-            if (a.n_slots > 1) {
-                *reinterpret_cast<f32x4 *>(a.part_o + row_of_part(a, u, w) * D + ch * 4) = all;
-            } else {
-                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row_of_q(a, w) * D + ch * 4) = make_uint2(pack_bf16(all[0] * inv, all[1] * inv), pack_bf16(all[2] * inv, all[3] * inv));
-            }
+        if (ch == 0)
+            put_ml(a, u, w, most, sum);
+        if (a.n_slots > 1) {
+            *reinterpret_cast<f32x4 *>(a.part_o + row_of_part(a, u, w) * D + ch * 4) = all;
+        } else {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row_of_q(a, w) * D + ch * 4) = make_uint2(pack_bf16(all[0] * inv, all[1] * inv), pack_bf16(all[2] * inv, all[3] * inv));
         }
-    } else {
+    }
+}
+
+template <int D, int QT, int WR>
+struct RowsGeom {
+    static constexpr int THREADS = 64 * WR, CAP = 16 * QT * WR, ROW = 2 * D, KEYS = D == 256 ? 32 : 64, TILE = KEYS * ROW, STAGE = 2 * TILE, NS = 3;
+    static constexpr int LOADS = TILE / 1024 / WR;                          // of a wave, a tile and K or V: rows of one chunk
+    static constexpr int MAIN = NS * STAGE;
+    static_assert(LOADS * 1024 * WR == TILE && KEYS / WR <= 16, "loads");
+    static int bytes(int words) { return MAIN + WR * 8 + (words > 1 ? CAP * words * 8 + DREAM_MAX_TREE * 4 : 0); }
+};
+
+// Many rows: the waves share the tiles and have rows of their own; one barrier a tile, two tiles on their way.
+template <int D, int QT, int WR, bool SPARSE>
+__global__ __launch_bounds__(64 * WR) void paged_rows_kernel(PagedAttnArgs a)
+{
+    using G = RowsGeom<D, QT, WR>;
+    constexpr int ROW = G::ROW, KEYS = G::KEYS, LPR = ROW / 16, RPI = 1024 / ROW, NS = G::NS;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
+    int32_t *flags = reinterpret_cast<int32_t *>(smem + G::MAIN);
+    uint64_t *masks = reinterpret_cast<uint64_t *>(flags + 2 * WR);
+    int32_t *parents = reinterpret_cast<int32_t *>(masks + G::CAP * a.words);
+
+    Unit u;
+    int rg;
+    if (!unit_at(a, G::CAP, u, rg))
+        return;
+    const int prefix = u.shared ? 0 : uniform_load(a.prefix_len + u.b);
+    const int own_rows = wave * (KEYS / WR), own_chunk = own_rows & ~15;      // of a tile: the rows that this wave asks for, and the chunk that they lie in
+    int pages = 0;
+    auto ask_pages = [&](int first) { pages = page_of_tile(a, u.b, (first + lane * u.splits) * KEYS + own_chunk); };
+    if (!SPARSE && !a.n_groups)
+        ask_pages(u.split);
+    int parent = -1;
+    if (!u.shared && a.words == 1 && !a.tree_mask)
+        parent = a.parent[(int64_t)u.b * a.n_tree + min(lane, a.n_tree - 1)];
+    if (!unit_of(a, G::CAP, lane, rg, prefix, u))
+        return;
+    PageList<G::THREADS> list;
+    if constexpr (SPARSE)
+        list.build(a, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (a.words > 1 ? G::CAP * a.words + DREAM_MAX_TREE / 2 : 0)), 0);
+    QueryRows<D, QT, SPARSE> rows;
+    const int first_row = u.row0 + wave * QT * 16;
+    rows.load(a, u, first_row, c, g);
+    const int tile0 = u.lo / KEYS + u.split;
+    if (!SPARSE && a.n_groups)
+        ask_pages(tile0);
+
+    const int foff = fragment_k<ROW>(c, g), voff = fragment_v<ROW>(c, g);
+    const int krow = lane / LPR, k_lane = krow * ROW + piece_k<ROW>(lane), v_lane = krow * ROW + piece_v<ROW>(lane);
+    auto chunk = [&](int i, int at) -> Chunk {
+        if constexpr (SPARSE) {
+            return listed_chunk(a, list, i * KEYS + at);
+        } else {
+            const int pos = (tile0 + i * u.splits) * KEYS + at;
+            return Chunk{0, pos, pos < u.hi, true, true};
+        }
+    };
+    auto ask = [&](int i, int stage) {
+        int page, x;
+        if constexpr (SPARSE) {
+            x = i * KEYS + own_rows;
+            page = __builtin_amdgcn_readfirstlane(list.phys[min(x >> a.lg_page, list.n - 1)]);
+        } else {
+            if ((i & 63) == 0 && i)
+                ask_pages(tile0 + i * u.splits);
+            x = (tile0 + i * u.splits) * KEYS + own_rows;
+            page = __builtin_amdgcn_readlane(pages, i & 63);
+        }
+        const int64_t from = ((((int64_t)page * a.hkv + u.kvh) << a.lg_page) + (x & ((1 << a.lg_page) - 1))) * ROW;
+        const uint32_t to = lds0 + stage * G::STAGE + wave * G::LOADS * 1024;
 #pragma unroll
-        for (int qt = 0; qt < QT; qt++) {
-            const int j = u.row0 + (wr * QT + qt) * 16 + c;
-            if (j >= u.n_rows)
-                continue;
-            const Row w = row_at(a, u, j);
-            if (g == 0)
-                put_ml(a, u, w, m[qt], l[qt]);
-            if (a.n_slots > 1) {
-                float *row = a.part_o + row_of_part(a, u, w) * D + 4 * g;
+        for (int j = 0; j < G::LOADS; j++)
+            lds_load16(a.k + from + j * 1024, (uint32_t)(k_lane ^ swizzle_k<ROW>(wave * G::LOADS + j)), to + j * 1024);
 #pragma unroll
-                for (int dt = 0; dt < NDT; dt++)
-                    *reinterpret_cast<f32x4 *>(row + dt * 16) = o[qt][dt];
-            } else {
-                const float inv = l[qt] == 0.0f ? 0.0f : 1.0f / l[qt];
-                uint16_t *row = static_cast<uint16_t *>(a.out) + row_of_q(a, w) * D + 4 * g;
+        for (int j = 0; j < G::LOADS; j++)
+            lds_load16(a.v + from + j * 1024, (uint32_t)(v_lane ^ swizzle_v<ROW>(wave * G::LOADS + j)), to + G::TILE + j * 1024);
+    };
+    // Zeros over the values of rows that are nobody's, by the wave that loaded them
+    auto clear_dead = [&](int i, int stage) {
+        const Chunk ch = chunk(i, own_chunk);
+        if (rows.plain(u, ch))
+            return;
 #pragma unroll
-                for (int dt = 0; dt < NDT; dt++)
-                    *reinterpret_cast<uint2 *>(row + dt * 16) = make_uint2(pack_bf16(o[qt][dt][0] * inv, o[qt][dt][1] * inv), pack_bf16(o[qt][dt][2] * inv, o[qt][dt][3] * inv));
+        for (int j = 0; j < G::LOADS; j++) {
+            const int pos = ch.pos + (own_rows & 15) + j * RPI + krow;
+            if (!(ch.live && ((ch.prefix && pos >= u.lo && pos < u.P) || (ch.tree && pos >= u.P && pos < u.hi))))
+                *reinterpret_cast<u32x4 *>(smem + stage * G::STAGE + G::TILE + (wave * G::LOADS + j) * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+        }
+    };
+    auto take = [&](int steps) {
+        int stage = 0, next = NS - 1;
+        for (int i = 0; i < steps; i++) {
+            if (i + NS - 1 <= steps)
+                wait_loads<(NS - 2) * 2 * G::LOADS>();
+            else
+                wait_loads<0>();
+            clear_dead(i, stage);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the tile is there, and all have done with the stage that is loaded next
+            if (i + NS - 1 < steps)
+                ask(i + NS - 1, next);
+            const unsigned char *kt = smem + stage * G::STAGE, *vt = kt + G::TILE;
+#pragma unroll
+            for (int sub = 0; sub < KEYS / 32; sub++) {
+                Chunk ch[2] = {chunk(i, sub * 32), chunk(i, sub * 32 + 16)};
+                const bool straight = rows.plain(u, ch[0]) && rows.plain(u, ch[1]);
+                uint32_t in;
+                if (!rows.seen_by(a, list, ch, straight, in))
+                    continue;
+                f32x4 s[2][QT];
+                bf16x8 pf[QT];
+                rows.scores(kt + sub * 32 * ROW, here(foff), s);
+                if (straight && a.scale_log2 >= 0.0f)
+                    rows.template softmax<true>(a, u, ch, in, g, s, pf);
+                else
+                    rows.template softmax<false>(a, u, ch, in, g, s, pf);
+                rows.add_values(vt + sub * 32 * ROW, here(voff), pf);
             }
+            stage = stage == NS - 1 ? 0 : stage + 1;
+            next = next == NS - 1 ? 0 : next + 1;
+        }
+    };
+    const int steps = SPARSE ? ((list.n << a.lg_page) + KEYS - 1) / KEYS : u.hi > u.lo ? max(0, ((u.hi + KEYS - 1) / KEYS - tile0 + u.splits - 1) / u.splits) : 0;
+#pragma unroll
+    for (int i = 0; i < NS - 1; i++)
+        if (i < steps)
+            ask(i, i);
+    rows.see(a, u, first_row, G::CAP, parent, c, tid, G::THREADS, masks, parents, wave * QT * 16);
+    take(steps);
+
+    const bool strange = rows.finish() || (SPARSE && list.all > list.n);      // (a list longer than what it was planned for: row by row)
+    if (lane == 0)
+        flags[wave] = strange;
+    __syncthreads();
+    int again = 0;
+#pragma unroll
+    for (int w = 0; w < WR; w++)
+        again |= flags[w];
+    if (again) {
+        attend_again<D, G::THREADS, SPARSE>((const __attribute__((address_space(4))) PagedAttnArgs *)__builtin_amdgcn_kernarg_segment_ptr(), G::CAP, KEYS, KEYS, smem);
+        return;
+    }
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++) {
+        const int j = first_row + qt * 16 + c;
+        if (j >= u.n_rows)
+            continue;
+        const Row w = row_at(a, u, j);
+        if (g == 0)
+            put_ml(a, u, w, rows.m[qt], rows.l[qt]);
+        if (a.n_slots > 1) {
+            float *row = a.part_o + row_of_part(a, u, w) * D + 4 * g;
+#pragma unroll
+            for (int dt = 0; dt < D / 16; dt++)
+                *reinterpret_cast<f32x4 *>(row + dt * 16) = rows.o[qt][dt];
+        } else {
+            const float inv = rows.l[qt] == 0.0f ? 0.0f : 1.0f / rows.l[qt];
+            uint16_t *row = static_cast<uint16_t *>(a.out) + row_of_q(a, w) * D + 4 * g;
+#pragma unroll
+            for (int dt = 0; dt < D / 16; dt++)
+                *reinterpret_cast<uint2 *>(row + dt * 16) =
+                    make_uint2(pack_bf16(rows.o[qt][dt][0] * inv, rows.o[qt][dt][1] * inv), pack_bf16(rows.o[qt][dt][2] * inv, rows.o[qt][dt][3] * inv));
         }
     }
 }
 
 // ---- the parts of a row, in their order: D / 4 lanes a row -----------------------------------------------------------
+__device__ __forceinline__ bool in_a_group(const PagedAttnArgs &a, int b)
+{
+    int lo = 0, hi = a.n_groups;      // group_start ascends: the last group that starts at b or in front
+    while (lo < hi) {
+        const int g = (lo + hi) / 2;
+        if (a.group_start[g] <= b)
+            lo = g + 1;
+        else
+            hi = g;
+    }
+    return lo > 0 && b < a.group_start[lo];
+}
 template <class T, int D>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a)
 {
@@ -871,13 +1136,8 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a)
     w.b = head / (uint32_t)a.hkv;
     w.node = (uint32_t)w.r / (uint32_t)a.group;
     w.head = (head - w.b * a.hkv) * a.group + w.r - w.node * a.group;
-    int first_slot = 0;
-    if (a.shared_slots) {                 // a sequence outside every group has no shared parts
-        bool in = false;
-        for (int g = 0; g < a.n_groups && !in; g++)
-            in = a.group_start[g] <= w.b && w.b < a.group_start[g + 1];
-        first_slot = in ? 0 : a.shared_slots;
-    }
+    // (a sequence outside every group has no shared parts)
+    const int first_slot = a.shared_slots && !in_a_group(a, w.b) ? a.shared_slots : 0;
     float most = -INFINITY, sum = 0.0f;
     for (int s = first_slot; s < a.n_slots; s++)
         most = fmaxf(most, a.part_ml[s * a.all_rows + id].x);
@@ -904,139 +1164,174 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a)
 // ------------------------------------------------------------------------------------------------
 // host side
 // ------------------------------------------------------------------------------------------------
-struct Shape {                            // of a launch's workgroups: query tiles of a wave, waves for rows, waves for keys; qt = 0: float32
-    int qt, wr, wk;
-    int cap() const { return qt ? 16 * qt * wr : SINGLE_ROWS; }
-    int keys(int D) const { return wr == 1 || D == 256 ? 32 : 64; }
-    int threads() const { return qt ? 64 * wr * wk : 256; }
+enum Form { SINGLY, KEYS, ROWS };
+struct Shape {                            // of a launch's workgroups
+    Form form;
+    int qt, waves;                        // query tiles of a wave
+    int cap() const { return form == SINGLY ? SINGLE_ROWS : form == KEYS ? 16 * qt : 16 * qt * waves; }
+    int keys(int D) const { return form == SINGLY ? SINGLE_RUN : form == KEYS ? 32 * waves : D == 256 ? 32 : 64; }      // that a step of a workgroup takes
+    bool operator==(const Shape &o) const { return form == o.form && qt == o.qt && waves == o.waves; }
 };
-struct Launch {
+struct Segment {
     Shape shape;
-    int splits, row_groups, streams;
+    Part part;
 };
 struct PagedPlan {
-    Launch shared, own;
-    int n_slots;
+    Segment shared, own;
+    int n_slots, shared_slots;
     int64_t all_rows;
     size_t bytes;
 };
 
+// The shapes there are
+constexpr int keys_waves(int D, int qt) { return D == 256 || qt == 4 ? 4 : 8; }
+constexpr int keys_tiles(int D) { return D == 256 ? 1 : D == 128 ? 2 : 4; }      // at most
+constexpr int rows_tiles(int D) { return D == 256 ? 1 : 2; }
+
 Shape shape_for(int D, bool f32, int64_t rows)
 {
     if (f32)
-        return {0, 1, 4};
-    const int wk = D == 256 ? 2 : 4;
-    if (rows <= 16)
-        return {1, 1, wk};
-    if (rows <= 32)
-        return {2, 1, wk};
-    if (D == 256)
-        return {1, 8, 1};
-    if (rows <= 64)
-        return {4, 1, wk};
-    return rows <= 128 ? Shape{2, 4, 1} : Shape{2, 8, 1};
+        return {SINGLY, 0, 4};
+    const int tiles = q_tiles_override(), waves = tile_waves_override();
+    if (waves == 8 || (!waves && !tiles && rows > 16 * keys_tiles(D)))
+        return {ROWS, rows_tiles(D), 8};
+    const int qt = tiles ? tiles : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    const int most = keys_tiles(D), taken = qt >= most ? most : qt >= 2 ? 2 : 1;
+    return {KEYS, taken, keys_waves(D, taken)};
 }
 
 int splits_for(const Shape &s, int D, int64_t units, int64_t keys)
 {
-    const int64_t tiles = (keys + s.keys(D) - 1) / s.keys(D), least = s.wk > 1 ? 2 * s.wk : 4;
+    const int64_t steps = (keys + s.keys(D) - 1) / s.keys(D);
     if (const int forced = kv_splits_override())
         return forced < 64 ? forced : 64;
     int64_t n = 256 / (units > 0 ? units : 1);
-    if (n > tiles / least)
-        n = tiles / least;
+    if (n > steps / 2)
+        n = steps / 2;
     return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
 }
+// So that the lists of selected pages hold all that a workgroup's rows may see
+int least_splits(const dream_page_desc *pages, int32_t n_tree, int64_t max_kv, int64_t seen_pages)
+{
+    int64_t most = (max_kv + pages->page_size - 1) / pages->page_size;
+    if (seen_pages > 0 && seen_pages * n_tree < most)
+        most = seen_pages * n_tree;
+    return ceil_div(most + n_tree / pages->page_size + 2, n_tree > 64 ? SPARSE_LIST / 2 : SPARSE_LIST);
+}
 
-PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32_t n_tree, int64_t max_kv, int32_t n_groups, int64_t max_shared, int64_t seen_pages)
+PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32_t n_tree, int64_t max_kv, int32_t n_groups, int64_t max_shared, bool sparse, int64_t seen_pages)
 {
     PagedPlan p = {};
+    const int D = d->head_dim;
     const int64_t capacity = paged_rows(pages), rows = (int64_t)n_tree * (d->n_q_heads / d->n_kv_heads);
     max_kv = max_kv < 1 ? 1 : max_kv > capacity ? capacity : max_kv;
     max_shared = max_shared < 1 ? 1 : max_shared > max_kv ? max_kv : max_shared;
     const bool f32 = d->dtype == DREAM_F32;
-    p.own.shape = shape_for(d->head_dim, f32, rows);
-    p.own.row_groups = ceil_div(rows, p.own.shape.cap());
-    const int64_t heads = (int64_t)d->batch * d->n_kv_heads;
+    auto segment = [&](Segment &s, int64_t of, int64_t row_groups, int64_t heads, int64_t keys, int least) {
+        s.part.row_groups = (int)row_groups;
+        s.part.splits = splits_for(s.shape, D, heads * of, keys);
+        if (s.part.splits < least)
+            s.part.splits = least;
+        s.part.streams = (int)(heads * s.part.splits);
+        s.part.blocks = ceil_div(s.part.streams, 8) * 8 * s.part.row_groups;
+        s.part.slot = p.n_slots;
+        p.n_slots += s.part.splits;
+    };
+    if (n_groups) {
+        p.shared.shape = shape_for(D, f32, d->batch * rows / n_groups);
+        const int64_t groups = d->batch * rows / p.shared.shape.cap();
+        segment(p.shared, groups + 1, groups + n_groups, d->n_kv_heads, max_shared, 1);
+        p.shared_slots = p.n_slots;
+    }
+    p.own.shape = shape_for(D, f32, rows);
+    const int64_t heads = (int64_t)d->batch * d->n_kv_heads, row_groups = ceil_div(rows, p.own.shape.cap());
     int64_t own_keys = n_groups ? max_kv - max_shared + 1 : max_kv;
     if (seen_pages > 0 && seen_pages * pages->page_size + n_tree < own_keys)
         own_keys = seen_pages * pages->page_size + n_tree;
-    p.own.splits = splits_for(p.own.shape, d->head_dim, heads * p.own.row_groups, own_keys);
-    p.own.streams = (int)(heads * p.own.splits);
-    p.n_slots = p.own.splits;
+    segment(p.own, row_groups, row_groups, heads, own_keys, sparse ? least_splits(pages, n_tree, max_kv, seen_pages) : 1);
     p.all_rows = heads * rows;
-    if (n_groups) {
-        p.shared.shape = shape_for(d->head_dim, f32, d->batch * rows / n_groups);
-        p.shared.row_groups = (int)(d->batch * rows / p.shared.shape.cap() + n_groups);
-        p.shared.splits = splits_for(p.shared.shape, d->head_dim, (int64_t)d->n_kv_heads * (p.shared.row_groups - n_groups + 1), max_shared);
-        p.shared.streams = d->n_kv_heads * p.shared.splits;
-        p.n_slots += p.shared.splits;
-    }
-    p.bytes = p.n_slots > 1 ? (size_t)p.n_slots * p.all_rows * (d->head_dim + 2) * 4 : 0;
+    p.bytes = p.n_slots > 1 ? (size_t)p.n_slots * p.all_rows * (D + 2) * 4 : 0;
     return p;
 }
 
-template <int D, int QT, int WR, int WK, bool SPARSE>
-int launch_bf16(PagedAttnArgs &a, int blocks, hipStream_t st)
+// One kernel: of the bytes of LDS that it may take, and its launch
+template <class F>
+int launch_kernel(F *kernel, const PagedAttnArgs &a, int threads, size_t lds, const char *name, hipStream_t st)
 {
-    using G = PagedGeom<D, QT, WR, WK>;
-    static std::atomic<uint64_t> done{0};
-    using List = PageList<G::KEYS, G::THREADS, SPARSE>;
-    a.list_size = SPARSE ? List::SCAN / a.splits + 2 : DENSE_LIST;
-    const size_t lds = (size_t)G::MASKS + G::small(a.words) + List::bytes(a.list_size, a.words);
-    auto *kernel = &paged_attn_kernel<D, QT, WR, WK, SPARSE>;
-    if (int rc = raise_lds_limit(done, reinterpret_cast<const void *>(kernel), 160 * 1024, "paged attention"))
-        return rc;
     if (lds > 160 * 1024)
-        return fail(DREAM_ERR_UNSUPPORTED, "paged attention: %zu bytes of LDS", lds);
-    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(G::THREADS), lds, st, a);
-    return check_launch("paged_attn_kernel");
+        return fail(DREAM_ERR_UNSUPPORTED, "%s: %zu bytes of LDS", name, lds);
+    hipLaunchKernelGGL(kernel, dim3(a.shared.blocks + a.own.blocks), dim3(threads), lds, st, a);
+    return check_launch(name);
+}
+template <int THREADS, bool SPARSE>
+size_t list_bytes(PagedAttnArgs &a)
+{
+    using List = PageList<THREADS>;
+    if (!SPARSE)
+        return 0;
+    a.list_size = a.words > 1 ? SPARSE_LIST / 2 : SPARSE_LIST;
+    return List::bytes(a.list_size, a.words);
+}
+template <int D, int QT, int NW, bool SPARSE>
+int launch_keys(PagedAttnArgs &a, hipStream_t st, bool set_up)
+{
+    using G = KeysGeom<D, QT, NW>;
+    static std::atomic<uint64_t> done{0};
+    auto *kernel = &paged_keys_kernel<D, QT, NW, SPARSE>;
+    int rc = raise_lds_limit(done, reinterpret_cast<const void *>(kernel), 160 * 1024, "paged attention");
+    if (rc || set_up)
+        return rc;
+    const size_t list = list_bytes<G::THREADS, SPARSE>(a), main = G::bytes(a.words) + list, again = single_bytes<D, G::THREADS>(G::CAP, a.words) + list;
+    return launch_kernel(kernel, a, G::THREADS, main > again ? main : again, "paged_keys_kernel", st);
+}
+template <int D, int QT, int WR, bool SPARSE>
+int launch_rows(PagedAttnArgs &a, hipStream_t st, bool set_up)
+{
+    using G = RowsGeom<D, QT, WR>;
+    static std::atomic<uint64_t> done{0};
+    auto *kernel = &paged_rows_kernel<D, QT, WR, SPARSE>;
+    int rc = raise_lds_limit(done, reinterpret_cast<const void *>(kernel), 160 * 1024, "paged attention");
+    if (rc || set_up)
+        return rc;
+    const size_t list = list_bytes<G::THREADS, SPARSE>(a), main = G::bytes(a.words) + list, again = single_bytes<D, G::THREADS>(G::CAP, a.words) + list;
+    return launch_kernel(kernel, a, G::THREADS, main > again ? main : again, "paged_rows_kernel", st);
 }
 
 template <int D, bool SPARSE>
-int launch_part(PagedAttnArgs &a, const Launch &l, hipStream_t st)
+int launch_shape(PagedAttnArgs &a, const Shape &s, hipStream_t st, bool set_up = false)
 {
-    a.splits = l.splits;
-    a.streams = l.streams;
-    a.row_groups = l.row_groups;
-    const int blocks = ceil_div(l.streams, 8) * 8 * l.row_groups;
-    const Shape s = l.shape;
-    if (s.qt == 0) {
-        using List = PageList<64, 256, SPARSE>;
-        a.list_size = SPARSE ? List::SCAN / a.splits + 2 : DENSE_LIST;
-        const size_t lds = 16 * D + SINGLE_ROWS * a.words * 8 + DREAM_MAX_TREE * 4 + List::bytes(a.list_size, a.words);
-        hipLaunchKernelGGL((paged_f32_kernel<D, SPARSE>), dim3(blocks), dim3(256), lds, st, a);
-        return check_launch("paged_f32_kernel");
+    if (s.form == SINGLY) {
+        const size_t list = list_bytes<256, SPARSE>(a);
+        return launch_kernel(&paged_f32_kernel<D, SPARSE>, a, 256, single_bytes<D, 256>(SINGLE_ROWS, a.words) + list, "paged_f32_kernel", st);
     }
-    constexpr int WK = D == 256 ? 2 : 4;
-    if (s.wr == 1 && s.qt == 1)
-        return launch_bf16<D, 1, 1, WK, SPARSE>(a, blocks, st);
-    if (s.wr == 1 && s.qt == 2)
-        return launch_bf16<D, 2, 1, WK, SPARSE>(a, blocks, st);
-    if constexpr (D == 256) {
-        return launch_bf16<D, 1, 8, 1, SPARSE>(a, blocks, st);
-    } else {
-        if (s.wr == 1)
-            return launch_bf16<D, 4, 1, WK, SPARSE>(a, blocks, st);
-        return s.wr == 4 ? launch_bf16<D, 2, 4, 1, SPARSE>(a, blocks, st) : launch_bf16<D, 2, 8, 1, SPARSE>(a, blocks, st);
-    }
+    if (s.form == ROWS)
+        return launch_rows<D, rows_tiles(D), 8, SPARSE>(a, st, set_up);
+    if (s.qt == 1)
+        return launch_keys<D, 1, keys_waves(D, 1), SPARSE>(a, st, set_up);
+    if constexpr (keys_tiles(D) == 4)
+        if (s.qt == 4)
+            return launch_keys<D, 4, keys_waves(D, 4), SPARSE>(a, st, set_up);
+    if constexpr (keys_tiles(D) >= 2)
+        return launch_keys<D, 2, keys_waves(D, 2), SPARSE>(a, st, set_up);
+    return DREAM_ERR_UNSUPPORTED;      // (no such shape)
 }
 
 template <int D, bool SPARSE>
 int launch_all(PagedAttnArgs &a, const PagedPlan &p, bool f32, hipStream_t st)
 {
     a.n_slots = p.n_slots;
+    a.shared_slots = p.shared_slots;
     a.all_rows = p.all_rows;
-    a.shared_slots = a.n_groups ? p.shared.splits : 0;
-    if (!SPARSE && a.n_groups) {
-        a.shared = 1;
-        a.slot = 0;
-        if (int rc = launch_part<D, false>(a, p.shared, st))
+    a.shared = p.shared.part;
+    a.own = p.own.part;
+    if (!SPARSE && a.n_groups && !(p.shared.shape == p.own.shape)) {      // two kernels
+        a.own.blocks = 0;
+        if (int rc = launch_shape<D, false>(a, p.shared.shape, st))
             return rc;
+        a.shared.blocks = 0;
+        a.own = p.own.part;
     }
-    a.shared = 0;
-    a.slot = a.shared_slots;
-    if (int rc = launch_part<D, SPARSE>(a, p.own, st))
+    if (int rc = launch_shape<D, SPARSE>(a, p.own.shape, st))
         return rc;
     if (p.n_slots == 1)
         return DREAM_OK;
@@ -1046,6 +1341,15 @@ int launch_all(PagedAttnArgs &a, const PagedPlan &p, bool f32, hipStream_t st)
     else
         hipLaunchKernelGGL((paged_join_kernel<uint16_t, D>), dim3(blocks), dim3(256), 0, st, a);
     return check_launch("paged_join_kernel");
+}
+template <int D, bool SPARSE>
+int set_up()
+{
+    PagedAttnArgs a = {};
+    for (int qt = 1; qt <= keys_tiles(D); qt *= 2)
+        if (int rc = launch_shape<D, SPARSE>(a, {KEYS, qt, keys_waves(D, qt)}, nullptr, true))
+            return rc;
+    return launch_shape<D, SPARSE>(a, {ROWS, rows_tiles(D), 8}, nullptr, true);
 }
 
 int check_attn(const char *who, const dream_attn_desc *d, const dream_page_desc *pages, int32_t n_tree, int32_t n_groups)
@@ -1084,13 +1388,21 @@ int run(const char *who, const dream_attn_desc *d, const dream_page_desc *pages,
 
 }  // namespace
 
+int dream::paged_attn_init()
+{
+    for (int rc : {set_up<64, false>(), set_up<64, true>(), set_up<128, false>(), set_up<128, true>(), set_up<256, false>(), set_up<256, true>()})
+        if (rc)
+            return rc;
+    return DREAM_OK;
+}
+
 extern "C" {
 
 size_t dream_paged_verify_attn_workspace(const dream_attn_desc *desc, const dream_page_desc *pages, int32_t n_tree, int64_t max_kv_len, int32_t n_groups, int64_t max_shared_len)
 {
     if (check_attn("dream_paged_verify_attn_workspace", desc, pages, n_tree, n_groups))
         return DREAM_WORKSPACE_MIN_BYTES;
-    const size_t n = plan_for(desc, pages, n_tree, max_kv_len, n_groups, max_shared_len, 0).bytes;
+    const size_t n = plan_for(desc, pages, n_tree, max_kv_len, n_groups, max_shared_len, false, 0).bytes;
     return n < DREAM_WORKSPACE_MIN_BYTES ? DREAM_WORKSPACE_MIN_BYTES : n;
 }
 
@@ -1107,14 +1419,14 @@ int dream_paged_verify_attn(const dream_attn_desc *desc, const dream_page_desc *
     a.q = static_cast<const unsigned char *>(q); a.k = static_cast<const unsigned char *>(k_pages); a.v = static_cast<const unsigned char *>(v_pages);
     a.table = page_table; a.prefix_len = prefix_len; a.n_tree = n_tree; a.parent = parent; a.tree_mask = tree_mask; a.n_groups = n_groups; a.group_start = group_start;
     a.shared_len = shared_len; a.out = out; a.lse = lse;
-    return run(who, desc, pages, a, plan_for(desc, pages, n_tree, max_kv_len, n_groups, max_shared_len, 0), workspace, workspace_bytes, stream);
+    return run(who, desc, pages, a, plan_for(desc, pages, n_tree, max_kv_len, n_groups, max_shared_len, false, 0), workspace, workspace_bytes, stream);
 }
 
 size_t dream_sparse_verify_attn_workspace(const dream_attn_desc *desc, const dream_page_desc *pages, int32_t n_tree, int64_t max_kv_len, int32_t max_pages_seen)
 {
     if (check_attn("dream_sparse_verify_attn_workspace", desc, pages, n_tree, 0))
         return DREAM_WORKSPACE_MIN_BYTES;
-    const size_t n = plan_for(desc, pages, n_tree, max_kv_len, 0, 0, max_pages_seen).bytes;
+    const size_t n = plan_for(desc, pages, n_tree, max_kv_len, 0, 0, true, max_pages_seen).bytes;
     return n < DREAM_WORKSPACE_MIN_BYTES ? DREAM_WORKSPACE_MIN_BYTES : n;
 }
 
@@ -1130,7 +1442,7 @@ int dream_sparse_verify_attn(const dream_attn_desc *desc, const dream_page_desc 
     PagedAttnArgs a = {};
     a.q = static_cast<const unsigned char *>(q); a.k = static_cast<const unsigned char *>(k_pages); a.v = static_cast<const unsigned char *>(v_pages);
     a.table = page_table; a.nodes = page_nodes; a.prefix_len = prefix_len; a.n_tree = n_tree; a.parent = parent; a.tree_mask = tree_mask; a.out = out; a.lse = lse;
-    return run(who, desc, pages, a, plan_for(desc, pages, n_tree, max_kv_len, 0, 0, max_pages_seen), workspace, workspace_bytes, stream);
+    return run(who, desc, pages, a, plan_for(desc, pages, n_tree, max_kv_len, 0, 0, true, max_pages_seen), workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

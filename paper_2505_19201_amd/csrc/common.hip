@@ -1,5 +1,6 @@
 // Error reporting, launch-shape overrides, the read-only measurement kernel and tree validation shared by all entry points.
 #include "common.h"
+#include "paged.h"
 #include "dream_tuning.h"
 #include <string.h>
 
@@ -93,6 +94,8 @@ int dream_init(void)
         rc = compress_init();
     if (!rc)
         rc = project_init();
+    if (!rc)
+        rc = paged_attn_init();
     if (!rc)
         rc = dream_accept_static_init();
     return rc;

@@ -9,6 +9,7 @@ namespace dream {
 
 constexpr int MIN_PAGE = 16, MAX_PAGE = 256;
 
+int paged_attn_init();      // part of dream_init()
 int check_pages(const char *who, const dream_attn_desc *desc, const dream_page_desc *pages);
 
 inline int log2_of(int32_t power) { return __builtin_ctz((unsigned)power); }
