@@ -393,6 +393,7 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
             if (sees) {
                 const T *k = reinterpret_cast<const T *>(a.k) + row;
                 float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
                 for (int i = 0; i < D; i += N) {
                     const u32x4 raw = *reinterpret_cast<const u32x4 *>(k + i);
 #pragma unroll
@@ -596,21 +597,24 @@ struct QueryRows {
     // All rows of the chunk are everyone's (or everyone's whose page it is)
     __device__ __forceinline__ bool plain(const Unit &u, const Chunk &c) const { return c.live && c.prefix && c.pos >= u.lo && c.pos + 16 <= whole; }
 
-    // Online softmax of 32 keys; bit h * QT + qt of `in`: does the row see chunk h's page (selected pages).  WHOLE: all rows of both chunks are everyone's (or everyone's whose page it is).
-    // (Two functions with a raise of the reference each: values that either kind of tile may have written are copied on both.)
-    template <bool WHOLE>
-    __device__ __forceinline__ void softmax(const PagedAttnArgs &a, const Unit &u, const Chunk (&ch)[2], uint32_t in, int g, f32x4 (&s)[2][QT], bf16x8 (&pf)[QT])
+    // Online softmax of 32 keys; bit h * QT + qt of `in`: does the row see chunk h's page (selected pages).  whole: all rows of both chunks are everyone's (or everyone's whose page it is).
+    __device__ __forceinline__ void softmax(const PagedAttnArgs &a, const Unit &u, const Chunk (&ch)[2], bool whole, uint32_t in, int g, f32x4 (&s)[2][QT], bf16x8 (&pf)[QT])
     {
         const float scale_log2 = a.scale_log2;
         float top[QT];
+        if (whole) {
 #pragma unroll
-        for (int qt = 0; qt < QT; qt++) {
-            if constexpr (WHOLE && SPARSE) {
-                const float x = in >> qt & 1u ? largest(s[0][qt]) : -INFINITY, y = in >> (QT + qt) & 1u ? largest(s[1][qt]) : -INFINITY;
-                top[qt] = fmaxf(x, y) * scale_log2;
-            } else if constexpr (WHOLE) {
-                top[qt] = fmaxf(largest(s[0][qt]), largest(s[1][qt])) * scale_log2;
-            } else {
+            for (int qt = 0; qt < QT; qt++) {
+                if constexpr (SPARSE) {
+                    const float x = in >> qt & 1u ? largest(s[0][qt]) : -INFINITY, y = in >> (QT + qt) & 1u ? largest(s[1][qt]) : -INFINITY;
+                    top[qt] = fmaxf(x, y) * scale_log2;
+                } else {
+                    top[qt] = fmaxf(largest(s[0][qt]), largest(s[1][qt])) * scale_log2;
+                }
+            }
+        } else {
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++) {
 #pragma unroll
                 for (int h = 0; h < 2; h++) {
                     const int pos = ch[h].pos + 4 * g;
@@ -633,12 +637,11 @@ struct QueryRows {
 #pragma unroll
         for (int qt = 0; qt < QT; qt++)
             raise = raise || top[qt] > m[qt] + SLACK;
-        if (__any(raise)) {
+        if (__any(raise)) {      // (one place, and no branch of its own for a lane: sums that may have come by two ways would be copied on both)
 #pragma unroll
             for (int qt = 0; qt < QT; qt++) {
                 float x = fmaxf(top[qt], __shfl_xor(top[qt], 16));
                 x = fmaxf(x, __shfl_xor(x, 32));
-                // (no branch of its own: sums that lanes may or may not have changed would be held twice)
                 const bool up = x > m[qt] + SLACK;
                 const float f = up ? __builtin_amdgcn_exp2f(m[qt] - x) : 1.0f;       // 0 where nothing was seen before
                 m[qt] = up ? x : m[qt];
@@ -648,17 +651,18 @@ struct QueryRows {
                     o[qt][dt] *= f;
             }
         }
+        const float scaled = whole ? scale_log2 : 1.0f;
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
             const float ref = fmaxf(m[qt], -FLT_MAX);      // where all scores so far are -inf, their weight is 0 and not exp(-inf + inf)
             float sum = 0.0f;
 #pragma unroll
             for (int h = 0; h < 2; h++) {
-                const bool out = WHOLE && SPARSE && !(in >> (h * QT + qt) & 1u);
-                const float mult = out ? 0.0f : WHOLE ? scale_log2 : 1.0f, less = out ? -INFINITY : -ref;
+                const bool out = SPARSE && whole && !(in >> (h * QT + qt) & 1u);
+                const float mult = out ? 0.0f : scaled, less = out ? -INFINITY : -ref;
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
-                    const float p = __builtin_amdgcn_exp2f(WHOLE ? __builtin_fmaf(s[h][qt][r], mult, less) : s[h][qt][r] + less);
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][qt][r], mult, less));
                     sum += p;
                     pf[qt][h * 4 + r] = (__bf16)p;      // rounded as the matrix instruction takes it, half a step of 2^-8; the sum stays float32
                 }
@@ -723,7 +727,7 @@ __device__ __forceinline__ int page_of_tile(const PagedAttnArgs &a, int b, int r
 
 // Takes a workgroup's rows again, where a sum is not finite.  Not part of the kernels' code: it would have registers of its own beside theirs.
 template <int D, int THREADS, bool SPARSE>
-__device__ __noinline__ void attend_again(const __attribute__((address_space(4))) PagedAttnArgs *kernel_args, int cap, int tile, int run, unsigned char *smem)
+__device__ __forceinline__ void attend_again(const __attribute__((address_space(4))) PagedAttnArgs *kernel_args, int cap, int tile, int run, unsigned char *smem)
 {
     const PagedAttnArgs &a = *(const PagedAttnArgs *)kernel_args;
     Unit u;
@@ -862,10 +866,7 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
             wait_lds();
             if (i + 1 < steps)
                 ask_k(i + 1);
-            if (straight && a.scale_log2 >= 0.0f)
-                rows.template softmax<true>(a, u, ch, in, g, s, pf);
-            else
-                rows.template softmax<false>(a, u, ch, in, g, s, pf);
+            rows.softmax(a, u, ch, straight && a.scale_log2 >= 0.0f, in, g, s, pf);
             if (i + 1 < steps)
                 wait_loads<G::LOADS>();
             else
@@ -1055,10 +1056,7 @@ __global__ __launch_bounds__(64 * WR) void paged_rows_kernel(PagedAttnArgs a)
                 f32x4 s[2][QT];
                 bf16x8 pf[QT];
                 rows.scores(kt + sub * 32 * ROW, here(foff), s);
-                if (straight && a.scale_log2 >= 0.0f)
-                    rows.template softmax<true>(a, u, ch, in, g, s, pf);
-                else
-                    rows.template softmax<false>(a, u, ch, in, g, s, pf);
+                rows.softmax(a, u, ch, straight && a.scale_log2 >= 0.0f, in, g, s, pf);
                 rows.add_values(vt + sub * 32 * ROW, here(voff), pf);
             }
             stage = stage == NS - 1 ? 0 : stage + 1;
@@ -1185,7 +1183,7 @@ struct PagedPlan {
 
 // The shapes there are
 constexpr int keys_waves(int D, int qt) { return D == 256 || qt == 4 ? 4 : 8; }
-constexpr int keys_tiles(int D) { return D == 256 ? 1 : D == 128 ? 2 : 4; }      // at most
+constexpr int keys_tiles(int D) { return D == 256 ? 2 : 4; }      // at most
 constexpr int rows_tiles(int D) { return D == 256 ? 1 : 2; }
 
 Shape shape_for(int D, bool f32, int64_t rows)
