@@ -505,8 +505,8 @@ __device__ __forceinline__ int here_scalar(int x)
 __device__ __forceinline__ float largest(f32x4 a) { return fmaxf(fmaxf(fmaxf(a[0], a[1]), a[2]), a[3]); }
 
 // The query rows of a wave, QT tiles of 16, and their sums.  Lane (c, g) = (lane % 16, lane / 16) has of row c: of the queries the channels 8 g .. of every 32; of O^T the channels
-// 16 dt + 4 g + r; and scores of the keys 4 g + r of every 16.
-template <int D, int QT, bool SPARSE>
+// 16 dt + 4 g + r; and scores of the keys 4 g + r of every 16.  A step takes NC chunks of 16 keys.
+template <int D, int QT, int NC, bool SPARSE>
 struct QueryRows {
     static constexpr int ROW = 2 * D, NKS = D / 32, NDT = D / 16;
     bf16x8 qf[QT][NKS];
@@ -572,51 +572,43 @@ struct QueryRows {
         }
     }
 
-    // S^T = K Q^T of 32 keys
-    __device__ __forceinline__ void scores(const unsigned char *kt, int foff, f32x4 (&s)[2][QT]) const
+    // S^T = K Q^T of a step's keys
+    __device__ __forceinline__ void scores(const unsigned char *kt, int foff, f32x4 (&s)[NC][QT]) const
     {
-        bf16x8 kf[NKS][2];
 #pragma unroll
-        for (int ks = 0; ks < NKS; ks++)
+        for (int h0 = 0; h0 < NC; h0 += 2) {
+            bf16x8 kf[NKS][2];
 #pragma unroll
-            for (int h = 0; h < 2; h++)
-                kf[ks][h] = *reinterpret_cast<const bf16x8 *>(kt + h * 16 * ROW + at_key_step(foff, ks));
+            for (int ks = 0; ks < NKS; ks++)
 #pragma unroll
-        for (int h = 0; h < 2; h++)
-#pragma unroll
-            for (int qt = 0; qt < QT; qt++)
-                s[h][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int ks = 0; ks < NKS; ks++)
+                for (int h = 0; h < 2; h++)
+                    kf[ks][h] = *reinterpret_cast<const bf16x8 *>(kt + (h0 + h) * 16 * ROW + at_key_step(foff, ks));
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
                 for (int qt = 0; qt < QT; qt++)
-                    s[h][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks][h], qf[qt][ks], s[h][qt], 0, 0, 0);
+                    s[h0 + h][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < NKS; ks++)
+#pragma unroll
+                for (int h = 0; h < 2; h++)
+#pragma unroll
+                    for (int qt = 0; qt < QT; qt++)
+                        s[h0 + h][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks][h], qf[qt][ks], s[h0 + h][qt], 0, 0, 0);
+        }
     }
     // All rows of the chunk are everyone's (or everyone's whose page it is)
     __device__ __forceinline__ bool plain(const Unit &u, const Chunk &c) const { return c.live && c.prefix && c.pos >= u.lo && c.pos + 16 <= whole; }
 
-    // Online softmax of 32 keys; bit h * QT + qt of `in`: does the row see chunk h's page (selected pages).  whole: all rows of both chunks are everyone's (or everyone's whose page it is).
-    __device__ __forceinline__ void softmax(const PagedAttnArgs &a, const Unit &u, const Chunk (&ch)[2], bool whole, uint32_t in, int g, f32x4 (&s)[2][QT], bf16x8 (&pf)[QT])
+    // Online softmax of a step; bit h * QT + qt of `in`: does the row see chunk h's page (selected pages).  whole: all rows of the chunks are everyone's (or everyone's whose page it is).
+    __device__ __forceinline__ void softmax(const PagedAttnArgs &a, const Unit &u, const Chunk (&ch)[NC], bool whole, uint32_t in, int g, f32x4 (&s)[NC][QT], bf16x8 (&pf)[NC / 2][QT])
     {
         const float scale_log2 = a.scale_log2;
-        float top[QT];
-        if (whole) {
+        if (!whole) {
 #pragma unroll
-            for (int qt = 0; qt < QT; qt++) {
-                if constexpr (SPARSE) {
-                    const float x = in >> qt & 1u ? largest(s[0][qt]) : -INFINITY, y = in >> (QT + qt) & 1u ? largest(s[1][qt]) : -INFINITY;
-                    top[qt] = fmaxf(x, y) * scale_log2;
-                } else {
-                    top[qt] = fmaxf(largest(s[0][qt]), largest(s[1][qt])) * scale_log2;
-                }
-            }
-        } else {
+            for (int qt = 0; qt < QT; qt++)
 #pragma unroll
-            for (int qt = 0; qt < QT; qt++) {
-#pragma unroll
-                for (int h = 0; h < 2; h++) {
+                for (int h = 0; h < NC; h++) {
                     const int pos = ch[h].pos + 4 * g;
                     uint32_t vis = 0u;
                     if (ch[h].live && ch[h].prefix && (!SPARSE || (in >> (h * QT + qt) & 1u))) {
@@ -630,8 +622,19 @@ struct QueryRows {
                     for (int r = 0; r < 4; r++)
                         s[h][qt][r] = vis >> r & 1u ? s[h][qt][r] * scale_log2 : -INFINITY;
                 }
-                top[qt] = fmaxf(largest(s[0][qt]), largest(s[1][qt]));
+            in = ~0u;                             // (done)
+        }
+        const float scaled = whole ? scale_log2 : 1.0f;
+        float top[QT];
+#pragma unroll
+        for (int qt = 0; qt < QT; qt++) {
+            top[qt] = -INFINITY;
+#pragma unroll
+            for (int h = 0; h < NC; h++) {
+                const float x = largest(s[h][qt]);
+                top[qt] = fmaxf(top[qt], SPARSE && !(in >> (h * QT + qt) & 1u) ? -INFINITY : x);
             }
+            top[qt] *= scaled;
         }
         bool raise = false;
 #pragma unroll
@@ -651,38 +654,39 @@ struct QueryRows {
                     o[qt][dt] *= f;
             }
         }
-        const float scaled = whole ? scale_log2 : 1.0f;
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
             const float ref = fmaxf(m[qt], -FLT_MAX);      // where all scores so far are -inf, their weight is 0 and not exp(-inf + inf)
             float sum = 0.0f;
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                const bool out = SPARSE && whole && !(in >> (h * QT + qt) & 1u);
+            for (int h = 0; h < NC; h++) {
+                const bool out = SPARSE && !(in >> (h * QT + qt) & 1u);
                 const float mult = out ? 0.0f : scaled, less = out ? -INFINITY : -ref;
 #pragma unroll
                 for (int r = 0; r < 4; r++) {
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][qt][r], mult, less));
                     sum += p;
-                    pf[qt][h * 4 + r] = (__bf16)p;      // rounded as the matrix instruction takes it, half a step of 2^-8; the sum stays float32
+                    pf[h / 2][qt][h % 2 * 4 + r] = (__bf16)p;      // rounded as the matrix instruction takes it, half a step of 2^-8; the sum stays float32
                 }
             }
             l[qt] += sum;
         }
     }
     // O^T += V^T P^T
-    __device__ __forceinline__ void add_values(const unsigned char *vt, int voff, const bf16x8 (&pf)[QT])
+    __device__ __forceinline__ void add_values(const unsigned char *vt, int voff, const bf16x8 (&pf)[NC / 2][QT])
     {
 #pragma unroll
-        for (int dt = 0; dt < NDT; dt++) {
-            const unsigned char *vp = vt + at_column_tile(voff, dt);
-            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)vp);
-            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(vp + 16 * ROW));
-            const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        for (int sub = 0; sub < NC / 2; sub++)
 #pragma unroll
-            for (int qt = 0; qt < QT; qt++)
-                o[qt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[qt], o[qt][dt], 0, 0, 0);
-        }
+            for (int dt = 0; dt < NDT; dt++) {
+                const unsigned char *vp = vt + sub * 32 * ROW + at_column_tile(voff, dt);
+                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)vp);
+                const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(vp + 16 * ROW));
+                const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int qt = 0; qt < QT; qt++)
+                    o[qt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[sub][qt], o[qt][dt], 0, 0, 0);
+            }
     }
     // The rows' sums over all four g; true where one is not finite
     __device__ __forceinline__ bool finish()
@@ -701,14 +705,14 @@ struct QueryRows {
         }
         return __any(strange != 0.0f);      // (0 * inf and 0 * NaN are NaN)
     }
-    // Of the pages of two chunks, which the rows see; false where none does
+    // Of the pages of a step's chunks, which the rows see; false where none does
     template <class List>
-    __device__ __forceinline__ bool seen_by(const PagedAttnArgs &a, const List &list, const Chunk (&ch)[2], bool straight, uint32_t &in) const
+    __device__ __forceinline__ bool seen_by(const PagedAttnArgs &a, const List &list, const Chunk (&ch)[NC], bool straight, uint32_t &in) const
     {
         in = 0u;
         if constexpr (SPARSE) {
 #pragma unroll
-            for (int h = 0; h < 2; h++)
+            for (int h = 0; h < NC; h++)
 #pragma unroll
                 for (int qt = 0; qt < QT; qt++)
                     in |= (uint32_t)(list.word[ch[h].entry * a.words + (node[qt] >> 6)] >> (node[qt] & 63) & 1) << (h * QT + qt);
@@ -784,7 +788,7 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
     PageList<G::THREADS> list;
     if constexpr (SPARSE)
         list.build(a, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (a.words > 1 ? G::CAP * a.words + DREAM_MAX_TREE / 2 : 0)), 0);
-    QueryRows<D, QT, SPARSE> rows;
+    QueryRows<D, QT, 2, SPARSE> rows;
     rows.load(a, u, u.row0, c, g);
     const int tile0 = u.lo / 32;
     if (!SPARSE && a.n_groups)
@@ -860,7 +864,7 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
             uint32_t in;
             rows.seen_by(a, list, ch, straight, in);
             f32x4 s[2][QT];
-            bf16x8 pf[QT];
+            bf16x8 pf[1][QT];
             wait_loads<G::LOADS>();
             rows.scores(smem + stage, here(foff), s);
             wait_lds();
@@ -945,21 +949,21 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
     }
 }
 
-template <int D, int QT, int WR>
+template <int D, int QT, int WR, int NS>
 struct RowsGeom {
-    static constexpr int THREADS = 64 * WR, CAP = 16 * QT * WR, ROW = 2 * D, KEYS = D == 256 ? 32 : 64, TILE = KEYS * ROW, STAGE = 2 * TILE, NS = 3;
+    static constexpr int THREADS = 64 * WR, CAP = 16 * QT * WR, ROW = 2 * D, KEYS = D == 256 ? 32 : 64, TILE = KEYS * ROW, STAGE = 2 * TILE;
     static constexpr int LOADS = TILE / 1024 / WR;                          // of a wave, a tile and K or V: rows of one chunk
     static constexpr int MAIN = NS * STAGE;
     static_assert(LOADS * 1024 * WR == TILE && KEYS / WR <= 16, "loads");
     static int bytes(int words) { return MAIN + WR * 8 + (words > 1 ? CAP * words * 8 + DREAM_MAX_TREE * 4 : 0); }
 };
 
-// Many rows: the waves share the tiles and have rows of their own; one barrier a tile, two tiles on their way.
-template <int D, int QT, int WR, bool SPARSE>
-__global__ __launch_bounds__(64 * WR) void paged_rows_kernel(PagedAttnArgs a)
+// Many rows: the waves share the tiles and have rows of their own; one barrier a tile, NS - 1 tiles on their way.
+template <int D, int QT, int WR, int NS, bool SPARSE>
+__global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PagedAttnArgs a)
 {
-    using G = RowsGeom<D, QT, WR>;
-    constexpr int ROW = G::ROW, KEYS = G::KEYS, LPR = ROW / 16, RPI = 1024 / ROW, NS = G::NS;
+    using G = RowsGeom<D, QT, WR, NS>;
+    constexpr int ROW = G::ROW, KEYS = G::KEYS, NC = KEYS / 16, LPR = ROW / 16, RPI = 1024 / ROW;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
@@ -985,7 +989,7 @@ __global__ __launch_bounds__(64 * WR) void paged_rows_kernel(PagedAttnArgs a)
     PageList<G::THREADS> list;
     if constexpr (SPARSE)
         list.build(a, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (a.words > 1 ? G::CAP * a.words + DREAM_MAX_TREE / 2 : 0)), 0);
-    QueryRows<D, QT, SPARSE> rows;
+    QueryRows<D, QT, NC, SPARSE> rows;
     const int first_row = u.row0 + wave * QT * 16;
     rows.load(a, u, first_row, c, g);
     const int tile0 = u.lo / KEYS + u.split;
@@ -1046,18 +1050,20 @@ __global__ __launch_bounds__(64 * WR) void paged_rows_kernel(PagedAttnArgs a)
             if (i + NS - 1 < steps)
                 ask(i + NS - 1, next);
             const unsigned char *kt = smem + stage * G::STAGE, *vt = kt + G::TILE;
+            Chunk ch[NC];
+            bool straight = true;
 #pragma unroll
-            for (int sub = 0; sub < KEYS / 32; sub++) {
-                Chunk ch[2] = {chunk(i, sub * 32), chunk(i, sub * 32 + 16)};
-                const bool straight = rows.plain(u, ch[0]) && rows.plain(u, ch[1]);
-                uint32_t in;
-                if (!rows.seen_by(a, list, ch, straight, in))
-                    continue;
-                f32x4 s[2][QT];
-                bf16x8 pf[QT];
-                rows.scores(kt + sub * 32 * ROW, here(foff), s);
+            for (int h = 0; h < NC; h++) {
+                ch[h] = chunk(i, h * 16);
+                straight = straight && rows.plain(u, ch[h]);
+            }
+            uint32_t in;
+            if (rows.seen_by(a, list, ch, straight, in)) {
+                f32x4 s[NC][QT];
+                bf16x8 pf[NC / 2][QT];
+                rows.scores(kt, here(foff), s);
                 rows.softmax(a, u, ch, straight && a.scale_log2 >= 0.0f, in, g, s, pf);
-                rows.add_values(vt + sub * 32 * ROW, here(voff), pf);
+                rows.add_values(vt, here(voff), pf);
             }
             stage = stage == NS - 1 ? 0 : stage + 1;
             next = next == NS - 1 ? 0 : next + 1;
@@ -1192,7 +1198,7 @@ Shape shape_for(int D, bool f32, int64_t rows)
         return {SINGLY, 0, 4};
     const int tiles = q_tiles_override(), waves = tile_waves_override();
     if (waves == 8 || (!waves && !tiles && rows > 16 * keys_tiles(D)))
-        return {ROWS, rows_tiles(D), 8};
+        return tiles == 1 ? Shape{ROWS, 1, 4} : tiles == 2 ? Shape{ROWS, rows_tiles(D), 4} : Shape{ROWS, rows_tiles(D), 8};
     const int qt = tiles ? tiles : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
     const int most = keys_tiles(D), taken = qt >= most ? most : qt >= 2 ? 2 : 1;
     return {KEYS, taken, keys_waves(D, taken)};
@@ -1282,12 +1288,12 @@ int launch_keys(PagedAttnArgs &a, hipStream_t st, bool set_up)
     const size_t list = list_bytes<G::THREADS, SPARSE>(a), main = G::bytes(a.words) + list, again = single_bytes<D, G::THREADS>(G::CAP, a.words) + list;
     return launch_kernel(kernel, a, G::THREADS, main > again ? main : again, "paged_keys_kernel", st);
 }
-template <int D, int QT, int WR, bool SPARSE>
+template <int D, int QT, int WR, int NS, bool SPARSE>
 int launch_rows(PagedAttnArgs &a, hipStream_t st, bool set_up)
 {
-    using G = RowsGeom<D, QT, WR>;
+    using G = RowsGeom<D, QT, WR, NS>;
     static std::atomic<uint64_t> done{0};
-    auto *kernel = &paged_rows_kernel<D, QT, WR, SPARSE>;
+    auto *kernel = &paged_rows_kernel<D, QT, WR, NS, SPARSE>;
     int rc = raise_lds_limit(done, reinterpret_cast<const void *>(kernel), 160 * 1024, "paged attention");
     if (rc || set_up)
         return rc;
@@ -1303,7 +1309,7 @@ int launch_shape(PagedAttnArgs &a, const Shape &s, hipStream_t st, bool set_up =
         return launch_kernel(&paged_f32_kernel<D, SPARSE>, a, 256, single_bytes<D, 256>(SINGLE_ROWS, a.words) + list, "paged_f32_kernel", st);
     }
     if (s.form == ROWS)
-        return launch_rows<D, rows_tiles(D), 8, SPARSE>(a, st, set_up);
+        return s.waves == 8 ? launch_rows<D, rows_tiles(D), 8, 3, SPARSE>(a, st, set_up) : s.qt == rows_tiles(D) ? launch_rows<D, rows_tiles(D), 4, 2, SPARSE>(a, st, set_up) : launch_rows<D, 1, 4, 2, SPARSE>(a, st, set_up);
     if (s.qt == 1)
         return launch_keys<D, 1, keys_waves(D, 1), SPARSE>(a, st, set_up);
     if constexpr (keys_tiles(D) == 4)
