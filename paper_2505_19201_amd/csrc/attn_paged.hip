@@ -572,59 +572,56 @@ struct QueryRows {
         }
     }
 
-    // S^T = K Q^T of a step's keys
-    __device__ __forceinline__ void scores(const unsigned char *kt, int foff, f32x4 (&s)[NC][QT]) const
+    // S^T = K Q^T of chunks h0 and h0 + 1
+    __device__ __forceinline__ void scores(const unsigned char *kt, int foff, int h0, f32x4 (&s)[NC][QT]) const
     {
+        bf16x8 kf[NKS][2];
 #pragma unroll
-        for (int h0 = 0; h0 < NC; h0 += 2) {
-            bf16x8 kf[NKS][2];
+        for (int ks = 0; ks < NKS; ks++)
 #pragma unroll
-            for (int ks = 0; ks < NKS; ks++)
+            for (int h = 0; h < 2; h++)
+                kf[ks][h] = *reinterpret_cast<const bf16x8 *>(kt + (h0 + h) * 16 * ROW + at_key_step(foff, ks));
 #pragma unroll
-                for (int h = 0; h < 2; h++)
-                    kf[ks][h] = *reinterpret_cast<const bf16x8 *>(kt + (h0 + h) * 16 * ROW + at_key_step(foff, ks));
+        for (int h = 0; h < 2; h++)
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++)
+                s[h0 + h][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < NKS; ks++)
 #pragma unroll
             for (int h = 0; h < 2; h++)
 #pragma unroll
                 for (int qt = 0; qt < QT; qt++)
-                    s[h0 + h][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < NKS; ks++)
-#pragma unroll
-                for (int h = 0; h < 2; h++)
-#pragma unroll
-                    for (int qt = 0; qt < QT; qt++)
-                        s[h0 + h][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks][h], qf[qt][ks], s[h0 + h][qt], 0, 0, 0);
-        }
+                    s[h0 + h][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[ks][h], qf[qt][ks], s[h0 + h][qt], 0, 0, 0);
     }
     // All rows of the chunk are everyone's (or everyone's whose page it is)
     __device__ __forceinline__ bool plain(const Unit &u, const Chunk &c) const { return c.live && c.prefix && c.pos >= u.lo && c.pos + 16 <= whole; }
 
-    // Online softmax of a step; bit h * QT + qt of `in`: does the row see chunk h's page (selected pages).  whole: all rows of the chunks are everyone's (or everyone's whose page it is).
-    __device__ __forceinline__ void softmax(const PagedAttnArgs &a, const Unit &u, const Chunk (&ch)[NC], bool whole, uint32_t in, int g, f32x4 (&s)[NC][QT], bf16x8 (&pf)[NC / 2][QT])
+    // Of a step that is not everyone's: scores as multiples of an octave, -inf for what a row does not see.  Bit h * QT + qt of `in`: does the row see chunk h's page (selected pages).
+    __device__ __forceinline__ void mask(const PagedAttnArgs &a, const Unit &u, const Chunk (&ch)[NC], uint32_t in, int g, f32x4 (&s)[NC][QT]) const
     {
-        const float scale_log2 = a.scale_log2;
-        if (!whole) {
 #pragma unroll
-            for (int qt = 0; qt < QT; qt++)
+        for (int qt = 0; qt < QT; qt++)
 #pragma unroll
-                for (int h = 0; h < NC; h++) {
-                    const int pos = ch[h].pos + 4 * g;
-                    uint32_t vis = 0u;
-                    if (ch[h].live && ch[h].prefix && (!SPARSE || (in >> (h * QT + qt) & 1u))) {
-#pragma unroll
-                        for (int r = 0; r < 4; r++)
-                            vis |= (uint32_t)(pos + r >= u.lo && pos + r < limit[qt]) << r;
-                    }
-                    if (ch[h].live && ch[h].tree && !u.shared)
-                        vis |= four_nodes(a, small[qt], large + qt * 16 * a.words, pos - u.P);
+            for (int h = 0; h < NC; h++) {
+                const int pos = ch[h].pos + 4 * g;
+                uint32_t vis = 0u;
+                if (ch[h].live && ch[h].prefix && (!SPARSE || (in >> (h * QT + qt) & 1u))) {
 #pragma unroll
                     for (int r = 0; r < 4; r++)
-                        s[h][qt][r] = vis >> r & 1u ? s[h][qt][r] * scale_log2 : -INFINITY;
+                        vis |= (uint32_t)(pos + r >= u.lo && pos + r < limit[qt]) << r;
                 }
-            in = ~0u;                             // (done)
-        }
-        const float scaled = whole ? scale_log2 : 1.0f;
+                if (ch[h].live && ch[h].tree && !u.shared)
+                    vis |= four_nodes(a, small[qt], large + qt * 16 * a.words, pos - u.P);
+#pragma unroll
+                for (int r = 0; r < 4; r++)
+                    s[h][qt][r] = vis >> r & 1u ? s[h][qt][r] * a.scale_log2 : -INFINITY;
+            }
+    }
+    // Online softmax of a step, first half: the references where its scores (times `scaled` octaves) exceed them.  (What masked steps and others do apart is mask() alone: values that may have come
+    // by two ways would be held twice.)
+    __device__ __forceinline__ void raise(float scaled, uint32_t in, const f32x4 (&s)[NC][QT])
+    {
         float top[QT];
 #pragma unroll
         for (int qt = 0; qt < QT; qt++) {
@@ -636,11 +633,11 @@ struct QueryRows {
             }
             top[qt] *= scaled;
         }
-        bool raise = false;
+        bool above = false;
 #pragma unroll
         for (int qt = 0; qt < QT; qt++)
-            raise = raise || top[qt] > m[qt] + SLACK;
-        if (__any(raise)) {      // (one place, and no branch of its own for a lane: sums that may have come by two ways would be copied on both)
+            above = above || top[qt] > m[qt] + SLACK;
+        if (__any(above)) {      // (no branch of its own for a lane, for the same reason)
 #pragma unroll
             for (int qt = 0; qt < QT; qt++) {
                 float x = fmaxf(top[qt], __shfl_xor(top[qt], 16));
@@ -654,39 +651,80 @@ struct QueryRows {
                     o[qt][dt] *= f;
             }
         }
-#pragma unroll
-        for (int qt = 0; qt < QT; qt++) {
-            const float ref = fmaxf(m[qt], -FLT_MAX);      // where all scores so far are -inf, their weight is 0 and not exp(-inf + inf)
-            float sum = 0.0f;
-#pragma unroll
-            for (int h = 0; h < NC; h++) {
-                const bool out = SPARSE && !(in >> (h * QT + qt) & 1u);
-                const float mult = out ? 0.0f : scaled, less = out ? -INFINITY : -ref;
-#pragma unroll
-                for (int r = 0; r < 4; r++) {
-                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][qt][r], mult, less));
-                    sum += p;
-                    pf[h / 2][qt][h % 2 * 4 + r] = (__bf16)p;      // rounded as the matrix instruction takes it, half a step of 2^-8; the sum stays float32
-                }
-            }
-            l[qt] += sum;
-        }
     }
-    // O^T += V^T P^T
-    __device__ __forceinline__ void add_values(const unsigned char *vt, int voff, const bf16x8 (&pf)[NC / 2][QT])
+    // Second half: the weights of slice i (query tile i % QT, chunk i / QT), and their sum
+    __device__ __forceinline__ void weigh(float scaled, uint32_t in, int i, const f32x4 (&s)[NC][QT], bf16x8 (&pf)[NC / 2][QT])
     {
+        const int qt = i % QT, h = i / QT;
+        const float ref = fmaxf(m[qt], -FLT_MAX);      // where all scores so far are -inf, their weight is 0 and not exp(-inf + inf)
+        const bool out = SPARSE && !(in >> (h * QT + qt) & 1u);
+        const float mult = out ? 0.0f : scaled, less = out ? -INFINITY : -ref;
+        float p[4];
 #pragma unroll
-        for (int sub = 0; sub < NC / 2; sub++)
+        for (int r = 0; r < 4; r++) {
+            p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][qt][r], mult, less));
+            pf[h / 2][qt][h % 2 * 4 + r] = (__bf16)p[r];      // rounded as the matrix instruction takes it, half a step of 2^-8; the sum stays float32
+        }
+        l[qt] += (p[0] + p[1]) + (p[2] + p[3]);
+    }
+    static constexpr int SLICES = NC * QT, STEPS = NC / 2 * NKS;
+    // The scores of the next step, and meanwhile this one's weights: every STEPS-th part of the products (two chunks, 32 channels) is followed by its part of the weights, and its keys are asked
+    // for two parts ahead.  (Left to itself the compiler asks for them when it needs them: 1621 clocks for a tile of 64 keys and 32 rows of 128; 512 of matrix products.)
+    __device__ __forceinline__ void scores_and_weights(const unsigned char *kt, int foff, f32x4 (&next)[NC][QT], float scaled, uint32_t in, const f32x4 (&s)[NC][QT], bf16x8 (&pf)[NC / 2][QT])
+    {
+        constexpr int AHEAD = STEPS < 2 ? STEPS : 2;
+        bf16x8 kf[AHEAD + 1][2];
+        auto ask = [&](int i) {
 #pragma unroll
-            for (int dt = 0; dt < NDT; dt++) {
-                const unsigned char *vp = vt + sub * 32 * ROW + at_column_tile(voff, dt);
-                const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)vp);
-                const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(vp + 16 * ROW));
-                const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+            for (int h = 0; h < 2; h++)
+                kf[i % (AHEAD + 1)][h] = *reinterpret_cast<const bf16x8 *>(kt + (i / NKS * 2 + h) * 16 * ROW + at_key_step(foff, i % NKS));
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; i++)
+            ask(i);
+#pragma unroll
+        for (int h = 0; h < NC; h++)
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++)
+                next[h][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < STEPS; i++) {
+            if (i + AHEAD < STEPS)
+                ask(i + AHEAD);
+#pragma unroll
+            for (int j = i * SLICES / STEPS; j < (i + 1) * SLICES / STEPS; j++)
+                weigh(scaled, in, j, s, pf);
+#pragma unroll
+            for (int h = 0; h < 2; h++)
 #pragma unroll
                 for (int qt = 0; qt < QT; qt++)
-                    o[qt][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[sub][qt], o[qt][dt], 0, 0, 0);
-            }
+                    next[i / NKS * 2 + h][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i % (AHEAD + 1)][h], qf[qt][i % NKS], next[i / NKS * 2 + h][qt], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    // O^T += V^T P^T; values are asked for two parts (16 channels of 32 keys) ahead of their products
+    __device__ __forceinline__ void add_values(const unsigned char *vt, int voff, const bf16x8 (&pf)[NC / 2][QT])
+    {
+        constexpr int PARTS = NC / 2 * NDT, AHEAD = 4;
+        bf16x8 vf[AHEAD + 1];
+        auto ask = [&](int i) {
+            const unsigned char *vp = vt + i / NDT * 32 * ROW + at_column_tile(voff, i % NDT);
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)vp);
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(vp + 16 * ROW));
+            vf[i % (AHEAD + 1)] = __builtin_bit_cast(bf16x8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+#pragma unroll
+        for (int i = 0; i < AHEAD; i++)
+            ask(i);
+#pragma unroll
+        for (int i = 0; i < PARTS; i++) {
+            if (i + AHEAD < PARTS)
+                ask(i + AHEAD);
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++)
+                o[qt][i % NDT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i % (AHEAD + 1)], pf[i / NDT][qt], o[qt][i % NDT], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
     // The rows' sums over all four g; true where one is not finite
     __device__ __forceinline__ bool finish()
@@ -866,11 +904,19 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
             f32x4 s[2][QT];
             bf16x8 pf[1][QT];
             wait_loads<G::LOADS>();
-            rows.scores(smem + stage, here(foff), s);
+            rows.scores(smem + stage, here(foff), 0, s);
             wait_lds();
             if (i + 1 < steps)
                 ask_k(i + 1);
-            rows.softmax(a, u, ch, straight && a.scale_log2 >= 0.0f, in, g, s, pf);
+            const bool masked = !straight || a.scale_log2 < 0.0f;      // (the largest score of a negative scale is the smallest product)
+            if (masked)
+                rows.mask(a, u, ch, in, g, s);
+            const float scaled = masked ? 1.0f : a.scale_log2;
+            in = masked ? ~0u : in;
+            rows.raise(scaled, in, s);
+#pragma unroll
+            for (int j = 0; j < rows.SLICES; j++)
+                rows.weigh(scaled, in, j, s, pf);
             if (i + 1 < steps)
                 wait_loads<G::LOADS>();
             else
@@ -1006,26 +1052,25 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PagedAttnArgs a)
             return Chunk{0, pos, pos < u.hi, true, true};
         }
     };
-    auto ask = [&](int i, int stage) {
+    // Keys of tile i to their stage, values to theirs (behind the last tile the last page again: such keys are never used)
+    auto place = [&](int i) {
         int page, x;
         if constexpr (SPARSE) {
             x = i * KEYS + own_rows;
             page = __builtin_amdgcn_readfirstlane(list.phys[min(x >> a.lg_page, list.n - 1)]);
         } else {
-            if ((i & 63) == 0 && i)
-                ask_pages(tile0 + i * u.splits);
             x = (tile0 + i * u.splits) * KEYS + own_rows;
             page = __builtin_amdgcn_readlane(pages, i & 63);
         }
-        const int64_t from = ((((int64_t)page * a.hkv + u.kvh) << a.lg_page) + (x & ((1 << a.lg_page) - 1))) * ROW;
-        const uint32_t to = lds0 + stage * G::STAGE + wave * G::LOADS * 1024;
-#pragma unroll
-        for (int j = 0; j < G::LOADS; j++)
-            lds_load16(a.k + from + j * 1024, (uint32_t)(k_lane ^ swizzle_k<ROW>(wave * G::LOADS + j)), to + j * 1024);
-#pragma unroll
-        for (int j = 0; j < G::LOADS; j++)
-            lds_load16(a.v + from + j * 1024, (uint32_t)(v_lane ^ swizzle_v<ROW>(wave * G::LOADS + j)), to + G::TILE + j * 1024);
+        return ((((int64_t)page * a.hkv + u.kvh) << a.lg_page) + (x & ((1 << a.lg_page) - 1))) * ROW;
     };
+    auto ask_tile = [&](const unsigned char *from, int lane_at, bool values, int stage) {
+        const uint32_t to = lds0 + (values ? NS + stage : stage) * G::TILE + wave * G::LOADS * 1024;
+#pragma unroll
+        for (int j = 0; j < G::LOADS; j++)
+            lds_load16(from + j * 1024, (uint32_t)(lane_at ^ (values ? swizzle_v<ROW>(wave * G::LOADS + j) : swizzle_k<ROW>(wave * G::LOADS + j))), to + j * 1024);
+    };
+    auto after = [](int stage) { return stage == NS - 1 ? 0 : stage + 1; };
     // Zeros over the values of rows that are nobody's, by the wave that loaded them
     auto clear_dead = [&](int i, int stage) {
         const Chunk ch = chunk(i, own_chunk);
@@ -1035,47 +1080,121 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PagedAttnArgs a)
         for (int j = 0; j < G::LOADS; j++) {
             const int pos = ch.pos + (own_rows & 15) + j * RPI + krow;
             if (!(ch.live && ((ch.prefix && pos >= u.lo && pos < u.P) || (ch.tree && pos >= u.P && pos < u.hi))))
-                *reinterpret_cast<u32x4 *>(smem + stage * G::STAGE + G::TILE + (wave * G::LOADS + j) * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
-        }
-    };
-    auto take = [&](int steps) {
-        int stage = 0, next = NS - 1;
-        for (int i = 0; i < steps; i++) {
-            if (i + NS - 1 <= steps)
-                wait_loads<(NS - 2) * 2 * G::LOADS>();
-            else
-                wait_loads<0>();
-            clear_dead(i, stage);
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the tile is there, and all have done with the stage that is loaded next
-            if (i + NS - 1 < steps)
-                ask(i + NS - 1, next);
-            const unsigned char *kt = smem + stage * G::STAGE, *vt = kt + G::TILE;
-            Chunk ch[NC];
-            bool straight = true;
-#pragma unroll
-            for (int h = 0; h < NC; h++) {
-                ch[h] = chunk(i, h * 16);
-                straight = straight && rows.plain(u, ch[h]);
-            }
-            uint32_t in;
-            if (rows.seen_by(a, list, ch, straight, in)) {
-                f32x4 s[NC][QT];
-                bf16x8 pf[NC / 2][QT];
-                rows.scores(kt, here(foff), s);
-                rows.softmax(a, u, ch, straight && a.scale_log2 >= 0.0f, in, g, s, pf);
-                rows.add_values(vt, here(voff), pf);
-            }
-            stage = stage == NS - 1 ? 0 : stage + 1;
-            next = next == NS - 1 ? 0 : next + 1;
+                *reinterpret_cast<u32x4 *>(smem + (NS + stage) * G::TILE + (wave * G::LOADS + j) * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
         }
     };
     const int steps = SPARSE ? ((list.n << a.lg_page) + KEYS - 1) / KEYS : u.hi > u.lo ? max(0, ((u.hi + KEYS - 1) / KEYS - tile0 + u.splits - 1) / u.splits) : 0;
+
+    // What is known of a tile: scores and how they are to be read; have: some of the wave's rows see it
+    struct Tile {
+        f32x4 s[NC][QT];
+        float scaled;
+        uint32_t in;
+        bool have;
+    };
+    auto look = [&](int i, Tile &t) {
+        Chunk ch[NC];
+        bool straight = true;
 #pragma unroll
-    for (int i = 0; i < NS - 1; i++)
-        if (i < steps)
-            ask(i, i);
+        for (int h = 0; h < NC; h++) {
+            ch[h] = chunk(i, h * 16);
+            straight = straight && rows.plain(u, ch[h]);
+        }
+        t.scaled = straight && a.scale_log2 >= 0.0f ? a.scale_log2 : 1.0f;      // (the largest score of a negative scale is the smallest product)
+        t.have = rows.seen_by(a, list, ch, straight, t.in);
+        return !straight || a.scale_log2 < 0.0f;
+    };
+    bf16x8 pf[NC / 2][QT];
+    // Scores that have come: what nobody sees is left out, the references are raised
+    auto settle = [&](int i, Tile &t, bool masked) {
+        if (masked) {
+            Chunk ch[NC];
+#pragma unroll
+            for (int h = 0; h < NC; h++)
+                ch[h] = chunk(i, h * 16);
+            rows.mask(a, u, ch, t.in, g, t.s);
+            t.in = ~0u;
+        }
+        rows.raise(t.scaled, t.in, t.s);
+    };
+    auto add_values = [&](int stage) { rows.add_values(smem + (NS + stage) * G::TILE, here(voff), pf); };
+    // Interval i: the keys of tile i + 1 and the values of tile i are there; those that NS - 1 intervals later need are asked for
+    int64_t next_v = 0;             // where the values lie that are asked for next
+    int k_stage = 0, v_stage = 0, k_ask = 0, v_ask = 0;
+    auto ask = [&](int i) {         // what interval i needs
+        ask_tile(a.v + next_v, v_lane, true, v_ask);
+        if (!SPARSE && (i + 1 & 63) == 0 && i + 1 < steps)
+            ask_pages(tile0 + (i + 1) * u.splits);
+        next_v = place(min(i + 1, steps - 1));
+        ask_tile(a.k + next_v, k_lane, false, k_ask);
+        k_ask = after(k_ask);
+        v_ask = after(v_ask);
+    };
+    if (steps > 0) {
+        next_v = place(0);
+        ask_tile(a.k + next_v, k_lane, false, 0);
+        k_ask = after(0);
+#pragma unroll
+        for (int i = 0; i < NS - 1; i++)
+            if (i < steps)
+                ask(i);
+    }
     rows.see(a, u, first_row, G::CAP, parent, c, tid, G::THREADS, masks, parents, wave * QT * 16);
-    take(steps);
+    if (steps > 0) {
+        if (steps >= NS - 1)
+            wait_loads<(NS - 1) * 2 * G::LOADS>();
+        else
+            wait_loads<0>();
+        asm volatile("s_barrier" ::: "memory");
+        Tile even, odd;
+        {
+            const bool masked = look(0, even);
+            if (even.have) {
+#pragma unroll
+                for (int h = 0; h < NC; h += 2)
+                    rows.scores(smem, here(foff), h, even.s);
+                settle(0, even, masked);
+            }
+        }
+        // Interval i: the weights of tile i while the matrix cores are at the scores of tile i + 1, then the values of tile i, then what the new scores change
+        auto interval = [&](int i, Tile &t, Tile &n) {
+            if (i + NS - 2 < steps)
+                wait_loads<(NS - 2) * 2 * G::LOADS>();
+            else
+                wait_loads<0>();
+            clear_dead(i, v_stage);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the tiles are there, and all have done with the stages that are loaded next
+            if (i + NS - 1 < steps)
+                ask(i + NS - 1);
+            k_stage = after(k_stage);
+            const unsigned char *kt = smem + k_stage * G::TILE;
+            bool masked = false;
+            n.have = false;
+            if (i + 1 < steps)
+                masked = look(i + 1, n);
+            if (t.have && n.have) {
+                rows.scores_and_weights(kt, here(foff), n.s, t.scaled, t.in, t.s, pf);
+            } else if (t.have) {
+#pragma unroll
+                for (int j = 0; j < rows.SLICES; j++)
+                    rows.weigh(t.scaled, t.in, j, t.s, pf);
+            } else if (n.have) {
+#pragma unroll
+                for (int h = 0; h < NC; h += 2)
+                    rows.scores(kt, here(foff), h, n.s);
+            }
+            if (t.have)
+                add_values(v_stage);
+            if (n.have)
+                settle(i + 1, n, masked);
+            v_stage = after(v_stage);
+        };
+        for (int i = 0; i < steps; i += 2) {
+            interval(i, even, odd);
+            if (i + 1 < steps)
+                interval(i + 1, odd, even);
+        }
+    }
 
     const bool strange = rows.finish() || (SPARSE && list.all > list.n);      // (a list longer than what it was planned for: row by row)
     if (lane == 0)
