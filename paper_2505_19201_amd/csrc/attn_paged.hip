@@ -28,6 +28,7 @@ constexpr float SLACK = 8.0f;             // octaves a score may exceed its row'
 // One of a launch's two kinds of workgroups: those of the shared positions, and those of what is a sequence's own.
 struct Part {
     int32_t blocks, streams, row_groups, splits, slot;      // workgroups; units of a sequence or all groups, KV head and split; workgroups of a unit; its first slot
+    uint32_t row_groups_magic, splits_magic;                // for divide()
 };
 struct PagedAttnArgs {
     const unsigned char *q, *k, *v;
@@ -40,8 +41,19 @@ struct PagedAttnArgs {
     int32_t batch, n_tree, words, hq, hkv, group, rows;      // rows: query rows of a sequence and KV head
     int32_t lg_page, n_pages, max_pages, n_groups, n_slots, shared_slots, list_size;
     float scale_log2;
+    uint32_t hkv_magic, group_magic, rows_magic;
     Part shared, own;
 };
+// What stands ahead of a workgroup's first loads, as plain arguments of the kernels: those are in scalar registers when a wave starts, the structure is a trip to memory away.  Of the own part.
+#define PLAIN const int32_t *table, const int32_t *prefix_len, int32_t max_pages, int32_t hkv, uint32_t hkv_magic, int32_t shared_blocks, int32_t row_groups, uint32_t row_groups_magic, int32_t splits, \
+              uint32_t splits_magic, int32_t streams, int32_t lg_and_early
+
+// x / d by a multiplication, magic = (2^32 - 1) / d
+__device__ __forceinline__ uint32_t divide(uint32_t x, uint32_t d, uint32_t magic)
+{
+    const uint32_t q = __umulhi(x, magic);
+    return x - q * d >= d ? q + 1 : q;
+}
 
 // What a workgroup does.
 struct Unit {
@@ -99,28 +111,37 @@ __device__ __forceinline__ void group_of_tile(const PagedAttnArgs &a, int t, int
 }
 
 // Workgroup ids that are congruent mod 8 run on one XCD: row groups that read the same keys meet in one L2.  What needs no load; false: there is no such unit.
-__device__ __forceinline__ bool unit_at(const PagedAttnArgs &a, int cap, Unit &u, int &rg)
+__device__ __forceinline__ bool unit_at(const PagedAttnArgs &a, int hkv, uint32_t hkv_magic, uint32_t shared_blocks, uint32_t row_groups, uint32_t row_groups_magic, uint32_t splits,
+                                        uint32_t splits_magic, uint32_t streams, int cap, Unit &u, int &rg)
 {
-    const uint32_t block = blockIdx.x;
-    u.shared = block < (uint32_t)a.shared.blocks;
-    const uint32_t row_groups = u.shared ? a.shared.row_groups : a.own.row_groups, streams = u.shared ? a.shared.streams : a.own.streams;
-    u.splits = u.shared ? a.shared.splits : a.own.splits;
-    const uint32_t at = (block - (u.shared ? 0 : a.shared.blocks)) >> 3, slot = at / row_groups, stream = slot * 8 + (block & 7);
+    uint32_t block = blockIdx.x;
+    u.shared = block < shared_blocks;
+    if (u.shared) {
+        row_groups = a.shared.row_groups;
+        row_groups_magic = a.shared.row_groups_magic;
+        splits = a.shared.splits;
+        splits_magic = a.shared.splits_magic;
+        streams = a.shared.streams;
+    } else {
+        block -= shared_blocks;
+    }
+    const uint32_t at = block >> 3, slot = divide(at, row_groups, row_groups_magic), stream = slot * 8 + (block & 7);
     rg = at - slot * row_groups;
-    const uint32_t head = stream / (uint32_t)u.splits;
-    u.split = stream - head * u.splits;
-    u.slot = (u.shared ? a.shared.slot : a.own.slot) + u.split;
-    const uint32_t b = head / (uint32_t)a.hkv;      // (shared: 0)
-    u.kvh = head - b * a.hkv;
+    const uint32_t head = divide(stream, splits, splits_magic), b = divide(head, hkv, hkv_magic);      // (shared: b is 0)
+    u.splits = splits;
+    u.split = stream - head * splits;
+    u.kvh = head - b * hkv;
     u.b = b;
     u.row0 = rg * cap;
-    u.n_rows = a.rows;
     u.lo = 0;
     return stream < streams;
 }
+#define UNIT_AT(cap) unit_at(a, hkv, hkv_magic, shared_blocks, row_groups, row_groups_magic, splits, splits_magic, streams, cap, u, rg)
 // And what does: the prefix length (asked for by the caller), the groups
 __device__ __forceinline__ bool unit_of(const PagedAttnArgs &a, int cap, int lane, int rg, int prefix, Unit &u)
 {
+    u.slot = (u.shared ? a.shared.slot : a.own.slot) + u.split;
+    u.n_rows = a.rows;
     if (u.shared) {
         int n, shared;
         group_of_tile(a, rg, cap, lane, u.b, n, shared, u.row0);
@@ -250,11 +271,11 @@ __device__ __forceinline__ Row row_at(const PagedAttnArgs &a, const Unit &u, int
     w.b = u.b;
     w.r = j;
     if (u.shared) {
-        const int s = (uint32_t)j / (uint32_t)a.rows;
+        const int s = divide(j, a.rows, a.rows_magic);
         w.b += s;
         w.r = j - s * a.rows;
     }
-    w.node = (uint32_t)w.r / (uint32_t)a.group;
+    w.node = divide(w.r, a.group, a.group_magic);
     w.head = u.kvh * a.group + w.r - w.node * a.group;
     return w;
 }
@@ -471,14 +492,14 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
 // float32: there for its precision and for small shapes.
 constexpr int SINGLE_ROWS = 4, SINGLE_RUN = 64;
 template <int D, bool SPARSE>
-__global__ __launch_bounds__(256) void paged_f32_kernel(PagedAttnArgs a)
+__global__ __launch_bounds__(256) void paged_f32_kernel(PLAIN, PagedAttnArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     Unit u;
     int rg;
-    if (!unit_at(a, SINGLE_ROWS, u, rg))
+    if (!UNIT_AT(SINGLE_ROWS))
         return;
-    const int prefix = u.shared ? 0 : uniform_load(a.prefix_len + u.b);
+    const int prefix = u.shared ? 0 : uniform_load(prefix_len + u.b);
     if (unit_of(a, SINGLE_ROWS, threadIdx.x & 63, rg, prefix, u))
         attend_rows_singly<float, D, 256, SPARSE>(a, u, SINGLE_ROWS, SINGLE_RUN, SINGLE_RUN, smem);
 }
@@ -760,38 +781,53 @@ struct QueryRows {
     }
 };
 
-// The page of this lane's tile of a run of 64 (tile first + lane * stride; `further`: rows into it)
-__device__ __forceinline__ int page_of_tile(const PagedAttnArgs &a, int b, int row)
+// Byte offset of a lane's row, held as two registers and read by another lane's number
+struct Offset {
+    uint32_t lo, hi;
+    __device__ __forceinline__ void set(const PagedAttnArgs &a, int kvh, int page, int row, int row_bytes)
+    {
+        page = min(max(page, 0), a.n_pages - 1);
+        const uint64_t x = (((uint64_t)((uint64_t)(uint32_t)page * (uint32_t)a.hkv + (uint32_t)kvh) << a.lg_page) + (uint32_t)(row & ((1 << a.lg_page) - 1))) * (uint32_t)row_bytes;
+        lo = (uint32_t)x;
+        hi = (uint32_t)(x >> 32);
+    }
+    __device__ __forceinline__ int64_t of(int lane) const { return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi, lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)lo, lane)); }
+};
+// N pieces of 1024 bytes, one behind the other in memory and in LDS; lane_at(j): of the lane's 16 bytes in piece j
+template <int N, class F>
+__device__ __forceinline__ void lds_load_run(const void *from, F lane_at, uint32_t to)
 {
-    const int32_t *table = a.table + (int64_t)b * a.max_pages;
-    return min(max(table[min(row >> a.lg_page, a.max_pages - 1)], 0), a.n_pages - 1);
-}
-
-// Takes a workgroup's rows again, where a sum is not finite.  Not part of the kernels' code: it would have registers of its own beside theirs.
-template <int D, int THREADS, bool SPARSE>
-__device__ __forceinline__ void attend_again(const __attribute__((address_space(4))) PagedAttnArgs *kernel_args, int cap, int tile, int run, unsigned char *smem)
-{
-    const PagedAttnArgs &a = *(const PagedAttnArgs *)kernel_args;
-    Unit u;
-    int rg;
-    if (!unit_at(a, cap, u, rg))
-        return;
-    const int prefix = u.shared ? 0 : uniform_load(a.prefix_len + u.b);
-    if (unit_of(a, cap, threadIdx.x & 63, rg, prefix, u))
-        attend_rows_singly<uint16_t, D, THREADS, SPARSE>(a, u, cap, tile, run, smem);
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"   // m0 is reserved; naming it as clobbered is right all the same
+    if constexpr (N >= 4) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\ts_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5\n\t"
+                     "s_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5\n\ts_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5" ::"s"(to),
+                     "v"(lane_at(0)), "v"(lane_at(1) + 1024u), "v"(lane_at(2) + 2048u), "v"(lane_at(3) + 3072u), "s"(from)
+                     : "memory", "m0", "scc");
+        lds_load_run<N - 4>(static_cast<const char *>(from) + 4096, [&](int j) { return lane_at(j + 4); }, to + 4096);
+    } else if constexpr (N >= 2) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\ts_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" ::"s"(to), "v"(lane_at(0)),
+                     "v"(lane_at(1) + 1024u), "s"(from)
+                     : "memory", "m0", "scc");
+        lds_load_run<N - 2>(static_cast<const char *>(from) + 2048, [&](int j) { return lane_at(j + 2); }, to + 2048);
+    } else if constexpr (N == 1) {
+        lds_load16(from, lane_at(0), to);
+    }
+#pragma clang diagnostic pop
 }
 
 template <int D, int QT, int NW>
 struct KeysGeom {
     static constexpr int THREADS = 64 * NW, CAP = 16 * QT, ROW = 2 * D, TILE = 32 * ROW, LOADS = TILE / 1024;
-    static constexpr int STAGES = NW * 2 * TILE, JOIN = NW * CAP * (D + 4) * 4, MAIN = STAGES > JOIN ? STAGES : JOIN;
+    static constexpr int MAIN = NW * 2 * TILE;
+    static_assert(CAP * D * 4 <= 2 * TILE, "a wave's sums fit its stage");
     static int bytes(int words) { return MAIN + NW * CAP * 8 + NW * 8 + (words > 1 ? CAP * words * 8 + DREAM_MAX_TREE * 4 : 0); }
 };
 
 // Few rows: the waves take the key tiles in turn, each for all of the rows, and never meet until the end.  A wave asks for its next keys as soon as a tile's scores are there, and for its next
 // values as soon as they are added up.
 template <int D, int QT, int NW, bool SPARSE>
-__global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
+__global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArgs a)
 {
     using G = KeysGeom<D, QT, NW>;
     constexpr int ROW = G::ROW, LPR = ROW / 16, RPI = 1024 / ROW, HALF = G::LOADS / 2;
@@ -805,18 +841,20 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
 
     Unit u;
     int rg;
-    if (!unit_at(a, G::CAP, u, rg))
+    if (!UNIT_AT(G::CAP))
         return;
     // what needs no load is asked for first: of an own part the pages of the wave's tiles, the prefix length, the tree, the queries
-    const int prefix = u.shared ? 0 : uniform_load(a.prefix_len + u.b);
+    const int prefix = u.shared ? 0 : uniform_load(prefix_len + u.b);
     const int stride = u.splits * NW, mine = u.split * NW + wave;
-    int pages[2] = {0, 0};
-    auto ask_pages = [&](int first) {
+    const bool early = !SPARSE && lg_and_early >> 8;       // no groups: the first tile is the first, whatever else the call holds
+    const int lg_page = lg_and_early & 255;
+    int page[2] = {0, 0};
+    auto ask_pages = [&](int first) {      // of tiles first + lane * stride
 #pragma unroll
         for (int h = 0; h < 2; h++)
-            pages[h] = page_of_tile(a, u.b, (first + lane * stride) * 32 + h * 16);
+            page[h] = table[(int64_t)u.b * max_pages + min(((first + lane * stride) * 2 + h) >> (lg_page - 4), max_pages - 1)];
     };
-    if (!SPARSE && !a.n_groups)
+    if (early)
         ask_pages(mine);
     int parent = -1;
     if (!u.shared && a.words == 1 && !a.tree_mask)
@@ -829,7 +867,7 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
     QueryRows<D, QT, 2, SPARSE> rows;
     rows.load(a, u, u.row0, c, g);
     const int tile0 = u.lo / 32;
-    if (!SPARSE && a.n_groups)
+    if (!SPARSE && !early)
         ask_pages(tile0 + mine);
 
     const int foff = fragment_k<ROW>(c, g), voff = fragment_v<ROW>(c, g);
@@ -843,40 +881,36 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
             return Chunk{0, pos, pos < u.hi, true, true};
         }
     };
-    auto place = [&](int i, int h) {              // of the chunk's rows, in bytes
-        int page, at;
-        if constexpr (SPARSE) {
-            const int x = (wave + i * NW) * 32 + h * 16;
-            page = __builtin_amdgcn_readfirstlane(list.phys[min(x >> a.lg_page, list.n - 1)]);
-            at = x;
-        } else {
-            page = __builtin_amdgcn_readlane(pages[h], i & 63);
-            at = (tile0 + mine + i * stride) * 32 + h * 16;
-        }
-        return ((((int64_t)page * a.hkv + u.kvh) << a.lg_page) + (at & ((1 << a.lg_page) - 1))) * ROW;
-    };
-    auto ask_k = [&](int i) {
-        if (!SPARSE && (i & 63) == 0 && i)
-            ask_pages(tile0 + mine + i * stride);
+    Offset offset[2];                             // of the chunks of the lane's tile (of the list's: in units of a run of 64 as well)
+    auto locate = [&](int i) {                    // tiles i .. i + 63
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const unsigned char *from = a.k + place(i, h);
-            const int at = here(k_lane);
-            const uint32_t to = here_scalar(lds0 + stage);
+            if constexpr (SPARSE) {
+                const int x = (wave + (i + lane) * NW) * 32 + h * 16;
+                offset[h].set(a, u.kvh, list.phys[min(x >> lg_page, list.n - 1)], x, ROW);
+            } else {
+                offset[h].set(a, u.kvh, page[h], (tile0 + mine + (i + lane) * stride) * 32 + h * 16, ROW);
+            }
+        }
+    };
+    auto place = [&](int i, int h) { return offset[h].of(i & 63); };
+    auto ask_k = [&](int i) {
+        if ((i & 63) == 0) {
+            if (!SPARSE && i)
+                ask_pages(tile0 + mine + i * stride);
+            locate(i);
+        }
 #pragma unroll
-            for (int j = 0; j < HALF; j++)
-                lds_load16(from + j * 1024, (uint32_t)(at ^ swizzle_k<ROW>(h * HALF + j)), to + (h * HALF + j) * 1024);
+        for (int h = 0; h < 2; h++) {
+            const int at = here(k_lane);
+            lds_load_run<HALF>(a.k + place(i, h), [&](int j) { return (uint32_t)(at ^ swizzle_k<ROW>(h * HALF + j)); }, here_scalar(lds0 + stage) + h * HALF * 1024);
         }
     };
     auto ask_v = [&](int i) {
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-            const unsigned char *from = a.v + place(i, h);
             const int at = here(v_lane);
-            const uint32_t to = here_scalar(lds0 + stage + G::TILE);
-#pragma unroll
-            for (int j = 0; j < HALF; j++)
-                lds_load16(from + j * 1024, (uint32_t)(at ^ swizzle_v<ROW>(h * HALF + j)), to + (h * HALF + j) * 1024);
+            lds_load_run<HALF>(a.v + place(i, h), [&](int j) { return (uint32_t)(at ^ swizzle_v<ROW>(h * HALF + j)); }, here_scalar(lds0 + stage) + G::TILE + h * HALF * 1024);
         }
     };
     // Zeros over the values of rows that are nobody's
@@ -937,7 +971,7 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
     rows.see(a, u, u.row0, G::CAP, parent, c, tid, G::THREADS, masks, parents, 0);
     take(steps);
 
-    // ---- the waves' sums
+    // ---- the waves' sums meet, each wave's in its own stage: 16-byte piece i of row r at i ^ (r mod 16)
     const bool strange = rows.finish() || (SPARSE && list.all > list.n);      // (a list longer than what it was planned for: row by row)
     if (lane == 0)
         flags[wave] = strange;
@@ -945,44 +979,38 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PagedAttnArgs a)
 #pragma unroll
         for (int qt = 0; qt < QT; qt++)
             s_ml[wave * G::CAP + qt * 16 + c] = make_float2(rows.m[qt], rows.l[qt]);
+#pragma unroll
+    for (int qt = 0; qt < QT; qt++)
+#pragma unroll
+        for (int dt = 0; dt < D / 16; dt++)
+            *reinterpret_cast<f32x4 *>(smem + stage + (qt * 16 + c) * (4 * D) + ((dt * 4 + g) ^ c) * 16) = rows.o[qt][dt];
     __syncthreads();
     int again = 0;
 #pragma unroll
     for (int w = 0; w < NW; w++)
         again |= flags[w];
     if (again) {
-        attend_again<D, G::THREADS, SPARSE>((const __attribute__((address_space(4))) PagedAttnArgs *)__builtin_amdgcn_kernarg_segment_ptr(), G::CAP, 32, 32 * NW, smem);
+        __syncthreads();
+        attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(a, u, G::CAP, 32, 32 * NW, smem);
         return;
     }
-    constexpr int STR = D + 4;
-    float *join = reinterpret_cast<float *>(smem);
-#pragma unroll
-    for (int qt = 0; qt < QT; qt++) {
-        float most = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < NW; w++)
-            most = fmaxf(most, s_ml[w * G::CAP + qt * 16 + c].x);
-        const float f = rows.m[qt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(rows.m[qt] - most);
-        float *row = join + ((wave * QT + qt) * 16 + c) * STR + 4 * g;
-#pragma unroll
-        for (int dt = 0; dt < D / 16; dt++)
-            *reinterpret_cast<f32x4 *>(row + dt * 16) = rows.o[qt][dt] * f;
-    }
-    __syncthreads();
     const int count = min(G::CAP, u.n_rows - u.row0);
     for (int i = tid; i < count * (D / 4); i += G::THREADS) {
         const int j = i / (D / 4), ch = i % (D / 4);
         const Row w = row_at(a, u, u.row0 + j);
+        float2 ml[NW];
         float most = -INFINITY, sum = 0.0f;
-#pragma unroll
-        for (int x = 0; x < NW; x++)
-            most = fmaxf(most, s_ml[x * G::CAP + j].x);
         f32x4 all = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < NW; x++) {
-            const float2 ml = s_ml[x * G::CAP + j];
-            sum += ml.x == -INFINITY ? 0.0f : ml.y * __builtin_amdgcn_exp2f(ml.x - most);
-            all += *reinterpret_cast<const f32x4 *>(join + (x * G::CAP + j) * STR + ch * 4);
+            ml[x] = s_ml[x * G::CAP + j];
+            most = fmaxf(most, ml[x].x);
+        }
+#pragma unroll
+        for (int x = 0; x < NW; x++) {
+            const float f = ml[x].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[x].x - most);
+            sum = __builtin_fmaf(ml[x].y, f, sum);
+            all += *reinterpret_cast<const f32x4 *>(smem + x * 2 * G::TILE + j * (4 * D) + (ch ^ (j & 15)) * 16) * f;
         }
         if (ch == 0)
             put_ml(a, u, w, most, sum);
@@ -1006,7 +1034,7 @@ struct RowsGeom {
 
 // Many rows: the waves share the tiles and have rows of their own; one barrier a tile, NS - 1 tiles on their way.
 template <int D, int QT, int WR, int NS, bool SPARSE>
-__global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PagedAttnArgs a)
+__global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttnArgs a)
 {
     using G = RowsGeom<D, QT, WR, NS>;
     constexpr int ROW = G::ROW, KEYS = G::KEYS, NC = KEYS / 16, LPR = ROW / 16, RPI = 1024 / ROW;
@@ -1019,13 +1047,15 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PagedAttnArgs a)
 
     Unit u;
     int rg;
-    if (!unit_at(a, G::CAP, u, rg))
+    if (!UNIT_AT(G::CAP))
         return;
-    const int prefix = u.shared ? 0 : uniform_load(a.prefix_len + u.b);
+    const int prefix = u.shared ? 0 : uniform_load(prefix_len + u.b);
     const int own_rows = wave * (KEYS / WR), own_chunk = own_rows & ~15;      // of a tile: the rows that this wave asks for, and the chunk that they lie in
-    int pages = 0;
-    auto ask_pages = [&](int first) { pages = page_of_tile(a, u.b, (first + lane * u.splits) * KEYS + own_chunk); };
-    if (!SPARSE && !a.n_groups)
+    const bool early = !SPARSE && lg_and_early >> 8;       // no groups: the first tile is the first, whatever else the call holds
+    const int lg_page = lg_and_early & 255;
+    int page = 0;
+    auto ask_pages = [&](int first) { page = table[(int64_t)u.b * max_pages + min(((first + lane * u.splits) * KEYS + own_chunk) >> lg_page, max_pages - 1)]; };      // of tiles first + lane * splits
+    if (early)
         ask_pages(u.split);
     int parent = -1;
     if (!u.shared && a.words == 1 && !a.tree_mask)
@@ -1039,7 +1069,7 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PagedAttnArgs a)
     const int first_row = u.row0 + wave * QT * 16;
     rows.load(a, u, first_row, c, g);
     const int tile0 = u.lo / KEYS + u.split;
-    if (!SPARSE && a.n_groups)
+    if (!SPARSE && !early)
         ask_pages(tile0);
 
     const int foff = fragment_k<ROW>(c, g), voff = fragment_v<ROW>(c, g);
@@ -1052,23 +1082,18 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PagedAttnArgs a)
             return Chunk{0, pos, pos < u.hi, true, true};
         }
     };
-    // Keys of tile i to their stage, values to theirs (behind the last tile the last page again: such keys are never used)
-    auto place = [&](int i) {
-        int page, x;
+    Offset offset;                                         // of the wave's rows of the lane's tile
+    auto locate = [&](int i) {                             // tiles i .. i + 63
         if constexpr (SPARSE) {
-            x = i * KEYS + own_rows;
-            page = __builtin_amdgcn_readfirstlane(list.phys[min(x >> a.lg_page, list.n - 1)]);
+            const int x = (i + lane) * KEYS + own_rows;
+            offset.set(a, u.kvh, list.phys[min(x >> lg_page, list.n - 1)], x, ROW);
         } else {
-            x = (tile0 + i * u.splits) * KEYS + own_rows;
-            page = __builtin_amdgcn_readlane(pages, i & 63);
+            offset.set(a, u.kvh, page, (tile0 + (i + lane) * u.splits) * KEYS + own_rows, ROW);
         }
-        return ((((int64_t)page * a.hkv + u.kvh) << a.lg_page) + (x & ((1 << a.lg_page) - 1))) * ROW;
     };
     auto ask_tile = [&](const unsigned char *from, int lane_at, bool values, int stage) {
-        const uint32_t to = lds0 + (values ? NS + stage : stage) * G::TILE + wave * G::LOADS * 1024;
-#pragma unroll
-        for (int j = 0; j < G::LOADS; j++)
-            lds_load16(from + j * 1024, (uint32_t)(lane_at ^ (values ? swizzle_v<ROW>(wave * G::LOADS + j) : swizzle_k<ROW>(wave * G::LOADS + j))), to + j * 1024);
+        lds_load_run<G::LOADS>(from, [&](int j) { return (uint32_t)(lane_at ^ (values ? swizzle_v<ROW>(wave * G::LOADS + j) : swizzle_k<ROW>(wave * G::LOADS + j))); },
+                               lds0 + (values ? NS + stage : stage) * G::TILE + wave * G::LOADS * 1024);
     };
     auto after = [](int stage) { return stage == NS - 1 ? 0 : stage + 1; };
     // Zeros over the values of rows that are nobody's, by the wave that loaded them
@@ -1095,10 +1120,15 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PagedAttnArgs a)
     auto look = [&](int i, Tile &t) {
         Chunk ch[NC];
         bool straight = true;
+        if constexpr (SPARSE) {
 #pragma unroll
-        for (int h = 0; h < NC; h++) {
-            ch[h] = chunk(i, h * 16);
-            straight = straight && rows.plain(u, ch[h]);
+            for (int h = 0; h < NC; h++) {
+                ch[h] = chunk(i, h * 16);
+                straight = straight && rows.plain(u, ch[h]);
+            }
+        } else {
+            const int pos = (tile0 + i * u.splits) * KEYS;
+            straight = pos >= u.lo && pos + KEYS <= rows.whole;
         }
         t.scaled = straight && a.scale_log2 >= 0.0f ? a.scale_log2 : 1.0f;      // (the largest score of a negative scale is the smallest product)
         t.have = rows.seen_by(a, list, ch, straight, t.in);
@@ -1123,15 +1153,19 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PagedAttnArgs a)
     int k_stage = 0, v_stage = 0, k_ask = 0, v_ask = 0;
     auto ask = [&](int i) {         // what interval i needs
         ask_tile(a.v + next_v, v_lane, true, v_ask);
-        if (!SPARSE && (i + 1 & 63) == 0 && i + 1 < steps)
-            ask_pages(tile0 + (i + 1) * u.splits);
-        next_v = place(min(i + 1, steps - 1));
+        if ((i + 1 & 63) == 0 && i + 1 < steps) {
+            if (!SPARSE)
+                ask_pages(tile0 + (i + 1) * u.splits);
+            locate(i + 1);
+        }
+        next_v = offset.of(min(i + 1, steps - 1) & 63);      // (behind the last tile that one again: such keys are never used)
         ask_tile(a.k + next_v, k_lane, false, k_ask);
         k_ask = after(k_ask);
         v_ask = after(v_ask);
     };
     if (steps > 0) {
-        next_v = place(0);
+        locate(0);
+        next_v = offset.of(0);
         ask_tile(a.k + next_v, k_lane, false, 0);
         k_ask = after(0);
 #pragma unroll
@@ -1205,7 +1239,7 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PagedAttnArgs a)
     for (int w = 0; w < WR; w++)
         again |= flags[w];
     if (again) {
-        attend_again<D, G::THREADS, SPARSE>((const __attribute__((address_space(4))) PagedAttnArgs *)__builtin_amdgcn_kernarg_segment_ptr(), G::CAP, KEYS, KEYS, smem);
+        attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(a, u, G::CAP, KEYS, KEYS, smem);
         return;
     }
 #pragma unroll
@@ -1307,9 +1341,11 @@ struct PagedPlan {
 };
 
 // The shapes there are
-constexpr int keys_waves(int D, int qt) { return D == 256 || qt == 4 ? 4 : 8; }
-constexpr int keys_tiles(int D) { return D == 256 ? 2 : 4; }      // at most
+constexpr int keys_waves(int D) { return D == 256 ? 4 : 8; }
+constexpr int keys_tiles(int D) { return D == 256 ? 1 : 2; }      // at most
 constexpr int rows_tiles(int D) { return D == 256 ? 1 : 2; }
+
+uint32_t magic_for(uint32_t d) { return 0xffffffffu / d; }
 
 Shape shape_for(int D, bool f32, int64_t rows)
 {
@@ -1319,8 +1355,7 @@ Shape shape_for(int D, bool f32, int64_t rows)
     if (waves == 8 || (!waves && !tiles && rows > 16 * keys_tiles(D)))
         return tiles == 1 ? Shape{ROWS, 1, 4} : tiles == 2 ? Shape{ROWS, rows_tiles(D), 4} : Shape{ROWS, rows_tiles(D), 8};
     const int qt = tiles ? tiles : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    const int most = keys_tiles(D), taken = qt >= most ? most : qt >= 2 ? 2 : 1;
-    return {KEYS, taken, keys_waves(D, taken)};
+    return {KEYS, qt < keys_tiles(D) ? qt : keys_tiles(D), keys_waves(D)};
 }
 
 int splits_for(const Shape &s, int D, int64_t units, int64_t keys)
@@ -1357,6 +1392,8 @@ PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32
             s.part.splits = least;
         s.part.streams = (int)(heads * s.part.splits);
         s.part.blocks = ceil_div(s.part.streams, 8) * 8 * s.part.row_groups;
+        s.part.row_groups_magic = magic_for(s.part.row_groups);
+        s.part.splits_magic = magic_for(s.part.splits);
         s.part.slot = p.n_slots;
         p.n_slots += s.part.splits;
     };
@@ -1383,7 +1420,8 @@ int launch_kernel(F *kernel, const PagedAttnArgs &a, int threads, size_t lds, co
 {
     if (lds > 160 * 1024)
         return fail(DREAM_ERR_UNSUPPORTED, "%s: %zu bytes of LDS", name, lds);
-    hipLaunchKernelGGL(kernel, dim3(a.shared.blocks + a.own.blocks), dim3(threads), lds, st, a);
+    hipLaunchKernelGGL(kernel, dim3(a.shared.blocks + a.own.blocks), dim3(threads), lds, st, a.table, a.prefix_len, a.max_pages, a.hkv, a.hkv_magic, a.shared.blocks, a.own.row_groups,
+                       a.own.row_groups_magic, a.own.splits, a.own.splits_magic, a.own.streams, a.lg_page | (a.n_groups ? 0 : 256), a);
     return check_launch(name);
 }
 template <int THREADS, bool SPARSE>
@@ -1429,14 +1467,10 @@ int launch_shape(PagedAttnArgs &a, const Shape &s, hipStream_t st, bool set_up =
     }
     if (s.form == ROWS)
         return s.waves == 8 ? launch_rows<D, rows_tiles(D), 8, 3, SPARSE>(a, st, set_up) : s.qt == rows_tiles(D) ? launch_rows<D, rows_tiles(D), 4, 2, SPARSE>(a, st, set_up) : launch_rows<D, 1, 4, 2, SPARSE>(a, st, set_up);
-    if (s.qt == 1)
-        return launch_keys<D, 1, keys_waves(D, 1), SPARSE>(a, st, set_up);
-    if constexpr (keys_tiles(D) == 4)
-        if (s.qt == 4)
-            return launch_keys<D, 4, keys_waves(D, 4), SPARSE>(a, st, set_up);
     if constexpr (keys_tiles(D) >= 2)
-        return launch_keys<D, 2, keys_waves(D, 2), SPARSE>(a, st, set_up);
-    return DREAM_ERR_UNSUPPORTED;      // (no such shape)
+        if (s.qt == 2)
+            return launch_keys<D, 2, keys_waves(D), SPARSE>(a, st, set_up);
+    return launch_keys<D, 1, keys_waves(D), SPARSE>(a, st, set_up);
 }
 
 template <int D, bool SPARSE>
@@ -1469,10 +1503,10 @@ template <int D, bool SPARSE>
 int set_up()
 {
     PagedAttnArgs a = {};
-    for (int qt = 1; qt <= keys_tiles(D); qt *= 2)
-        if (int rc = launch_shape<D, SPARSE>(a, {KEYS, qt, keys_waves(D, qt)}, nullptr, true))
+    for (const Shape &s : {Shape{KEYS, 1, keys_waves(D)}, Shape{KEYS, keys_tiles(D), keys_waves(D)}, Shape{ROWS, 1, 4}, Shape{ROWS, rows_tiles(D), 4}, Shape{ROWS, rows_tiles(D), 8}})
+        if (int rc = launch_shape<D, SPARSE>(a, s, nullptr, true))
             return rc;
-    return launch_shape<D, SPARSE>(a, {ROWS, rows_tiles(D), 8}, nullptr, true);
+    return DREAM_OK;
 }
 
 int check_attn(const char *who, const dream_attn_desc *d, const dream_page_desc *pages, int32_t n_tree, int32_t n_groups)
@@ -1500,6 +1534,7 @@ int run(const char *who, const dream_attn_desc *d, const dream_page_desc *pages,
     a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)p.n_slots * p.all_rows * d->head_dim);
     a.batch = d->batch; a.hq = d->n_q_heads; a.hkv = d->n_kv_heads; a.group = a.hq / a.hkv; a.rows = a.n_tree * a.group; a.words = (a.n_tree + 63) / 64;
     a.lg_page = log2_of(pages->page_size); a.n_pages = pages->n_pages; a.max_pages = pages->max_pages;
+    a.hkv_magic = magic_for(a.hkv); a.group_magic = magic_for(a.group); a.rows_magic = magic_for(a.rows);
     const float scale = d->scale != 0.0f ? d->scale : 1.0f / sqrtf((float)d->head_dim);
     a.scale_log2 = scale * 1.4426950408889634f;
     const bool f32 = d->dtype == DREAM_F32;
