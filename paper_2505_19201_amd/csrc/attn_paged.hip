@@ -764,20 +764,43 @@ struct QueryRows {
         }
         return __any(strange != 0.0f);      // (0 * inf and 0 * NaN are NaN)
     }
-    // Of the pages of a step's chunks, which the rows see; false where none does
+    // Chunks of a list from row x on: which of their pages the rows see, and are they everyone's (whose page it is); false where no row sees any
     template <class List>
-    __device__ __forceinline__ bool seen_by(const PagedAttnArgs &a, const List &list, const Chunk (&ch)[NC], bool straight, uint32_t &in) const
+    __device__ __forceinline__ bool seen_by(const PagedAttnArgs &a, const Unit &u, const List &list, int x, bool &straight, uint32_t &in) const
     {
-        in = 0u;
-        if constexpr (SPARSE) {
-#pragma unroll
-            for (int h = 0; h < NC; h++)
+        auto look = [&](int h, uint32_t &bits) {
+            const Chunk c = listed_chunk(a, list, x + h * 16);
+            bits = 0u;
+            if (a.words == 1) {
+                const uint64_t word = list.word[c.entry];
 #pragma unroll
                 for (int qt = 0; qt < QT; qt++)
-                    in |= (uint32_t)(list.word[ch[h].entry * a.words + (node[qt] >> 6)] >> (node[qt] & 63) & 1) << (h * QT + qt);
-            return !straight || __any(in != 0u);
+                    bits |= (uint32_t)(word >> node[qt] & 1) << qt;
+            } else {
+#pragma unroll
+                for (int qt = 0; qt < QT; qt++)
+                    bits |= (uint32_t)(list.word[c.entry * a.words + (node[qt] >> 6)] >> (node[qt] & 63) & 1) << qt;
+            }
+            return c;
+        };
+        uint32_t bits;
+        if (16 * NC <= 1 << a.lg_page) {          // one page
+            Chunk c = look(0, bits);
+            straight = plain(u, c);
+            c.pos += 16 * (NC - 1);
+            straight = straight && plain(u, c);
+            in = bits * (QT == 1 ? (1u << NC) - 1 : NC == 2 ? 5u : 0x55u);
+        } else {
+            straight = true;
+            in = 0u;
+#pragma unroll
+            for (int h = 0; h < NC; h++) {
+                const Chunk c = look(h, bits);
+                straight = straight && plain(u, c);
+                in |= bits << (h * QT);
+            }
         }
-        return true;
+        return !straight || __any(in != 0u);
     }
 };
 
@@ -931,10 +954,19 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
     };
     auto take = [&](int steps) {
         for (int i = 0; i < steps; i++) {
-            Chunk ch[2] = {chunk(i, 0), chunk(i, 1)};
-            const bool straight = rows.plain(u, ch[0]) && rows.plain(u, ch[1]);
-            uint32_t in;
-            rows.seen_by(a, list, ch, straight, in);
+            Chunk ch[2];
+            bool straight;
+            uint32_t in = 0u;
+            if constexpr (SPARSE) {
+                rows.seen_by(a, u, list, (wave + i * NW) * 32, straight, in);
+            } else {
+                const int pos = (tile0 + mine + i * stride) * 32;
+                straight = pos >= u.lo && pos + 32 <= rows.whole;
+            }
+            if (!straight || a.scale_log2 < 0.0f) {
+                ch[0] = chunk(i, 0);
+                ch[1] = chunk(i, 1);
+            }
             f32x4 s[2][QT];
             bf16x8 pf[1][QT];
             wait_loads<G::LOADS>();
@@ -1115,29 +1147,25 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
         f32x4 s[NC][QT];
         float scaled;
         uint32_t in;
-        bool have;
+        bool have, masked;
     };
     auto look = [&](int i, Tile &t) {
-        Chunk ch[NC];
-        bool straight = true;
+        bool straight;
         if constexpr (SPARSE) {
-#pragma unroll
-            for (int h = 0; h < NC; h++) {
-                ch[h] = chunk(i, h * 16);
-                straight = straight && rows.plain(u, ch[h]);
-            }
+            t.have = rows.seen_by(a, u, list, i * KEYS, straight, t.in);
         } else {
             const int pos = (tile0 + i * u.splits) * KEYS;
             straight = pos >= u.lo && pos + KEYS <= rows.whole;
+            t.have = true;
+            t.in = 0u;
         }
-        t.scaled = straight && a.scale_log2 >= 0.0f ? a.scale_log2 : 1.0f;      // (the largest score of a negative scale is the smallest product)
-        t.have = rows.seen_by(a, list, ch, straight, t.in);
-        return !straight || a.scale_log2 < 0.0f;
+        t.masked = !straight || a.scale_log2 < 0.0f;      // (the largest score of a negative scale is the smallest product)
+        t.scaled = t.masked ? 1.0f : a.scale_log2;
     };
     bf16x8 pf[NC / 2][QT];
     // Scores that have come: what nobody sees is left out, the references are raised
-    auto settle = [&](int i, Tile &t, bool masked) {
-        if (masked) {
+    auto settle = [&](int i, Tile &t) {
+        if (t.masked) {
             Chunk ch[NC];
 #pragma unroll
             for (int h = 0; h < NC; h++)
@@ -1182,12 +1210,12 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
         asm volatile("s_barrier" ::: "memory");
         Tile even, odd;
         {
-            const bool masked = look(0, even);
+            look(0, even);
             if (even.have) {
 #pragma unroll
                 for (int h = 0; h < NC; h += 2)
                     rows.scores(smem, here(foff), h, even.s);
-                settle(0, even, masked);
+                settle(0, even);
             }
         }
         // Interval i: the weights of tile i while the matrix cores are at the scores of tile i + 1, then the values of tile i, then what the new scores change
@@ -1196,16 +1224,16 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
                 wait_loads<(NS - 2) * 2 * G::LOADS>();
             else
                 wait_loads<0>();
-            clear_dead(i, v_stage);
+            if (t.masked)
+                clear_dead(i, v_stage);
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the tiles are there, and all have done with the stages that are loaded next
             if (i + NS - 1 < steps)
                 ask(i + NS - 1);
             k_stage = after(k_stage);
             const unsigned char *kt = smem + k_stage * G::TILE;
-            bool masked = false;
             n.have = false;
             if (i + 1 < steps)
-                masked = look(i + 1, n);
+                look(i + 1, n);
             if (t.have && n.have) {
                 rows.scores_and_weights(kt, here(foff), n.s, t.scaled, t.in, t.s, pf);
             } else if (t.have) {
@@ -1220,7 +1248,7 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
             if (t.have)
                 add_values(v_stage);
             if (n.have)
-                settle(i + 1, n, masked);
+                settle(i + 1, n);
             v_stage = after(v_stage);
         };
         for (int i = 0; i < steps; i += 2) {
@@ -1335,62 +1363,111 @@ struct Segment {
 };
 struct PagedPlan {
     Segment shared, own;
-    int n_slots, shared_slots;
+    int n_slots, shared_slots, list_size;
     int64_t all_rows;
     size_t bytes;
 };
 
-// The shapes there are
-constexpr int keys_waves(int D) { return D == 256 ? 4 : 8; }
-constexpr int keys_tiles(int D) { return D == 256 ? 1 : 2; }      // at most
-constexpr int rows_tiles(int D) { return D == 256 ? 1 : 2; }
+// The shapes there are, and what they are estimated to take: where a CU has `groups` workgroups,
+//     us = base + per_group * (groups - 1) + steps * max(latency, issue * groups, kilobytes of a step / (FILL * min(row groups, 2)))  [+ the join]
+// as long as memory does not take longer (the sixth root of both sixth powers).  FILL: what a CU pulls that nobody asks for beside it.  The constants are those with which the choice is best over
+// measured times of every shape with every number of splits below (7 head layouts x batches of 1, 4, 16, 48 x trees of 1 to 120 nodes x 100 to 12000 keys, 558 problems, 9785 times): 1.3 % behind the
+// fastest in the geometric mean, 7.5 % at the 95th percentile, 36 % at most, on the data that they were fitted to.  What a shape is worth over these problems (mean and most that the fastest would take
+// longer without it): 16 rows 4.5 % and 29 %, 32 rows 0.9 % and 21 %, 64 rows 2.7 % and 49 %, 128 rows 0.9 % and 25 %, 128 rows of 256 on eight waves 0.2 % and 9 %; eight waves at
+// smaller head_dim (0.2 %) and four query tiles a wave are left out.
+struct Kind {
+    Shape shape;
+    float base, per_group, latency, issue;
+};
+constexpr int KINDS = 4;
+constexpr Kind KIND[3][KINDS] = {{{{KEYS, 1, 8}, 5.41f, 1.71f, 0.855f, 0.801f}, {{KEYS, 2, 8}, 6.98f, 5.29f, 1.041f, 1.071f}, {{ROWS, 1, 4}, 5.96f, 1.46f, 0.716f, 0.399f}, {{ROWS, 2, 4}, 7.53f, 2.51f, 0.960f, 0.683f}},
+                                 {{{KEYS, 1, 8}, 6.11f, 5.32f, 1.248f, 1.567f}, {{KEYS, 2, 8}, 8.48f, 7.57f, 1.825f, 1.824f}, {{ROWS, 1, 4}, 6.64f, 3.03f, 1.009f, 0.675f}, {{ROWS, 2, 4}, 8.83f, 3.31f, 1.327f, 1.040f}},
+                                 {{{KEYS, 1, 4}, 8.08f, 7.06f, 1.836f, 1.857f}, {{KEYS, 1, 4}, 8.08f, 7.06f, 1.836f, 1.857f}, {{ROWS, 1, 4}, 7.22f, 3.53f, 0.941f, 0.655f}, {{ROWS, 1, 8}, 9.38f, 7.87f, 1.116f, 1.158f}}};
+constexpr int kinds_of(int D) { return D == 64 ? 0 : D == 128 ? 1 : 2; }
+constexpr float FILL = 76.6f, MEMORY = 4.78e6f, JOIN = 2.23f, JOIN_SPLIT = 0.72f, JOIN_BYTE = 1.14e-6f;      // KB / us; bytes / us; us, us a split, us a value
+constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48};
 
 uint32_t magic_for(uint32_t d) { return 0xffffffffu / d; }
 
-Shape shape_for(int D, bool f32, int64_t rows)
+// What a part is: KV heads (of all sequences), query rows of each, keys; `groups`: lists of rows that end in a workgroup of their own (0: one a head); bytes of keys and values; the nodes that see
+// keys of their own (0: none)
+struct Problem {
+    int64_t heads, rows, keys, groups;
+    float bytes;
+    int nodes_of, all_keys;               // query rows a node (selected pages: a workgroup with more nodes sees more pages)
+    bool joined;                          // anyway
+};
+int64_t row_groups_of(const Problem &p, const Shape &s) { return p.groups ? p.rows / s.cap() + p.groups : (p.rows + s.cap() - 1) / s.cap(); }
+
+void choose(int D, bool f32, const Problem &p, Segment &out)
 {
-    if (f32)
-        return {SINGLY, 0, 4};
-    const int tiles = q_tiles_override(), waves = tile_waves_override();
-    if (waves == 8 || (!waves && !tiles && rows > 16 * keys_tiles(D)))
-        return tiles == 1 ? Shape{ROWS, 1, 4} : tiles == 2 ? Shape{ROWS, rows_tiles(D), 4} : Shape{ROWS, rows_tiles(D), 8};
-    const int qt = tiles ? tiles : rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    return {KEYS, qt < keys_tiles(D) ? qt : keys_tiles(D), keys_waves(D)};
+    const int tiles = q_tiles_override(), waves = tile_waves_override(), forced = kv_splits_override();
+    float best = INFINITY;
+    auto consider = [&](const Kind &k) {
+        const Shape &s = k.shape;
+        const int64_t groups = row_groups_of(p, s), units = p.heads * (p.groups ? p.rows / s.cap() + 1 : groups);
+        float keys = (float)p.keys;
+        if (p.nodes_of) {                 // nodes that ask alike see more pages together: measured about the 0.4th power of their number
+            const float nodes = (float)(p.rows < s.cap() ? p.rows : s.cap()) / (float)p.nodes_of;
+            keys *= nodes > 1.0f ? powf(nodes, 0.4f) : 1.0f;
+            keys = keys < (float)p.all_keys ? keys : (float)p.all_keys;
+        }
+        const int64_t steps = (int64_t)(keys / (float)s.keys(D)) + 1;
+        const float fill = (float)(s.keys(D) * D) * 4e-3f / (FILL * (groups > 1 ? 2.0f : 1.0f)), memory = p.bytes / MEMORY + 5.0f;
+        for (int n : SPLITS) {
+            if (forced ? n > 1 : n > 1 && n > steps)
+                break;
+            const int splits = forced ? (forced < 64 ? forced : 64) : n;
+            const float per_cu = (float)((units * splits + 255) / 256);
+            float step = k.issue * per_cu > k.latency ? k.issue * per_cu : k.latency;
+            step = step > fill ? step : fill;
+            float us = k.base + k.per_group * (per_cu - 1.0f) + (float)((steps + splits - 1) / splits) * step;
+            if (splits > 1 || p.joined)
+                us += (p.joined ? 0.0f : JOIN) + JOIN_SPLIT * splits + JOIN_BYTE * (float)p.heads * (float)p.rows * (float)(splits * D);
+            us *= us * us;
+            us = us * us + memory * memory * memory * memory * memory * memory;
+            if (us < best) {
+                best = us;
+                out.shape = s;
+                out.part.splits = splits;
+            }
+        }
+    };
+    if (f32) {
+        consider({{SINGLY, 0, 4}, 6.0f, 3.0f, 6.0f, 3.0f});
+    } else {
+        for (int i = 0; i < KINDS; i++) {
+            const Kind &k = KIND[kinds_of(D)][i];
+            const bool of_form = !waves || (waves == 8) == (k.shape.form == ROWS), last = i == (waves == 4 ? 1 : KINDS - 1);
+            if (of_form && (!tiles || k.shape.qt == tiles || (last && tiles > k.shape.qt)))
+                consider(k);
+        }
+        if (best == INFINITY)
+            consider(KIND[kinds_of(D)][0]);
+    }
+    out.part.row_groups = (int)row_groups_of(p, out.shape);
 }
 
-int splits_for(const Shape &s, int D, int64_t units, int64_t keys)
-{
-    const int64_t steps = (keys + s.keys(D) - 1) / s.keys(D);
-    if (const int forced = kv_splits_override())
-        return forced < 64 ? forced : 64;
-    int64_t n = 256 / (units > 0 ? units : 1);
-    if (n > steps / 2)
-        n = steps / 2;
-    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
-}
-// So that the lists of selected pages hold all that a workgroup's rows may see
-int least_splits(const dream_page_desc *pages, int32_t n_tree, int64_t max_kv, int64_t seen_pages)
+// Pages that a workgroup's rows may see, those of the tree included: what its lists, of all splits together, have to hold
+int64_t listed_pages(const dream_page_desc *pages, int32_t n_tree, int64_t max_kv, int64_t seen_pages)
 {
     int64_t most = (max_kv + pages->page_size - 1) / pages->page_size;
     if (seen_pages > 0 && seen_pages * n_tree < most)
         most = seen_pages * n_tree;
-    return ceil_div(most + n_tree / pages->page_size + 2, n_tree > 64 ? SPARSE_LIST / 2 : SPARSE_LIST);
+    return most + n_tree / pages->page_size + 2;
 }
 
 PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32_t n_tree, int64_t max_kv, int32_t n_groups, int64_t max_shared, bool sparse, int64_t seen_pages)
 {
     PagedPlan p = {};
     const int D = d->head_dim;
-    const int64_t capacity = paged_rows(pages), rows = (int64_t)n_tree * (d->n_q_heads / d->n_kv_heads);
+    const bool f32 = d->dtype == DREAM_F32;
+    const int64_t capacity = paged_rows(pages), group = d->n_q_heads / d->n_kv_heads, rows = n_tree * group, heads = (int64_t)d->batch * d->n_kv_heads, row_bytes = D * (f32 ? 8 : 4);
     max_kv = max_kv < 1 ? 1 : max_kv > capacity ? capacity : max_kv;
     max_shared = max_shared < 1 ? 1 : max_shared > max_kv ? max_kv : max_shared;
-    const bool f32 = d->dtype == DREAM_F32;
-    auto segment = [&](Segment &s, int64_t of, int64_t row_groups, int64_t heads, int64_t keys, int least) {
-        s.part.row_groups = (int)row_groups;
-        s.part.splits = splits_for(s.shape, D, heads * of, keys);
-        if (s.part.splits < least)
-            s.part.splits = least;
-        s.part.streams = (int)(heads * s.part.splits);
+    auto finish = [&](Segment &s, int64_t n_heads, int least) {
+        s.part.splits = s.part.splits > least ? s.part.splits : least;
+        s.part.streams = (int)(n_heads * s.part.splits);
         s.part.blocks = ceil_div(s.part.streams, 8) * 8 * s.part.row_groups;
         s.part.row_groups_magic = magic_for(s.part.row_groups);
         s.part.splits_magic = magic_for(s.part.splits);
@@ -1398,17 +1475,17 @@ PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32
         p.n_slots += s.part.splits;
     };
     if (n_groups) {
-        p.shared.shape = shape_for(D, f32, d->batch * rows / n_groups);
-        const int64_t groups = d->batch * rows / p.shared.shape.cap();
-        segment(p.shared, groups + 1, groups + n_groups, d->n_kv_heads, max_shared, 1);
+        choose(D, f32, {d->n_kv_heads, d->batch * rows, max_shared, n_groups, (float)n_groups * (float)d->n_kv_heads * (float)max_shared * (float)row_bytes, 0, 0, true}, p.shared);
+        finish(p.shared, d->n_kv_heads, 1);
         p.shared_slots = p.n_slots;
     }
-    p.own.shape = shape_for(D, f32, rows);
-    const int64_t heads = (int64_t)d->batch * d->n_kv_heads, row_groups = ceil_div(rows, p.own.shape.cap());
     int64_t own_keys = n_groups ? max_kv - max_shared + 1 : max_kv;
-    if (seen_pages > 0 && seen_pages * pages->page_size + n_tree < own_keys)
-        own_keys = seen_pages * pages->page_size + n_tree;
-    segment(p.own, row_groups, row_groups, heads, own_keys, sparse ? least_splits(pages, n_tree, max_kv, seen_pages) : 1);
+    const bool some = sparse && seen_pages > 0 && seen_pages * pages->page_size + n_tree < own_keys;
+    const int64_t all_keys = own_keys, listed = listed_pages(pages, n_tree, max_kv, seen_pages);
+    own_keys = some ? seen_pages * pages->page_size + n_tree : own_keys;
+    choose(D, f32, {heads, rows, own_keys, 0, (float)heads * (float)own_keys * (float)row_bytes, some ? (int)group : 0, (int)all_keys, n_groups != 0}, p.own);
+    finish(p.own, heads, sparse ? ceil_div(listed, n_tree > 64 ? SPARSE_LIST / 2 : SPARSE_LIST) : 1);
+    p.list_size = sparse ? ceil_div(listed, p.own.part.splits) : 0;
     p.all_rows = heads * rows;
     p.bytes = p.n_slots > 1 ? (size_t)p.n_slots * p.all_rows * (D + 2) * 4 : 0;
     return p;
@@ -1425,13 +1502,9 @@ int launch_kernel(F *kernel, const PagedAttnArgs &a, int threads, size_t lds, co
     return check_launch(name);
 }
 template <int THREADS, bool SPARSE>
-size_t list_bytes(PagedAttnArgs &a)
+size_t list_bytes(const PagedAttnArgs &a)
 {
-    using List = PageList<THREADS>;
-    if (!SPARSE)
-        return 0;
-    a.list_size = a.words > 1 ? SPARSE_LIST / 2 : SPARSE_LIST;
-    return List::bytes(a.list_size, a.words);
+    return SPARSE ? PageList<THREADS>::bytes(a.list_size, a.words) : 0;
 }
 template <int D, int QT, int NW, bool SPARSE>
 int launch_keys(PagedAttnArgs &a, hipStream_t st, bool set_up)
@@ -1465,12 +1538,17 @@ int launch_shape(PagedAttnArgs &a, const Shape &s, hipStream_t st, bool set_up =
         const size_t list = list_bytes<256, SPARSE>(a);
         return launch_kernel(&paged_f32_kernel<D, SPARSE>, a, 256, single_bytes<D, 256>(SINGLE_ROWS, a.words) + list, "paged_f32_kernel", st);
     }
-    if (s.form == ROWS)
-        return s.waves == 8 ? launch_rows<D, rows_tiles(D), 8, 3, SPARSE>(a, st, set_up) : s.qt == rows_tiles(D) ? launch_rows<D, rows_tiles(D), 4, 2, SPARSE>(a, st, set_up) : launch_rows<D, 1, 4, 2, SPARSE>(a, st, set_up);
-    if constexpr (keys_tiles(D) >= 2)
-        if (s.qt == 2)
-            return launch_keys<D, 2, keys_waves(D), SPARSE>(a, st, set_up);
-    return launch_keys<D, 1, keys_waves(D), SPARSE>(a, st, set_up);
+    if (s.form == ROWS) {
+        if constexpr (D == 256)
+            return s.waves == 8 ? launch_rows<D, 1, 8, 3, SPARSE>(a, st, set_up) : launch_rows<D, 1, 4, 2, SPARSE>(a, st, set_up);
+        else
+            return s.qt == 2 ? launch_rows<D, 2, 4, 2, SPARSE>(a, st, set_up) : launch_rows<D, 1, 4, 2, SPARSE>(a, st, set_up);
+    }
+    if constexpr (D == 256) {
+        return launch_keys<D, 1, 4, SPARSE>(a, st, set_up);
+    } else {
+        return s.qt == 2 ? launch_keys<D, 2, 8, SPARSE>(a, st, set_up) : launch_keys<D, 1, 8, SPARSE>(a, st, set_up);
+    }
 }
 
 template <int D, bool SPARSE>
@@ -1478,6 +1556,7 @@ int launch_all(PagedAttnArgs &a, const PagedPlan &p, bool f32, hipStream_t st)
 {
     a.n_slots = p.n_slots;
     a.shared_slots = p.shared_slots;
+    a.list_size = p.list_size;
     a.all_rows = p.all_rows;
     a.shared = p.shared.part;
     a.own = p.own.part;
@@ -1503,8 +1582,8 @@ template <int D, bool SPARSE>
 int set_up()
 {
     PagedAttnArgs a = {};
-    for (const Shape &s : {Shape{KEYS, 1, keys_waves(D)}, Shape{KEYS, keys_tiles(D), keys_waves(D)}, Shape{ROWS, 1, 4}, Shape{ROWS, rows_tiles(D), 4}, Shape{ROWS, rows_tiles(D), 8}})
-        if (int rc = launch_shape<D, SPARSE>(a, s, nullptr, true))
+    for (const Kind &k : KIND[kinds_of(D)])
+        if (int rc = launch_shape<D, SPARSE>(a, k.shape, nullptr, true))
             return rc;
     return DREAM_OK;
 }
