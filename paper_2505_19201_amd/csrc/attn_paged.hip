@@ -825,7 +825,7 @@ __device__ __forceinline__ void lds_load_run(const void *from, F lane_at, uint32
     if constexpr (N >= 4) {
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\ts_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5\n\t"
                      "s_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5\n\ts_add_u32 m0, m0, 1024\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %5" ::"s"(to),
-                     "v"(lane_at(0)), "v"(lane_at(1) + 1024u), "v"(lane_at(2) + 2048u), "v"(lane_at(3) + 3072u), "s"(from)
+                     "v"(lane_at(0)), "v"(lane_at(1) + 1024u), "v"(lane_at(2) + 2 * 1024u), "v"(lane_at(3) + 3 * 1024u), "s"(from)
                      : "memory", "m0", "scc");
         lds_load_run<N - 4>(static_cast<const char *>(from) + 4096, [&](int j) { return lane_at(j + 4); }, to + 4096);
     } else if constexpr (N >= 2) {

@@ -7,7 +7,7 @@
 //
 // Two launches.  score_kernel: S^T = pages x nodes by v_mfma_i32_16x16x64_i8, the parts c+ against U and c- against W one behind the other.  The heads' numbers add up before the product (it is linear in
 // them): the sum, at most 64 * 127, goes in as two numbers, 64 hi + lo.  choose_kernel: a wave per node finds the n_best-th score by halving the range of the scores, taken as whole numbers
-// in their order, until as many lie above as are wanted; where equal scores straddle the border the lower pages win.
+// in their order, until as many lie above as are wanted; where equal scores straddle the border the lower pages win.  (Sixteen waves for the only node of a step of one token.)
 #include <type_traits>
 #include "paged.h"
 
@@ -17,7 +17,7 @@ namespace {
 
 constexpr int NODES = 64;            // of a workgroup: the bits of a word
 constexpr int PAGES = 64;            // of a workgroup of score_kernel: 16 for each wave
-constexpr int RANGE = 2048;          // pages whose words choose_kernel holds at a time
+constexpr int RANGE = 2048;          // pages whose bits choose_kernel holds at a time where no lane holds their scores
 
 struct SelectArgs {
     const void *q, *bounds;
@@ -36,273 +36,363 @@ __device__ __forceinline__ int pages_of(const SelectArgs &a, int b)
 // The least e in [-100, 122] with top <= 127 * 2^e; top >= 0
 __device__ __forceinline__ int least_exponent(float top) { return min(max((int)((__float_as_uint(top) + 0x1ffffu) >> 23) - 133, -100), 122); }
 
+// Sixteen values of a row as they stand in memory
 template <class T>
-struct Sixteen {                     // values of a row
-    float v[16];
+struct Sixteen {
+    static constexpr int N = sizeof(T);
+    u32x4 raw[N];
     __device__ __forceinline__ void load(const T *p)
     {
-        if constexpr (std::is_same_v<T, float>) {
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(p + i * 4);
-#pragma unroll
-                for (int e = 0; e < 4; e++)
-                    v[i * 4 + e] = x[e];
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const u32x4 x = *reinterpret_cast<const u32x4 *>(p + i * 8);
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    v[i * 8 + e * 2] = __uint_as_float(x[e] << 16);
-                    v[i * 8 + e * 2 + 1] = __uint_as_float(x[e] & 0xffff0000u);
-                }
-            }
-        }
+        for (int i = 0; i < N; i++)
+            raw[i] = reinterpret_cast<const u32x4 *>(p)[i];
+    }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (std::is_same_v<T, float>)
+            return __uint_as_float(raw[i >> 2][i & 3]);
+        else
+            return __uint_as_float(i & 1 ? raw[i >> 3][i >> 1 & 3] & 0xffff0000u : raw[i >> 3][i >> 1 & 3] << 16);
     }
     __device__ __forceinline__ float top() const
     {
         float t = 0.0f;
 #pragma unroll
         for (int i = 0; i < 16; i++)
-            t = __builtin_elementwise_maximum(t, __builtin_fabsf(v[i]));      // (a NaN stays)
+            t = __builtin_elementwise_maximum(t, __builtin_fabsf((*this)[i]));      // (a NaN stays)
         return t;
     }
 };
 
-__device__ __forceinline__ int byte_of(int x, int at) { return (x & 255) << (8 * at); }
+// Lowest bytes of four numbers, in order
+__device__ __forceinline__ uint32_t bytes_of(int a, int b, int c, int d)
+{
+    return __builtin_amdgcn_perm((uint32_t)b, (uint32_t)a, 0x0c0c0400u) | __builtin_amdgcn_perm((uint32_t)d, (uint32_t)c, 0x04000c0cu);
+}
 
 template <class T, int UP>
 __device__ __forceinline__ i32x4 bound_codes(const Sixteen<T> &x, float scale)
 {
-    i32x4 r = {0, 0, 0, 0};
+    i32x4 r;
+    auto code = [&](int i) { return (int)(UP ? ceilf(x[i] * scale) : floorf(x[i] * scale)); };
 #pragma unroll
-    for (int i = 0; i < 16; i++) {
-        const float y = x.v[i] * scale;
-        r[i >> 2] |= byte_of((int)(UP ? ceilf(y) : floorf(y)), i & 3);
-    }
+    for (int i = 0; i < 4; i++)
+        r[i] = (int)bytes_of(code(4 * i), code(4 * i + 1), code(4 * i + 2), code(4 * i + 3));
     return r;
 }
 
-// A workgroup: 64 pages against 64 nodes of a sequence and KV head.
+// A workgroup: 64 pages against 64 nodes of a sequence and KV head; waves 16 pages x 64 channels each.  Latency bounds it (a workgroup reads some 60 KB and multiplies for 300 clocks): everything
+// that is read is asked for at the start, queries before they are needed twice over, bounds of pages before it is known whether they are live.
 template <class T, int D>
-__global__ __launch_bounds__(256) void score_kernel(SelectArgs a)
+__global__ __launch_bounds__(4 * D) void score_kernel(SelectArgs a)
 {
     constexpr int KS = D / 64, NSTR = 4 * D + 16;         // bytes of a node in LDS: positive hi, lo, negative hi, lo
+    constexpr int SSTR = PAGES + 17;                      // (a step of 17 banks from node to node)
+    constexpr int HEADS = std::is_same_v<T, float> ? 2 : 4;      // that a lane holds at a time
     __shared__ __attribute__((aligned(16))) unsigned char s_q[NODES * NSTR];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    __shared__ int s_sum[NODES * SSTR], s_exponent[PAGES];
+    __shared__ float s_top[KS][PAGES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4, pt = wave & 3, ks = wave >> 2;
     const int groups = (a.n_tree + NODES - 1) / NODES;
-    const int b = blockIdx.z, kvh = blockIdx.y / groups, node0 = (blockIdx.y - kvh * groups) * NODES, n_nodes = min(NODES, a.n_tree - node0);
-    const int n = pages_of(a, b), page0 = blockIdx.x * PAGES;
-    // (only pages in between are ranked)
-    if (page0 >= n - a.n_last || page0 + PAGES <= a.n_first)
-        return;
-    // the pages' bounds are on their way while the queries become whole numbers
-    const int mine = min(page0 + wave * 16 + c, n - 1);
-    const int id = min(max(a.table[(int64_t)b * a.max_pages + mine], 0), a.n_pages - 1);
-    const T *bound = static_cast<const T *>(a.bounds) + ((int64_t)id * a.hkv + kvh) * 2 * D;
-    Sixteen<T> u[KS], w[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ks++) {
-        u[ks].load(bound + ks * 64 + g * 16);
-        w[ks].load(bound + D + ks * 64 + g * 16);
-    }
+    const int b = blockIdx.z, kvh = blockIdx.y / groups, node0 = (blockIdx.y - kvh * groups) * NODES, n_nodes = min(NODES, a.n_tree - node0), page0 = blockIdx.x * PAGES;
+    const int entry = a.table[(int64_t)b * a.max_pages + min(page0 + pt * 16 + c, a.max_pages - 1)];
     // ---- queries: D / 16 lanes a node
     constexpr int LANES = D / 16;
-    for (int at = tid / LANES; at < (n_nodes + 15) / 16 * 16; at += 256 / LANES) {
-        const int node = min(at, n_nodes - 1), part = tid % LANES;
-        const T *q = static_cast<const T *>(a.q) + (((int64_t)b * a.n_tree + node0 + node) * a.hq + (int64_t)kvh * a.group) * D + part * 16;
+    const int at = tid / LANES, part = tid % LANES;
+    const bool quantises = at < (n_nodes + 15) / 16 * 16;
+    const T *q = static_cast<const T *>(a.q) + (((int64_t)b * a.n_tree + node0 + min(at, n_nodes - 1)) * a.hq + (int64_t)kvh * a.group) * D + part * 16;
+    Sixteen<T> x[HEADS];
+    auto heads_from = [&](int h) {                // (heads behind the last: the last again)
+#pragma unroll
+        for (int i = 0; i < HEADS; i++)
+            x[i].load(q + (int64_t)min(h + i, a.group - 1) * D);
+    };
+    if (quantises)
+        heads_from(0);
+    // ---- bounds of this wave's sixteen pages
+    const T *bound = static_cast<const T *>(a.bounds) + ((int64_t)min(max(entry, 0), a.n_pages - 1) * a.hkv + kvh) * 2 * D + ks * 64 + g * 16;
+    Sixteen<T> u, w;
+    u.load(bound);
+    w.load(bound + D);
+    const int n = pages_of(a, b);
+    if (page0 >= n - a.n_last || page0 + PAGES <= a.n_first)      // (only pages in between are ranked)
+        return;
+    for (int i = tid; i < NODES * SSTR; i += 4 * D)
+        s_sum[i] = 0;
+    if (quantises) {
         float top = 0.0f;
-        for (int h = 0; h < a.group; h++) {
-            Sixteen<T> x;
-            x.load(q + (int64_t)h * D);
-            top = fmaxf(top, x.top());
+        for (int h = 0;;) {
+#pragma unroll
+            for (int i = 0; i < HEADS; i++)
+                top = fmaxf(top, x[i].top());
+            h += HEADS;
+            if (h >= a.group)
+                break;
+            heads_from(h);
         }
 #pragma unroll
         for (int s = 1; s < LANES; s *= 2)
             top = fmaxf(top, __shfl_xor(top, s));
         const float scale = __uint_as_float((uint32_t)(127 - least_exponent(top)) << 23);
-        int pos[16], neg[16];
+        float sum[16], size[16];                  // of the heads' whole numbers: at most 64 * 127, exact
 #pragma unroll
         for (int i = 0; i < 16; i++)
-            pos[i] = neg[i] = 0;
-        for (int h = 0; h < a.group; h++) {
-            Sixteen<T> x;
-            x.load(q + (int64_t)h * D);
+            sum[i] = size[i] = 0.0f;
+        for (int h = 0; h < a.group; h += HEADS) {
+            if (a.group > HEADS)
+                heads_from(h);
 #pragma unroll
-            for (int i = 0; i < 16; i++) {
-                const int v = (int)rintf(x.v[i] * scale);
-                pos[i] += max(v, 0);
-                neg[i] += max(-v, 0);
+            for (int j = 0; j < HEADS; j++)
+                if (h + j < a.group) {
+#pragma unroll
+                    for (int i = 0; i < 16; i++) {
+                        const float v = rintf(x[j][i] * scale);
+                        sum[i] += v;
+                        size[i] += __builtin_fabsf(v);
+                    }
+                }
+        }
+        // Two at a time as 16-bit halves: bits 6 to 13 are the quotient by 64, with its sign
+        i32x4 d[4];
+#pragma unroll
+        for (int k = 0; k < 2; k++)
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                uint32_t two[2];
+#pragma unroll
+                for (int e = 0; e < 2; e++) {
+                    auto part_of = [&](int j) { return (uint32_t)(int)((k ? sum[j] - size[j] : sum[j] + size[j]) * 0.5f); };
+                    two[e] = __builtin_amdgcn_perm(part_of(4 * i + 2 * e + 1), part_of(4 * i + 2 * e), 0x05040100u);
+                }
+                d[2 * k][i] = (int)__builtin_amdgcn_perm(two[1] >> 6, two[0] >> 6, 0x06040200u);
+                d[2 * k + 1][i] = (int)(__builtin_amdgcn_perm(two[1], two[0], 0x06040200u) & 0x3f3f3f3fu);
             }
-        }
-        i32x4 d[4] = {};
-#pragma unroll
-        for (int i = 0; i < 16; i++) {
-            d[0][i >> 2] |= byte_of(pos[i] >> 6, i & 3);
-            d[1][i >> 2] |= byte_of(pos[i] & 63, i & 3);
-            d[2][i >> 2] |= byte_of(neg[i] >> 6, i & 3);
-            d[3][i >> 2] |= byte_of(neg[i] & 63, i & 3);
-        }
 #pragma unroll
         for (int i = 0; i < 4; i++)
             *reinterpret_cast<i32x4 *>(s_q + at * NSTR + i * D + part * 16) = d[i];
     }
-    // ---- this wave's sixteen pages
-    float top = 0.0f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ks++)
-        top = __builtin_elementwise_maximum(top, __builtin_elementwise_maximum(u[ks].top(), w[ks].top()));
+    float top = __builtin_elementwise_maximum(u.top(), w.top());
     top = __builtin_elementwise_maximum(top, __shfl_xor(top, 16));
     top = __builtin_elementwise_maximum(top, __shfl_xor(top, 32));
+    if (g == 0)
+        s_top[ks][pt * 16 + c] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < KS; i++)
+        top = __builtin_elementwise_maximum(top, s_top[i][pt * 16 + c]);
     const int e = top <= 3.4028234e38f ? least_exponent(top) : 1000;
     const float scale = __uint_as_float((uint32_t)(127 - min(e, 122)) << 23);
-    i32x4 up[KS], down[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ks++) {
-        up[ks] = bound_codes<T, 1>(u[ks], scale);
-        down[ks] = bound_codes<T, 0>(w[ks], scale);
-    }
-    int exponent[4];
-#pragma unroll
-    for (int r = 0; r < 4; r++)
-        exponent[r] = __shfl(e, 4 * g + r);
-    __syncthreads();
-    const int first = page0 + wave * 16 + 4 * g;
+    if (ks == 0 && g == 0)
+        s_exponent[pt * 16 + c] = e;
+    const i32x4 up = bound_codes<T, 1>(u, scale), down = bound_codes<T, 0>(w, scale);
     for (int nt = 0; nt * 16 < n_nodes; nt++) {
-        const unsigned char *row = s_q + (nt * 16 + c) * NSTR + g * 16;
-        i32x4 hi = {0, 0, 0, 0}, lo = {0, 0, 0, 0}, nhi = {0, 0, 0, 0}, nlo = {0, 0, 0, 0};
+        const unsigned char *row = s_q + (nt * 16 + c) * NSTR + ks * 64 + g * 16;
+        auto codes = [&](int i) { return *reinterpret_cast<const i32x4 *>(row + i * D); };
+        i32x4 hi = {0, 0, 0, 0}, lo = {0, 0, 0, 0};
+        hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(up, codes(0), hi, 0, 0, 0);
+        lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(up, codes(1), lo, 0, 0, 0);
+        hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(down, codes(2), hi, 0, 0, 0);
+        lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(down, codes(3), lo, 0, 0, 0);
 #pragma unroll
-        for (int ks = 0; ks < KS; ks++) {
-            auto part = [&](int i) { return *reinterpret_cast<const i32x4 *>(row + i * D + ks * 64); };
-            hi = __builtin_amdgcn_mfma_i32_16x16x64_i8(up[ks], part(0), hi, 0, 0, 0);
-            lo = __builtin_amdgcn_mfma_i32_16x16x64_i8(up[ks], part(1), lo, 0, 0, 0);
-            nhi = __builtin_amdgcn_mfma_i32_16x16x64_i8(down[ks], part(2), nhi, 0, 0, 0);
-            nlo = __builtin_amdgcn_mfma_i32_16x16x64_i8(down[ks], part(3), nlo, 0, 0, 0);
-        }
-        const int node = nt * 16 + c;
+        for (int r = 0; r < 4; r++)
+            atomicAdd(&s_sum[(nt * 16 + c) * SSTR + pt * 16 + 4 * g + r], hi[r] * 64 + lo[r]);      // (whole numbers: any order)
+    }
+    __syncthreads();
+    for (int node = tid / 16; node < n_nodes; node += D / 4) {
+        const int page = tid % 16 * 4;
         u32x4 key;
 #pragma unroll
         for (int r = 0; r < 4; r++) {
-            const float s = ldexpf((float)((hi[r] - nhi[r]) * 64 + (lo[r] - nlo[r])), exponent[r]);
-            const uint32_t bits = __float_as_uint(exponent[r] > 122 ? INFINITY : s);
+            const int exponent = s_exponent[page + r];
+            const float s = ldexpf((float)s_sum[node * SSTR + page + r], exponent);
+            const uint32_t bits = __float_as_uint(exponent > 122 ? INFINITY : s);
             key[r] = bits >> 31 ? ~bits : bits | 0x80000000u;      // in the scores' order
         }
-        if (node < n_nodes)
-            *reinterpret_cast<u32x4 *>(a.keys + (((int64_t)b * a.hkv + kvh) * a.n_tree + node0 + node) * a.stride + first) = key;
+        *reinterpret_cast<u32x4 *>(a.keys + (((int64_t)b * a.hkv + kvh) * a.n_tree + node0 + node) * a.stride + page0 + page) = key;
     }
 }
 
-// A workgroup per 64 nodes of a sequence and KV head, a wave per node.  VALUES: scores a lane holds (0: they are read again every time).
-template <int VALUES>
-__global__ __launch_bounds__(1024) void choose_kernel(SelectArgs a)
+// TEAM waves to a node (one, or all of the workgroup: its barriers are among those); VALUES: scores that a lane holds (0: they are read again every time; TEAM is 1 then).  The nodes' choices meet in LDS as one bit a page and leave it as
+// their part of every page's word.
+template <int VALUES, int TEAM>
+__global__ __launch_bounds__(TEAM == 1 ? 512 : 1024) void choose_kernel(SelectArgs a)
 {
-    __shared__ uint64_t s_words[RANGE];
-    __shared__ uint32_t s_border[NODES], s_ties[NODES];      // scores above the border are in, and of those at it the pages below s_ties
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), waves = blockDim.x >> 6;
-    const int b = blockIdx.z, kvh = blockIdx.y, node0 = blockIdx.x * NODES, n_nodes = min(NODES, a.n_tree - node0);
+    static_assert(TEAM == 1 || TEAM == 16);
+    constexpr int WAVES = TEAM == 1 ? 8 : 16, HERE = WAVES / TEAM, HELD = VALUES ? VALUES * TEAM * 64 : RANGE;      // nodes of a workgroup; pages that it holds at a time
+    __shared__ uint64_t s_bits[HERE][HELD / 64];
+    __shared__ uint32_t s_team[2][WAVES][2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), member = wave % TEAM, at = wave / TEAM;
+    const int b = blockIdx.z, kvh = blockIdx.y, node0 = blockIdx.x * HERE, node = min(node0 + at, a.n_tree - 1);
+    const uint32_t *scores = a.keys + (((int64_t)b * a.hkv + kvh) * a.n_tree + node) * a.stride;
+    // scores are asked for before it is known how many there are (the array has as many as a lane asks for, of pages that may be none)
+    uint32_t held[VALUES ? VALUES : 1];
+    if constexpr (VALUES > 0) {
+#pragma unroll
+        for (int i = 0; i < VALUES; i++)
+            held[i] = a.n_best > 0 ? scores[min((i * TEAM + member) * 64 + lane, a.stride - 1)] : 0u;
+    }
     const int n = pages_of(a, b), lo = min(a.n_first, n), hi = max(n - a.n_last, lo), between = hi - lo;
-    const int words = (a.n_tree + 63) / 64;
-    auto scores = [&](int node) { return a.keys + (((int64_t)b * a.hkv + kvh) * a.n_tree + node0 + node) * a.stride; };
-    if (a.n_best > 0 && a.n_best < between) {
-        for (int node = wave; node < n_nodes; node += waves) {
-            const uint32_t *key = scores(node) + lo;
-            uint32_t held[VALUES ? VALUES : 1];
-            uint32_t most = 0u, least = ~0u;
+    const bool ranked = a.n_best > 0 && a.n_best < between;
+    uint32_t border = 0u, ties = ~0u;             // scores above the border are in, and of those at it the pages below `ties`
+    if (ranked) {
+        uint32_t most = 0u, least = ~0u;
+        if constexpr (VALUES > 0) {
+#pragma unroll
+            for (int i = 0; i < VALUES; i++) {
+                const int page = (i * TEAM + member) * 64 + lane;
+                const bool in = page >= lo && page < hi;
+                most = in ? max(most, held[i]) : most;
+                least = in ? min(least, held[i]) : least;
+                held[i] = in ? held[i] : 0u;      // (no score is 0: that would be a NaN's)
+            }
+        } else {
+            for (int page = lo + lane; page < hi; page += 64) {
+                most = max(most, scores[page]);
+                least = min(least, scores[page]);
+            }
+        }
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) {
+            most = max(most, (uint32_t)__shfl_xor((int)most, s));
+            least = min(least, (uint32_t)__shfl_xor((int)least, s));
+        }
+        int turn = 0;
+        if constexpr (TEAM > 1) {
+            if (lane == 0) {
+                s_team[1][wave][0] = most;
+                s_team[1][wave][1] = least;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < TEAM; w++) {
+                most = max(most, s_team[1][at * TEAM + w][0]);
+                least = min(least, s_team[1][at * TEAM + w][1]);
+            }
+        }
+        auto count = [&](uint32_t from) {         // scores at or above it; by all of the team, as often
+            int sum = 0;
             if constexpr (VALUES > 0) {
 #pragma unroll
-                for (int i = 0; i < VALUES; i++) {
-                    const int at = i * 64 + lane;
-                    held[i] = key[min(at, between - 1)];
-                }
-#pragma unroll
-                for (int i = 0; i < VALUES; i++) {
-                    most = max(most, held[i]);
-                    least = min(least, held[i]);
-                    held[i] = i * 64 + lane < between ? held[i] : 0u;      // (no score is 0: that would be a NaN's)
-                }
+                for (int i = 0; i < VALUES; i++)
+                    sum += __popcll(__ballot(held[i] >= from));
             } else {
-                for (int at = lane; at < between; at += 64) {
-                    most = max(most, key[at]);
-                    least = min(least, key[at]);
-                }
+                for (int page = lo; page < hi; page += 64)
+                    sum += __popcll(__ballot(page + lane < hi && scores[min(page + lane, hi - 1)] >= from));
             }
+            if constexpr (TEAM > 1) {
+                if (lane == 0)
+                    s_team[0][wave][turn] = sum;
+                __syncthreads();
+                sum = 0;
 #pragma unroll
-            for (int s = 1; s < 64; s *= 2) {
-                most = max(most, (uint32_t)__shfl_xor((int)most, s));
-                least = min(least, (uint32_t)__shfl_xor((int)least, s));
+                for (int w = 0; w < TEAM; w++)
+                    sum += s_team[0][at * TEAM + w][turn];
+                sum = __builtin_amdgcn_readfirstlane(sum);
+                turn ^= 1;
             }
-            auto count = [&](uint32_t from) {      // scores at or above it
-                int sum = 0;
-                if constexpr (VALUES > 0) {
-#pragma unroll
-                    for (int i = 0; i < VALUES; i++)
-                        sum += __popcll(__ballot(held[i] >= from));
-                } else {
-                    for (int at = 0; at < between; at += 64)
-                        sum += __popcll(__ballot(at + lane < between && key[min(at + lane, between - 1)] >= from));
-                }
-                return sum;
-            };
-            // count(from) >= n_best > count(above), above - from shrinking to 1
-            uint32_t from = __builtin_amdgcn_readfirstlane((int)least), above = (uint32_t)__builtin_amdgcn_readfirstlane((int)most) + 1u;
-            int have = between;
-            while (have != a.n_best && above - from > 1u) {
-                const uint32_t middle = from + (above - from) / 2u;
-                const int k = count(middle);
-                if (k >= a.n_best) {
-                    from = middle;
-                    have = k;
-                } else {
-                    above = middle;
-                }
+            return sum;
+        };
+        // count(from) >= n_best > count(above), above - from shrinking to 1
+        uint32_t from = __builtin_amdgcn_readfirstlane((int)least), above = (uint32_t)__builtin_amdgcn_readfirstlane((int)most) + 1u;
+        int have = between, over = 0;
+        while (have != a.n_best && above - from > 1u) {
+            const uint32_t middle = from + (above - from) / 2u;
+            const int k = count(middle);
+            if (k >= a.n_best) {
+                from = middle;
+                have = k;
+            } else {
+                above = middle;
+                over = k;
             }
-            uint32_t ties = ~0u;
-            if (have != a.n_best) {      // the equal scores at the border: the lower pages
-                int room = a.n_best - count(from + 1u);
-                for (int at = 0; at < between; at += 64) {
-                    const uint64_t equal = __ballot(at + lane < between && key[min(at + lane, between - 1)] == from);
+        }
+        border = from;
+        if (have != a.n_best) {                   // the equal scores at the border (`over` are above it): the lower pages
+            int room = a.n_best - over;
+            if constexpr (TEAM == 1) {
+                for (int page = lo & ~63; page < hi; page += 64) {
+                    const uint64_t equal = __ballot(page + lane >= lo && page + lane < hi && scores[min(max(page + lane, lo), hi - 1)] == from);
                     const int k = __popcll(equal);
-                    if (k >= room) {      // the page behind the last one taken
+                    if (k >= room) {              // the page behind the last one taken
                         const bool last = equal >> lane & 1 && __popcll(equal & ((2ull << lane) - 1)) == room;
-                        ties = (uint32_t)(lo + at + __builtin_ctzll(__ballot(last)) + 1);
+                        ties = (uint32_t)(page + __builtin_ctzll(__ballot(last)) + 1);
                         break;
                     }
                     room -= k;
                 }
-            }
-            if (lane == 0) {
-                s_border[node] = from;
-                s_ties[node] = ties;
-            }
-        }
-    }
-    const uint64_t all = n_nodes == 64 ? ~0ull : (1ull << n_nodes) - 1;
-    for (int page0 = 0; page0 < a.max_pages; page0 += RANGE) {
-        const int pages = min(RANGE, a.max_pages - page0);
-        __syncthreads();      // (the borders are there; the range before is written)
-        for (int i = tid; i < pages; i += blockDim.x) {
-            const int page = page0 + i;
-            s_words[i] = page < n && (page < lo || page >= hi || a.n_best >= between) ? all : 0ull;
-        }
-        __syncthreads();
-        if (a.n_best > 0 && a.n_best < between) {
-            const int first = max(lo, page0), last = min(hi, page0 + pages);
-            for (int node = wave; node < n_nodes; node += waves) {
-                const uint32_t *key = scores(node);
-                const uint32_t border = s_border[node], ties = s_ties[node];
-                for (int page = first + lane; page < last; page += 64) {
-                    const uint32_t x = key[page];
-                    if (x > border || (x == border && (uint32_t)page < ties))
-                        atomicOr(reinterpret_cast<unsigned long long *>(s_words + page - page0), 1ull << node);
+            } else {
+                // by halving again: the least page with `room` equal ones below it
+                uint32_t low = 0u, high = (uint32_t)hi;
+                while (high - low > 1u) {
+                    const uint32_t middle = low + (high - low) / 2u;
+                    int sum = 0;
+#pragma unroll
+                    for (int i = 0; i < (VALUES ? VALUES : 1); i++)
+                        sum += __popcll(__ballot(held[i] == from && (uint32_t)((i * TEAM + member) * 64 + lane) < middle));
+                    if (lane == 0)
+                        s_team[0][wave][turn] = sum;
+                    __syncthreads();
+                    sum = 0;
+#pragma unroll
+                    for (int w = 0; w < TEAM; w++)
+                        sum += s_team[0][at * TEAM + w][turn];
+                    turn ^= 1;
+                    if (__builtin_amdgcn_readfirstlane(sum) >= room)
+                        high = middle;
+                    else
+                        low = middle;
                 }
+                ties = high;
+            }
+        }
+    }
+    auto takes = [&](int page, uint32_t score) {
+        return page < n && (page < lo || page >= hi || (a.n_best > 0 && (!ranked || score > border || (score == border && (uint32_t)page < ties))));
+    };
+    const int words = (a.n_tree + 63) / 64, rest = a.n_tree - node0;      // nodes from this workgroup's first on
+    const bool there = node0 + at < a.n_tree;
+    uint64_t *out = a.page_nodes + ((int64_t)b * a.hkv + kvh) * a.max_pages * words + node0 / 64;
+    const int live = min(n, a.max_pages);
+    for (int page0 = 0; page0 < live; page0 += HELD) {      // (pages that lanes hold are all there are)
+        __syncthreads();                          // (the range before is written)
+        if constexpr (VALUES > 0) {
+#pragma unroll
+            for (int i = 0; i < VALUES; i++) {
+                const int page = (i * TEAM + member) * 64 + lane;
+                const uint64_t bits = there ? __ballot(takes(page, held[i])) : 0ull;
+                if (lane == 0)
+                    s_bits[at][i * TEAM + member] = bits;
+            }
+        } else {
+            for (int i = 0; i < HELD / 64; i++) {
+                const int page = page0 + i * 64 + lane;
+                const uint64_t bits = there ? __ballot(takes(page, scores[min(page, a.stride - 1)])) : 0ull;
+                if (lane == 0)
+                    s_bits[at][i] = bits;
             }
         }
         __syncthreads();
-        for (int i = tid; i < pages; i += blockDim.x)
-            a.page_nodes[(((int64_t)b * a.hkv + kvh) * a.max_pages + page0 + i) * words + blockIdx.x] = s_words[i];
+        for (int i = tid; i < min(HELD, live - page0); i += 64 * WAVES) {
+            uint32_t mine = 0u;
+#pragma unroll
+            for (int w = 0; w < HERE; w++)
+                mine |= (uint32_t)(s_bits[w][i >> 6] >> (i & 63) & 1) << w;
+            uint64_t *word = out + (int64_t)(page0 + i) * words;
+            const int first = node0 & 63;         // of the word's bits; the last workgroup of a word writes what is left of it
+            if (first == 0 && rest <= HERE)
+                *word = mine;
+            else if (HERE > 1) {
+                uint8_t *parts = reinterpret_cast<uint8_t *>(word);
+                parts[first / 8] = (uint8_t)mine;
+                if (rest <= HERE)
+                    for (int k = first / 8 + 1; k < 8; k++)
+                        parts[k] = 0;
+            }
+        }
     }
+    if ((node0 & 63) == 0)                        // words of pages that there are not
+        for (int page = live + tid; page < a.max_pages; page += 64 * WAVES)
+            out[(int64_t)page * words] = 0ull;
 }
 
 int select_stride(const dream_page_desc *pages, int32_t n_tree, int64_t max_kv_len)
@@ -330,13 +420,23 @@ int launch_select(const SelectArgs &a, int D, int B, hipStream_t st)
     const int groups = ceil_div(a.n_tree, NODES);
     if (a.n_best > 0) {
         auto *score = D == 64 ? &score_kernel<T, 64> : D == 128 ? &score_kernel<T, 128> : &score_kernel<T, 256>;
-        hipLaunchKernelGGL(score, dim3(a.stride / PAGES, a.hkv * groups, B), dim3(256), 0, st, a);
+        hipLaunchKernelGGL(score, dim3(a.stride / PAGES, a.hkv * groups, B), dim3(4 * D), 0, st, a);
         if (int rc = check_launch("score_kernel"))
             return rc;
     }
-    auto *choose = a.stride <= 256 ? &choose_kernel<4> : a.stride <= 2048 ? &choose_kernel<32> : &choose_kernel<0>;
-    const int waves = a.n_tree >= 16 ? 16 : a.n_tree;
-    hipLaunchKernelGGL(choose, dim3(groups, a.hkv, B), dim3(waves < 4 ? 256 : waves * 64), 0, st, a);
+    // One token: all of a workgroup's waves rank its pages together
+    if (a.n_tree == 1 && a.stride > 256 && a.stride <= 8192) {
+        auto *choose = a.stride <= 2048 ? &choose_kernel<2, 16> : &choose_kernel<8, 16>;
+        hipLaunchKernelGGL(choose, dim3(1, a.hkv, B), dim3(1024), 0, st, a);
+    } else {
+        auto *choose = a.stride <= 128    ? &choose_kernel<2, 1>
+                       : a.stride <= 256  ? &choose_kernel<4, 1>
+                       : a.stride <= 512  ? &choose_kernel<8, 1>
+                       : a.stride <= 1024 ? &choose_kernel<16, 1>
+                       : a.stride <= 2048 ? &choose_kernel<32, 1>
+                                          : &choose_kernel<0, 1>;
+        hipLaunchKernelGGL(choose, dim3(ceil_div(a.n_tree, 8), a.hkv, B), dim3(512), 0, st, a);
+    }
     return check_launch("choose_kernel");
 }
 

@@ -203,6 +203,13 @@ SELECT = [
     (64, 1, 64, 3, [90], 1, 1, 10, "bf16"),
     (4, 2, 128, 9, [200, 3], 1, 1, 10, "f32"),
     (2, 2, 256, 5, [90], 1, 1, 10, "f32"),
+    (4, 2, 64, 1, [300, 2048], 1, 1, 16, "bf16"),
+    (2, 2, 64, 1, [3000, 8], 2, 3, 100, "bf16"),
+    (1, 1, 64, 1, [8300], 0, 1, 7, "bf16"),
+    (4, 2, 64, 20, [600, 1024], 1, 1, 40, "bf16"),
+    (2, 1, 64, 70, [1500, 33], 1, 2, 64, "bf16"),
+    (14, 2, 128, 67, [400], 1, 1, 12, "bf16"),
+    (10, 2, 64, 17, [90, 5], 1, 0, 12, "f32"),
 ]
 
 
