@@ -57,8 +57,9 @@ __device__ __forceinline__ uint32_t divide(uint32_t x, uint32_t d, uint32_t magi
 
 // What a workgroup does.
 struct Unit {
-    bool shared;
+    bool shared, alone;                                 // alone: outside every group, where there are some
     int b, kvh, split, splits, slot, row0, n_rows;      // the sequence whose pages are read; its slot; rows are numbered through the sequences from b on
+    uint32_t splits_magic;
     int lo, hi, P;                                      // positions [lo, hi), of which those from P on are the tree's
 };
 
@@ -129,11 +130,13 @@ __device__ __forceinline__ bool unit_at(const PagedAttnArgs &a, int hkv, uint32_
     rg = at - slot * row_groups;
     const uint32_t head = divide(stream, splits, splits_magic), b = divide(head, hkv, hkv_magic);      // (shared: b is 0)
     u.splits = splits;
+    u.splits_magic = splits_magic;
     u.split = stream - head * splits;
     u.kvh = head - b * hkv;
     u.b = b;
     u.row0 = rg * cap;
     u.lo = 0;
+    u.alone = false;
     return stream < streams;
 }
 #define UNIT_AT(cap) unit_at(a, hkv, hkv_magic, shared_blocks, row_groups, row_groups_magic, splits, splits_magic, streams, cap, u, rg)
@@ -151,8 +154,11 @@ __device__ __forceinline__ bool unit_of(const PagedAttnArgs &a, int cap, int lan
     }
     u.P = clamped_prefix(a, prefix);
     u.hi = u.P + a.n_tree;
-    if (a.n_groups)
-        u.lo = min(max(shared_by(a, u.b, lane), 0), u.P);
+    if (a.n_groups) {
+        const int shared = shared_by(a, u.b, lane);
+        u.alone = shared < 0;
+        u.lo = min(max(shared, 0), u.P);
+    }
     return true;
 }
 
@@ -168,8 +174,23 @@ struct PageList {
     uint32_t *logical;
     uint64_t *word;
     int n, all;                     // entries; this split's pages
+    int32_t id[EACH + 1];           // of a thread's pages, one in front of them first; which nodes see them (trees of one word)
+    uint64_t seen[EACH];
 
-    // By all threads; starts and ends with a barrier.
+    // Of the thread's pages from `first` on: needs no length, so the first are asked for with it
+    __device__ __forceinline__ void ask(const PagedAttnArgs &a, const Unit &u, int first)
+    {
+        const int32_t *table = a.table + (int64_t)u.b * a.max_pages;
+        const uint64_t *nodes = a.nodes + ((int64_t)u.b * a.hkv + u.kvh) * a.max_pages * a.words;
+#pragma unroll
+        for (int i = 0; i <= EACH; i++)
+            id[i] = table[min(max(first + i - 1, 0), a.max_pages - 1)];
+        if (a.words == 1)
+#pragma unroll
+            for (int i = 0; i < EACH; i++)
+                seen[i] = nodes[min(first + i, a.max_pages - 1)];
+    }
+    // By all threads, each of which has asked for its first pages; starts and ends with a barrier.
     __device__ __forceinline__ void build(const PagedAttnArgs &a, const Unit &u, int cap, int tid, unsigned char *smem, int skip)
     {
         phys = reinterpret_cast<int32_t *>(smem);
@@ -178,7 +199,6 @@ struct PageList {
         int32_t *counts = reinterpret_cast<int32_t *>(smem + (8 + 8 * a.words) * a.list_size);
         const int in_prefix = (u.P + (1 << a.lg_page) - 1) >> a.lg_page, tree_page = u.P >> a.lg_page;
         const int total = in_prefix + ((u.hi - 1) >> a.lg_page) - tree_page + 1;
-        const int32_t *table = a.table + (int64_t)u.b * a.max_pages;
         const int lane = tid & 63, wave = tid >> 6;
         const uint64_t *nodes = a.nodes + ((int64_t)u.b * a.hkv + u.kvh) * a.max_pages * a.words;
         const int node0 = (uint32_t)u.row0 / (uint32_t)a.group, node1 = (uint32_t)(min(u.row0 + cap, u.n_rows) - 1) / (uint32_t)a.group;
@@ -186,17 +206,21 @@ struct PageList {
             const int lo = max(node0 - 64 * w, 0), hi = min(node1 - 64 * w, 63);
             return lo > hi ? 0ull : ~0ull >> (63 - hi) & ~0ull << lo;
         };
-        auto upto = [&](int r) { return r > u.split ? (int)((uint32_t)(r - u.split + u.splits - 1) / (uint32_t)u.splits) : 0; };      // this split's among the first r
+        auto upto = [&](int r) { return r > u.split ? (int)divide(r - u.split + u.splits - 1, u.splits, u.splits_magic) : 0; };      // this split's among the first r
         int rank = 0;
         for (int scanned = 0; scanned < total; scanned += SCAN) {
             __syncthreads();
             int taken = 0;
             uint32_t mine = 0;
             const int v0 = scanned + tid * EACH;
+            if (scanned)
+                ask(a, u, v0);
 #pragma unroll
             for (int i = 0; i < EACH; i++) {
                 bool in = v0 + i >= in_prefix && v0 + i < total;
-                if (v0 + i < in_prefix)
+                if (a.words == 1)
+                    in = in || (v0 + i < in_prefix && (seen[i] & ours(0)) != 0ull);
+                else if (v0 + i < in_prefix)
                     for (int w = 0; w < a.words; w++)
                         in = in || (nodes[(int64_t)(v0 + i) * a.words + w] & ours(w)) != 0ull;
                 mine |= (uint32_t)in << i;
@@ -218,18 +242,21 @@ struct PageList {
                 r += w < wave ? x : 0;
                 rank += x;
             }
+#pragma unroll
             for (int i = 0; i < EACH; i++) {
-                if (!(mine >> i & 1))
-                    continue;
                 const int at = upto(r) - skip;
-                if ((uint32_t)r % (uint32_t)u.splits == (uint32_t)u.split && at >= 0 && at < a.list_size) {
-                    const int v = v0 + i, page = v < in_prefix ? v : tree_page + v - in_prefix;
-                    phys[at] = min(max(table[page], 0), a.n_pages - 1);
-                    logical[at] = (uint32_t)page | (v < in_prefix ? 0u : TREE_PAGE);
-                    for (int w = 0; w < a.words; w++)
-                        word[at * a.words + w] = v < in_prefix ? nodes[(int64_t)v * a.words + w] : 0ull;
+                if ((mine >> i & 1) && at * u.splits + skip * u.splits + u.split == r && at >= 0 && at < a.list_size) {
+                    const int v = v0 + i;
+                    const bool prefix = v < in_prefix, in_front = !prefix && tree_page < in_prefix;      // (the tree begins in the prefix's last page)
+                    phys[at] = min(max(in_front ? id[i] : id[i + 1], 0), a.n_pages - 1);
+                    logical[at] = (uint32_t)(prefix ? v : tree_page + v - in_prefix) | (prefix ? 0u : TREE_PAGE);
+                    if (a.words == 1)
+                        word[at] = prefix ? seen[i] : 0ull;
+                    else
+                        for (int w = 0; w < a.words; w++)
+                            word[at * a.words + w] = prefix ? nodes[(int64_t)v * a.words + w] : 0ull;
                 }
-                r++;
+                r += mine >> i & 1;
             }
         }
         all = __builtin_amdgcn_readfirstlane(upto(rank));
@@ -290,6 +317,14 @@ __device__ __forceinline__ void put_ml(const PagedAttnArgs &a, const Unit &u, co
         a.part_ml[row_of_part(a, u, w)] = make_float2(m, l);
     else if (a.lse)
         a.lse[((int64_t)w.b * a.hq + w.head) * a.n_tree + w.node] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
+}
+// The rows of a sequence outside every group have empty shared parts
+__device__ __forceinline__ void no_shared_parts(const PagedAttnArgs &a, const Unit &u, int cap, int tid, int threads)
+{
+    if (u.split == 0)
+        for (int j = u.row0 + tid; j < min(u.row0 + cap, u.n_rows); j += threads)
+            for (int s = 0; s < a.shared_slots; s++)
+                a.part_ml[(int64_t)s * a.all_rows + ((int64_t)u.b * a.hkv + u.kvh) * a.rows + j] = make_float2(-INFINITY, 0.0f);
 }
 __device__ __forceinline__ uint32_t pack_bf16(float x, float y)
 {
@@ -454,6 +489,7 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
         if constexpr (SPARSE) {
             int skip = 0;
             do {
+                list.ask(a, u, tid * list.EACH);
                 list.build(a, u, cap, tid, reinterpret_cast<unsigned char *>(parents + DREAM_MAX_TREE), skip);
                 for (int x0 = 0; x0 < list.n << a.lg_page; x0 += 64) {
                     const int e = min((x0 + lane) >> a.lg_page, list.n - 1);
@@ -500,8 +536,11 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PLAIN, PagedAttnArgs a)
     if (!UNIT_AT(SINGLE_ROWS))
         return;
     const int prefix = u.shared ? 0 : uniform_load(prefix_len + u.b);
-    if (unit_of(a, SINGLE_ROWS, threadIdx.x & 63, rg, prefix, u))
-        attend_rows_singly<float, D, 256, SPARSE>(a, u, SINGLE_ROWS, SINGLE_RUN, SINGLE_RUN, smem);
+    if (!unit_of(a, SINGLE_ROWS, threadIdx.x & 63, rg, prefix, u))
+        return;
+    if (u.alone)
+        no_shared_parts(a, u, SINGLE_ROWS, threadIdx.x, 256);
+    attend_rows_singly<float, D, 256, SPARSE>(a, u, SINGLE_ROWS, SINGLE_RUN, SINGLE_RUN, smem);
 }
 
 // ---- bf16 ------------------------------------------------------------------------------------------------------------
@@ -877,6 +916,9 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
         for (int h = 0; h < 2; h++)
             page[h] = table[(int64_t)u.b * max_pages + min(((first + lane * stride) * 2 + h) >> (lg_page - 4), max_pages - 1)];
     };
+    PageList<G::THREADS> list;
+    if constexpr (SPARSE)
+        list.ask(a, u, tid * list.EACH);
     if (early)
         ask_pages(mine);
     int parent = -1;
@@ -884,7 +926,8 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
         parent = a.parent[(int64_t)u.b * a.n_tree + min(lane, a.n_tree - 1)];
     if (!unit_of(a, G::CAP, lane, rg, prefix, u))
         return;
-    PageList<G::THREADS> list;
+    if (u.alone)
+        no_shared_parts(a, u, G::CAP, tid, G::THREADS);
     if constexpr (SPARSE)
         list.build(a, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (a.words > 1 ? G::CAP * a.words + DREAM_MAX_TREE / 2 : 0)), 0);
     QueryRows<D, QT, 2, SPARSE> rows;
@@ -1087,6 +1130,9 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
     const int lg_page = lg_and_early & 255;
     int page = 0;
     auto ask_pages = [&](int first) { page = table[(int64_t)u.b * max_pages + min(((first + lane * u.splits) * KEYS + own_chunk) >> lg_page, max_pages - 1)]; };      // of tiles first + lane * splits
+    PageList<G::THREADS> list;
+    if constexpr (SPARSE)
+        list.ask(a, u, tid * list.EACH);
     if (early)
         ask_pages(u.split);
     int parent = -1;
@@ -1094,7 +1140,8 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
         parent = a.parent[(int64_t)u.b * a.n_tree + min(lane, a.n_tree - 1)];
     if (!unit_of(a, G::CAP, lane, rg, prefix, u))
         return;
-    PageList<G::THREADS> list;
+    if (u.alone)
+        no_shared_parts(a, u, G::CAP, tid, G::THREADS);
     if constexpr (SPARSE)
         list.build(a, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (a.words > 1 ? G::CAP * a.words + DREAM_MAX_TREE / 2 : 0)), 0);
     QueryRows<D, QT, NC, SPARSE> rows;
@@ -1294,56 +1341,53 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
     }
 }
 
-// ---- the parts of a row, in their order: D / 4 lanes a row -----------------------------------------------------------
-__device__ __forceinline__ bool in_a_group(const PagedAttnArgs &a, int b)
-{
-    int lo = 0, hi = a.n_groups;      // group_start ascends: the last group that starts at b or in front
-    while (lo < hi) {
-        const int g = (lo + hi) / 2;
-        if (a.group_start[g] <= b)
-            lo = g + 1;
-        else
-            hi = g;
-    }
-    return lo > 0 && b < a.group_start[lo];
-}
-template <class T, int D>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a)
+// ---- the parts of a row, in their order: D / 4 lanes a row, AT parts at a time ------------------------------------------
+template <class T, int D, int AT>
+__global__ __launch_bounds__(256) void paged_join_kernel(const float *part_o, const float2 *part_ml, void *out, float *lse, uint32_t all_rows, int n_slots, uint32_t rows, uint32_t rows_magic, uint32_t hkv,
+                                                         uint32_t hkv_magic, uint32_t group, uint32_t group_magic, int hq, int n_tree)
 {
     constexpr int LANES = D / 4;
-    const int64_t id = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const uint32_t id = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
     const int ch = threadIdx.x % LANES;
-    if (id >= a.all_rows)
+    if (id >= all_rows)
         return;
-    const uint32_t head = (uint32_t)(id / a.rows);
-    Row w;
-    w.r = (int)(id - (int64_t)head * a.rows);
-    w.b = head / (uint32_t)a.hkv;
-    w.node = (uint32_t)w.r / (uint32_t)a.group;
-    w.head = (head - w.b * a.hkv) * a.group + w.r - w.node * a.group;
-    // (a sequence outside every group has no shared parts)
-    const int first_slot = a.shared_slots && !in_a_group(a, w.b) ? a.shared_slots : 0;
-    float most = -INFINITY, sum = 0.0f;
-    for (int s = first_slot; s < a.n_slots; s++)
-        most = fmaxf(most, a.part_ml[s * a.all_rows + id].x);
+    float most = -FLT_MAX, sum = 0.0f;
     f32x4 all = {0.f, 0.f, 0.f, 0.f};
-    for (int s = first_slot; s < a.n_slots; s++) {
-        const float2 ml = a.part_ml[s * a.all_rows + id];
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(a.part_o + (s * a.all_rows + id) * D + ch * 4);
-        if (ml.y != 0.0f) {               // (NaN: not 0)
-            const float f = __builtin_amdgcn_exp2f(fmaxf(ml.x, -FLT_MAX) - fmaxf(most, -FLT_MAX));
-            sum = __builtin_fmaf(ml.y, f, sum);
-            all += x * f;
+    for (int s0 = 0; s0 < n_slots; s0 += AT) {
+        float2 ml[AT];
+        f32x4 x[AT];
+#pragma unroll
+        for (int i = 0; i < AT; i++) {
+            const int64_t row = (int64_t)min(s0 + i, n_slots - 1) * all_rows + id;
+            ml[i] = part_ml[row];
+            x[i] = *reinterpret_cast<const f32x4 *>(part_o + row * D + ch * 4);
         }
+        float top = most;
+#pragma unroll
+        for (int i = 0; i < AT; i++)
+            top = fmaxf(top, ml[i].x);
+        const float raised = __builtin_amdgcn_exp2f(most - top);
+        sum *= raised;
+        all *= raised;
+        most = top;
+#pragma unroll
+        for (int i = 0; i < AT; i++)
+            if (s0 + i < n_slots && ml[i].y != 0.0f) {      // (NaN: not 0.  A part without keys holds anything)
+                const float f = __builtin_amdgcn_exp2f(fmaxf(ml[i].x, -FLT_MAX) - most);
+                sum = __builtin_fmaf(ml[i].y, f, sum);
+                all += x[i] * f;
+            }
     }
+    const uint32_t head = divide(id, rows, rows_magic), b = divide(head, hkv, hkv_magic), r = id - head * rows, node = divide(r, group, group_magic);
+    const int q_head = (int)((head - b * hkv) * group + r - node * group);
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    if (ch == 0 && a.lse)
-        a.lse[((int64_t)w.b * a.hq + w.head) * a.n_tree + w.node] = sum == 0.0f ? -INFINITY : (most + __log2f(sum)) * 0.6931471805599453f;
-    const int64_t at = row_of_q(a, w) * D + ch * 4;
+    if (ch == 0 && lse)
+        lse[((int64_t)b * hq + q_head) * n_tree + node] = sum == 0.0f ? -INFINITY : (most + __log2f(sum)) * 0.6931471805599453f;
+    const int64_t at = (((int64_t)b * n_tree + node) * hq + q_head) * D + ch * 4;
     if constexpr (std::is_same_v<T, float>)
-        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at) = all * inv;
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(out) + at) = all * inv;
     else
-        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) = make_uint2(pack_bf16(all[0] * inv, all[1] * inv), pack_bf16(all[2] * inv, all[3] * inv));
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(out) + at) = make_uint2(pack_bf16(all[0] * inv, all[1] * inv), pack_bf16(all[2] * inv, all[3] * inv));
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1395,42 +1439,75 @@ struct Problem {
     int64_t heads, rows, keys, groups;
     float bytes;
     int nodes_of, all_keys;               // query rows a node (selected pages: a workgroup with more nodes sees more pages)
-    bool joined;                          // anyway
 };
 int64_t row_groups_of(const Problem &p, const Shape &s) { return p.groups ? p.rows / s.cap() + p.groups : (p.rows + s.cap() - 1) / s.cap(); }
 
-void choose(int D, bool f32, const Problem &p, Segment &out)
+// A part in workgroups of one shape: workgroups of a split, steps of a unit, what a step cannot be shorter than
+struct Load {
+    float units, steps, step, joined;     // joined: us that its splits' join takes for each
+    int64_t most_splits;
+};
+Load load_of(int D, const Problem &p, const Kind &k)
+{
+    const Shape &s = k.shape;
+    const int64_t groups = row_groups_of(p, s), units = p.heads * (p.groups ? p.rows / s.cap() + 1 : groups);
+    float keys = (float)p.keys;
+    if (p.nodes_of) {                     // nodes that ask alike see more pages together: measured about the 0.4th power of their number
+        const float nodes = (float)(p.rows < s.cap() ? p.rows : s.cap()) / (float)p.nodes_of;
+        keys *= nodes > 1.0f ? powf(nodes, 0.4f) : 1.0f;
+        keys = keys < (float)p.all_keys ? keys : (float)p.all_keys;
+    }
+    const int64_t steps = (int64_t)(keys / (float)s.keys(D)) + 1;
+    const float fill = (float)(s.keys(D) * D) * 4e-3f / (FILL * (groups > 1 ? 2.0f : 1.0f));
+    return {(float)units, (float)steps, k.latency > fill ? k.latency : fill, JOIN_SPLIT + JOIN_BYTE * (float)p.heads * (float)p.rows * (float)D, steps};
+}
+float sixth_roots_power(float us, float memory)
+{
+    us *= us * us;
+    memory *= memory * memory;
+    return us * us + memory * memory;
+}
+// What a launch takes with so many splits of a part, and of a second one beside it, to the sixth power; `joined`: the part's rows have others, in a launch of their own
+float launch_time(const Kind &k, const Load &x, int splits, bool joined, const Load *y, int y_splits, float memory)
+{
+    const float x_steps = (float)(((int)x.steps + splits - 1) / splits), y_steps = y ? (float)(((int)y->steps + y_splits - 1) / y_splits) : 0.0f;
+    const float units = x.units * splits + (y ? y->units * y_splits : 0.0f), per_cu = (float)(((int64_t)units + 255) / 256);
+    // (one part: a CU's busiest workgroups are as long as any other)
+    const float work = y ? k.issue * (x.units * splits * x_steps + y->units * y_splits * y_steps) / 256.0f : k.issue * per_cu * x_steps;
+    const float chain = y && y_steps * y->step > x_steps * x.step ? y_steps * y->step : x_steps * x.step;
+    float us = k.base + k.per_group * (per_cu - 1.0f) + (chain > work ? chain : work);
+    us += y ? x.joined * splits + y->joined * y_splits : joined ? x.joined * splits : splits > 1 ? JOIN + x.joined * splits : 0.0f;
+    return sixth_roots_power(us, memory);
+}
+
+// The best of the shapes and splits for a part, or for two parts in one launch, by launch_time
+float choose(int D, bool f32, const Problem &p, bool joined, Segment &out, const Problem *p2 = nullptr, Segment *out2 = nullptr)
 {
     const int tiles = q_tiles_override(), waves = tile_waves_override(), forced = kv_splits_override();
+    const float memory = (p.bytes + (p2 ? p2->bytes : 0.0f)) / MEMORY + 5.0f;
     float best = INFINITY;
     auto consider = [&](const Kind &k) {
-        const Shape &s = k.shape;
-        const int64_t groups = row_groups_of(p, s), units = p.heads * (p.groups ? p.rows / s.cap() + 1 : groups);
-        float keys = (float)p.keys;
-        if (p.nodes_of) {                 // nodes that ask alike see more pages together: measured about the 0.4th power of their number
-            const float nodes = (float)(p.rows < s.cap() ? p.rows : s.cap()) / (float)p.nodes_of;
-            keys *= nodes > 1.0f ? powf(nodes, 0.4f) : 1.0f;
-            keys = keys < (float)p.all_keys ? keys : (float)p.all_keys;
-        }
-        const int64_t steps = (int64_t)(keys / (float)s.keys(D)) + 1;
-        const float fill = (float)(s.keys(D) * D) * 4e-3f / (FILL * (groups > 1 ? 2.0f : 1.0f)), memory = p.bytes / MEMORY + 5.0f;
-        for (int n : SPLITS) {
-            if (forced ? n > 1 : n > 1 && n > steps)
+        const Load x = load_of(D, p, k), y = p2 ? load_of(D, *p2, k) : Load{};
+        for (int m : SPLITS) {
+            if (p2 && !forced && (m > 4 || (m > 1 && m > y.most_splits)))
                 break;
-            const int splits = forced ? (forced < 64 ? forced : 64) : n;
-            const float per_cu = (float)((units * splits + 255) / 256);
-            float step = k.issue * per_cu > k.latency ? k.issue * per_cu : k.latency;
-            step = step > fill ? step : fill;
-            float us = k.base + k.per_group * (per_cu - 1.0f) + (float)((steps + splits - 1) / splits) * step;
-            if (splits > 1 || p.joined)
-                us += (p.joined ? 0.0f : JOIN) + JOIN_SPLIT * splits + JOIN_BYTE * (float)p.heads * (float)p.rows * (float)(splits * D);
-            us *= us * us;
-            us = us * us + memory * memory * memory * memory * memory * memory;
-            if (us < best) {
-                best = us;
-                out.shape = s;
-                out.part.splits = splits;
+            for (int n : SPLITS) {
+                if (forced ? n > 1 : n > 1 && n > x.most_splits)
+                    break;
+                const int splits = forced ? (forced < 64 ? forced : 64) : n;
+                const float us = launch_time(k, x, splits, joined, p2 ? &y : nullptr, forced ? splits : m, memory);
+                if (us < best) {
+                    best = us;
+                    out.shape = k.shape;
+                    out.part.splits = splits;
+                    if (p2) {
+                        out2->shape = k.shape;
+                        out2->part.splits = forced ? splits : m;
+                    }
+                }
             }
+            if (!p2 || forced)
+                break;
         }
     };
     if (f32) {
@@ -1446,6 +1523,9 @@ void choose(int D, bool f32, const Problem &p, Segment &out)
             consider(KIND[kinds_of(D)][0]);
     }
     out.part.row_groups = (int)row_groups_of(p, out.shape);
+    if (p2)
+        out2->part.row_groups = (int)row_groups_of(*p2, out2->shape);
+    return powf(best, 1.0f / 6.0f);
 }
 
 // Pages that a workgroup's rows may see, those of the tree included: what its lists, of all splits together, have to hold
@@ -1474,16 +1554,24 @@ PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32
         s.part.slot = p.n_slots;
         p.n_slots += s.part.splits;
     };
-    if (n_groups) {
-        choose(D, f32, {d->n_kv_heads, d->batch * rows, max_shared, n_groups, (float)n_groups * (float)d->n_kv_heads * (float)max_shared * (float)row_bytes, 0, 0, true}, p.shared);
-        finish(p.shared, d->n_kv_heads, 1);
-        p.shared_slots = p.n_slots;
-    }
     int64_t own_keys = n_groups ? max_kv - max_shared + 1 : max_kv;
     const bool some = sparse && seen_pages > 0 && seen_pages * pages->page_size + n_tree < own_keys;
     const int64_t all_keys = own_keys, listed = listed_pages(pages, n_tree, max_kv, seen_pages);
     own_keys = some ? seen_pages * pages->page_size + n_tree : own_keys;
-    choose(D, f32, {heads, rows, own_keys, 0, (float)heads * (float)own_keys * (float)row_bytes, some ? (int)group : 0, (int)all_keys, n_groups != 0}, p.own);
+    const Problem own = {heads, rows, own_keys, 0, (float)heads * (float)own_keys * (float)row_bytes, some ? (int)group : 0, (int)all_keys};
+    if (n_groups) {
+        const Problem shared = {d->n_kv_heads, d->batch * rows, max_shared, n_groups, (float)n_groups * (float)d->n_kv_heads * (float)max_shared * (float)row_bytes, 0, 0};
+        Segment together, beside;
+        const float one = choose(D, f32, shared, true, together, &own, &beside), two = choose(D, f32, shared, true, p.shared) + choose(D, f32, own, true, p.own);
+        if (one <= two) {
+            p.shared = together;
+            p.own = beside;
+        }
+        finish(p.shared, d->n_kv_heads, 1);
+        p.shared_slots = p.n_slots;
+    } else {
+        choose(D, f32, own, false, p.own);
+    }
     finish(p.own, heads, sparse ? ceil_div(listed, n_tree > 64 ? SPARSE_LIST / 2 : SPARSE_LIST) : 1);
     p.list_size = sparse ? ceil_div(listed, p.own.part.splits) : 0;
     p.all_rows = heads * rows;
@@ -1571,11 +1659,14 @@ int launch_all(PagedAttnArgs &a, const PagedPlan &p, bool f32, hipStream_t st)
         return rc;
     if (p.n_slots == 1)
         return DREAM_OK;
-    const int blocks = ceil_div(p.all_rows, 256 / (D / 4));
+    auto join = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(ceil_div(p.all_rows, 256 / (D / 4))), dim3(256), 0, st, a.part_o, a.part_ml, a.out, a.lse, (uint32_t)p.all_rows, p.n_slots, a.rows, a.rows_magic, a.hkv,
+                           a.hkv_magic, a.group, a.group_magic, a.hq, a.n_tree);
+    };
     if (f32)
-        hipLaunchKernelGGL((paged_join_kernel<float, D>), dim3(blocks), dim3(256), 0, st, a);
+        join(p.n_slots <= 2 ? &paged_join_kernel<float, D, 2> : p.n_slots <= 4 ? &paged_join_kernel<float, D, 4> : &paged_join_kernel<float, D, 8>);
     else
-        hipLaunchKernelGGL((paged_join_kernel<uint16_t, D>), dim3(blocks), dim3(256), 0, st, a);
+        join(p.n_slots <= 2 ? &paged_join_kernel<uint16_t, D, 2> : p.n_slots <= 4 ? &paged_join_kernel<uint16_t, D, 4> : &paged_join_kernel<uint16_t, D, 8>);
     return check_launch("paged_join_kernel");
 }
 template <int D, bool SPARSE>
