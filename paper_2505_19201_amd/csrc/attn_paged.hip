@@ -48,6 +48,17 @@ struct PagedAttnArgs {
 #define PLAIN const int32_t *table, const int32_t *prefix_len, int32_t max_pages, int32_t hkv, uint32_t hkv_magic, int32_t shared_blocks, int32_t row_groups, uint32_t row_groups_magic, int32_t splits, \
               uint32_t splits_magic, int32_t streams, int32_t lg_and_early
 
+constexpr int PLAIN_BYTES = 2 * 8 + 10 * 4;      // of them, the structure lies behind
+static_assert(PLAIN_BYTES % alignof(PagedAttnArgs) == 0);
+// The structure once more, for what is at a kernel's end: what is used there alone is loaded there, instead of being held (and, where pages are listed, spilled) from the start on
+__device__ __forceinline__ const PagedAttnArgs &args_again()
+{
+    typedef const __attribute__((address_space(4))) char *Arguments;
+    Arguments p = (Arguments)__builtin_amdgcn_kernarg_segment_ptr() + PLAIN_BYTES;
+    asm volatile("" : "+s"(p));
+    return *(const PagedAttnArgs *)p;
+}
+
 // x / d by a multiplication, magic = (2^32 - 1) / d
 __device__ __forceinline__ uint32_t divide(uint32_t x, uint32_t d, uint32_t magic)
 {
@@ -139,7 +150,7 @@ __device__ __forceinline__ bool unit_at(const PagedAttnArgs &a, int hkv, uint32_
     u.alone = false;
     return stream < streams;
 }
-#define UNIT_AT(cap) unit_at(a, hkv, hkv_magic, shared_blocks, row_groups, row_groups_magic, splits, splits_magic, streams, cap, u, rg)
+#define UNIT_AT(args, cap) unit_at(args, hkv, hkv_magic, shared_blocks, row_groups, row_groups_magic, splits, splits_magic, streams, cap, u, rg)
 // And what does: the prefix length (asked for by the caller), the groups
 __device__ __forceinline__ bool unit_of(const PagedAttnArgs &a, int cap, int lane, int rg, int prefix, Unit &u)
 {
@@ -533,7 +544,7 @@ __global__ __launch_bounds__(256) void paged_f32_kernel(PLAIN, PagedAttnArgs a)
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     Unit u;
     int rg;
-    if (!UNIT_AT(SINGLE_ROWS))
+    if (!UNIT_AT(a, SINGLE_ROWS))
         return;
     const int prefix = u.shared ? 0 : uniform_load(prefix_len + u.b);
     if (!unit_of(a, SINGLE_ROWS, threadIdx.x & 63, rg, prefix, u))
@@ -889,7 +900,7 @@ struct KeysGeom {
 // Few rows: the waves take the key tiles in turn, each for all of the rows, and never meet until the end.  A wave asks for its next keys as soon as a tile's scores are there, and for its next
 // values as soon as they are added up.
 template <int D, int QT, int NW, bool SPARSE>
-__global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArgs a)
+__global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArgs first)
 {
     using G = KeysGeom<D, QT, NW>;
     constexpr int ROW = G::ROW, LPR = ROW / 16, RPI = 1024 / ROW, HALF = G::LOADS / 2;
@@ -899,11 +910,11 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
     float2 *s_ml = reinterpret_cast<float2 *>(smem + G::MAIN);
     int32_t *flags = reinterpret_cast<int32_t *>(s_ml + NW * G::CAP);
     uint64_t *masks = reinterpret_cast<uint64_t *>(flags + 2 * NW);
-    int32_t *parents = reinterpret_cast<int32_t *>(masks + G::CAP * a.words);
+    int32_t *parents = reinterpret_cast<int32_t *>(masks + G::CAP * first.words);
 
     Unit u;
     int rg;
-    if (!UNIT_AT(G::CAP))
+    if (!UNIT_AT(first, G::CAP))
         return;
     // what needs no load is asked for first: of an own part the pages of the wave's tiles, the prefix length, the tree, the queries
     const int prefix = u.shared ? 0 : uniform_load(prefix_len + u.b);
@@ -918,18 +929,19 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
     };
     PageList<G::THREADS> list;
     if constexpr (SPARSE)
-        list.ask(a, u, tid * list.EACH);
+        list.ask(first, u, tid * list.EACH);
     if (early)
         ask_pages(mine);
     int parent = -1;
-    if (!u.shared && a.words == 1 && !a.tree_mask)
-        parent = a.parent[(int64_t)u.b * a.n_tree + min(lane, a.n_tree - 1)];
-    if (!unit_of(a, G::CAP, lane, rg, prefix, u))
+    if (!u.shared && first.words == 1 && !first.tree_mask)
+        parent = first.parent[(int64_t)u.b * first.n_tree + min(lane, first.n_tree - 1)];
+    if (!unit_of(first, G::CAP, lane, rg, prefix, u))
         return;
     if (u.alone)
-        no_shared_parts(a, u, G::CAP, tid, G::THREADS);
+        no_shared_parts(first, u, G::CAP, tid, G::THREADS);
     if constexpr (SPARSE)
-        list.build(a, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (a.words > 1 ? G::CAP * a.words + DREAM_MAX_TREE / 2 : 0)), 0);
+        list.build(first, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (first.words > 1 ? G::CAP * first.words + DREAM_MAX_TREE / 2 : 0)), 0);
+    const PagedAttnArgs &a = SPARSE ? args_again() : first;
     QueryRows<D, QT, 2, SPARSE> rows;
     rows.load(a, u, u.row0, c, g);
     const int tile0 = u.lo / 32;
@@ -1060,19 +1072,20 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
         for (int dt = 0; dt < D / 16; dt++)
             *reinterpret_cast<f32x4 *>(smem + stage + (qt * 16 + c) * (4 * D) + ((dt * 4 + g) ^ c) * 16) = rows.o[qt][dt];
     __syncthreads();
+    const PagedAttnArgs &z = args_again();
     int again = 0;
 #pragma unroll
     for (int w = 0; w < NW; w++)
         again |= flags[w];
     if (again) {
         __syncthreads();
-        attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(a, u, G::CAP, 32, 32 * NW, smem);
+        attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(z, u, G::CAP, 32, 32 * NW, smem);
         return;
     }
     const int count = min(G::CAP, u.n_rows - u.row0);
     for (int i = tid; i < count * (D / 4); i += G::THREADS) {
         const int j = i / (D / 4), ch = i % (D / 4);
-        const Row w = row_at(a, u, u.row0 + j);
+        const Row w = row_at(z, u, u.row0 + j);
         float2 ml[NW];
         float most = -INFINITY, sum = 0.0f;
         f32x4 all = {0.f, 0.f, 0.f, 0.f};
@@ -1088,12 +1101,12 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
             all += *reinterpret_cast<const f32x4 *>(smem + x * 2 * G::TILE + j * (4 * D) + (ch ^ (j & 15)) * 16) * f;
         }
         if (ch == 0)
-            put_ml(a, u, w, most, sum);
-        if (a.n_slots > 1) {
-            *reinterpret_cast<f32x4 *>(a.part_o + row_of_part(a, u, w) * D + ch * 4) = all;
+            put_ml(z, u, w, most, sum);
+        if (z.n_slots > 1) {
+            *reinterpret_cast<f32x4 *>(z.part_o + row_of_part(z, u, w) * D + ch * 4) = all;
         } else {
             const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + row_of_q(a, w) * D + ch * 4) = make_uint2(pack_bf16(all[0] * inv, all[1] * inv), pack_bf16(all[2] * inv, all[3] * inv));
+            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(z.out) + row_of_q(z, w) * D + ch * 4) = make_uint2(pack_bf16(all[0] * inv, all[1] * inv), pack_bf16(all[2] * inv, all[3] * inv));
         }
     }
 }
@@ -1109,7 +1122,7 @@ struct RowsGeom {
 
 // Many rows: the waves share the tiles and have rows of their own; one barrier a tile, NS - 1 tiles on their way.
 template <int D, int QT, int WR, int NS, bool SPARSE>
-__global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttnArgs a)
+__global__ __launch_bounds__(64 * WR, D == 64 && QT == 1 && !SPARSE ? 4 : 2) void paged_rows_kernel(PLAIN, PagedAttnArgs first)
 {
     using G = RowsGeom<D, QT, WR, NS>;
     constexpr int ROW = G::ROW, KEYS = G::KEYS, NC = KEYS / 16, LPR = ROW / 16, RPI = 1024 / ROW;
@@ -1118,11 +1131,11 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
     int32_t *flags = reinterpret_cast<int32_t *>(smem + G::MAIN);
     uint64_t *masks = reinterpret_cast<uint64_t *>(flags + 2 * WR);
-    int32_t *parents = reinterpret_cast<int32_t *>(masks + G::CAP * a.words);
+    int32_t *parents = reinterpret_cast<int32_t *>(masks + G::CAP * first.words);
 
     Unit u;
     int rg;
-    if (!UNIT_AT(G::CAP))
+    if (!UNIT_AT(first, G::CAP))
         return;
     const int prefix = u.shared ? 0 : uniform_load(prefix_len + u.b);
     const int own_rows = wave * (KEYS / WR), own_chunk = own_rows & ~15;      // of a tile: the rows that this wave asks for, and the chunk that they lie in
@@ -1132,18 +1145,19 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
     auto ask_pages = [&](int first) { page = table[(int64_t)u.b * max_pages + min(((first + lane * u.splits) * KEYS + own_chunk) >> lg_page, max_pages - 1)]; };      // of tiles first + lane * splits
     PageList<G::THREADS> list;
     if constexpr (SPARSE)
-        list.ask(a, u, tid * list.EACH);
+        list.ask(first, u, tid * list.EACH);
     if (early)
         ask_pages(u.split);
     int parent = -1;
-    if (!u.shared && a.words == 1 && !a.tree_mask)
-        parent = a.parent[(int64_t)u.b * a.n_tree + min(lane, a.n_tree - 1)];
-    if (!unit_of(a, G::CAP, lane, rg, prefix, u))
+    if (!u.shared && first.words == 1 && !first.tree_mask)
+        parent = first.parent[(int64_t)u.b * first.n_tree + min(lane, first.n_tree - 1)];
+    if (!unit_of(first, G::CAP, lane, rg, prefix, u))
         return;
     if (u.alone)
-        no_shared_parts(a, u, G::CAP, tid, G::THREADS);
+        no_shared_parts(first, u, G::CAP, tid, G::THREADS);
     if constexpr (SPARSE)
-        list.build(a, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (a.words > 1 ? G::CAP * a.words + DREAM_MAX_TREE / 2 : 0)), 0);
+        list.build(first, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (first.words > 1 ? G::CAP * first.words + DREAM_MAX_TREE / 2 : 0)), 0);
+    const PagedAttnArgs &a = SPARSE ? args_again() : first;
     QueryRows<D, QT, NC, SPARSE> rows;
     const int first_row = u.row0 + wave * QT * 16;
     rows.load(a, u, first_row, c, g);
@@ -1309,12 +1323,14 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
     if (lane == 0)
         flags[wave] = strange;
     __syncthreads();
+    const PagedAttnArgs &z = args_again();
     int again = 0;
 #pragma unroll
     for (int w = 0; w < WR; w++)
         again |= flags[w];
     if (again) {
-        attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(a, u, G::CAP, KEYS, KEYS, smem);
+        __syncthreads();
+        attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(z, u, G::CAP, KEYS, KEYS, smem);
         return;
     }
 #pragma unroll
@@ -1322,17 +1338,17 @@ __global__ __launch_bounds__(64 * WR, 2) void paged_rows_kernel(PLAIN, PagedAttn
         const int j = first_row + qt * 16 + c;
         if (j >= u.n_rows)
             continue;
-        const Row w = row_at(a, u, j);
+        const Row w = row_at(z, u, j);
         if (g == 0)
-            put_ml(a, u, w, rows.m[qt], rows.l[qt]);
-        if (a.n_slots > 1) {
-            float *row = a.part_o + row_of_part(a, u, w) * D + 4 * g;
+            put_ml(z, u, w, rows.m[qt], rows.l[qt]);
+        if (z.n_slots > 1) {
+            float *row = z.part_o + row_of_part(z, u, w) * D + 4 * g;
 #pragma unroll
             for (int dt = 0; dt < D / 16; dt++)
                 *reinterpret_cast<f32x4 *>(row + dt * 16) = rows.o[qt][dt];
         } else {
             const float inv = rows.l[qt] == 0.0f ? 0.0f : 1.0f / rows.l[qt];
-            uint16_t *row = static_cast<uint16_t *>(a.out) + row_of_q(a, w) * D + 4 * g;
+            uint16_t *row = static_cast<uint16_t *>(z.out) + row_of_q(z, w) * D + 4 * g;
 #pragma unroll
             for (int dt = 0; dt < D / 16; dt++)
                 *reinterpret_cast<uint2 *>(row + dt * 16) =
@@ -1415,21 +1431,21 @@ struct PagedPlan {
 // The shapes there are, and what they are estimated to take: where a CU has `groups` workgroups,
 //     us = base + per_group * (groups - 1) + steps * max(latency, issue * groups, kilobytes of a step / (FILL * min(row groups, 2)))  [+ the join]
 // as long as memory does not take longer (the sixth root of both sixth powers).  FILL: what a CU pulls that nobody asks for beside it.  The constants are those with which the choice is best over
-// measured times of every shape with every number of splits below (7 head layouts x batches of 1, 4, 16, 48 x trees of 1 to 120 nodes x 100 to 12000 keys, 558 problems, 9785 times): 1.3 % behind the
-// fastest in the geometric mean, 7.5 % at the 95th percentile, 36 % at most, on the data that they were fitted to.  What a shape is worth over these problems (mean and most that the fastest would take
-// longer without it): 16 rows 4.5 % and 29 %, 32 rows 0.9 % and 21 %, 64 rows 2.7 % and 49 %, 128 rows 0.9 % and 25 %, 128 rows of 256 on eight waves 0.2 % and 9 %; eight waves at
+// measured times of every shape with every number of splits below (7 head layouts x batches of 1, 4, 16, 48 x trees of 1 to 120 nodes x 100 to 12000 keys, 558 problems, 9785 times): 1.5 % behind the
+// fastest in the geometric mean, 8 % at the 95th percentile, 39 % at most, on the data that they were fitted to.  What a shape is worth over these problems (mean and most that the fastest would take
+// longer without it): 16 rows 3.1 % and 24 %, 32 rows 0.5 % and 17 %, 64 rows 2.9 % and 54 %, 128 rows 0.9 % and 25 %, 128 rows of 256 on eight waves 0.1 % and 5 %; eight waves at
 // smaller head_dim (0.2 %) and four query tiles a wave are left out.
 struct Kind {
     Shape shape;
     float base, per_group, latency, issue;
 };
 constexpr int KINDS = 4;
-constexpr Kind KIND[3][KINDS] = {{{{KEYS, 1, 8}, 5.41f, 1.71f, 0.855f, 0.801f}, {{KEYS, 2, 8}, 6.98f, 5.29f, 1.041f, 1.071f}, {{ROWS, 1, 4}, 5.96f, 1.46f, 0.716f, 0.399f}, {{ROWS, 2, 4}, 7.53f, 2.51f, 0.960f, 0.683f}},
-                                 {{{KEYS, 1, 8}, 6.11f, 5.32f, 1.248f, 1.567f}, {{KEYS, 2, 8}, 8.48f, 7.57f, 1.825f, 1.824f}, {{ROWS, 1, 4}, 6.64f, 3.03f, 1.009f, 0.675f}, {{ROWS, 2, 4}, 8.83f, 3.31f, 1.327f, 1.040f}},
-                                 {{{KEYS, 1, 4}, 8.08f, 7.06f, 1.836f, 1.857f}, {{KEYS, 1, 4}, 8.08f, 7.06f, 1.836f, 1.857f}, {{ROWS, 1, 4}, 7.22f, 3.53f, 0.941f, 0.655f}, {{ROWS, 1, 8}, 9.38f, 7.87f, 1.116f, 1.158f}}};
+constexpr Kind KIND[3][KINDS] = {{{{KEYS, 1, 8}, 5.63f, 1.64f, 0.834f, 0.770f}, {{KEYS, 2, 8}, 7.12f, 5.07f, 1.049f, 1.075f}, {{ROWS, 1, 4}, 5.79f, 1.48f, 0.772f, 0.359f}, {{ROWS, 2, 4}, 7.58f, 2.26f, 0.954f, 0.670f}},
+                                 {{{KEYS, 1, 8}, 6.22f, 5.03f, 1.312f, 1.563f}, {{KEYS, 2, 8}, 8.59f, 7.55f, 1.522f, 1.801f}, {{ROWS, 1, 4}, 6.64f, 2.69f, 0.996f, 0.657f}, {{ROWS, 2, 4}, 8.76f, 2.77f, 1.322f, 1.017f}},
+                                 {{{KEYS, 1, 4}, 8.17f, 7.01f, 1.692f, 1.832f}, {{KEYS, 1, 4}, 8.17f, 7.01f, 1.692f, 1.832f}, {{ROWS, 1, 4}, 7.43f, 3.07f, 0.934f, 0.622f}, {{ROWS, 1, 8}, 9.52f, 6.35f, 1.137f, 1.137f}}};
 constexpr int kinds_of(int D) { return D == 64 ? 0 : D == 128 ? 1 : 2; }
-constexpr float FILL = 76.6f, MEMORY = 4.78e6f, JOIN = 2.23f, JOIN_SPLIT = 0.72f, JOIN_BYTE = 1.14e-6f;      // KB / us; bytes / us; us, us a split, us a value
-constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48};
+constexpr float FILL = 87.2f, MEMORY = 4.90e6f, JOIN = 2.18f, JOIN_SPLIT = 0.106f, JOIN_BYTE = 1.27e-6f;      // KB / us; bytes / us; us, us a split, us a value
+constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48}, MOST_SPLITS = 128;      // of a part; of both, where they are forced
 
 uint32_t magic_for(uint32_t d) { return 0xffffffffu / d; }
 
@@ -1480,8 +1496,8 @@ float launch_time(const Kind &k, const Load &x, int splits, bool joined, const L
     return sixth_roots_power(us, memory);
 }
 
-// The best of the shapes and splits for a part, or for two parts in one launch, by launch_time
-float choose(int D, bool f32, const Problem &p, bool joined, Segment &out, const Problem *p2 = nullptr, Segment *out2 = nullptr)
+// The best of the shapes and splits, `most` at most, for a part, or for two parts in one launch, by launch_time
+float choose(int D, bool f32, const Problem &p, bool joined, int most, Segment &out, const Problem *p2 = nullptr, Segment *out2 = nullptr)
 {
     const int tiles = q_tiles_override(), waves = tile_waves_override(), forced = kv_splits_override();
     const float memory = (p.bytes + (p2 ? p2->bytes : 0.0f)) / MEMORY + 5.0f;
@@ -1489,12 +1505,13 @@ float choose(int D, bool f32, const Problem &p, bool joined, Segment &out, const
     auto consider = [&](const Kind &k) {
         const Load x = load_of(D, p, k), y = p2 ? load_of(D, *p2, k) : Load{};
         for (int m : SPLITS) {
-            if (p2 && !forced && (m > 4 || (m > 1 && m > y.most_splits)))
+            if (p2 && !forced && (m > 4 || (m > 1 && (m > y.most_splits || m >= most))))
                 break;
+            const int room = !p2 ? most : forced ? most / 2 : most - m;      // (1 at least)
             for (int n : SPLITS) {
-                if (forced ? n > 1 : n > 1 && n > x.most_splits)
+                if (n > 1 && (forced || n > x.most_splits || n > room))
                     break;
-                const int splits = forced ? (forced < 64 ? forced : 64) : n;
+                const int splits = !forced ? n : forced < room ? forced : room;
                 const float us = launch_time(k, x, splits, joined, p2 ? &y : nullptr, forced ? splits : m, memory);
                 if (us < best) {
                     best = us;
@@ -1537,7 +1554,8 @@ int64_t listed_pages(const dream_page_desc *pages, int32_t n_tree, int64_t max_k
     return most + n_tree / pages->page_size + 2;
 }
 
-PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32_t n_tree, int64_t max_kv, int32_t n_groups, int64_t max_shared, bool sparse, int64_t seen_pages)
+// most_slots: parts that there is room for, 2 at least where there are groups
+PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32_t n_tree, int64_t max_kv, int32_t n_groups, int64_t max_shared, bool sparse, int64_t seen_pages, int most_slots = MOST_SPLITS)
 {
     PagedPlan p = {};
     const int D = d->head_dim;
@@ -1562,7 +1580,9 @@ PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32
     if (n_groups) {
         const Problem shared = {d->n_kv_heads, d->batch * rows, max_shared, n_groups, (float)n_groups * (float)d->n_kv_heads * (float)max_shared * (float)row_bytes, 0, 0};
         Segment together, beside;
-        const float one = choose(D, f32, shared, true, together, &own, &beside), two = choose(D, f32, shared, true, p.shared) + choose(D, f32, own, true, p.own);
+        const float one = choose(D, f32, shared, true, most_slots, together, &own, &beside);
+        float two = choose(D, f32, shared, true, most_slots - 1, p.shared);
+        two += choose(D, f32, own, true, most_slots - p.shared.part.splits, p.own);
         if (one <= two) {
             p.shared = together;
             p.own = beside;
@@ -1570,7 +1590,7 @@ PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32
         finish(p.shared, d->n_kv_heads, 1);
         p.shared_slots = p.n_slots;
     } else {
-        choose(D, f32, own, false, p.own);
+        choose(D, f32, own, false, most_slots, p.own);
     }
     finish(p.own, heads, sparse ? ceil_div(listed, n_tree > 64 ? SPARSE_LIST / 2 : SPARSE_LIST) : 1);
     p.list_size = sparse ? ceil_div(listed, p.own.part.splits) : 0;
@@ -1692,14 +1712,24 @@ int check_attn(const char *who, const dream_attn_desc *d, const dream_page_desc 
     return DREAM_OK;
 }
 
-int run(const char *who, const dream_attn_desc *d, const dream_page_desc *pages, PagedAttnArgs &a, const PagedPlan &p, void *ws, size_t ws_bytes, void *stream)
+// Plan: from how many parts there is room for
+template <class Plan>
+int run(const char *who, const dream_attn_desc *d, const dream_page_desc *pages, PagedAttnArgs &a, Plan plan, void *ws, size_t ws_bytes, void *stream)
 {
     if (!a.q || !a.k || !a.v || !a.table || !a.prefix_len || (!a.parent && !a.tree_mask) || !a.out || !ws)
         return fail(DREAM_ERR_INVALID_ARG, "%s: NULL argument", who);
     if ((reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v) | reinterpret_cast<uintptr_t>(a.out) | reinterpret_cast<uintptr_t>(ws)) & 15)
         return fail(DREAM_ERR_INVALID_ARG, "%s: a tensor is not 16-byte aligned", who);
-    if (ws_bytes < p.bytes)
-        return fail(DREAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, p.bytes);
+    PagedPlan p = plan(MOST_SPLITS);
+    if (ws_bytes < p.bytes) {                 // one that another call's size was asked for: fewer parts
+        const size_t needed = p.bytes, room = ws_bytes / (p.bytes / p.n_slots);
+        if (room > 1)
+            p = plan((int)room);
+        else if (!a.n_groups)
+            p = plan(1);
+        if (ws_bytes < p.bytes)
+            return fail(DREAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, needed);
+    }
     a.part_o = static_cast<float *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)p.n_slots * p.all_rows * d->head_dim);
     a.batch = d->batch; a.hq = d->n_q_heads; a.hkv = d->n_kv_heads; a.group = a.hq / a.hkv; a.rows = a.n_tree * a.group; a.words = (a.n_tree + 63) / 64;
@@ -1747,7 +1777,8 @@ int dream_paged_verify_attn(const dream_attn_desc *desc, const dream_page_desc *
     a.q = static_cast<const unsigned char *>(q); a.k = static_cast<const unsigned char *>(k_pages); a.v = static_cast<const unsigned char *>(v_pages);
     a.table = page_table; a.prefix_len = prefix_len; a.n_tree = n_tree; a.parent = parent; a.tree_mask = tree_mask; a.n_groups = n_groups; a.group_start = group_start;
     a.shared_len = shared_len; a.out = out; a.lse = lse;
-    return run(who, desc, pages, a, plan_for(desc, pages, n_tree, max_kv_len, n_groups, max_shared_len, false, 0), workspace, workspace_bytes, stream);
+    auto plan = [&](int slots) { return plan_for(desc, pages, n_tree, max_kv_len, n_groups, max_shared_len, false, 0, slots); };
+    return run(who, desc, pages, a, plan, workspace, workspace_bytes, stream);
 }
 
 size_t dream_sparse_verify_attn_workspace(const dream_attn_desc *desc, const dream_page_desc *pages, int32_t n_tree, int64_t max_kv_len, int32_t max_pages_seen)
@@ -1770,7 +1801,8 @@ int dream_sparse_verify_attn(const dream_attn_desc *desc, const dream_page_desc 
     PagedAttnArgs a = {};
     a.q = static_cast<const unsigned char *>(q); a.k = static_cast<const unsigned char *>(k_pages); a.v = static_cast<const unsigned char *>(v_pages);
     a.table = page_table; a.nodes = page_nodes; a.prefix_len = prefix_len; a.n_tree = n_tree; a.parent = parent; a.tree_mask = tree_mask; a.out = out; a.lse = lse;
-    return run(who, desc, pages, a, plan_for(desc, pages, n_tree, max_kv_len, 0, 0, true, max_pages_seen), workspace, workspace_bytes, stream);
+    auto plan = [&](int slots) { return plan_for(desc, pages, n_tree, max_kv_len, 0, 0, true, max_pages_seen, slots); };
+    return run(who, desc, pages, a, plan, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"
