@@ -27,10 +27,10 @@ struct SelectArgs {
     int32_t n_tree, hq, hkv, group, lg_page, n_pages, max_pages, max_prefix, stride, n_first, n_last, n_best;
 };
 
-__device__ __forceinline__ int pages_of(const SelectArgs &a, int b)
+__device__ __forceinline__ int pages_of(const int32_t *prefix_len, int b, int max_prefix, int lg_page)
 {
-    const int P = min(max(uniform_load(a.prefix_len + b), 0), a.max_prefix);
-    return (P + (1 << a.lg_page) - 1) >> a.lg_page;
+    const int P = min(max(uniform_load(prefix_len + b), 0), max_prefix);
+    return (P + (1 << lg_page) - 1) >> lg_page;
 }
 
 // The least e in [-100, 122] with top <= 127 * 2^e; top >= 0
@@ -81,10 +81,13 @@ __device__ __forceinline__ i32x4 bound_codes(const Sixteen<T> &x, float scale)
     return r;
 }
 
+// (Plain arguments: they are in registers when a wave starts.)
+//
 // A workgroup: 64 pages against 64 nodes of a sequence and KV head; waves 16 pages x 64 channels each.  Latency bounds it (a workgroup reads some 60 KB and multiplies for 300 clocks): everything
 // that is read is asked for at the start, queries before they are needed twice over, bounds of pages before it is known whether they are live.
 template <class T, int D>
-__global__ __launch_bounds__(4 * D) void score_kernel(SelectArgs a)
+__global__ __launch_bounds__(4 * D) void score_kernel(const int32_t *table, const T *queries, const T *bounds, const int32_t *prefix_len, int n_tree, int hq, int hkv, int group, int max_pages, int n_pages, int max_prefix,
+                                                      int lg_page, int n_first, int n_last, int stride, uint32_t *keys)
 {
     constexpr int KS = D / 64, NSTR = 4 * D + 16;         // bytes of a node in LDS: positive hi, lo, negative hi, lo
     constexpr int SSTR = PAGES + 17;                      // (a step of 17 banks from node to node)
@@ -93,29 +96,29 @@ __global__ __launch_bounds__(4 * D) void score_kernel(SelectArgs a)
     __shared__ int s_sum[NODES * SSTR], s_exponent[PAGES];
     __shared__ float s_top[KS][PAGES];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4, pt = wave & 3, ks = wave >> 2;
-    const int groups = (a.n_tree + NODES - 1) / NODES;
-    const int b = blockIdx.z, kvh = blockIdx.y / groups, node0 = (blockIdx.y - kvh * groups) * NODES, n_nodes = min(NODES, a.n_tree - node0), page0 = blockIdx.x * PAGES;
-    const int entry = a.table[(int64_t)b * a.max_pages + min(page0 + pt * 16 + c, a.max_pages - 1)];
+    const int groups = (n_tree + NODES - 1) / NODES;
+    const int b = blockIdx.z, kvh = blockIdx.y / groups, node0 = (blockIdx.y - kvh * groups) * NODES, n_nodes = min(NODES, n_tree - node0), page0 = blockIdx.x * PAGES;
+    const int entry = table[(int64_t)b * max_pages + min(page0 + pt * 16 + c, max_pages - 1)];
     // ---- queries: D / 16 lanes a node
     constexpr int LANES = D / 16;
     const int at = tid / LANES, part = tid % LANES;
     const bool quantises = at < (n_nodes + 15) / 16 * 16;
-    const T *q = static_cast<const T *>(a.q) + (((int64_t)b * a.n_tree + node0 + min(at, n_nodes - 1)) * a.hq + (int64_t)kvh * a.group) * D + part * 16;
+    const T *q = queries + (((int64_t)b * n_tree + node0 + min(at, n_nodes - 1)) * hq + (int64_t)kvh * group) * D + part * 16;
     Sixteen<T> x[HEADS];
     auto heads_from = [&](int h) {                // (heads behind the last: the last again)
 #pragma unroll
         for (int i = 0; i < HEADS; i++)
-            x[i].load(q + (int64_t)min(h + i, a.group - 1) * D);
+            x[i].load(q + (int64_t)min(h + i, group - 1) * D);
     };
     if (quantises)
         heads_from(0);
     // ---- bounds of this wave's sixteen pages
-    const T *bound = static_cast<const T *>(a.bounds) + ((int64_t)min(max(entry, 0), a.n_pages - 1) * a.hkv + kvh) * 2 * D + ks * 64 + g * 16;
+    const T *bound = bounds + ((int64_t)min(max(entry, 0), n_pages - 1) * hkv + kvh) * 2 * D + ks * 64 + g * 16;
     Sixteen<T> u, w;
     u.load(bound);
     w.load(bound + D);
-    const int n = pages_of(a, b);
-    if (page0 >= n - a.n_last || page0 + PAGES <= a.n_first)      // (only pages in between are ranked)
+    const int n = pages_of(prefix_len, b, max_prefix, lg_page);
+    if (page0 >= n - n_last || page0 + PAGES <= n_first)      // (only pages in between are ranked)
         return;
     for (int i = tid; i < NODES * SSTR; i += 4 * D)
         s_sum[i] = 0;
@@ -126,7 +129,7 @@ __global__ __launch_bounds__(4 * D) void score_kernel(SelectArgs a)
             for (int i = 0; i < HEADS; i++)
                 top = fmaxf(top, x[i].top());
             h += HEADS;
-            if (h >= a.group)
+            if (h >= group)
                 break;
             heads_from(h);
         }
@@ -138,12 +141,12 @@ __global__ __launch_bounds__(4 * D) void score_kernel(SelectArgs a)
 #pragma unroll
         for (int i = 0; i < 16; i++)
             sum[i] = size[i] = 0.0f;
-        for (int h = 0; h < a.group; h += HEADS) {
-            if (a.group > HEADS)
+        for (int h = 0; h < group; h += HEADS) {
+            if (group > HEADS)
                 heads_from(h);
 #pragma unroll
             for (int j = 0; j < HEADS; j++)
-                if (h + j < a.group) {
+                if (h + j < group) {
 #pragma unroll
                     for (int i = 0; i < 16; i++) {
                         const float v = rintf(x[j][i] * scale);
@@ -208,31 +211,32 @@ __global__ __launch_bounds__(4 * D) void score_kernel(SelectArgs a)
             const uint32_t bits = __float_as_uint(exponent > 122 ? INFINITY : s);
             key[r] = bits >> 31 ? ~bits : bits | 0x80000000u;      // in the scores' order
         }
-        *reinterpret_cast<u32x4 *>(a.keys + (((int64_t)b * a.hkv + kvh) * a.n_tree + node0 + node) * a.stride + page0 + page) = key;
+        *reinterpret_cast<u32x4 *>(keys + (((int64_t)b * hkv + kvh) * n_tree + node0 + node) * stride + page0 + page) = key;
     }
 }
 
 // TEAM waves to a node (one, or all of the workgroup: its barriers are among those); VALUES: scores that a lane holds (0: they are read again every time; TEAM is 1 then).  The nodes' choices meet in LDS as one bit a page and leave it as
 // their part of every page's word.
 template <int VALUES, int TEAM>
-__global__ __launch_bounds__(TEAM == 1 ? 512 : 1024) void choose_kernel(SelectArgs a)
+__global__ __launch_bounds__(TEAM == 1 ? 512 : 1024) void choose_kernel(const uint32_t *keys, const int32_t *prefix_len, uint64_t *page_nodes, int n_tree, int hkv, int stride, int max_pages, int max_prefix, int lg_page,
+                                                                         int n_first, int n_last, int n_best)
 {
     static_assert(TEAM == 1 || TEAM == 16);
     constexpr int WAVES = TEAM == 1 ? 8 : 16, HERE = WAVES / TEAM, HELD = VALUES ? VALUES * TEAM * 64 : RANGE;      // nodes of a workgroup; pages that it holds at a time
     __shared__ uint64_t s_bits[HERE][HELD / 64];
     __shared__ uint32_t s_team[2][WAVES][2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), member = wave % TEAM, at = wave / TEAM;
-    const int b = blockIdx.z, kvh = blockIdx.y, node0 = blockIdx.x * HERE, node = min(node0 + at, a.n_tree - 1);
-    const uint32_t *scores = a.keys + (((int64_t)b * a.hkv + kvh) * a.n_tree + node) * a.stride;
+    const int b = blockIdx.z, kvh = blockIdx.y, node0 = blockIdx.x * HERE, node = min(node0 + at, n_tree - 1);
+    const uint32_t *scores = keys + (((int64_t)b * hkv + kvh) * n_tree + node) * stride;
     // scores are asked for before it is known how many there are (the array has as many as a lane asks for, of pages that may be none)
     uint32_t held[VALUES ? VALUES : 1];
     if constexpr (VALUES > 0) {
 #pragma unroll
         for (int i = 0; i < VALUES; i++)
-            held[i] = a.n_best > 0 ? scores[min((i * TEAM + member) * 64 + lane, a.stride - 1)] : 0u;
+            held[i] = n_best > 0 ? scores[min((i * TEAM + member) * 64 + lane, stride - 1)] : 0u;
     }
-    const int n = pages_of(a, b), lo = min(a.n_first, n), hi = max(n - a.n_last, lo), between = hi - lo;
-    const bool ranked = a.n_best > 0 && a.n_best < between;
+    const int n = pages_of(prefix_len, b, max_prefix, lg_page), lo = min(n_first, n), hi = max(n - n_last, lo), between = hi - lo;
+    const bool ranked = n_best > 0 && n_best < between;
     uint32_t border = 0u, ties = ~0u;             // scores above the border are in, and of those at it the pages below `ties`
     if (ranked) {
         uint32_t most = 0u, least = ~0u;
@@ -295,10 +299,10 @@ __global__ __launch_bounds__(TEAM == 1 ? 512 : 1024) void choose_kernel(SelectAr
         // count(from) >= n_best > count(above), above - from shrinking to 1
         uint32_t from = __builtin_amdgcn_readfirstlane((int)least), above = (uint32_t)__builtin_amdgcn_readfirstlane((int)most) + 1u;
         int have = between, over = 0;
-        while (have != a.n_best && above - from > 1u) {
+        while (have != n_best && above - from > 1u) {
             const uint32_t middle = from + (above - from) / 2u;
             const int k = count(middle);
-            if (k >= a.n_best) {
+            if (k >= n_best) {
                 from = middle;
                 have = k;
             } else {
@@ -307,8 +311,8 @@ __global__ __launch_bounds__(TEAM == 1 ? 512 : 1024) void choose_kernel(SelectAr
             }
         }
         border = from;
-        if (have != a.n_best) {                   // the equal scores at the border (`over` are above it): the lower pages
-            int room = a.n_best - over;
+        if (have != n_best) {                   // the equal scores at the border (`over` are above it): the lower pages
+            int room = n_best - over;
             if constexpr (TEAM == 1) {
                 for (int page = lo & ~63; page < hi; page += 64) {
                     const uint64_t equal = __ballot(page + lane >= lo && page + lane < hi && scores[min(max(page + lane, lo), hi - 1)] == from);
@@ -347,12 +351,12 @@ __global__ __launch_bounds__(TEAM == 1 ? 512 : 1024) void choose_kernel(SelectAr
         }
     }
     auto takes = [&](int page, uint32_t score) {
-        return page < n && (page < lo || page >= hi || (a.n_best > 0 && (!ranked || score > border || (score == border && (uint32_t)page < ties))));
+        return page < n && (page < lo || page >= hi || (n_best > 0 && (!ranked || score > border || (score == border && (uint32_t)page < ties))));
     };
-    const int words = (a.n_tree + 63) / 64, rest = a.n_tree - node0;      // nodes from this workgroup's first on
-    const bool there = node0 + at < a.n_tree;
-    uint64_t *out = a.page_nodes + ((int64_t)b * a.hkv + kvh) * a.max_pages * words + node0 / 64;
-    const int live = min(n, a.max_pages);
+    const int words = (n_tree + 63) / 64, rest = n_tree - node0;      // nodes from this workgroup's first on
+    const bool there = node0 + at < n_tree;
+    uint64_t *out = page_nodes + ((int64_t)b * hkv + kvh) * max_pages * words + node0 / 64;
+    const int live = min(n, max_pages);
     for (int page0 = 0; page0 < live; page0 += HELD) {      // (pages that lanes hold are all there are)
         __syncthreads();                          // (the range before is written)
         if constexpr (VALUES > 0) {
@@ -366,7 +370,7 @@ __global__ __launch_bounds__(TEAM == 1 ? 512 : 1024) void choose_kernel(SelectAr
         } else {
             for (int i = 0; i < HELD / 64; i++) {
                 const int page = page0 + i * 64 + lane;
-                const uint64_t bits = there ? __ballot(takes(page, scores[min(page, a.stride - 1)])) : 0ull;
+                const uint64_t bits = there ? __ballot(takes(page, scores[min(page, stride - 1)])) : 0ull;
                 if (lane == 0)
                     s_bits[at][i] = bits;
             }
@@ -391,7 +395,7 @@ __global__ __launch_bounds__(TEAM == 1 ? 512 : 1024) void choose_kernel(SelectAr
         }
     }
     if ((node0 & 63) == 0)                        // words of pages that there are not
-        for (int page = live + tid; page < a.max_pages; page += 64 * WAVES)
+        for (int page = live + tid; page < max_pages; page += 64 * WAVES)
             out[(int64_t)page * words] = 0ull;
 }
 
@@ -420,23 +424,26 @@ int launch_select(const SelectArgs &a, int D, int B, hipStream_t st)
     const int groups = ceil_div(a.n_tree, NODES);
     if (a.n_best > 0) {
         auto *score = D == 64 ? &score_kernel<T, 64> : D == 128 ? &score_kernel<T, 128> : &score_kernel<T, 256>;
-        hipLaunchKernelGGL(score, dim3(a.stride / PAGES, a.hkv * groups, B), dim3(4 * D), 0, st, a);
+        hipLaunchKernelGGL(score, dim3(a.stride / PAGES, a.hkv * groups, B), dim3(4 * D), 0, st, a.table, static_cast<const T *>(a.q), static_cast<const T *>(a.bounds), a.prefix_len, a.n_tree, a.hq,
+                           a.hkv, a.group, a.max_pages, a.n_pages, a.max_prefix, a.lg_page, a.n_first, a.n_last, a.stride, a.keys);
         if (int rc = check_launch("score_kernel"))
             return rc;
     }
+    auto choose = [&](auto kernel, int nodes, int threads) {      // nodes of a workgroup
+        hipLaunchKernelGGL(kernel, dim3(ceil_div(a.n_tree, nodes), a.hkv, B), dim3(threads), 0, st, a.keys, a.prefix_len, a.page_nodes, a.n_tree, a.hkv, a.stride, a.max_pages, a.max_prefix, a.lg_page, a.n_first,
+                           a.n_last, a.n_best);
+    };
     // One token: all of a workgroup's waves rank its pages together
-    if (a.n_tree == 1 && a.stride > 256 && a.stride <= 8192) {
-        auto *choose = a.stride <= 2048 ? &choose_kernel<2, 16> : &choose_kernel<8, 16>;
-        hipLaunchKernelGGL(choose, dim3(1, a.hkv, B), dim3(1024), 0, st, a);
-    } else {
-        auto *choose = a.stride <= 128    ? &choose_kernel<2, 1>
-                       : a.stride <= 256  ? &choose_kernel<4, 1>
-                       : a.stride <= 512  ? &choose_kernel<8, 1>
-                       : a.stride <= 1024 ? &choose_kernel<16, 1>
-                       : a.stride <= 2048 ? &choose_kernel<32, 1>
-                                          : &choose_kernel<0, 1>;
-        hipLaunchKernelGGL(choose, dim3(ceil_div(a.n_tree, 8), a.hkv, B), dim3(512), 0, st, a);
-    }
+    if (a.n_tree == 1 && a.stride > 256 && a.stride <= 8192)
+        choose(a.stride <= 2048 ? &choose_kernel<2, 16> : &choose_kernel<8, 16>, 1, 1024);
+    else
+        choose(a.stride <= 128    ? &choose_kernel<2, 1>
+               : a.stride <= 256  ? &choose_kernel<4, 1>
+               : a.stride <= 512  ? &choose_kernel<8, 1>
+               : a.stride <= 1024 ? &choose_kernel<16, 1>
+               : a.stride <= 2048 ? &choose_kernel<32, 1>
+                                  : &choose_kernel<0, 1>,
+               8, 512);
     return check_launch("choose_kernel");
 }
 

@@ -55,60 +55,82 @@ struct AppendArgs {
     float amplitude;
 };
 
+// N neighbouring values as they stand in memory: 16 bytes as words (as an array of values they would be kept in memory, not in registers), or one or two values
 template <class T, int N>
 struct Piece {
-    T v[N];
+    static constexpr bool WIDE = sizeof(T) * N == 16, NARROW_TYPE = sizeof(T) == 2;
+    using Raw = std::conditional_t<WIDE, u32x4, T[N]>;
+    Raw raw;
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if constexpr (WIDE) {
+            raw = *reinterpret_cast<const u32x4 *>(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                raw[i] = p[i];
+        }
+    }
+    __device__ __forceinline__ void store(T *p) const
+    {
+        if constexpr (WIDE) {
+            *reinterpret_cast<u32x4 *>(p) = raw;
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; i++)
+                p[i] = raw[i];
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (!NARROW_TYPE)
+            return WIDE ? __uint_as_float(raw[i]) : raw[i];
+        else if constexpr (WIDE)
+            return __uint_as_float(i & 1 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16);
+        else
+            return bf16_bits_to_float(raw[i]);
+    }
+    // Values i and i + 1 (i alone, if it is the only one), each rounded once to the type
+    __device__ __forceinline__ void set(int i, float x, float y)
+    {
+        if constexpr (!NARROW_TYPE && WIDE) {
+            raw[i] = __float_as_uint(x);
+            raw[i + 1] = __float_as_uint(y);
+        } else if constexpr (!NARROW_TYPE) {
+            raw[i] = x;
+            if constexpr (N > 1)
+                raw[i + 1] = y;
+        } else if constexpr (WIDE) {
+            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+            raw[i / 2] = __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
+        } else {
+            raw[i] = __builtin_bit_cast(uint16_t, (__bf16)x);
+            if constexpr (N > 1)
+                raw[i + 1] = __builtin_bit_cast(uint16_t, (__bf16)y);
+        }
+    }
 };
-template <class T>
-__device__ __forceinline__ float widen(T v)
+
+// The value of something that is the same in every lane
+template <class V>
+__device__ __forceinline__ V here(V v)
 {
-    if constexpr (std::is_same_v<T, float>)
-        return v;
-    else
-        return bf16_bits_to_float(v);
-}
-template <class T>
-__device__ __forceinline__ T narrow(float v)
-{
-    if constexpr (std::is_same_v<T, float>)
-        return v;
-    else
-        return __builtin_bit_cast(uint16_t, (__bf16)v);
-}
-template <class T, int N>
-__device__ __forceinline__ Piece<T, N> load_piece(const T *p)
-{
-    Piece<T, N> r;
-    if constexpr (sizeof(T) * N == 16) {
-        r = __builtin_bit_cast(Piece<T, N>, *reinterpret_cast<const u32x4 *>(p));
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; i++)
-            r.v[i] = p[i];
-    }
-    return r;
-}
-template <class T, int N>
-__device__ __forceinline__ void store_piece(T *p, const Piece<T, N> &r)
-{
-    if constexpr (sizeof(T) * N == 16) {
-        *reinterpret_cast<u32x4 *>(p) = __builtin_bit_cast(u32x4, r);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; i++)
-            p[i] = r.v[i];
-    }
+    asm volatile("" : "+s"(v));
+    return v;
 }
 
 // One workgroup per row, or where there are few rows several: a row's angles are formed once and lie in LDS while its first pieces are on their way.  A thread takes pieces of a head, N values each
-// (in the half layout with the N values rot / 2 further on).  PAIRED: the pairs are neighbours (2i, 2i + 1); else (i, i + rot / 2).
+// (in the half layout with the N values rot / 2 further on).  What the first loads need are
+// plain arguments, in registers when a wave starts, and what a piece chooses from is chosen by value (of
+// variables the compiler chooses an address instead, in a copy of theirs in memory: 312 bytes a thread).  PAIRED: the pairs are neighbours (2i, 2i + 1); else (i, i + rot / 2).
 template <class T, bool PAIRED, int N>
-__global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
+__global__ __launch_bounds__(256) void append_kernel(const int32_t *row_base, const int32_t *table, const int32_t *pos_base, const T *q, const T *k, const T *v, int n_rows, uint32_t rows_magic, int max_pages, int lg_page,
+                                                                int hq, int hkv, uint32_t pieces_magic, uint32_t vpieces_magic, T *q_out, T *k_pages, T *v_pages, AppendArgs a)
 {
     constexpr int NV = 16 / sizeof(T);               // values of a piece that does not turn
     __shared__ float2 s_turn[128];
     const int tid = threadIdx.x;
-    const int b = a.rows_magic ? quick_div(blockIdx.x, a.rows_magic) : blockIdx.x / a.n_rows, r = blockIdx.x - b * a.n_rows;
+    const int b = rows_magic ? quick_div(blockIdx.x, rows_magic) : blockIdx.x / n_rows, r = blockIdx.x - b * n_rows;
     const int D = a.head_dim, rot = a.rot, half = rot / 2, pieces = a.pieces;
     const int turned = rot ? (PAIRED ? rot : half) / N : 0;     // pieces of a head that turn; the others are copied
     const int stride = gridDim.y * 256;
@@ -118,25 +140,25 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
 #pragma unroll
     for (int i = 0; i < DREAM_MAX_TREE / 64; i++) {
         const int node = i * 64 + (tid & 63);
-        par[i] = walk && node < a.n_rows ? a.parent[(int64_t)b * a.n_rows + node] : -1;
+        par[i] = walk && node < n_rows ? a.parent[(int64_t)b * n_rows + node] : -1;
     }
-    const int live = a.n_live ? uniform_load(a.n_live + b) : a.n_rows;
-    const int base = uniform_load(a.row_base + b), start = !rot ? 0 : a.pos ? uniform_load(a.pos + blockIdx.x) : a.pos_base ? uniform_load(a.pos_base + b) : base;
+    const int live = a.n_live ? uniform_load(a.n_live + b) : n_rows;
+    const int base = uniform_load(row_base + b), start = !rot ? 0 : a.pos ? uniform_load(a.pos + blockIdx.x) : pos_base ? uniform_load(pos_base + b) : base;
     const int64_t row = (int64_t)base + (a.row_index ? uniform_load(a.row_index + blockIdx.x) : r);
     const float freq = rot ? a.inv_freq[tid < half ? tid : 0] : 0.0f;
     if (r >= live)
         return;
-    const int page = row >= 0 && row >> a.lg_page < a.max_pages ? uniform_load(a.table + (int64_t)b * a.max_pages + (row >> a.lg_page)) : -1;
+    const int page = row >= 0 && row >> lg_page < max_pages ? uniform_load(table + (int64_t)b * max_pages + (row >> lg_page)) : -1;
     Piece<T, N> x[BATCH], y[BATCH];
     Piece<T, NV> w[BATCH];
     auto source = [&](int idx, bool &value, int &h, int &it) {      // of piece idx: its tensor's row of heads, its head and its place there
         value = idx >= a.end_k;
-        const T *src = static_cast<const T *>(idx < a.end_q ? a.q : value ? a.v : a.k);
-        const int at = idx - (idx < a.end_q ? 0 : value ? a.end_k : a.end_q), per = value ? D / NV : pieces;
-        const uint32_t magic = value ? a.vpieces_magic : a.pieces_magic;
+        const T *src = idx < a.end_q ? here(q) : value ? here(v) : here(k);
+        const int at = idx - (idx < a.end_q ? 0 : value ? here(a.end_k) : here(a.end_q)), per = value ? D / NV : pieces;
+        const uint32_t magic = value ? here(vpieces_magic) : here(pieces_magic);
         h = magic ? quick_div(at, magic) : at / per;
         it = at - h * per;
-        return src + ((int64_t)blockIdx.x * (idx < a.end_q ? a.hq : a.hkv) + h) * D;
+        return src + ((int64_t)blockIdx.x * (idx < a.end_q ? here(hq) : here(hkv)) + h) * D;
     };
     auto channel = [&](int it) { return PAIRED || it < turned ? it * N : it * N + half; };
     auto request = [&](int first) {
@@ -147,13 +169,15 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
                 bool value;
                 int h, it;
                 const T *src = source(idx, value, h, it);
-                if (value) {
-                    w[u] = load_piece<T, NV>(src + it * NV);
+                if constexpr (N == NV) {              // a value's piece is one that does not turn
+                    x[u].load(src + (value ? it * N : channel(it)));
+                } else if (value) {
+                    w[u].load(src + it * NV);
                 } else {
-                    x[u] = load_piece<T, N>(src + channel(it));
-                    if (!PAIRED && it < turned)
-                        y[u] = load_piece<T, N>(src + channel(it) + half);
+                    x[u].load(src + channel(it));
                 }
+                if (!PAIRED && !value && it < turned)
+                    y[u].load(src + channel(it) + half);
             }
         }
     };
@@ -184,7 +208,7 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
     }
     __syncthreads();
     const bool kept = page >= 0 && page < a.n_pages;
-    const int64_t in_pool = (((int64_t)(kept ? page : 0) * a.hkv << a.lg_page) + (row & ((1 << a.lg_page) - 1))) * D;      // of head 0
+    const int64_t in_pool = (((int64_t)(kept ? page : 0) * hkv << lg_page) + (row & ((1 << lg_page) - 1))) * D;      // of head 0
     for (int first = blockIdx.y * 256; first < a.end_v; first += stride * BATCH) {
         if (first >= stride)
             request(first);
@@ -196,33 +220,33 @@ __global__ __launch_bounds__(256) void append_kernel(AppendArgs a)
             bool value;
             int h, it;
             source(idx, value, h, it);
-            T *dst = idx < a.end_q ? static_cast<T *>(a.q_out) + ((int64_t)blockIdx.x * a.hq + h) * D
-                                   : static_cast<T *>(value ? a.v_pages : a.k_pages) + in_pool + ((int64_t)h << a.lg_page) * D;
-            if (value) {
-                store_piece(dst + it * NV, w[u]);
+            T *dst = idx < a.end_q ? here(q_out) + ((int64_t)blockIdx.x * here(hq) + h) * D
+                                   : (value ? here(v_pages) : here(k_pages)) + in_pool + ((int64_t)h << lg_page) * D;
+            if (N != NV && value) {
+                w[u].store(dst + it * NV);
                 continue;
             }
-            if (it < turned) {
+            if (!value && it < turned) {
                 if constexpr (PAIRED) {
 #pragma unroll
                     for (int i = 0; i < N; i += 2) {
                         const float2 t = s_turn[it * (N / 2) + i / 2];
-                        const float p = widen(x[u].v[i]), q = widen(x[u].v[i + 1]);
-                        x[u].v[i] = narrow<T>(p * t.x - q * t.y);
-                        x[u].v[i + 1] = narrow<T>(p * t.y + q * t.x);
+                        const float p = x[u][i], q = x[u][i + 1];
+                        x[u].set(i, p * t.x - q * t.y, p * t.y + q * t.x);
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < N; i++) {
-                        const float2 t = s_turn[it * N + i];
-                        const float p = widen(x[u].v[i]), q = widen(y[u].v[i]);
-                        x[u].v[i] = narrow<T>(p * t.x - q * t.y);
-                        y[u].v[i] = narrow<T>(p * t.y + q * t.x);
+                    for (int i = 0; i < N; i += 2) {
+                        constexpr int SECOND = N > 1;
+                        const float2 t0 = s_turn[it * N + i], t1 = s_turn[it * N + i + SECOND];
+                        const float p0 = x[u][i], q0 = y[u][i], p1 = x[u][i + SECOND], q1 = y[u][i + SECOND];
+                        x[u].set(i, p0 * t0.x - q0 * t0.y, p1 * t1.x - q1 * t1.y);
+                        y[u].set(i, p0 * t0.y + q0 * t0.x, p1 * t1.y + q1 * t1.x);
                     }
-                    store_piece(dst + channel(it) + half, y[u]);
+                    y[u].store(dst + channel(it) + half);
                 }
             }
-            store_piece(dst + channel(it), x[u]);
+            x[u].store(dst + (value ? it * N : channel(it)));
         }
     }
 }
@@ -233,7 +257,9 @@ int launch_append(const AppendArgs &a, bool paired, bool wide, int64_t rows, hip
     constexpr int N = 16 / sizeof(T);
     auto *kernel = paired ? (wide ? &append_kernel<T, true, N> : &append_kernel<T, true, 2>) : wide ? &append_kernel<T, false, N> : &append_kernel<T, false, 1>;
     const int64_t parts = 1024 / rows, most = (a.end_v + 255) / 256;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)rows, (unsigned)(parts < 1 ? 1 : parts < most ? parts : most)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)rows, (unsigned)(parts < 1 ? 1 : parts < most ? parts : most)), dim3(256), 0, st, a.row_base, a.table,
+                       a.pos_base, static_cast<const T *>(a.q), static_cast<const T *>(a.k), static_cast<const T *>(a.v), a.n_rows, a.rows_magic, a.max_pages, a.lg_page, a.hq, a.hkv, a.pieces_magic,
+                       a.vpieces_magic, static_cast<T *>(a.q_out), static_cast<T *>(a.k_pages), static_cast<T *>(a.v_pages), a);
     return check_launch("append_kernel");
 }
 
@@ -312,59 +338,77 @@ struct BoundsArgs {
     int32_t hkv, lg_page, n_pages, max_pages, slots;
 };
 
-// A workgroup per page of a sequence's run, and head: a thread has 16 bytes of a row, the rows of a page are shared out over 256 / (row / 16) threads that meet in LDS.
+// A workgroup per page of a sequence's run, and head: a thread has 16 bytes of a row, the rows of a page are shared out over 256 / (row / 16) threads; those of a wave meet by exchange, the waves in
+// LDS.  (Plain arguments: they are in registers when a wave starts.)
 template <class T, int D>
-__global__ __launch_bounds__(256) void bounds_kernel(BoundsArgs a)
+__global__ __launch_bounds__(256) void bounds_kernel(const int32_t *table, const int32_t *from_len, const int32_t *to_len, const T *k, int lg_page, int max_pages, int n_pages, int hkv, int slots, T *bounds)
 {
     constexpr int N = 16 / sizeof(T), PER_ROW = D / N, ROWS = 256 / PER_ROW;
-    __shared__ float s_most[256 * N], s_least[256 * N];
-    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, c = tid % PER_ROW, r0 = tid / PER_ROW;
-    const int ps = 1 << a.lg_page, rows = a.max_pages << a.lg_page;
-    const int from = a.from_len ? min(max(uniform_load(a.from_len + b), 0), rows) : 0, to = min(uniform_load(a.to_len + b), rows);
+    __shared__ __attribute__((aligned(16))) float s_ends[4][2][D];      // of a wave's rows: largest and smallest
+    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, c = tid % PER_ROW, r0 = tid / PER_ROW;
+    const int ps = 1 << lg_page, rows = max_pages << lg_page;
+    const int from = from_len ? min(max(uniform_load(from_len + b), 0), rows) : 0, to = min(uniform_load(to_len + b), rows);
     if (to <= from)
         return;
-    for (int i = (from >> a.lg_page) + blockIdx.x; (i << a.lg_page) < to; i += a.slots) {
-        const int page = uniform_load(a.table + (int64_t)b * a.max_pages + i);
-        if (page < 0 || page >= a.n_pages)
+    for (int i = (from >> lg_page) + blockIdx.x; (i << lg_page) < to; i += slots) {
+        const int page = uniform_load(table + (int64_t)b * max_pages + i);
+        if (page < 0 || page >= n_pages)
             continue;
-        const int live = min(ps, to - (i << a.lg_page));
-        const T *src = static_cast<const T *>(a.k) + (((int64_t)page * a.hkv + h) << a.lg_page) * D + c * N;
+        const int live = min(ps, to - (i << lg_page));
+        const T *src = k + (((int64_t)page * hkv + h) << lg_page) * D + c * N;
         float most[N], least[N];
 #pragma unroll
         for (int e = 0; e < N; e++)
             most[e] = -INFINITY, least[e] = INFINITY;
 #pragma unroll 4
         for (int r = r0; r < live; r += ROWS) {
-            const Piece<T, N> x = load_piece<T, N>(src + (int64_t)r * D);
+            Piece<T, N> x;
+            x.load(src + (int64_t)r * D);
 #pragma unroll
             for (int e = 0; e < N; e++) {
-                const float v = widen(x.v[e]);
+                const float v = x[e];
                 const bool finite = fabsf(v) <= FLT_MAX;
                 most[e] = fmaxf(most[e], finite ? v : INFINITY);
                 least[e] = fminf(least[e], finite ? v : -INFINITY);
             }
         }
 #pragma unroll
-        for (int e = 0; e < N; e++)
-            s_most[e * 256 + tid] = most[e], s_least[e * 256 + tid] = least[e];
-        __syncthreads();
-        if (tid < PER_ROW) {
-#pragma unroll
-            for (int e = 0; e < N; e++)
-                for (int r = 1; r < ROWS; r++) {
-                    most[e] = fmaxf(most[e], s_most[e * 256 + r * PER_ROW + tid]);
-                    least[e] = fminf(least[e], s_least[e * 256 + r * PER_ROW + tid]);
-                }
-            Piece<T, N> up, down;
+        for (int d = PER_ROW; d < 64; d *= 2)
 #pragma unroll
             for (int e = 0; e < N; e++) {
-                const bool finite = most[e] <= FLT_MAX && least[e] >= -FLT_MAX;
-                up.v[e] = narrow<T>(finite ? most[e] : INFINITY);
-                down.v[e] = narrow<T>(finite ? least[e] : -INFINITY);
+                most[e] = fmaxf(most[e], __shfl_xor(most[e], d));
+                least[e] = fminf(least[e], __shfl_xor(least[e], d));
             }
-            T *dst = static_cast<T *>(a.bounds) + ((int64_t)page * a.hkv + h) * 2 * D + tid * N;
-            store_piece(dst, up);
-            store_piece(dst + D, down);
+        if ((tid & 63) < PER_ROW)
+#pragma unroll
+            for (int e = 0; e < N; e += 4) {
+                *reinterpret_cast<f32x4 *>(&s_ends[wave][0][c * N + e]) = f32x4{most[e], most[e + 1], most[e + 2], most[e + 3]};
+                *reinterpret_cast<f32x4 *>(&s_ends[wave][1][c * N + e]) = f32x4{least[e], least[e + 1], least[e + 2], least[e + 3]};
+            }
+        __syncthreads();
+        if (tid < PER_ROW) {
+            Piece<T, N> up, down;
+            float high[N], low[N];
+#pragma unroll
+            for (int e = 0; e < N; e++) {
+                high[e] = s_ends[0][0][tid * N + e], low[e] = s_ends[0][1][tid * N + e];
+#pragma unroll
+                for (int w = 1; w < 4; w++) {
+                    high[e] = fmaxf(high[e], s_ends[w][0][tid * N + e]);
+                    low[e] = fminf(low[e], s_ends[w][1][tid * N + e]);
+                }
+                const bool finite = high[e] <= FLT_MAX && low[e] >= -FLT_MAX;
+                high[e] = finite ? high[e] : INFINITY;
+                low[e] = finite ? low[e] : -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                up.set(e, high[e], high[e + 1]);
+                down.set(e, low[e], low[e + 1]);
+            }
+            T *dst = bounds + ((int64_t)page * hkv + h) * 2 * D + tid * N;
+            up.store(dst);
+            down.store(dst + D);
         }
         __syncthreads();
     }
@@ -374,7 +418,8 @@ template <class T>
 int launch_bounds(const BoundsArgs &a, int D, int B, hipStream_t st)
 {
     auto *kernel = D == 64 ? &bounds_kernel<T, 64> : D == 128 ? &bounds_kernel<T, 128> : &bounds_kernel<T, 256>;
-    hipLaunchKernelGGL(kernel, dim3(a.slots, a.hkv, B), dim3(256), 0, st, a);
+    hipLaunchKernelGGL(kernel, dim3(a.slots, a.hkv, B), dim3(256), 0, st, a.table, a.from_len, a.to_len, static_cast<const T *>(a.k), a.lg_page, a.max_pages, a.n_pages, a.hkv, a.slots,
+                       static_cast<T *>(a.bounds));
     return check_launch("bounds_kernel");
 }
 
