@@ -15,6 +15,8 @@ pytestmark = pytest.mark.gpu
 def _automatic():
     yield
     dream.dream_set_kv_splits(0)
+    dream.dream_set_tile_waves(0)
+    dream.dream_set_q_tiles(0)
 
 
 class Problem:
@@ -138,6 +140,9 @@ SHARED = [
     (4, 2, 64, 21, [140, 133], 32, dict(groups=[(0, 2, 128)], given=True)),
     (4, 2, 128, 90, [140, 333], 32, dict(groups=[(0, 2, 128)])),
     (4, 2, 64, 9, [70, 71, 64], 16, dict(dtype="f32", groups=[(0, 3, 50)])),
+    (4, 2, 64, 5, [50, 70, 64, 90], 16, dict(groups=[(2, 2, 48)])),                          # sequences in front of the first group
+    (4, 2, 128, 40, [50, 70, 64], 16, dict(groups=[(1, 2, 48)])),
+    (4, 2, 64, 5, [50, 70, 64], 16, dict(groups=[(2, 1, 48)], dtype="f32")),
     (4, 2, 128, 9, [70, 71, 64], 64, dict(groups=[(0, 3, 50)], scale=-0.2)),
 ]
 SPARSE = [
@@ -199,6 +204,44 @@ def test_every_number_of_rows(D, rows):
         p = Problem(1, 1, D, rows, [100, 71], 16, seed=rows, **more)
         p.call()
         p.check()
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("waves,tiles", [(4, 1), (4, 2), (8, 1), (8, 2)])
+def test_every_shape(D, waves, tiles):
+    """Whatever the call's sizes would have chosen; one split and several, steps that start and end anywhere."""
+    dream.dream_set_tile_waves(waves)
+    dream.dream_set_q_tiles(tiles)
+    for splits, more in ((1, {}), (3, dict(groups=[(0, 2, 49)])), (2, dict(sparse=0.4)), (1, dict(sparse=0.1))):
+        dream.dream_set_kv_splits(splits)
+        for T, prefix, page in ((1, [333, 0], 16), (20, [100, 71], 32), (35, [1030, 65], 64), (130, [300, 49], 16)):
+            p = Problem(4, 2, D, T, prefix, page, seed=T, **more)
+            p.call()
+            p.check()
+
+
+@pytest.mark.parametrize("case", [DENSE[7], DENSE[16], SHARED[1], SHARED[5], SPARSE[4], SPARSE[9]], ids=lambda c: str(c)[:50])
+@pytest.mark.parametrize("wrong", [1, 10 ** 12])
+def test_lengths_that_are_hints_only_choose_the_launch(case, wrong):
+    p = Problem(*case[:6], **case[6])
+    p.max_kv = max(wrong, p.T)
+    p.groups = p.groups[:3] + (wrong,)
+    p.call()
+    p.check()
+
+
+@pytest.mark.parametrize("case", [DENSE[16], DENSE[17], DENSE[23], SHARED[1], SHARED[5], SPARSE[1], SPARSE[4]], ids=lambda c: str(c)[:50])
+def test_workspaces_of_other_calls_hold_fewer_parts(case):
+    """Any size from that of the fewest parts on; nothing behind it is written."""
+    p = Problem(*case[:6], **case[6])
+    slot = p.B * case[0] * p.T * (p.D + 2) * 4
+    parts = 1 + (p.groups[0] > 0)
+    for size in (256 if parts == 1 else parts * slot, parts * slot + 4, (parts + 1) * slot + 36, 5 * slot + 4):
+        ws = dream.alloc_workspace(size + 4096).fill_(0x55)
+        p.out.fill_(7.0)
+        p.call(ws[:size])
+        p.check()
+        assert bool((ws[size:] == 0x55).all())
 
 
 @pytest.mark.parametrize("value", [np.nan, np.inf, -np.inf])
