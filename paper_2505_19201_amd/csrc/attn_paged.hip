@@ -411,25 +411,29 @@ __device__ __forceinline__ uint32_t four_nodes(const PagedAttnArgs &a, uint64_t 
 }
 
 // ---- row by row ------------------------------------------------------------------------------------------------------
-// LDS of attend_rows_singly: queries, masks, parents, the list
-template <int D, int THREADS>
-constexpr int single_masks() { return THREADS / 64 * D * 4; }
-template <int D, int THREADS>
-int single_bytes(int cap, int words) { return single_masks<D, THREADS>() + cap * words * 8 + DREAM_MAX_TREE * 4; }
+// LDS of attend_rows_singly: masks, parents, the list
+int single_bytes(int cap, int words) { return cap * words * 8 + DREAM_MAX_TREE * 4; }
 
-// The workgroup's rows, one to a wave at a time: a lane takes a key's whole product, then D / 64 channels of the weighted sum.  Only rows that the node sees are read.  Where the keys are shared
-// out, a workgroup has every splits-th run of `run` keys from the tile of `tile` keys on that holds the first.
+// The workgroup's rows, one to a wave at a time.  64 keys: each lane looks one up, then 16 bytes of a row are a lane's, so that a wave reads several whole rows at a time; keys and values are asked for
+// together.  What the node does not see has no weight, whatever it holds.  Where the keys are shared out, a workgroup has every splits-th run of `run` keys from the tile of `tile` keys on that holds
+// the first.  (A lane with a key's whole product, and values key by key: 60 nodes x 764 keys x 32 heads of 128 float32 146 us, ROWSTIME with rows read whole.)
 template <class T, int D, int THREADS, bool SPARSE>
 __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const Unit &u, int cap, int tile, int run, unsigned char *smem)
 {
-    constexpr int NW = THREADS / 64, CH = D / 64, N = 16 / sizeof(T);
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    constexpr int NW = THREADS / 64, N = 16 / sizeof(T), LANES = D / N, G = 64 / LANES;      // values of a lane; lanes of a row; rows that a wave reads at a time
+    constexpr int MOST = std::is_same_v<T, float> ? 16 : 4, BATCH = MOST < LANES ? MOST : LANES;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), piece = lane % LANES, in_group = lane / LANES;
     const int count = min(cap, u.n_rows - u.row0), ps_mask = (1 << a.lg_page) - 1;
-    float *q = reinterpret_cast<float *>(smem) + wave * D;
-    uint64_t *masks = reinterpret_cast<uint64_t *>(smem + single_masks<D, THREADS>());
+    uint64_t *masks = reinterpret_cast<uint64_t *>(smem);
     int32_t *parents = reinterpret_cast<int32_t *>(masks + cap * a.words);
     PageList<THREADS> list;
     const int32_t *table = a.table + (int64_t)u.b * a.max_pages;
+    auto value = [](const u32x4 &raw, int i) {
+        if constexpr (std::is_same_v<T, float>)
+            return __uint_as_float(raw[i]);
+        else
+            return __uint_as_float(i & 1 ? raw[i / 2] & 0xffff0000u : raw[i / 2] << 16);
+    };
     if (!u.shared)
         build_masks(a, u, masks, parents, cap, tid, THREADS);
     for (int j0 = 0; j0 < count; j0 += NW) {
@@ -437,63 +441,59 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
         const int j = min(j0 + wave, count - 1);
         const Row w = row_at(a, u, u.row0 + j);
         const int limit = row_limit(a, u, w);
-        for (int i = lane; i < D; i += 64) {
-            const T *p = reinterpret_cast<const T *>(a.q) + row_of_q(a, w) * D + i;
-            if constexpr (std::is_same_v<T, float>)
-                q[i] = *p;
-            else
-                q[i] = bf16_bits_to_float(*p);
-        }
-        wave_lds_fence();
-        float m = -INFINITY, l = 0.0f, o[CH];
+        const u32x4 q = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const T *>(a.q) + row_of_q(a, w) * D + piece * N);
+        float m = -INFINITY, l = 0.0f, o[N];      // (the lanes of a row hold the same)
 #pragma unroll
-        for (int i = 0; i < CH; i++)
+        for (int i = 0; i < N; i++)
             o[i] = 0.0f;
         // 64 keys: this lane's row of the page and where it stands; `kind`: which of them are meant (1: the prefix's, 2: the tree's)
         auto keys = [&](bool there, int page, int pos, int kind, const uint64_t *word) {
             const int node = pos - u.P;
             const bool in_prefix = (kind & 1) && pos >= u.lo && pos < limit && (!SPARSE || (word[w.node >> 6] >> (w.node & 63) & 1));
             const bool in_tree = (kind & 2) && !u.shared && node >= 0 && node < a.n_tree && (masks[j * a.words + (node >> 6)] >> (node & 63) & 1);
-            const bool sees = there && (in_prefix || in_tree);
-            float s = -INFINITY;
+            const uint64_t seen = __ballot(there && (in_prefix || in_tree));
             const int64_t row = ((((int64_t)page * a.hkv + u.kvh) << a.lg_page) + (pos & ps_mask)) * D;
-            if (sees) {
-                const T *k = reinterpret_cast<const T *>(a.k) + row;
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
-                for (int i = 0; i < D; i += N) {
-                    const u32x4 raw = *reinterpret_cast<const u32x4 *>(k + i);
+#pragma unroll 1
+            for (int k0 = 0; k0 < 64; k0 += BATCH * G) {
+                if (!(seen >> k0 & (BATCH * G == 64 ? ~0ull : (1ull << (BATCH * G & 63)) - 1)))
+                    continue;
+                u32x4 k[BATCH], v[BATCH];
 #pragma unroll
-                    for (int d = 0; d < 4; d++) {
-                        if constexpr (std::is_same_v<T, float>) {
-                            sum[d] = __builtin_fmaf(__uint_as_float(raw[d]), q[i + d], sum[d]);
-                        } else {
-                            sum[d] = __builtin_fmaf(__uint_as_float(raw[d] << 16), q[i + 2 * d], sum[d]);
-                            sum[d] = __builtin_fmaf(__uint_as_float(raw[d] & 0xffff0000u), q[i + 2 * d + 1], sum[d]);
-                        }
-                    }
+                for (int i = 0; i < BATCH; i++) {
+                    const int key = k0 + i * G + in_group;
+                    const int64_t of = (int64_t)((uint64_t)(uint32_t)__shfl((int)(row >> 32), key) << 32 | (uint32_t)__shfl((int)row, key)) + piece * N;
+                    k[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const T *>(a.k) + of);
+                    v[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const T *>(a.v) + of);
                 }
-                s = ((sum[0] + sum[1]) + (sum[2] + sum[3])) * a.scale_log2;
-            }
-            const float top = fmaxf(m, wave_max(s));
-            const float f = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top), ref = fmaxf(top, -FLT_MAX);
-            m = top;
-            const float p = sees ? __builtin_amdgcn_exp2f(s - ref) : 0.0f;
-            l = l * f + p;
+                float s[BATCH], top = m;
 #pragma unroll
-            for (int i = 0; i < CH; i++)
-                o[i] *= f;
-            for (uint64_t left = __ballot(sees && s != -INFINITY); left; left &= left - 1) {      // (a key of weight 0 through a score of -inf adds nothing, whatever its values)
-                const int key = __builtin_ctzll(left);
-                const float pk = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(p), key));
-                const int64_t of = (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(row >> 32), key) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)row, key));
-                const T *v = reinterpret_cast<const T *>(a.v) + of + lane * CH;
+                for (int i = 0; i < BATCH; i++) {
+                    float x = 0.0f;
 #pragma unroll
-                for (int i = 0; i < CH; i++) {
-                    if constexpr (std::is_same_v<T, float>)
-                        o[i] = __builtin_fmaf(pk, v[i], o[i]);
-                    else
-                        o[i] = __builtin_fmaf(pk, bf16_bits_to_float(v[i]), o[i]);
+                    for (int e = 0; e < N; e++)
+                        x = __builtin_fmaf(value(k[i], e), value(q, e), x);
+#pragma unroll
+                    for (int d = 1; d < LANES; d *= 2)
+                        x += __shfl_xor(x, d);
+                    s[i] = seen >> (k0 + i * G + in_group) & 1 ? x * a.scale_log2 : -INFINITY;
+                    top = fmaxf(top, s[i]);
+                }
+#pragma unroll
+                for (int d = LANES; d < 64; d *= 2)
+                    top = fmaxf(top, __shfl_xor(top, d));
+                const float f = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top), ref = fmaxf(top, -FLT_MAX);
+                m = top;
+                l *= f;
+#pragma unroll
+                for (int e = 0; e < N; e++)
+                    o[e] *= f;
+#pragma unroll
+                for (int i = 0; i < BATCH; i++) {
+                    const float p = seen >> (k0 + i * G + in_group) & 1 ? __builtin_amdgcn_exp2f(s[i] - ref) : 0.0f;
+                    l += p;
+#pragma unroll
+                    for (int e = 0; e < N; e++)      // (a key of weight 0 through a score of -inf adds nothing, whatever its values)
+                        o[e] = s[i] == -INFINITY ? o[e] : __builtin_fmaf(p, value(v[i], e), o[e]);
                 }
             }
         };
@@ -518,20 +518,30 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
                 }
             }
         }
-        l = wave_sum(l);
-        if (!mine)
+#pragma unroll
+        for (int d = LANES; d < 64; d *= 2) {
+            l += __shfl_xor(l, d);
+#pragma unroll
+            for (int e = 0; e < N; e++)
+                o[e] += __shfl_xor(o[e], d);
+        }
+        if (!mine || in_group)
             continue;
         if (lane == 0)
             put_ml(a, u, w, m, l);
+        if (a.n_slots > 1 || std::is_same_v<T, float>) {
+            float *to = (a.n_slots > 1 ? a.part_o + row_of_part(a, u, w) * D : static_cast<float *>(a.out) + row_of_q(a, w) * D) + piece * N;
+            const float divisor = a.n_slots > 1 ? 1.0f : l;
 #pragma unroll
-        for (int i = 0; i < CH; i++) {
-            const float x = a.n_slots > 1 ? o[i] : l == 0.0f ? 0.0f : o[i] / l;
-            if (a.n_slots > 1)
-                a.part_o[row_of_part(a, u, w) * D + lane * CH + i] = x;
-            else if constexpr (std::is_same_v<T, float>)
-                static_cast<float *>(a.out)[row_of_q(a, w) * D + lane * CH + i] = x;
-            else
-                static_cast<uint16_t *>(a.out)[row_of_q(a, w) * D + lane * CH + i] = __builtin_bit_cast(uint16_t, (__bf16)x);
+            for (int e = 0; e < N; e += 4)
+                *reinterpret_cast<f32x4 *>(to + e) = l == 0.0f ? f32x4{0.f, 0.f, 0.f, 0.f} : f32x4{o[e], o[e + 1], o[e + 2], o[e + 3]} / divisor;
+        } else {
+            u32x4 row = {0u, 0u, 0u, 0u};
+            if (l != 0.0f)
+#pragma unroll
+                for (int e = 0; e < N; e += 2)
+                    row[e / 2] = pack_bf16(o[e] / l, o[e + 1] / l);
+            *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) + row_of_q(a, w) * D + piece * N) = row;
         }
     }
 }
@@ -1623,7 +1633,7 @@ int launch_keys(PagedAttnArgs &a, hipStream_t st, bool set_up)
     int rc = raise_lds_limit(done, reinterpret_cast<const void *>(kernel), 160 * 1024, "paged attention");
     if (rc || set_up)
         return rc;
-    const size_t list = list_bytes<G::THREADS, SPARSE>(a), main = G::bytes(a.words) + list, again = single_bytes<D, G::THREADS>(G::CAP, a.words) + list;
+    const size_t list = list_bytes<G::THREADS, SPARSE>(a), main = G::bytes(a.words) + list, again = single_bytes(G::CAP, a.words) + list;
     return launch_kernel(kernel, a, G::THREADS, main > again ? main : again, "paged_keys_kernel", st);
 }
 template <int D, int QT, int WR, int NS, bool SPARSE>
@@ -1635,7 +1645,7 @@ int launch_rows(PagedAttnArgs &a, hipStream_t st, bool set_up)
     int rc = raise_lds_limit(done, reinterpret_cast<const void *>(kernel), 160 * 1024, "paged attention");
     if (rc || set_up)
         return rc;
-    const size_t list = list_bytes<G::THREADS, SPARSE>(a), main = G::bytes(a.words) + list, again = single_bytes<D, G::THREADS>(G::CAP, a.words) + list;
+    const size_t list = list_bytes<G::THREADS, SPARSE>(a), main = G::bytes(a.words) + list, again = single_bytes(G::CAP, a.words) + list;
     return launch_kernel(kernel, a, G::THREADS, main > again ? main : again, "paged_rows_kernel", st);
 }
 
@@ -1644,7 +1654,7 @@ int launch_shape(PagedAttnArgs &a, const Shape &s, hipStream_t st, bool set_up =
 {
     if (s.form == SINGLY) {
         const size_t list = list_bytes<256, SPARSE>(a);
-        return launch_kernel(&paged_f32_kernel<D, SPARSE>, a, 256, single_bytes<D, 256>(SINGLE_ROWS, a.words) + list, "paged_f32_kernel", st);
+        return launch_kernel(&paged_f32_kernel<D, SPARSE>, a, 256, single_bytes(SINGLE_ROWS, a.words) + list, "paged_f32_kernel", st);
     }
     if (s.form == ROWS) {
         if constexpr (D == 256)
