@@ -438,10 +438,10 @@ int dream_mx_verify_attn(const dream_attn_desc *desc, const void *q, const void 
  * page_size is 16, 32, 64, 128 or 256; max_pages * page_size is at most DREAM_MAX_WINDOW_ROWS, batch at most 65535,
  * n_q_heads and n_kv_heads at most 4096, D in {64, 128, 256}.  desc->s_max is not looked at: max_pages * page_size stands in its place.
  * An entry of the table outside [0, n_pages) is never followed: what would be written there is dropped, and in the
- * place of what would be read there some other page is.  Entries behind the last live page are not looked at, except that their
- * pages may be read where they share a tile of 64 rows with live ones (results do not depend on them).  Rows that a call writes must stand in pages that no other sequence
- * of the call writes to; a shared prefix that ends inside a page needs a copy of that page for every sequence
- * but one.
+ * place of what would be read there some other page is.  Entries behind the last live page may be anything, and so may
+ * what their pages hold: calls that read may ask for such pages before they know a sequence's length, and results do
+ * not depend on them.  Rows that a call writes must stand in pages that no other sequence of the call writes to; a
+ * shared prefix that ends inside a page needs a copy of that page for every sequence but one.
  *
  * dream_paged_append: the rows a step (or a prompt) adds, turned by their positions on the way.
  *   q, k, v     [B, n_rows, Hq, D] nullable, [B, n_rows, Hkv, D] of desc->dtype
@@ -461,17 +461,19 @@ int dream_mx_verify_attn(const dream_attn_desc *desc, const void *q, const void 
  * dream_paged_verify_attn: dream_tree_verify_attn over pages (n_tree = 1 is plain decoding), where a prefix that sequences
  *   share is read once for all of them.
  *   n_groups     0: nothing is shared.  Otherwise group g is the sequences group_start[g] .. group_start[g + 1] - 1 ([n_groups + 1] int32,
- *                ascending, from 0 to B), and positions below shared_len[g] ([n_groups] int32) of all of them are those of its
+ *                ascending, within 0 .. B), and positions below shared_len[g] ([n_groups] int32) of all of them are those of its
  *                first sequence: its entries of the page table are followed, those of the others not looked at.  A sequence
- *                sees shared positions below its own prefix length only.  n_groups at most B
+ *                sees shared positions below its own prefix length only; one in front of the first group or behind the last shares nothing.  n_groups at most B
  *   max_shared_len, max_kv_len   host-known upper bounds of shared_len and of prefix_len + n_tree; only used to choose the launch shape
+ *   workspace    what ..._workspace gives is what the fastest launch needs; that of another call of the same sequences and nodes does too, if
+ *                it holds one part of the rows (two, with groups): fewer parts are made then, and sums are added in another order.  DREAM_ERR_WORKSPACE below that
  *   A node that sees nothing yields a zero row and lse = -inf.  What a node does not see does not change its row, whatever it holds:
  *   NaN and infinities too.  Values and scores that are not finite: as in dream_window_verify_attn.  batch * n_q_heads at most 2^20, q and out 16-byte aligned.
  *
  * dream_page_bounds: of every page that rows from_len[b] .. to_len[b] - 1 (from_len NULL: 0) lie in, the largest and the
  *   smallest of its keys' values in every channel, over the page's rows below to_len[b]:
  *   bounds       [n_pages, Hkv, 2, D] of desc->dtype, 16-byte aligned: largest, then smallest.  A channel with a value that is not finite gets +inf
- *                and -inf.  Other pages' bounds keep their content
+ *                and -inf.  Other pages' bounds keep their content.  Sequences whose runs meet in a page must agree on its rows
  *   max_new      host-known upper bound of to_len - from_len; only used to choose the launch shape
  *
  * dream_page_select: which pages of its prefix each node is to see, for every KV head, by an upper bound of its scores there.

@@ -26,7 +26,9 @@ void dream_set_q_tiles(int32_t q_tiles);
  * 0 = automatic.
  * The calls with a window or over a 4-bit cache obey all three: splits as the power of two at or below, up to 64; query tiles of a wave of the kernel without
  * shared tiles (as many as it has at that head_dim); 4 = that kernel with 4 waves, 8 = the kernel with shared tiles where it
- * exists, and with dream_set_q_tiles(1) the other one's eight-wave form where that exists. */
+ * exists, and with dream_set_q_tiles(1) the other one's eight-wave form where that exists.
+ * The calls over pages (bf16) obey all three: splits up to 64, of the shared positions and of a sequence's own alike; 4 = the form whose waves share
+ * the keys out, 8 = the one whose waves share the tiles; query tiles of a wave, 1 or 2, as many as that form has at that head_dim. */
 void dream_set_tile_waves(int32_t waves);
 
 /* Polls after which a workgroup of dream_spec_accept stops waiting for the others of its sequence (workgroup 0 then

@@ -6,10 +6,10 @@
 // that share a KV head are one long list of query rows over the first sequence's pages; of the second, every sequence has its own.  Each set is cut further where there are too few workgroups, and
 // the parts are joined by a second kernel.
 //
-// A workgroup has QT tiles of 16 query rows in each of its waves, and a list of pages in LDS (physical page; for selected pages also where it stands in the sequence and which nodes see it), which it
-// takes tile by tile straight to LDS (the pages' addresses are scalars, 16 rows never leave a page).  S^T = K Q^T and O^T += V^T P^T by v_mfma_f32_16x16x32_bf16: a lane owns a query row, its
-// scores are the second product's operand as they come.  Two forms: WR = 1, few rows: the waves share the keys out and have stages of their own, so they meet only at the end; WR > 1, many rows: the
-// waves share the tiles and have rows of their own, one barrier a tile.
+// A workgroup has QT tiles of 16 query rows in each of its waves, and takes keys and values tile by tile straight to LDS: 16 rows never leave a page, so that a tile's addresses are scalars, of which
+// every lane holds those of one of the next 64 tiles.  (Selected pages stand in a list in LDS: the physical page, its place in the sequence, the nodes that see it.)  S^T = K Q^T and O^T += V^T P^T
+// by v_mfma_f32_16x16x32_bf16: a lane owns a query row, its scores are the second product's operand as they come.  Two forms: paged_keys_kernel, few rows: the waves share the keys out and have stages
+// of their own, so they meet only at the end; paged_rows_kernel, many rows: the waves share the tiles and have rows of their own, one barrier a tile.
 //
 // What rows that nobody sees hold does not matter: V's are overwritten with zeros in LDS.  A value that is not finite in a row that some nodes see and others do not would poison the others through
 // 0 * inf; instead of looking at every value, a workgroup looks at its sums at the end, and where one is not finite it takes its rows again, one by one over the keys they see (attend_rows_singly,
@@ -416,7 +416,8 @@ int single_bytes(int cap, int words) { return cap * words * 8 + DREAM_MAX_TREE *
 
 // The workgroup's rows, one to a wave at a time.  64 keys: each lane looks one up, then 16 bytes of a row are a lane's, so that a wave reads several whole rows at a time; keys and values are asked for
 // together.  What the node does not see has no weight, whatever it holds.  Where the keys are shared out, a workgroup has every splits-th run of `run` keys from the tile of `tile` keys on that holds
-// the first.  (A lane with a key's whole product, and values key by key: 60 nodes x 764 keys x 32 heads of 128 float32 146 us, ROWSTIME with rows read whole.)
+// the first.  (A lane with a key's whole product, and values key by key: 60 nodes x 764 keys x 32 heads of 128 in
+// float32 146 us, so 110; 21 nodes x 121 keys x 4 heads of 64 13.0 and 8.8.  A step of 64 keys takes 2.5 us at 64, 6.5 at 128: trips to memory.)
 template <class T, int D, int THREADS, bool SPARSE>
 __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const Unit &u, int cap, int tile, int run, unsigned char *smem)
 {
@@ -908,7 +909,8 @@ struct KeysGeom {
 };
 
 // Few rows: the waves take the key tiles in turn, each for all of the rows, and never meet until the end.  A wave asks for its next keys as soon as a tile's scores are there, and for its next
-// values as soon as they are added up.
+// values as soon as they are added up.  What bounds it: memory where caches are long (8 sequences of up to 16 100 rows, 8 KV heads of 128, one node: 439 MB in 84 us, 5.2 TB/s); where they are short, what a CU
+// pulls (75 to 87 KB a us) and the trips to memory ahead of the first scores and behind the last (one sequence, 60 nodes, 764 rows, 32 KV heads of 128: 12.3 us, of which a wave is in its tiles for 5).
 template <int D, int QT, int NW, bool SPARSE>
 __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArgs first)
 {
@@ -1130,7 +1132,10 @@ struct RowsGeom {
     static int bytes(int words) { return MAIN + WR * 8 + (words > 1 ? CAP * words * 8 + DREAM_MAX_TREE * 4 : 0); }
 };
 
-// Many rows: the waves share the tiles and have rows of their own; one barrier a tile, NS - 1 tiles on their way.
+// Many rows: the waves share the tiles and have rows of their own; one barrier a tile, NS - 1 tiles on their way.  What bounds it: issue.  A tile of 64 keys against a wave's 32 rows of 128 is 1024
+// clocks of matrix products and 3200 to 3700 of a lone wave's time (scores and exponentials 1450 to 1680, weighted sums 770 to 880, asking 380 to 470, references 330, the barrier 110), 2400 of each of two
+// on a SIMD; 580 TFLOP/s over the call below.  (8 sequences of 60 nodes with 4096 shared rows of 8 KV heads of 128, 32 query heads: 59 us, and 7 for the join.)  At head_dim 64 a wave of 16 rows is held to 128
+// registers, four waves a SIMD: 33 nodes of 32 sequences in groups 44.5 -> 40.2 us.
 template <int D, int QT, int WR, int NS, bool SPARSE>
 __global__ __launch_bounds__(64 * WR, D == 64 && QT == 1 && !SPARSE ? 4 : 2) void paged_rows_kernel(PLAIN, PagedAttnArgs first)
 {
@@ -1489,6 +1494,8 @@ Load load_of(int D, const Problem &p, const Kind &k)
 }
 float sixth_roots_power(float us, float memory)
 {
+    us *= 1e-3f;                          // (in ms: the longest calls take seconds, and 3e38 is not far from the sixth power of their microseconds)
+    memory *= 1e-3f;
     us *= us * us;
     memory *= memory * memory;
     return us * us + memory * memory;
@@ -1512,6 +1519,9 @@ float choose(int D, bool f32, const Problem &p, bool joined, int most, Segment &
     const int tiles = q_tiles_override(), waves = tile_waves_override(), forced = kv_splits_override();
     const float memory = (p.bytes + (p2 ? p2->bytes : 0.0f)) / MEMORY + 5.0f;
     float best = INFINITY;
+    out = Segment{};
+    if (p2)
+        *out2 = Segment{};
     auto consider = [&](const Kind &k) {
         const Load x = load_of(D, p, k), y = p2 ? load_of(D, *p2, k) : Load{};
         for (int m : SPLITS) {
@@ -1523,7 +1533,7 @@ float choose(int D, bool f32, const Problem &p, bool joined, int most, Segment &
                     break;
                 const int splits = !forced ? n : forced < room ? forced : room;
                 const float us = launch_time(k, x, splits, joined, p2 ? &y : nullptr, forced ? splits : m, memory);
-                if (us < best) {
+                if (us < best || !out.part.splits) {      // (the first, whatever it takes)
                     best = us;
                     out.shape = k.shape;
                     out.part.splits = splits;
@@ -1546,13 +1556,13 @@ float choose(int D, bool f32, const Problem &p, bool joined, int most, Segment &
             if (of_form && (!tiles || k.shape.qt == tiles || (last && tiles > k.shape.qt)))
                 consider(k);
         }
-        if (best == INFINITY)
+        if (!out.part.splits)
             consider(KIND[kinds_of(D)][0]);
     }
     out.part.row_groups = (int)row_groups_of(p, out.shape);
     if (p2)
         out2->part.row_groups = (int)row_groups_of(*p2, out2->shape);
-    return powf(best, 1.0f / 6.0f);
+    return 1e3f * powf(best, 1.0f / 6.0f);
 }
 
 // Pages that a workgroup's rows may see, those of the tree included: what its lists, of all splits together, have to hold

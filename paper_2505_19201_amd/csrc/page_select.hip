@@ -8,6 +8,8 @@
 // Two launches.  score_kernel: S^T = pages x nodes by v_mfma_i32_16x16x64_i8, the parts c+ against U and c- against W one behind the other.  The heads' numbers add up before the product (it is linear in
 // them): the sum, at most 64 * 127, goes in as two numbers, 64 hi + lo.  choose_kernel: a wave per node finds the n_best-th score by halving the range of the scores, taken as whole numbers
 // in their order, until as many lie above as are wanted; where equal scores straddle the border the lower pages win.  (Sixteen waves for the only node of a step of one token.)
+// What bounds them: trips to memory and, in the second, some twenty halvings one behind the other (8 sequences of 60 nodes, 250 pages of 64 rows, 8 KV heads of 128: 8.5 and 6.1 us; one node, 2047
+// pages: 5.8 and 8.4; 4 sequences of 33 nodes, 376 pages, 8 KV heads of 256: 8.5 and 6.7).
 #include <type_traits>
 #include "paged.h"
 

@@ -65,7 +65,7 @@ class Problem:
         self.desc = dream.attn_desc(B, Hq, Hkv, D, dream.BF16 if dtype == "bf16" else dream.F32, 0, scale)
         self.pd = dream.page_desc(page, self.pages.n_pages, self.pages.max_pages)
         self.table, self.len, self.par = self.pages.device_table(), wc.ints(prefix), wc.ints(self.parent)
-        self.groups = (len(groups), wc.ints([g[0] for g in groups] + [B]) if groups else None, wc.ints([g[2] for g in groups]) if groups else None,
+        self.groups = (len(groups), wc.ints([g[0] for g in groups] + [groups[-1][0] + groups[-1][1]]) if groups else None, wc.ints([g[2] for g in groups]) if groups else None,
                        max([g[2] for g in groups], default=0))
         self.max_kv = max(prefix) + T
         self.out = torch.full(self.q.shape, 7.0, dtype=self.q.dtype, device="cuda")
@@ -142,6 +142,7 @@ SHARED = [
     (4, 2, 64, 9, [70, 71, 64], 16, dict(dtype="f32", groups=[(0, 3, 50)])),
     (4, 2, 64, 5, [50, 70, 64, 90], 16, dict(groups=[(2, 2, 48)])),                          # sequences in front of the first group
     (4, 2, 128, 40, [50, 70, 64], 16, dict(groups=[(1, 2, 48)])),
+    (4, 2, 64, 5, [50, 70, 64, 90], 16, dict(groups=[(1, 2, 48)])),                          # and behind the last
     (4, 2, 64, 5, [50, 70, 64], 16, dict(groups=[(2, 1, 48)], dtype="f32")),
     (4, 2, 128, 9, [70, 71, 64], 64, dict(groups=[(0, 3, 50)], scale=-0.2)),
 ]

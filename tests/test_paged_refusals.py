@@ -1,6 +1,8 @@
 """No-GPU checks of what the calls for caches in pages refuse before anything is launched, at the limits that include/dream.h states, and of the definitions that the GPU tests compare with."""
 import ctypes as C
 import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -169,6 +171,18 @@ def test_workspaces(lib, call):
     else:                                             # a list holds 1024 pages
         assert call(desc=d, pages=pages, n_tree=60, max_kv_len=70000, workspace_bytes=2 * 2 * 60 * 32 * 130 * 4 - 1) == -3
         assert str(size(d, pages, 60, 70000)) in dream.dream_last_error()
+
+
+def test_launches_stay_within_their_limits(lib, tmp_path):
+    """tests/c/paged_launch_check.c stands in for HIP's launch functions: 22 kernels have a raised limit (4, 4 and 3 shapes at the three head_dims, each with and without selected pages), all are launched."""
+    gcc = shutil.which("gcc")
+    if gcc is None:
+        pytest.skip("no gcc")
+    root, libdir, exe = os.path.dirname(os.path.dirname(os.path.abspath(__file__))), os.path.dirname(dream.library_path()), str(tmp_path / "paged_launch_check")
+    subprocess.run([gcc, "-std=c99", "-Wall", "-Wextra", "-Werror", "-rdynamic", "-I", os.path.join(root, "include"), os.path.join(root, "tests", "c", "paged_launch_check.c"), "-o", exe,
+                    "-L", libdir, "-ldream", "-Wl,-rpath," + libdir], check=True, capture_output=True, text=True)
+    p = subprocess.run([exe], capture_output=True, text=True)
+    assert p.returncode == 0 and p.stdout.count("22 with a raised limit") == 2, p.stdout[-3000:] + p.stderr[-1000:]
 
 
 @every
