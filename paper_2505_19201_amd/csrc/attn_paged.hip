@@ -411,13 +411,30 @@ __device__ __forceinline__ uint32_t four_nodes(const PagedAttnArgs &a, uint64_t 
 }
 
 // ---- row by row ------------------------------------------------------------------------------------------------------
+// The sum over groups of N lanes (8 to 64), in all of them: neighbours, pairs, halves of a row of sixteen turned round, rows
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xf, 0xf, true)); }
+template <int N>
+__device__ __forceinline__ float lanes_sum(float x)
+{
+    x += from_lane<0xb1>(x);              // quad_perm [1, 0, 3, 2]
+    x += from_lane<0x4e>(x);              // quad_perm [2, 3, 0, 1]
+    x += from_lane<0x141>(x);             // row_half_mirror
+    if constexpr (N > 8)
+        x += from_lane<0x140>(x);         // row_mirror
+    if constexpr (N > 16)
+        x += __shfl_xor(x, 16);
+    if constexpr (N > 32)
+        x += __shfl_xor(x, 32);
+    return x;
+}
 // LDS of attend_rows_singly: masks, parents, the list
 int single_bytes(int cap, int words) { return cap * words * 8 + DREAM_MAX_TREE * 4; }
 
 // The workgroup's rows, one to a wave at a time.  64 keys: each lane looks one up, then 16 bytes of a row are a lane's, so that a wave reads several whole rows at a time; keys and values are asked for
 // together.  What the node does not see has no weight, whatever it holds.  Where the keys are shared out, a workgroup has every splits-th run of `run` keys from the tile of `tile` keys on that holds
 // the first.  (A lane with a key's whole product, and values key by key: 60 nodes x 764 keys x 32 heads of 128 in
-// float32 146 us, so 110; 21 nodes x 121 keys x 4 heads of 64 13.0 and 8.8.  A step of 64 keys takes 2.5 us at 64, 6.5 at 128: trips to memory.)
+// float32 146 us, so 78; 21 nodes x 121 keys x 4 heads of 64 13.0 and 8.0.  A step of 64 keys takes 1.7 us at 64, 4 at 128.)
 template <class T, int D, int THREADS, bool SPARSE>
 __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const Unit &u, int cap, int tile, int run, unsigned char *smem)
 {
@@ -453,7 +470,7 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
             const bool in_prefix = (kind & 1) && pos >= u.lo && pos < limit && (!SPARSE || (word[w.node >> 6] >> (w.node & 63) & 1));
             const bool in_tree = (kind & 2) && !u.shared && node >= 0 && node < a.n_tree && (masks[j * a.words + (node >> 6)] >> (node & 63) & 1);
             const uint64_t seen = __ballot(there && (in_prefix || in_tree));
-            const int64_t row = ((((int64_t)page * a.hkv + u.kvh) << a.lg_page) + (pos & ps_mask)) * D;
+            const uint32_t row = (((uint32_t)page * a.hkv + u.kvh) << a.lg_page) + (pos & ps_mask);      // (of the pool; 2^32 of the shortest rows are 512 GB)
 #pragma unroll 1
             for (int k0 = 0; k0 < 64; k0 += BATCH * G) {
                 if (!(seen >> k0 & (BATCH * G == 64 ? ~0ull : (1ull << (BATCH * G & 63)) - 1)))
@@ -462,10 +479,12 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
 #pragma unroll
                 for (int i = 0; i < BATCH; i++) {
                     const int key = k0 + i * G + in_group;
-                    const int64_t of = (int64_t)((uint64_t)(uint32_t)__shfl((int)(row >> 32), key) << 32 | (uint32_t)__shfl((int)row, key)) + piece * N;
+                    const int64_t of = (int64_t)(uint32_t)__shfl((int)row, key) * D + piece * N;
                     k[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const T *>(a.k) + of);
                     v[i] = *reinterpret_cast<const u32x4 *>(reinterpret_cast<const T *>(a.v) + of);
                 }
+                if constexpr (BATCH * G < 64)
+                    __builtin_amdgcn_sched_barrier(0);      // all are asked for before the first is looked at: 900 keys of 128 float32 94 -> 63 us; of 64, where they are all 64 keys, 30 -> 33
                 float s[BATCH], top = m;
 #pragma unroll
                 for (int i = 0; i < BATCH; i++) {
@@ -473,9 +492,7 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
 #pragma unroll
                     for (int e = 0; e < N; e++)
                         x = __builtin_fmaf(value(k[i], e), value(q, e), x);
-#pragma unroll
-                    for (int d = 1; d < LANES; d *= 2)
-                        x += __shfl_xor(x, d);
+                    x = lanes_sum<LANES>(x);
                     s[i] = seen >> (k0 + i * G + in_group) & 1 ? x * a.scale_log2 : -INFINITY;
                     top = fmaxf(top, s[i]);
                 }
@@ -511,12 +528,19 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
                 skip += a.list_size;
             } while (skip < list.all);
         } else {
-            for (int start = u.lo / tile * tile + u.split * run; start < u.hi; start += u.splits * run) {
-                const int end = min(start + run, u.hi);
-                for (int x0 = start; x0 < end; x0 += 64) {
-                    const int pos = x0 + lane;
-                    keys(pos < end, min(max(table[min(pos, u.hi - 1) >> a.lg_page], 0), a.n_pages - 1), pos, 3, nullptr);
+            // the pages of the keys that come next are asked for ahead of these
+            auto page_of = [&](int x0) { return table[min(x0 + lane, u.hi - 1) >> a.lg_page]; };
+            int start = u.lo / tile * tile + u.split * run, x0 = start, page = start < u.hi ? page_of(x0) : 0;
+            while (start < u.hi) {
+                const int end = min(start + run, u.hi), now = x0, id = page;
+                x0 += 64;
+                if (x0 >= end) {
+                    start += u.splits * run;
+                    x0 = start;
                 }
+                if (start < u.hi)
+                    page = page_of(x0);
+                keys(now + lane < end, min(max(id, 0), a.n_pages - 1), now + lane, 3, nullptr);
             }
         }
 #pragma unroll
