@@ -1402,7 +1402,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const float *part_o, co
                                                          uint32_t hkv_magic, uint32_t group, uint32_t group_magic, int hq, int n_tree)
 {
     constexpr int LANES = D / 4;
-    const uint32_t id = blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const uint32_t id = blockIdx.x * (blockDim.x / LANES) + threadIdx.x / LANES;
     const int ch = threadIdx.x % LANES;
     if (id >= all_rows)
         return;
@@ -1724,7 +1724,8 @@ int launch_all(PagedAttnArgs &a, const PagedPlan &p, bool f32, hipStream_t st)
     if (p.n_slots == 1)
         return DREAM_OK;
     auto join = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(ceil_div(p.all_rows, 256 / (D / 4))), dim3(256), 0, st, a.part_o, a.part_ml, a.out, a.lse, (uint32_t)p.all_rows, p.n_slots, a.rows, a.rows_magic, a.hkv,
+        const int threads = p.all_rows * (D / 4) <= 64 * 1024 ? 64 : 256;      // few rows over all CUs
+        hipLaunchKernelGGL(kernel, dim3(ceil_div(p.all_rows, threads / (D / 4))), dim3(threads), 0, st, a.part_o, a.part_ml, a.out, a.lse, (uint32_t)p.all_rows, p.n_slots, a.rows, a.rows_magic, a.hkv,
                            a.hkv_magic, a.group, a.group_magic, a.hq, a.n_tree);
     };
     if (f32)
