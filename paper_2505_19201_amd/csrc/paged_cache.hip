@@ -257,7 +257,7 @@ int launch_append(const AppendArgs &a, bool paired, bool wide, int64_t rows, hip
 {
     constexpr int N = 16 / sizeof(T);
     auto *kernel = paired ? (wide ? &append_kernel<T, true, N> : &append_kernel<T, true, 2>) : wide ? &append_kernel<T, false, N> : &append_kernel<T, false, 1>;
-    const int64_t parts = 1024 / rows, most = (a.end_v + 255) / 256;
+    const int64_t most = (a.end_v + 255) / 256, least = (a.end_v + 256 * BATCH - 1) / (256 * BATCH), parts = 1024 / rows > least ? 1024 / rows : least;      // no more than a thread has in flight (685 rows of 96 float32 heads of 128 18.2 -> 15.4 us)
     hipLaunchKernelGGL(kernel, dim3((unsigned)rows, (unsigned)(parts < 1 ? 1 : parts < most ? parts : most)), dim3(256), 0, st, a.row_base, a.table,
                        a.pos_base, static_cast<const T *>(a.q), static_cast<const T *>(a.k), static_cast<const T *>(a.v), a.n_rows, a.rows_magic, a.max_pages, a.lg_page, a.hq, a.hkv, a.pieces_magic,
                        a.vpieces_magic, static_cast<T *>(a.q_out), static_cast<T *>(a.k_pages), static_cast<T *>(a.v_pages), a);
@@ -339,17 +339,18 @@ struct BoundsArgs {
     int32_t hkv, lg_page, n_pages, max_pages, slots;
 };
 
-// A workgroup per page of a sequence's run, and head: a thread has 16 bytes of a row, the rows of a page are shared out over 256 / (row / 16) threads; those of a wave meet by exchange, the waves in
-// LDS.  (Plain arguments: they are in registers when a wave starts.)
-template <class T, int D>
+// A page of a sequence's run and head: TEAM waves, 4 (a workgroup) or, where that is at most 8 KB, 1.  A thread has 16 bytes of a row, the rows of a page are shared out over 64 TEAM / (row / 16) threads;
+// those of a wave meet by exchange, the waves in LDS.  (Plain arguments: they are in registers when a wave starts.)  One wave a page of 4 KB: 126 pages of 32 heads of 64 12.5 -> 7.3 us.
+template <class T, int D, int TEAM>
 __global__ __launch_bounds__(256) void bounds_kernel(const int32_t *table, const int32_t *from_len, const int32_t *to_len, const T *k, int lg_page, int max_pages, int n_pages, int hkv, int slots, T *bounds)
 {
-    constexpr int N = 16 / sizeof(T), PER_ROW = D / N, ROWS = 256 / PER_ROW;
-    __shared__ __attribute__((aligned(16))) float s_ends[4][2][D];      // of a wave's rows: largest and smallest
-    const int b = blockIdx.z, h = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, c = tid % PER_ROW, r0 = tid / PER_ROW;
+    constexpr int N = 16 / sizeof(T), PER_ROW = D / N, ROWS = 64 * TEAM / PER_ROW;
+    __shared__ __attribute__((aligned(16))) float s_ends[TEAM == 4 ? 4 : 1][2][D];      // of a wave's rows: largest and smallest
+    const int wave = threadIdx.x >> 6, tid = TEAM == 4 ? threadIdx.x : threadIdx.x & 63, c = tid % PER_ROW, r0 = tid / PER_ROW;
+    const int b = blockIdx.z, h = TEAM == 4 ? blockIdx.y : blockIdx.y * 4 + wave;
     const int ps = 1 << lg_page, rows = max_pages << lg_page;
     const int from = from_len ? min(max(uniform_load(from_len + b), 0), rows) : 0, to = min(uniform_load(to_len + b), rows);
-    if (to <= from)
+    if (to <= from || h >= hkv)
         return;
     for (int i = (from >> lg_page) + blockIdx.x; (i << lg_page) < to; i += slots) {
         const int page = uniform_load(table + (int64_t)b * max_pages + i);
@@ -380,46 +381,53 @@ __global__ __launch_bounds__(256) void bounds_kernel(const int32_t *table, const
                 most[e] = fmaxf(most[e], __shfl_xor(most[e], d));
                 least[e] = fminf(least[e], __shfl_xor(least[e], d));
             }
-        if ((tid & 63) < PER_ROW)
+        if constexpr (TEAM == 4) {
+            if ((tid & 63) < PER_ROW)
 #pragma unroll
-            for (int e = 0; e < N; e += 4) {
-                *reinterpret_cast<f32x4 *>(&s_ends[wave][0][c * N + e]) = f32x4{most[e], most[e + 1], most[e + 2], most[e + 3]};
-                *reinterpret_cast<f32x4 *>(&s_ends[wave][1][c * N + e]) = f32x4{least[e], least[e + 1], least[e + 2], least[e + 3]};
-            }
-        __syncthreads();
+                for (int e = 0; e < N; e += 4) {
+                    *reinterpret_cast<f32x4 *>(&s_ends[wave][0][c * N + e]) = f32x4{most[e], most[e + 1], most[e + 2], most[e + 3]};
+                    *reinterpret_cast<f32x4 *>(&s_ends[wave][1][c * N + e]) = f32x4{least[e], least[e + 1], least[e + 2], least[e + 3]};
+                }
+            __syncthreads();
+        }
         if (tid < PER_ROW) {
             Piece<T, N> up, down;
-            float high[N], low[N];
 #pragma unroll
             for (int e = 0; e < N; e++) {
-                high[e] = s_ends[0][0][tid * N + e], low[e] = s_ends[0][1][tid * N + e];
+                if constexpr (TEAM == 4) {
+                    most[e] = s_ends[0][0][tid * N + e], least[e] = s_ends[0][1][tid * N + e];
 #pragma unroll
-                for (int w = 1; w < 4; w++) {
-                    high[e] = fmaxf(high[e], s_ends[w][0][tid * N + e]);
-                    low[e] = fminf(low[e], s_ends[w][1][tid * N + e]);
+                    for (int w = 1; w < 4; w++) {
+                        most[e] = fmaxf(most[e], s_ends[w][0][tid * N + e]);
+                        least[e] = fminf(least[e], s_ends[w][1][tid * N + e]);
+                    }
                 }
-                const bool finite = high[e] <= FLT_MAX && low[e] >= -FLT_MAX;
-                high[e] = finite ? high[e] : INFINITY;
-                low[e] = finite ? low[e] : -INFINITY;
+                const bool finite = most[e] <= FLT_MAX && least[e] >= -FLT_MAX;
+                most[e] = finite ? most[e] : INFINITY;
+                least[e] = finite ? least[e] : -INFINITY;
             }
 #pragma unroll
             for (int e = 0; e < N; e += 2) {
-                up.set(e, high[e], high[e + 1]);
-                down.set(e, low[e], low[e + 1]);
+                up.set(e, most[e], most[e + 1]);
+                down.set(e, least[e], least[e + 1]);
             }
             T *dst = bounds + ((int64_t)page * hkv + h) * 2 * D + tid * N;
             up.store(dst);
             down.store(dst + D);
         }
-        __syncthreads();
+        if constexpr (TEAM == 4)
+            __syncthreads();
     }
 }
 
 template <class T>
 int launch_bounds(const BoundsArgs &a, int D, int B, hipStream_t st)
 {
-    auto *kernel = D == 64 ? &bounds_kernel<T, 64> : D == 128 ? &bounds_kernel<T, 128> : &bounds_kernel<T, 256>;
-    hipLaunchKernelGGL(kernel, dim3(a.slots, a.hkv, B), dim3(256), 0, st, a.table, a.from_len, a.to_len, static_cast<const T *>(a.k), a.lg_page, a.max_pages, a.n_pages, a.hkv, a.slots,
+    const bool small = ((int64_t)D * sizeof(T) << a.lg_page) <= 8192;
+    auto *kernel = D == 64    ? (small ? &bounds_kernel<T, 64, 1> : &bounds_kernel<T, 64, 4>)
+                   : D == 128 ? (small ? &bounds_kernel<T, 128, 1> : &bounds_kernel<T, 128, 4>)
+                              : (small ? &bounds_kernel<T, 256, 1> : &bounds_kernel<T, 256, 4>);
+    hipLaunchKernelGGL(kernel, dim3(a.slots, small ? (a.hkv + 3) / 4 : a.hkv, B), dim3(256), 0, st, a.table, a.from_len, a.to_len, static_cast<const T *>(a.k), a.lg_page, a.max_pages, a.n_pages, a.hkv, a.slots,
                        static_cast<T *>(a.bounds));
     return check_launch("bounds_kernel");
 }

@@ -154,7 +154,7 @@ def test_commit_drops_rows_of_pages_that_are_none():
     assert torch.equal(pool, want)
 
 
-@pytest.mark.parametrize("Hkv,D,page,dtype", [(2, 64, 16, "bf16"), (3, 128, 64, "bf16"), (1, 256, 256, "bf16"), (2, 128, 32, "f32"), (2, 64, 128, "f32"), (2, 256, 16, "f32")])
+@pytest.mark.parametrize("Hkv,D,page,dtype", [(2, 64, 16, "bf16"), (3, 128, 64, "bf16"), (1, 256, 256, "bf16"), (2, 128, 32, "f32"), (2, 64, 128, "f32"), (2, 256, 16, "f32"), (5, 64, 32, "bf16"), (3, 128, 16, "f32"), (6, 256, 16, "bf16")])
 @pytest.mark.parametrize("max_new", [1, 40, 10 ** 6])
 def test_bounds(Hkv, D, page, dtype, max_new):
     rng = np.random.default_rng([Hkv, D, page])
