@@ -1724,7 +1724,7 @@ int launch_all(PagedAttnArgs &a, const PagedPlan &p, bool f32, hipStream_t st)
     if (p.n_slots == 1)
         return DREAM_OK;
     auto join = [&](auto kernel) {
-        const int threads = p.all_rows * (D / 4) <= 64 * 1024 ? 64 : 256;      // few rows over all CUs
+        const int threads = p.all_rows * (D / 4) <= 64 * 1024 ? 64 : 256;      // few rows over all CUs (256 rows of 256, 24 parts: 7.2 -> 6.4 us; fewer parts: no difference)
         hipLaunchKernelGGL(kernel, dim3(ceil_div(p.all_rows, threads / (D / 4))), dim3(threads), 0, st, a.part_o, a.part_ml, a.out, a.lse, (uint32_t)p.all_rows, p.n_slots, a.rows, a.rows_magic, a.hkv,
                            a.hkv_magic, a.group, a.group_magic, a.hq, a.n_tree);
     };

@@ -7,7 +7,7 @@
 //
 // Two launches.  score_kernel: S^T = pages x nodes by v_mfma_i32_16x16x64_i8, the parts c+ against U and c- against W one behind the other.  The heads' numbers add up before the product (it is linear in
 // them): the sum, at most 64 * 127, goes in as two numbers, 64 hi + lo.  choose_kernel: a wave per node finds the n_best-th score by halving the range of the scores, taken as whole numbers
-// in their order, until as many lie above as are wanted; where equal scores straddle the border the lower pages win.  (Sixteen waves for the only node of a step of one token.)
+// in their order, until as many lie above as are wanted; where equal scores straddle the border the lower pages win.  (Sixteen waves where there is one node and many pages.)
 // What bounds them: trips to memory and, in the second, some twenty halvings one behind the other (8 sequences of 60 nodes, 250 pages of 64 rows, 8 KV heads of 128: 8.5 and 6.1 us; one node, 2047
 // pages: 5.8 and 8.4; 4 sequences of 33 nodes, 376 pages, 8 KV heads of 256: 8.5 and 6.7).
 #include <type_traits>
@@ -435,8 +435,9 @@ int launch_select(const SelectArgs &a, int D, int B, hipStream_t st)
         hipLaunchKernelGGL(kernel, dim3(ceil_div(a.n_tree, nodes), a.hkv, B), dim3(threads), 0, st, a.keys, a.prefix_len, a.page_nodes, a.n_tree, a.hkv, a.stride, a.max_pages, a.max_prefix, a.lg_page, a.n_first,
                            a.n_last, a.n_best);
     };
-    // One token: all of a workgroup's waves rank its pages together
-    if (a.n_tree == 1 && a.stride > 256 && a.stride <= 8192)
+    // One token, many pages: all of a workgroup's waves rank them together.  (With the scores, sixteen waves and one, us: 500 pages 12.0 and 10.3, 1000 13.0 and 13.6, 2000 14.4 and 21.0; of eight
+    // sequences 16.5 and 13.3, 21.7 and 21.5, 30.6 and 36.9.)
+    if (a.n_tree == 1 && a.stride > 1024 && a.stride <= 8192)
         choose(a.stride <= 2048 ? &choose_kernel<2, 16> : &choose_kernel<8, 16>, 1, 1024);
     else
         choose(a.stride <= 128    ? &choose_kernel<2, 1>

@@ -339,8 +339,9 @@ struct BoundsArgs {
     int32_t hkv, lg_page, n_pages, max_pages, slots;
 };
 
-// A page of a sequence's run and head: TEAM waves, 4 (a workgroup) or, where that is at most 8 KB, 1.  A thread has 16 bytes of a row, the rows of a page are shared out over 64 TEAM / (row / 16) threads;
-// those of a wave meet by exchange, the waves in LDS.  (Plain arguments: they are in registers when a wave starts.)  One wave a page of 4 KB: 126 pages of 32 heads of 64 12.5 -> 7.3 us.
+// A page of a sequence's run and head: TEAM waves, 4 (a workgroup) or, where that is at most 8 KB, or 16 of many, 1.  A thread has 16 bytes of a row, the rows of a page are shared out over 64 TEAM / (row / 16) threads;
+// those of a wave meet by exchange, the waves in LDS.  (Plain arguments: they are in registers when a wave starts.)  Four waves and one, us: 126
+// pages of 32 heads of 64, 4 KB 13.5 and 6.5, 66 of 8 KB 9.4 and 6.0; 256 of 8 heads of 128, 16 KB 8.3 and 7.1; 128 of 8 heads of 256, 16 KB 4.95 both; one of 8 heads, 8 KB 4.2 and 4.1, 16 KB 4.1 and 4.8.
 template <class T, int D, int TEAM>
 __global__ __launch_bounds__(256) void bounds_kernel(const int32_t *table, const int32_t *from_len, const int32_t *to_len, const T *k, int lg_page, int max_pages, int n_pages, int hkv, int slots, T *bounds)
 {
@@ -423,7 +424,8 @@ __global__ __launch_bounds__(256) void bounds_kernel(const int32_t *table, const
 template <class T>
 int launch_bounds(const BoundsArgs &a, int D, int B, hipStream_t st)
 {
-    const bool small = ((int64_t)D * sizeof(T) << a.lg_page) <= 8192;
+    const int64_t bytes = (int64_t)D * sizeof(T) << a.lg_page, units = (int64_t)a.slots * a.hkv * B;
+    const bool small = bytes <= 8192 || (bytes <= 16384 && units >= 2048);
     auto *kernel = D == 64    ? (small ? &bounds_kernel<T, 64, 1> : &bounds_kernel<T, 64, 4>)
                    : D == 128 ? (small ? &bounds_kernel<T, 128, 1> : &bounds_kernel<T, 128, 4>)
                               : (small ? &bounds_kernel<T, 256, 1> : &bounds_kernel<T, 256, 4>);
