@@ -531,12 +531,12 @@ def _plain_attend(s):
 
 
 def _exponent(top):
-    """The least whole e in [-100, 122] with top <= 127 * 2^e."""
-    return (((top.float().view(torch.int32) + 0x1FFFF) >> 23) - 133).clamp(-100, 122)
+    """The least whole e in [-100, 121] with top <= 127 * 2^e."""
+    return (((top.float().view(torch.int32) + 0x1FFFF) >> 23) - 133).clamp(-100, 121)
 
 
 def _scale(e):
-    """2^e in float32, |e| <= 122."""
+    """2^e in float32, |e| <= 121."""
     return ((e + 127) << 23).view(torch.float32)
 
 
@@ -671,9 +671,9 @@ def _exact_append(s):
 
 
 def _least_power(top):
-    """Least whole e in [-100, 122] with top <= 127 * 2^e, of numpy arrays in 64 bits."""
+    """Least whole e in [-100, 121] with top <= 127 * 2^e, of numpy arrays in 64 bits."""
     m, e = np.frexp(top / 127.0)
-    return np.where(top > 0, np.clip(e - (m == 0.5), -100, 122), -100)
+    return np.where(top > 0, np.clip(e - (m == 0.5), -100, 121), -100)
 
 
 def _exact_choice(s, l, b, walk_len, table):
