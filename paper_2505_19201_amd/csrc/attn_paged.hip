@@ -612,9 +612,16 @@ __device__ __forceinline__ float largest(f32x4 a) { return fmaxf(fmaxf(fmaxf(a[0
 
 // The query rows of a wave, QT tiles of 16, and their sums.  Lane (c, g) = (lane % 16, lane / 16) has of row c: of the queries the channels 8 g .. of every 32; of O^T the channels
 // 16 dt + 4 g + r; and scores of the keys 4 g + r of every 16.  A step takes NC chunks of 16 keys.
-template <int D, int QT, int NC, bool SPARSE>
+//
+// A weight goes into the second product as PIECES bf16 numbers, its value rounded and what that leaves: with two of them what is lost is 2^-16 of it, with one 2^-8, as much as the row's own rounding
+// (against 64 bits rows are off by 0.0017 and by 0.0023 of their size, root mean square).  Two where that costs little: bf16 weights in one part and in two, us a layer,
+//   keys, 128: one sequence, 60 nodes x 764 keys 12.2 and 12.4; 8 sequences, one node x 16 100 keys 86.1 and 86.1
+//   rows, 256: 16 sequences, one node x 8011 shared keys 31.2 and 32.0; selected pages, 4 x 33 nodes 66.9 and 70.0 (attention 44 of them)
+//   rows, 128: 8 x 60 nodes x 4096 shared keys 60.8 and 90.3 (the registers do not hold both), selected pages 86.5 and 94.3; 64: 32 x 33 nodes x 1600 shared keys 45.3 and 53.5; so one there
+template <int D, int QT, int NC, bool SPARSE, int PIECES>
 struct QueryRows {
     static constexpr int ROW = 2 * D, NKS = D / 32, NDT = D / 16;
+    typedef bf16x8 Weights[PIECES][NC / 2][QT];
     bf16x8 qf[QT][NKS];
     f32x4 o[QT][NDT];
     float m[QT], l[QT];
@@ -759,7 +766,7 @@ struct QueryRows {
         }
     }
     // Second half: the weights of slice i (query tile i % QT, chunk i / QT), and their sum
-    __device__ __forceinline__ void weigh(float scaled, uint32_t in, int i, const f32x4 (&s)[NC][QT], bf16x8 (&pf)[NC / 2][QT])
+    __device__ __forceinline__ void weigh(float scaled, uint32_t in, int i, const f32x4 (&s)[NC][QT], Weights &pf)
     {
         const int qt = i % QT, h = i / QT;
         const float ref = fmaxf(m[qt], -FLT_MAX);      // where all scores so far are -inf, their weight is 0 and not exp(-inf + inf)
@@ -769,14 +776,16 @@ struct QueryRows {
 #pragma unroll
         for (int r = 0; r < 4; r++) {
             p[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[h][qt][r], mult, less));
-            pf[h / 2][qt][h % 2 * 4 + r] = (__bf16)p[r];      // rounded as the matrix instruction takes it, half a step of 2^-8; the sum stays float32
+            pf[0][h / 2][qt][h % 2 * 4 + r] = (__bf16)p[r];      // (the sum stays float32, of the weights as they were)
+            if constexpr (PIECES > 1)
+                pf[1][h / 2][qt][h % 2 * 4 + r] = (__bf16)(p[r] - (float)(__bf16)p[r]);
         }
         l[qt] += (p[0] + p[1]) + (p[2] + p[3]);
     }
     static constexpr int SLICES = NC * QT, STEPS = NC / 2 * NKS;
     // The scores of the next step, and meanwhile this one's weights: every STEPS-th part of the products (two chunks, 32 channels) is followed by its part of the weights, and its keys are asked
     // for two parts ahead.  (Left to itself the compiler asks for them when it needs them: 1621 clocks for a tile of 64 keys and 32 rows of 128; 512 of matrix products.)
-    __device__ __forceinline__ void scores_and_weights(const unsigned char *kt, int foff, f32x4 (&next)[NC][QT], float scaled, uint32_t in, const f32x4 (&s)[NC][QT], bf16x8 (&pf)[NC / 2][QT])
+    __device__ __forceinline__ void scores_and_weights(const unsigned char *kt, int foff, f32x4 (&next)[NC][QT], float scaled, uint32_t in, const f32x4 (&s)[NC][QT], Weights &pf)
     {
         constexpr int AHEAD = STEPS < 2 ? STEPS : 2;
         bf16x8 kf[AHEAD + 1][2];
@@ -809,7 +818,7 @@ struct QueryRows {
         }
     }
     // O^T += V^T P^T; values are asked for two parts (16 channels of 32 keys) ahead of their products
-    __device__ __forceinline__ void add_values(const unsigned char *vt, int voff, const bf16x8 (&pf)[NC / 2][QT])
+    __device__ __forceinline__ void add_values(const unsigned char *vt, int voff, const Weights &pf)
     {
         constexpr int PARTS = NC / 2 * NDT, AHEAD = 4;
         bf16x8 vf[AHEAD + 1];
@@ -827,8 +836,10 @@ struct QueryRows {
             if (i + AHEAD < PARTS)
                 ask(i + AHEAD);
 #pragma unroll
-            for (int qt = 0; qt < QT; qt++)
-                o[qt][i % NDT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i % (AHEAD + 1)], pf[i / NDT][qt], o[qt][i % NDT], 0, 0, 0);
+            for (int part = 0; part < PIECES; part++)
+#pragma unroll
+                for (int qt = 0; qt < QT; qt++)
+                    o[qt][i % NDT] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i % (AHEAD + 1)], pf[part][i / NDT][qt], o[qt][i % NDT], 0, 0, 0);
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -978,7 +989,7 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
     if constexpr (SPARSE)
         list.build(first, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (first.words > 1 ? G::CAP * first.words + DREAM_MAX_TREE / 2 : 0)), 0);
     const PagedAttnArgs &a = SPARSE ? args_again() : first;
-    QueryRows<D, QT, 2, SPARSE> rows;
+    QueryRows<D, QT, 2, SPARSE, 2> rows;
     rows.load(a, u, u.row0, c, g);
     const int tile0 = u.lo / 32;
     if (!SPARSE && !early)
@@ -1059,7 +1070,7 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
                 ch[1] = chunk(i, 1);
             }
             f32x4 s[2][QT];
-            bf16x8 pf[1][QT];
+            typename decltype(rows)::Weights pf;
             wait_loads<G::LOADS>();
             rows.scores(smem + stage, here(foff), 0, s);
             wait_lds();
@@ -1197,7 +1208,7 @@ __global__ __launch_bounds__(64 * WR, D == 64 && QT == 1 && !SPARSE ? 4 : 2) voi
     if constexpr (SPARSE)
         list.build(first, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (first.words > 1 ? G::CAP * first.words + DREAM_MAX_TREE / 2 : 0)), 0);
     const PagedAttnArgs &a = SPARSE ? args_again() : first;
-    QueryRows<D, QT, NC, SPARSE> rows;
+    QueryRows<D, QT, NC, SPARSE, D == 256 ? 2 : 1> rows;
     const int first_row = u.row0 + wave * QT * 16;
     rows.load(a, u, first_row, c, g);
     const int tile0 = u.lo / KEYS + u.split;
@@ -1262,7 +1273,7 @@ __global__ __launch_bounds__(64 * WR, D == 64 && QT == 1 && !SPARSE ? 4 : 2) voi
         t.masked = !straight || a.scale_log2 < 0.0f;      // (the largest score of a negative scale is the smallest product)
         t.scaled = t.masked ? 1.0f : a.scale_log2;
     };
-    bf16x8 pf[NC / 2][QT];
+    typename decltype(rows)::Weights pf;
     // Scores that have come: what nobody sees is left out, the references are raised
     auto settle = [&](int i, Tile &t) {
         if (t.masked) {
