@@ -10,6 +10,7 @@
 // in their order, until as many lie above as are wanted; where equal scores straddle the border the lower pages win.  (Sixteen waves where there is one node and many pages.)
 // What bounds them: trips to memory and, in the second, some twenty halvings one behind the other (8 sequences of 60 nodes, 250 pages of 64 rows, 8 KV heads of 128: 8.5 and 6.1 us; one node, 2047
 // pages: 5.8 and 8.4; 4 sequences of 33 nodes, 376 pages, 8 KV heads of 256: 8.5 and 6.7).
+#include <float.h>
 #include <type_traits>
 #include "paged.h"
 
@@ -76,7 +77,11 @@ template <class T, int UP>
 __device__ __forceinline__ i32x4 bound_codes(const Sixteen<T> &x, float scale)
 {
     i32x4 r;
-    auto code = [&](int i) { return (int)(UP ? ceilf(x[i] * scale) : floorf(x[i] * scale)); };
+    // (a product that is less than any float is still not 0: rounded outwards it is a whole step)
+    auto code = [&](int i) {
+        const float v = x[i], p = v * scale;
+        return (int)(UP ? ceilf(v > 0.0f ? fmaxf(p, FLT_MIN) : p) : floorf(v < 0.0f ? fminf(p, -FLT_MIN) : p));
+    };
 #pragma unroll
     for (int i = 0; i < 4; i++)
         r[i] = (int)bytes_of(code(4 * i), code(4 * i + 1), code(4 * i + 2), code(4 * i + 3));
