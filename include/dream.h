@@ -490,7 +490,8 @@ int dream_mx_verify_attn(const dream_attn_desc *desc, const void *q, const void 
  * dream_sparse_verify_attn: dream_paged_verify_attn where node i sees of the prefix only the rows of pages whose bit in
  *   page_nodes is set for it (as dream_page_select writes it, or the caller's own), and the tree as ever.  Pages that no node of a sequence
  *   sees are not read.
- *   max_pages_seen   about how many pages a node sees; only used to choose the launch shape, 0 if unknown
+ *   max_pages_seen   about how many pages a node sees; only used to choose the launch shape, 0 if unknown.  (Where more are seen a workgroup goes through
+ *                    them list by list: slower than had it been known, not by much.)
  * ------------------------------------------------------------------------------------------- */
 typedef struct {
     int32_t page_size;  /* rows of a page: 16, 32, 64, 128 or 256                              */

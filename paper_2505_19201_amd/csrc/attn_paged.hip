@@ -66,6 +66,19 @@ __device__ __forceinline__ uint32_t divide(uint32_t x, uint32_t d, uint32_t magi
     return x - q * d >= d ? q + 1 : q;
 }
 
+// The same value, from which the compiler forms nothing ahead of the loop it stands in: the addresses of a step are a few instructions, and all of them kept are more registers than there are.
+__device__ __forceinline__ int here(int x)
+{
+    asm volatile("" : "+v"(x));
+    return x;
+}
+__device__ __forceinline__ int here_scalar(int x)
+{
+    x = __builtin_amdgcn_readfirstlane(x);
+    asm volatile("" : "+s"(x));
+    return x;
+}
+
 // What a workgroup does.
 struct Unit {
     bool shared, alone;                                 // alone: outside every group, where there are some
@@ -177,7 +190,7 @@ __device__ __forceinline__ bool unit_of(const PagedAttnArgs &a, int cap, int lan
 constexpr int SPARSE_LIST = 1024;              // entries of a list (trees of up to 64 nodes; others half of that)
 constexpr uint32_t TREE_PAGE = 1u << 31;      // of an entry of `logical`: the tree's rows in it are meant, otherwise the prefix's
 
-// The pages of a sequence that some node of the workgroup's rows sees, and those of the tree: of them, by their rank, every splits-th, in LDS, from the `skip`-th of these on.  Rows of the list are numbered through its pages.
+// The pages of a sequence that some node of the workgroup's rows sees, and those of the tree: of them, by their rank, every splits-th, in LDS, `list_size` of them from the `skip`-th of these on.  Rows of the list are numbered through its pages.
 template <int THREADS>
 struct PageList {
     static constexpr int EACH = THREADS == 512 ? 2 : 4, SCAN = EACH * THREADS;      // pages looked at at a time: by a thread; by all
@@ -322,13 +335,28 @@ __device__ __forceinline__ int64_t row_of_part(const PagedAttnArgs &a, const Uni
 // Prefix positions below this are the row's
 __device__ __forceinline__ int row_limit(const PagedAttnArgs &a, const Unit &u, const Row &w) { return u.shared ? min(u.hi, clamped_prefix(a, a.prefix_len[w.b])) : u.P; }
 
-__device__ __forceinline__ void put_ml(const PagedAttnArgs &a, const Unit &u, const Row &w, float m, float l)
+// part: in its part's slot, not as the row's own
+__device__ __forceinline__ void put_ml(const PagedAttnArgs &a, const Unit &u, const Row &w, float m, float l, bool part)
 {
-    if (a.n_slots > 1)
+    if (part)
         a.part_ml[row_of_part(a, u, w)] = make_float2(m, l);
     else if (a.lse)
         a.lse[((int64_t)w.b * a.hq + w.head) * a.n_tree + w.node] = l == 0.0f ? -INFINITY : (m + __log2f(l)) * 0.6931471805599453f;
 }
+// A row's reference and sum so far, and what those and the sums of its channels are to be multiplied with, where a list is not the first of its workgroup: what the lists in front of it gave stands in the
+// part's slot.  By all lanes of the row; what one of them writes there afterwards comes after all have read it (they are lanes of one wave).
+struct Earlier {
+    float old, now;                     // factors of what the slot holds, and of this list's
+    __device__ __forceinline__ void join(const PagedAttnArgs &a, const Unit &u, const Row &w, float &m, float &l)
+    {
+        const float2 ml = a.part_ml[row_of_part(a, u, w)];
+        const float top = fmaxf(ml.x, m);
+        old = ml.x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.x - top);
+        now = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);
+        l = __builtin_fmaf(ml.y, old, l * now);
+        m = top;
+    }
+};
 // The rows of a sequence outside every group have empty shared parts
 __device__ __forceinline__ void no_shared_parts(const PagedAttnArgs &a, const Unit &u, int cap, int tid, int threads)
 {
@@ -440,7 +468,7 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
 {
     constexpr int NW = THREADS / 64, N = 16 / sizeof(T), LANES = D / N, G = 64 / LANES;      // values of a lane; lanes of a row; rows that a wave reads at a time
     constexpr int MOST = std::is_same_v<T, float> ? 16 : 4, BATCH = MOST < LANES ? MOST : LANES;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), piece = lane % LANES, in_group = lane / LANES;
+    const int tid = here(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), piece = lane % LANES, in_group = lane / LANES;
     const int count = min(cap, u.n_rows - u.row0), ps_mask = (1 << a.lg_page) - 1;
     uint64_t *masks = reinterpret_cast<uint64_t *>(smem);
     int32_t *parents = reinterpret_cast<int32_t *>(masks + cap * a.words);
@@ -553,7 +581,7 @@ __device__ __forceinline__ void attend_rows_singly(const PagedAttnArgs &a, const
         if (!mine || in_group)
             continue;
         if (lane == 0)
-            put_ml(a, u, w, m, l);
+            put_ml(a, u, w, m, l, a.n_slots > 1);
         if (a.n_slots > 1 || std::is_same_v<T, float>) {
             float *to = (a.n_slots > 1 ? a.part_o + row_of_part(a, u, w) * D : static_cast<float *>(a.out) + row_of_q(a, w) * D) + piece * N;
             const float divisor = a.n_slots > 1 ? 1.0f : l;
@@ -596,18 +624,6 @@ __device__ __forceinline__ void wait_loads()
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-// The same value, from which the compiler forms nothing ahead of the loop it stands in: the addresses of a step are a few instructions, and all of them kept are more registers than there are.
-__device__ __forceinline__ int here(int x)
-{
-    asm volatile("" : "+v"(x));
-    return x;
-}
-__device__ __forceinline__ int here_scalar(int x)
-{
-    x = __builtin_amdgcn_readfirstlane(x);
-    asm volatile("" : "+s"(x));
-    return x;
-}
 __device__ __forceinline__ float largest(f32x4 a) { return fmaxf(fmaxf(fmaxf(a[0], a[1]), a[2]), a[3]); }
 
 // The query rows of a wave, QT tiles of 16, and their sums.  Lane (c, g) = (lane % 16, lane / 16) has of row c: of the queries the channels 8 g .. of every 32; of O^T the channels
@@ -952,7 +968,7 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
     using G = KeysGeom<D, QT, NW>;
     constexpr int ROW = G::ROW, LPR = ROW / 16, RPI = 1024 / ROW, HALF = G::LOADS / 2;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const int tid0 = threadIdx.x, lane0 = tid0 & 63, wave = __builtin_amdgcn_readfirstlane(tid0 >> 6);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
     float2 *s_ml = reinterpret_cast<float2 *>(smem + G::MAIN);
     int32_t *flags = reinterpret_cast<int32_t *>(s_ml + NW * G::CAP);
@@ -972,190 +988,206 @@ __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArg
     auto ask_pages = [&](int first) {      // of tiles first + lane * stride
 #pragma unroll
         for (int h = 0; h < 2; h++)
-            page[h] = table[(int64_t)u.b * max_pages + min(((first + lane * stride) * 2 + h) >> (lg_page - 4), max_pages - 1)];
+            page[h] = table[(int64_t)u.b * max_pages + min(((first + lane0 * stride) * 2 + h) >> (lg_page - 4), max_pages - 1)];
     };
     PageList<G::THREADS> list;
     if constexpr (SPARSE)
-        list.ask(first, u, tid * list.EACH);
+        list.ask(first, u, tid0 * list.EACH);
     if (early)
         ask_pages(mine);
     int parent = -1;
     if (!u.shared && first.words == 1 && !first.tree_mask)
-        parent = first.parent[(int64_t)u.b * first.n_tree + min(lane, first.n_tree - 1)];
-    if (!unit_of(first, G::CAP, lane, rg, prefix, u))
+        parent = first.parent[(int64_t)u.b * first.n_tree + min(lane0, first.n_tree - 1)];
+    if (!unit_of(first, G::CAP, lane0, rg, prefix, u))
         return;
     if (u.alone)
-        no_shared_parts(first, u, G::CAP, tid, G::THREADS);
-    if constexpr (SPARSE)
-        list.build(first, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (first.words > 1 ? G::CAP * first.words + DREAM_MAX_TREE / 2 : 0)), 0);
-    const PagedAttnArgs &a = SPARSE ? args_again() : first;
-    QueryRows<D, QT, 2, SPARSE, 2> rows;
-    rows.load(a, u, u.row0, c, g);
-    const int tile0 = u.lo / 32;
-    if (!SPARSE && !early)
-        ask_pages(tile0 + mine);
+        no_shared_parts(first, u, G::CAP, tid0, G::THREADS);
+    // Selected pages: list by list.  (One, but where more pages are seen than were expected: what the lists in front gave waits in the part's slot, and joins.)
+    for (int skip = 0;;) {
+        const int tid = SPARSE ? here(tid0) : tid0, lane = tid & 63, c = lane & 15, g = lane >> 4;      // (nothing but this is kept from list to list)
+        if constexpr (SPARSE)
+            list.build(args_again(), u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (first.words > 1 ? G::CAP * first.words + DREAM_MAX_TREE / 2 : 0)), skip);
+        const PagedAttnArgs &a = SPARSE ? args_again() : first;
+        QueryRows<D, QT, 2, SPARSE, 2> rows;
+        rows.load(a, u, u.row0, c, g);
+        const int tile0 = u.lo / 32;
+        if (!SPARSE && !early)
+            ask_pages(tile0 + mine);
 
-    const int foff = fragment_k<ROW>(c, g), voff = fragment_v<ROW>(c, g);
-    const int krow = lane / LPR, k_lane = krow * ROW + piece_k<ROW>(lane), v_lane = krow * ROW + piece_v<ROW>(lane);
-    const int stage = wave * 2 * G::TILE;
-    auto chunk = [&](int i, int h) -> Chunk {
-        if constexpr (SPARSE) {
-            return listed_chunk(a, list, (wave + i * NW) * 32 + h * 16);
-        } else {
-            const int pos = (tile0 + mine + i * stride) * 32 + h * 16;
-            return Chunk{0, pos, pos < u.hi, true, true};
-        }
-    };
-    Offset offset[2];                             // of the chunks of the lane's tile (of the list's: in units of a run of 64 as well)
-    auto locate = [&](int i) {                    // tiles i .. i + 63
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
+        const int foff = fragment_k<ROW>(c, g), voff = fragment_v<ROW>(c, g);
+        const int krow = lane / LPR, k_lane = krow * ROW + piece_k<ROW>(lane), v_lane = krow * ROW + piece_v<ROW>(lane);
+        const int stage = wave * 2 * G::TILE;
+        auto chunk = [&](int i, int h) -> Chunk {
             if constexpr (SPARSE) {
-                const int x = (wave + (i + lane) * NW) * 32 + h * 16;
-                offset[h].set(a, u.kvh, list.phys[min(x >> lg_page, list.n - 1)], x, ROW);
+                return listed_chunk(a, list, (wave + i * NW) * 32 + h * 16);
             } else {
-                offset[h].set(a, u.kvh, page[h], (tile0 + mine + (i + lane) * stride) * 32 + h * 16, ROW);
+                const int pos = (tile0 + mine + i * stride) * 32 + h * 16;
+                return Chunk{0, pos, pos < u.hi, true, true};
             }
-        }
-    };
-    auto place = [&](int i, int h) { return offset[h].of(i & 63); };
-    auto ask_k = [&](int i) {
-        if ((i & 63) == 0) {
-            if (!SPARSE && i)
-                ask_pages(tile0 + mine + i * stride);
-            locate(i);
-        }
+        };
+        Offset offset[2];                             // of the chunks of the lane's tile (of the list's: in units of a run of 64 as well)
+        auto locate = [&](int i) {                    // tiles i .. i + 63
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const int at = here(k_lane);
-            lds_load_run<HALF>(a.k + place(i, h), [&](int j) { return (uint32_t)(at ^ swizzle_k<ROW>(h * HALF + j)); }, here_scalar(lds0 + stage) + h * HALF * 1024);
-        }
-    };
-    auto ask_v = [&](int i) {
+            for (int h = 0; h < 2; h++) {
+                if constexpr (SPARSE) {
+                    const int x = (wave + (i + lane) * NW) * 32 + h * 16;
+                    offset[h].set(a, u.kvh, list.phys[min(x >> lg_page, list.n - 1)], x, ROW);
+                } else {
+                    offset[h].set(a, u.kvh, page[h], (tile0 + mine + (i + lane) * stride) * 32 + h * 16, ROW);
+                }
+            }
+        };
+        auto place = [&](int i, int h) { return offset[h].of(i & 63); };
+        auto ask_k = [&](int i) {
+            if ((i & 63) == 0) {
+                if (!SPARSE && i)
+                    ask_pages(tile0 + mine + i * stride);
+                locate(i);
+            }
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const int at = here(v_lane);
-            lds_load_run<HALF>(a.v + place(i, h), [&](int j) { return (uint32_t)(at ^ swizzle_v<ROW>(h * HALF + j)); }, here_scalar(lds0 + stage) + G::TILE + h * HALF * 1024);
-        }
-    };
-    // Zeros over the values of rows that are nobody's
-    auto clear_dead = [&](const Chunk (&ch)[2]) {
-        const int vat = here_scalar(stage + G::TILE);
+            for (int h = 0; h < 2; h++) {
+                const int at = here(k_lane);
+                lds_load_run<HALF>(a.k + place(i, h), [&](int j) { return (uint32_t)(at ^ swizzle_k<ROW>(h * HALF + j)); }, here_scalar(lds0 + stage) + h * HALF * 1024);
+            }
+        };
+        auto ask_v = [&](int i) {
 #pragma unroll
-        for (int h = 0; h < 2; h++) {
-            if (rows.plain(u, ch[h]))
-                continue;
+            for (int h = 0; h < 2; h++) {
+                const int at = here(v_lane);
+                lds_load_run<HALF>(a.v + place(i, h), [&](int j) { return (uint32_t)(at ^ swizzle_v<ROW>(h * HALF + j)); }, here_scalar(lds0 + stage) + G::TILE + h * HALF * 1024);
+            }
+        };
+        // Zeros over the values of rows that are nobody's
+        auto clear_dead = [&](const Chunk (&ch)[2]) {
+            const int vat = here_scalar(stage + G::TILE);
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                if (rows.plain(u, ch[h]))
+                    continue;
 #pragma unroll 1
-            for (int j = 0; j < HALF; j++) {
-                const int pos = ch[h].pos + j * RPI + krow;
-                if (!(ch[h].live && ((ch[h].prefix && pos >= u.lo && pos < u.P) || (ch[h].tree && pos >= u.P && pos < u.hi))))
-                    *reinterpret_cast<u32x4 *>(smem + vat + (h * HALF + j) * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+                for (int j = 0; j < HALF; j++) {
+                    const int pos = ch[h].pos + j * RPI + krow;
+                    if (!(ch[h].live && ((ch[h].prefix && pos >= u.lo && pos < u.P) || (ch[h].tree && pos >= u.P && pos < u.hi))))
+                        *reinterpret_cast<u32x4 *>(smem + vat + (h * HALF + j) * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+                }
             }
-        }
-        wait_lds();
-    };
-    auto take = [&](int steps) {
-        for (int i = 0; i < steps; i++) {
-            Chunk ch[2];
-            bool straight;
-            uint32_t in = 0u;
-            if constexpr (SPARSE) {
-                rows.seen_by(a, u, list, (wave + i * NW) * 32, straight, in);
-            } else {
-                const int pos = (tile0 + mine + i * stride) * 32;
-                straight = pos >= u.lo && pos + 32 <= rows.whole;
-            }
-            if (!straight || a.scale_log2 < 0.0f) {
-                ch[0] = chunk(i, 0);
-                ch[1] = chunk(i, 1);
-            }
-            f32x4 s[2][QT];
-            typename decltype(rows)::Weights pf;
-            wait_loads<G::LOADS>();
-            rows.scores(smem + stage, here(foff), 0, s);
             wait_lds();
-            if (i + 1 < steps)
-                ask_k(i + 1);
-            const bool masked = !straight || a.scale_log2 < 0.0f;      // (the largest score of a negative scale is the smallest product)
-            if (masked)
-                rows.mask(a, u, ch, in, g, s);
-            const float scaled = masked ? 1.0f : a.scale_log2;
-            in = masked ? ~0u : in;
-            rows.raise(scaled, in, s);
-#pragma unroll
-            for (int j = 0; j < rows.SLICES; j++)
-                rows.weigh(scaled, in, j, s, pf);
-            if (i + 1 < steps)
+        };
+        auto take = [&](int steps) {
+            for (int i = 0; i < steps; i++) {
+                Chunk ch[2];
+                bool straight;
+                uint32_t in = 0u;
+                if constexpr (SPARSE) {
+                    rows.seen_by(a, u, list, (wave + i * NW) * 32, straight, in);
+                } else {
+                    const int pos = (tile0 + mine + i * stride) * 32;
+                    straight = pos >= u.lo && pos + 32 <= rows.whole;
+                }
+                if (!straight || a.scale_log2 < 0.0f) {
+                    ch[0] = chunk(i, 0);
+                    ch[1] = chunk(i, 1);
+                }
+                f32x4 s[2][QT];
+                typename decltype(rows)::Weights pf;
                 wait_loads<G::LOADS>();
-            else
-                wait_loads<0>();
-            if (!straight)
-                clear_dead(ch);
-            rows.add_values(smem + stage + G::TILE, here(voff), pf);
-            wait_lds();
-            if (i + 1 < steps)
-                ask_v(i + 1);
+                rows.scores(smem + stage, here(foff), 0, s);
+                wait_lds();
+                if (i + 1 < steps)
+                    ask_k(i + 1);
+                const bool masked = !straight || a.scale_log2 < 0.0f;      // (the largest score of a negative scale is the smallest product)
+                if (masked)
+                    rows.mask(a, u, ch, in, g, s);
+                const float scaled = masked ? 1.0f : a.scale_log2;
+                in = masked ? ~0u : in;
+                rows.raise(scaled, in, s);
+#pragma unroll
+                for (int j = 0; j < rows.SLICES; j++)
+                    rows.weigh(scaled, in, j, s, pf);
+                if (i + 1 < steps)
+                    wait_loads<G::LOADS>();
+                else
+                    wait_loads<0>();
+                if (!straight)
+                    clear_dead(ch);
+                rows.add_values(smem + stage + G::TILE, here(voff), pf);
+                wait_lds();
+                if (i + 1 < steps)
+                    ask_v(i + 1);
+            }
+        };
+        const int steps = SPARSE ? (((list.n << a.lg_page) + 31) / 32 - wave + NW - 1) / NW : u.hi > u.lo ? ((u.hi + 31) / 32 - tile0 - mine + stride - 1) / stride : 0;
+        if (steps > 0) {
+            ask_k(0);
+            ask_v(0);
         }
-    };
-    const int steps = SPARSE ? (((list.n << a.lg_page) + 31) / 32 - wave + NW - 1) / NW : u.hi > u.lo ? ((u.hi + 31) / 32 - tile0 - mine + stride - 1) / stride : 0;
-    if (steps > 0) {
-        ask_k(0);
-        ask_v(0);
-    }
-    rows.see(a, u, u.row0, G::CAP, parent, c, tid, G::THREADS, masks, parents, 0);
-    take(steps);
+        rows.see(a, u, u.row0, G::CAP, parent, c, tid, G::THREADS, masks, parents, 0);
+        take(steps);
 
-    // ---- the waves' sums meet, each wave's in its own stage: 16-byte piece i of row r at i ^ (r mod 16)
-    const bool strange = rows.finish() || (SPARSE && list.all > list.n);      // (a list longer than what it was planned for: row by row)
-    if (lane == 0)
-        flags[wave] = strange;
-    if (g == 0)
+        // ---- the waves' sums meet, each wave's in its own stage: 16-byte piece i of row r at i ^ (r mod 16)
+        const bool strange = rows.finish();
+        if (lane == 0)
+            flags[wave] = strange;
+        if (g == 0)
+#pragma unroll
+            for (int qt = 0; qt < QT; qt++)
+                s_ml[wave * G::CAP + qt * 16 + c] = make_float2(rows.m[qt], rows.l[qt]);
 #pragma unroll
         for (int qt = 0; qt < QT; qt++)
-            s_ml[wave * G::CAP + qt * 16 + c] = make_float2(rows.m[qt], rows.l[qt]);
 #pragma unroll
-    for (int qt = 0; qt < QT; qt++)
-#pragma unroll
-        for (int dt = 0; dt < D / 16; dt++)
-            *reinterpret_cast<f32x4 *>(smem + stage + (qt * 16 + c) * (4 * D) + ((dt * 4 + g) ^ c) * 16) = rows.o[qt][dt];
-    __syncthreads();
-    const PagedAttnArgs &z = args_again();
-    int again = 0;
-#pragma unroll
-    for (int w = 0; w < NW; w++)
-        again |= flags[w];
-    if (again) {
+            for (int dt = 0; dt < D / 16; dt++)
+                *reinterpret_cast<f32x4 *>(smem + stage + (qt * 16 + c) * (4 * D) + ((dt * 4 + g) ^ c) * 16) = rows.o[qt][dt];
         __syncthreads();
-        attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(z, u, G::CAP, 32, 32 * NW, smem);
-        return;
-    }
-    const int count = min(G::CAP, u.n_rows - u.row0);
-    for (int i = tid; i < count * (D / 4); i += G::THREADS) {
-        const int j = i / (D / 4), ch = i % (D / 4);
-        const Row w = row_at(z, u, u.row0 + j);
-        float2 ml[NW];
-        float most = -INFINITY, sum = 0.0f;
-        f32x4 all = {0.f, 0.f, 0.f, 0.f};
+        const PagedAttnArgs &z = args_again();
+        int again = 0;
 #pragma unroll
-        for (int x = 0; x < NW; x++) {
-            ml[x] = s_ml[x * G::CAP + j];
-            most = fmaxf(most, ml[x].x);
-        }
+        for (int w = 0; w < NW; w++)
+            again |= flags[w];
+        if (again)
+            break;
+        const int count = min(G::CAP, u.n_rows - u.row0);
+        const bool more = SPARSE && skip + z.list_size < list.all;
+        for (int i = tid; i < count * (D / 4); i += G::THREADS) {
+            const int j = i / (D / 4), ch = i % (D / 4);
+            const Row w = row_at(z, u, u.row0 + j);
+            float2 ml[NW];
+            float most = -INFINITY, sum = 0.0f;
+            f32x4 all = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int x = 0; x < NW; x++) {
-            const float f = ml[x].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[x].x - most);
-            sum = __builtin_fmaf(ml[x].y, f, sum);
-            all += *reinterpret_cast<const f32x4 *>(smem + x * 2 * G::TILE + j * (4 * D) + (ch ^ (j & 15)) * 16) * f;
+            for (int x = 0; x < NW; x++) {
+                ml[x] = s_ml[x * G::CAP + j];
+                most = fmaxf(most, ml[x].x);
+            }
+#pragma unroll
+            for (int x = 0; x < NW; x++) {
+                const float f = ml[x].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[x].x - most);
+                sum = __builtin_fmaf(ml[x].y, f, sum);
+                all += *reinterpret_cast<const f32x4 *>(smem + x * 2 * G::TILE + j * (4 * D) + (ch ^ (j & 15)) * 16) * f;
+            }
+            float *slot = z.part_o + row_of_part(z, u, w) * D + ch * 4;
+            if (SPARSE && skip) {
+                Earlier earlier;
+                earlier.join(z, u, w, most, sum);
+                all = *reinterpret_cast<const f32x4 *>(slot) * earlier.old + all * earlier.now;
+            }
+            const bool part = z.n_slots > 1 || (SPARSE && more);
+            if (ch == 0)
+                put_ml(z, u, w, most, sum, part);
+            if (part) {
+                *reinterpret_cast<f32x4 *>(slot) = all;
+            } else {
+                const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+                *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(z.out) + row_of_q(z, w) * D + ch * 4) = make_uint2(pack_bf16(all[0] * inv, all[1] * inv), pack_bf16(all[2] * inv, all[3] * inv));
+            }
         }
-        if (ch == 0)
-            put_ml(z, u, w, most, sum);
-        if (z.n_slots > 1) {
-            *reinterpret_cast<f32x4 *>(z.part_o + row_of_part(z, u, w) * D + ch * 4) = all;
-        } else {
-            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-            *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(z.out) + row_of_q(z, w) * D + ch * 4) = make_uint2(pack_bf16(all[0] * inv, all[1] * inv), pack_bf16(all[2] * inv, all[3] * inv));
-        }
+        if (!more)
+            return;
+        skip += z.list_size;
+        list.ask(args_again(), u, tid * list.EACH);
     }
+    // a sum is not finite: all of the keys again, row by row
+    __syncthreads();
+    attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(args_again(), u, G::CAP, 32, 32 * NW, smem);
 }
 
 template <int D, int QT, int WR, int NS>
@@ -1177,7 +1209,7 @@ __global__ __launch_bounds__(64 * WR, D == 64 && QT == 1 && !SPARSE ? 4 : 2) voi
     using G = RowsGeom<D, QT, WR, NS>;
     constexpr int ROW = G::ROW, KEYS = G::KEYS, NC = KEYS / 16, LPR = ROW / 16, RPI = 1024 / ROW;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, g = lane >> 4;
+    const int tid0 = threadIdx.x, lane0 = tid0 & 63, wave = __builtin_amdgcn_readfirstlane(tid0 >> 6);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
     int32_t *flags = reinterpret_cast<int32_t *>(smem + G::MAIN);
     uint64_t *masks = reinterpret_cast<uint64_t *>(flags + 2 * WR);
@@ -1192,219 +1224,235 @@ __global__ __launch_bounds__(64 * WR, D == 64 && QT == 1 && !SPARSE ? 4 : 2) voi
     const bool early = !SPARSE && lg_and_early >> 8;       // no groups: the first tile is the first, whatever else the call holds
     const int lg_page = lg_and_early & 255;
     int page = 0;
-    auto ask_pages = [&](int first) { page = table[(int64_t)u.b * max_pages + min(((first + lane * u.splits) * KEYS + own_chunk) >> lg_page, max_pages - 1)]; };      // of tiles first + lane * splits
+    auto ask_pages = [&](int first) { page = table[(int64_t)u.b * max_pages + min(((first + lane0 * u.splits) * KEYS + own_chunk) >> lg_page, max_pages - 1)]; };      // of tiles first + lane * splits
     PageList<G::THREADS> list;
     if constexpr (SPARSE)
-        list.ask(first, u, tid * list.EACH);
+        list.ask(first, u, tid0 * list.EACH);
     if (early)
         ask_pages(u.split);
     int parent = -1;
     if (!u.shared && first.words == 1 && !first.tree_mask)
-        parent = first.parent[(int64_t)u.b * first.n_tree + min(lane, first.n_tree - 1)];
-    if (!unit_of(first, G::CAP, lane, rg, prefix, u))
+        parent = first.parent[(int64_t)u.b * first.n_tree + min(lane0, first.n_tree - 1)];
+    if (!unit_of(first, G::CAP, lane0, rg, prefix, u))
         return;
     if (u.alone)
-        no_shared_parts(first, u, G::CAP, tid, G::THREADS);
-    if constexpr (SPARSE)
-        list.build(first, u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (first.words > 1 ? G::CAP * first.words + DREAM_MAX_TREE / 2 : 0)), 0);
-    const PagedAttnArgs &a = SPARSE ? args_again() : first;
-    QueryRows<D, QT, NC, SPARSE, D == 256 ? 2 : 1> rows;
-    const int first_row = u.row0 + wave * QT * 16;
-    rows.load(a, u, first_row, c, g);
-    const int tile0 = u.lo / KEYS + u.split;
-    if (!SPARSE && !early)
-        ask_pages(tile0);
+        no_shared_parts(first, u, G::CAP, tid0, G::THREADS);
+    // Selected pages: list by list
+    for (int skip = 0;;) {
+        const int tid = SPARSE ? here(tid0) : tid0, lane = tid & 63, c = lane & 15, g = lane >> 4;      // (nothing but this is kept from list to list)
+        if constexpr (SPARSE)
+            list.build(args_again(), u, G::CAP, tid, reinterpret_cast<unsigned char *>(masks + (first.words > 1 ? G::CAP * first.words + DREAM_MAX_TREE / 2 : 0)), skip);
+        const PagedAttnArgs &a = SPARSE ? args_again() : first;
+        QueryRows<D, QT, NC, SPARSE, D == 256 ? 2 : 1> rows;
+        const int first_row = u.row0 + wave * QT * 16;
+        rows.load(a, u, first_row, c, g);
+        const int tile0 = u.lo / KEYS + u.split;
+        if (!SPARSE && !early)
+            ask_pages(tile0);
 
-    const int foff = fragment_k<ROW>(c, g), voff = fragment_v<ROW>(c, g);
-    const int krow = lane / LPR, k_lane = krow * ROW + piece_k<ROW>(lane), v_lane = krow * ROW + piece_v<ROW>(lane);
-    auto chunk = [&](int i, int at) -> Chunk {
-        if constexpr (SPARSE) {
-            return listed_chunk(a, list, i * KEYS + at);
-        } else {
-            const int pos = (tile0 + i * u.splits) * KEYS + at;
-            return Chunk{0, pos, pos < u.hi, true, true};
-        }
-    };
-    Offset offset;                                         // of the wave's rows of the lane's tile
-    auto locate = [&](int i) {                             // tiles i .. i + 63
-        if constexpr (SPARSE) {
-            const int x = (i + lane) * KEYS + own_rows;
-            offset.set(a, u.kvh, list.phys[min(x >> lg_page, list.n - 1)], x, ROW);
-        } else {
-            offset.set(a, u.kvh, page, (tile0 + (i + lane) * u.splits) * KEYS + own_rows, ROW);
-        }
-    };
-    auto ask_tile = [&](const unsigned char *from, int lane_at, bool values, int stage) {
-        lds_load_run<G::LOADS>(from, [&](int j) { return (uint32_t)(lane_at ^ (values ? swizzle_v<ROW>(wave * G::LOADS + j) : swizzle_k<ROW>(wave * G::LOADS + j))); },
-                               lds0 + (values ? NS + stage : stage) * G::TILE + wave * G::LOADS * 1024);
-    };
-    auto after = [](int stage) { return stage == NS - 1 ? 0 : stage + 1; };
-    // Zeros over the values of rows that are nobody's, by the wave that loaded them
-    auto clear_dead = [&](int i, int stage) {
-        const Chunk ch = chunk(i, own_chunk);
-        if (rows.plain(u, ch))
-            return;
-#pragma unroll
-        for (int j = 0; j < G::LOADS; j++) {
-            const int pos = ch.pos + (own_rows & 15) + j * RPI + krow;
-            if (!(ch.live && ((ch.prefix && pos >= u.lo && pos < u.P) || (ch.tree && pos >= u.P && pos < u.hi))))
-                *reinterpret_cast<u32x4 *>(smem + (NS + stage) * G::TILE + (wave * G::LOADS + j) * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
-        }
-    };
-    const int steps = SPARSE ? ((list.n << a.lg_page) + KEYS - 1) / KEYS : u.hi > u.lo ? max(0, ((u.hi + KEYS - 1) / KEYS - tile0 + u.splits - 1) / u.splits) : 0;
-
-    // What is known of a tile: scores and how they are to be read; have: some of the wave's rows see it
-    struct Tile {
-        f32x4 s[NC][QT];
-        float scaled;
-        uint32_t in;
-        bool have, masked;
-    };
-    auto look = [&](int i, Tile &t) {
-        bool straight;
-        if constexpr (SPARSE) {
-            t.have = rows.seen_by(a, u, list, i * KEYS, straight, t.in);
-        } else {
-            const int pos = (tile0 + i * u.splits) * KEYS;
-            straight = pos >= u.lo && pos + KEYS <= rows.whole;
-            t.have = true;
-            t.in = 0u;
-        }
-        t.masked = !straight || a.scale_log2 < 0.0f;      // (the largest score of a negative scale is the smallest product)
-        t.scaled = t.masked ? 1.0f : a.scale_log2;
-    };
-    typename decltype(rows)::Weights pf;
-    // Scores that have come: what nobody sees is left out, the references are raised
-    auto settle = [&](int i, Tile &t) {
-        if (t.masked) {
-            Chunk ch[NC];
-#pragma unroll
-            for (int h = 0; h < NC; h++)
-                ch[h] = chunk(i, h * 16);
-            rows.mask(a, u, ch, t.in, g, t.s);
-            t.in = ~0u;
-        }
-        rows.raise(t.scaled, t.in, t.s);
-    };
-    auto add_values = [&](int stage) { rows.add_values(smem + (NS + stage) * G::TILE, here(voff), pf); };
-    // Interval i: the keys of tile i + 1 and the values of tile i are there; those that NS - 1 intervals later need are asked for
-    int64_t next_v = 0;             // where the values lie that are asked for next
-    int k_stage = 0, v_stage = 0, k_ask = 0, v_ask = 0;
-    auto ask = [&](int i) {         // what interval i needs
-        ask_tile(a.v + next_v, v_lane, true, v_ask);
-        if ((i + 1 & 63) == 0 && i + 1 < steps) {
-            if (!SPARSE)
-                ask_pages(tile0 + (i + 1) * u.splits);
-            locate(i + 1);
-        }
-        next_v = offset.of(min(i + 1, steps - 1) & 63);      // (behind the last tile that one again: such keys are never used)
-        ask_tile(a.k + next_v, k_lane, false, k_ask);
-        k_ask = after(k_ask);
-        v_ask = after(v_ask);
-    };
-    if (steps > 0) {
-        locate(0);
-        next_v = offset.of(0);
-        ask_tile(a.k + next_v, k_lane, false, 0);
-        k_ask = after(0);
-#pragma unroll
-        for (int i = 0; i < NS - 1; i++)
-            if (i < steps)
-                ask(i);
-    }
-    rows.see(a, u, first_row, G::CAP, parent, c, tid, G::THREADS, masks, parents, wave * QT * 16);
-    if (steps > 0) {
-        if (steps >= NS - 1)
-            wait_loads<(NS - 1) * 2 * G::LOADS>();
-        else
-            wait_loads<0>();
-        asm volatile("s_barrier" ::: "memory");
-        Tile even, odd;
-        {
-            look(0, even);
-            if (even.have) {
-#pragma unroll
-                for (int h = 0; h < NC; h += 2)
-                    rows.scores(smem, here(foff), h, even.s);
-                settle(0, even);
+        const int foff = fragment_k<ROW>(c, g), voff = fragment_v<ROW>(c, g);
+        const int krow = lane / LPR, k_lane = krow * ROW + piece_k<ROW>(lane), v_lane = krow * ROW + piece_v<ROW>(lane);
+        auto chunk = [&](int i, int at) -> Chunk {
+            if constexpr (SPARSE) {
+                return listed_chunk(a, list, i * KEYS + at);
+            } else {
+                const int pos = (tile0 + i * u.splits) * KEYS + at;
+                return Chunk{0, pos, pos < u.hi, true, true};
             }
+        };
+        Offset offset;                                         // of the wave's rows of the lane's tile
+        auto locate = [&](int i) {                             // tiles i .. i + 63
+            if constexpr (SPARSE) {
+                const int x = (i + lane) * KEYS + own_rows;
+                offset.set(a, u.kvh, list.phys[min(x >> lg_page, list.n - 1)], x, ROW);
+            } else {
+                offset.set(a, u.kvh, page, (tile0 + (i + lane) * u.splits) * KEYS + own_rows, ROW);
+            }
+        };
+        auto ask_tile = [&](const unsigned char *from, int lane_at, bool values, int stage) {
+            lds_load_run<G::LOADS>(from, [&](int j) { return (uint32_t)(lane_at ^ (values ? swizzle_v<ROW>(wave * G::LOADS + j) : swizzle_k<ROW>(wave * G::LOADS + j))); },
+                                   lds0 + (values ? NS + stage : stage) * G::TILE + wave * G::LOADS * 1024);
+        };
+        auto after = [](int stage) { return stage == NS - 1 ? 0 : stage + 1; };
+        // Zeros over the values of rows that are nobody's, by the wave that loaded them
+        auto clear_dead = [&](int i, int stage) {
+            const Chunk ch = chunk(i, own_chunk);
+            if (rows.plain(u, ch))
+                return;
+#pragma unroll
+            for (int j = 0; j < G::LOADS; j++) {
+                const int pos = ch.pos + (own_rows & 15) + j * RPI + krow;
+                if (!(ch.live && ((ch.prefix && pos >= u.lo && pos < u.P) || (ch.tree && pos >= u.P && pos < u.hi))))
+                    *reinterpret_cast<u32x4 *>(smem + (NS + stage) * G::TILE + (wave * G::LOADS + j) * 1024 + lane * 16) = u32x4{0u, 0u, 0u, 0u};
+            }
+        };
+        const int steps = SPARSE ? ((list.n << a.lg_page) + KEYS - 1) / KEYS : u.hi > u.lo ? max(0, ((u.hi + KEYS - 1) / KEYS - tile0 + u.splits - 1) / u.splits) : 0;
+
+        // What is known of a tile: scores and how they are to be read; have: some of the wave's rows see it
+        struct Tile {
+            f32x4 s[NC][QT];
+            float scaled;
+            uint32_t in;
+            bool have, masked;
+        };
+        auto look = [&](int i, Tile &t) {
+            bool straight;
+            if constexpr (SPARSE) {
+                t.have = rows.seen_by(a, u, list, i * KEYS, straight, t.in);
+            } else {
+                const int pos = (tile0 + i * u.splits) * KEYS;
+                straight = pos >= u.lo && pos + KEYS <= rows.whole;
+                t.have = true;
+                t.in = 0u;
+            }
+            t.masked = !straight || a.scale_log2 < 0.0f;      // (the largest score of a negative scale is the smallest product)
+            t.scaled = t.masked ? 1.0f : a.scale_log2;
+        };
+        typename decltype(rows)::Weights pf;
+        // Scores that have come: what nobody sees is left out, the references are raised
+        auto settle = [&](int i, Tile &t) {
+            if (t.masked) {
+                Chunk ch[NC];
+#pragma unroll
+                for (int h = 0; h < NC; h++)
+                    ch[h] = chunk(i, h * 16);
+                rows.mask(a, u, ch, t.in, g, t.s);
+                t.in = ~0u;
+            }
+            rows.raise(t.scaled, t.in, t.s);
+        };
+        auto add_values = [&](int stage) { rows.add_values(smem + (NS + stage) * G::TILE, here(voff), pf); };
+        // Interval i: the keys of tile i + 1 and the values of tile i are there; those that NS - 1 intervals later need are asked for
+        int64_t next_v = 0;             // where the values lie that are asked for next
+        int k_stage = 0, v_stage = 0, k_ask = 0, v_ask = 0;
+        auto ask = [&](int i) {         // what interval i needs
+            ask_tile(a.v + next_v, v_lane, true, v_ask);
+            if ((i + 1 & 63) == 0 && i + 1 < steps) {
+                if (!SPARSE)
+                    ask_pages(tile0 + (i + 1) * u.splits);
+                locate(i + 1);
+            }
+            next_v = offset.of(min(i + 1, steps - 1) & 63);      // (behind the last tile that one again: such keys are never used)
+            ask_tile(a.k + next_v, k_lane, false, k_ask);
+            k_ask = after(k_ask);
+            v_ask = after(v_ask);
+        };
+        if (steps > 0) {
+            locate(0);
+            next_v = offset.of(0);
+            ask_tile(a.k + next_v, k_lane, false, 0);
+            k_ask = after(0);
+#pragma unroll
+            for (int i = 0; i < NS - 1; i++)
+                if (i < steps)
+                    ask(i);
         }
-        // Interval i: the weights of tile i while the matrix cores are at the scores of tile i + 1, then the values of tile i, then what the new scores change
-        auto interval = [&](int i, Tile &t, Tile &n) {
-            if (i + NS - 2 < steps)
-                wait_loads<(NS - 2) * 2 * G::LOADS>();
+        rows.see(a, u, first_row, G::CAP, parent, c, tid, G::THREADS, masks, parents, wave * QT * 16);
+        if (steps > 0) {
+            if (steps >= NS - 1)
+                wait_loads<(NS - 1) * 2 * G::LOADS>();
             else
                 wait_loads<0>();
-            if (t.masked)
-                clear_dead(i, v_stage);
-            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the tiles are there, and all have done with the stages that are loaded next
-            if (i + NS - 1 < steps)
-                ask(i + NS - 1);
-            k_stage = after(k_stage);
-            const unsigned char *kt = smem + k_stage * G::TILE;
-            n.have = false;
-            if (i + 1 < steps)
-                look(i + 1, n);
-            if (t.have && n.have) {
-                rows.scores_and_weights(kt, here(foff), n.s, t.scaled, t.in, t.s, pf);
-            } else if (t.have) {
+            asm volatile("s_barrier" ::: "memory");
+            Tile even, odd;
+            {
+                look(0, even);
+                if (even.have) {
 #pragma unroll
-                for (int j = 0; j < rows.SLICES; j++)
-                    rows.weigh(t.scaled, t.in, j, t.s, pf);
-            } else if (n.have) {
-#pragma unroll
-                for (int h = 0; h < NC; h += 2)
-                    rows.scores(kt, here(foff), h, n.s);
+                    for (int h = 0; h < NC; h += 2)
+                        rows.scores(smem, here(foff), h, even.s);
+                    settle(0, even);
+                }
             }
-            if (t.have)
-                add_values(v_stage);
-            if (n.have)
-                settle(i + 1, n);
-            v_stage = after(v_stage);
-        };
-        for (int i = 0; i < steps; i += 2) {
-            interval(i, even, odd);
-            if (i + 1 < steps)
-                interval(i + 1, odd, even);
+            // Interval i: the weights of tile i while the matrix cores are at the scores of tile i + 1, then the values of tile i, then what the new scores change
+            auto interval = [&](int i, Tile &t, Tile &n) {
+                if (i + NS - 2 < steps)
+                    wait_loads<(NS - 2) * 2 * G::LOADS>();
+                else
+                    wait_loads<0>();
+                if (t.masked)
+                    clear_dead(i, v_stage);
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");      // the tiles are there, and all have done with the stages that are loaded next
+                if (i + NS - 1 < steps)
+                    ask(i + NS - 1);
+                k_stage = after(k_stage);
+                const unsigned char *kt = smem + k_stage * G::TILE;
+                n.have = false;
+                if (i + 1 < steps)
+                    look(i + 1, n);
+                if (t.have && n.have) {
+                    rows.scores_and_weights(kt, here(foff), n.s, t.scaled, t.in, t.s, pf);
+                } else if (t.have) {
+#pragma unroll
+                    for (int j = 0; j < rows.SLICES; j++)
+                        rows.weigh(t.scaled, t.in, j, t.s, pf);
+                } else if (n.have) {
+#pragma unroll
+                    for (int h = 0; h < NC; h += 2)
+                        rows.scores(kt, here(foff), h, n.s);
+                }
+                if (t.have)
+                    add_values(v_stage);
+                if (n.have)
+                    settle(i + 1, n);
+                v_stage = after(v_stage);
+            };
+            for (int i = 0; i < steps; i += 2) {
+                interval(i, even, odd);
+                if (i + 1 < steps)
+                    interval(i + 1, odd, even);
+            }
         }
-    }
 
-    const bool strange = rows.finish() || (SPARSE && list.all > list.n);      // (a list longer than what it was planned for: row by row)
-    if (lane == 0)
-        flags[wave] = strange;
-    __syncthreads();
-    const PagedAttnArgs &z = args_again();
-    int again = 0;
-#pragma unroll
-    for (int w = 0; w < WR; w++)
-        again |= flags[w];
-    if (again) {
+        const bool strange = rows.finish();
+        if (lane == 0)
+            flags[wave] = strange;
         __syncthreads();
-        attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(z, u, G::CAP, KEYS, KEYS, smem);
-        return;
-    }
+        const PagedAttnArgs &z = args_again();
+        int again = 0;
 #pragma unroll
-    for (int qt = 0; qt < QT; qt++) {
-        const int j = first_row + qt * 16 + c;
-        if (j >= u.n_rows)
-            continue;
-        const Row w = row_at(z, u, j);
-        if (g == 0)
-            put_ml(z, u, w, rows.m[qt], rows.l[qt]);
-        if (z.n_slots > 1) {
-            float *row = z.part_o + row_of_part(z, u, w) * D + 4 * g;
+        for (int w = 0; w < WR; w++)
+            again |= flags[w];
+        if (again)
+            break;
+        const bool more = SPARSE && skip + z.list_size < list.all, part = z.n_slots > 1 || more;
 #pragma unroll
-            for (int dt = 0; dt < D / 16; dt++)
-                *reinterpret_cast<f32x4 *>(row + dt * 16) = rows.o[qt][dt];
-        } else {
-            const float inv = rows.l[qt] == 0.0f ? 0.0f : 1.0f / rows.l[qt];
-            uint16_t *row = static_cast<uint16_t *>(z.out) + row_of_q(z, w) * D + 4 * g;
+        for (int qt = 0; qt < QT; qt++) {
+            const int j = first_row + qt * 16 + c;
+            if (j >= u.n_rows)
+                continue;
+            const Row w = row_at(z, u, j);
+            float *slot = z.part_o + row_of_part(z, u, w) * D + 4 * g;
+            if (SPARSE && skip) {
+                Earlier earlier;
+                earlier.join(z, u, w, rows.m[qt], rows.l[qt]);
 #pragma unroll
-            for (int dt = 0; dt < D / 16; dt++)
-                *reinterpret_cast<uint2 *>(row + dt * 16) =
-                    make_uint2(pack_bf16(rows.o[qt][dt][0] * inv, rows.o[qt][dt][1] * inv), pack_bf16(rows.o[qt][dt][2] * inv, rows.o[qt][dt][3] * inv));
+                for (int dt = 0; dt < D / 16; dt++)
+                    rows.o[qt][dt] = *reinterpret_cast<const f32x4 *>(slot + dt * 16) * earlier.old + rows.o[qt][dt] * earlier.now;
+            }
+            if (g == 0)
+                put_ml(z, u, w, rows.m[qt], rows.l[qt], part);
+            if (part) {
+#pragma unroll
+                for (int dt = 0; dt < D / 16; dt++)
+                    *reinterpret_cast<f32x4 *>(slot + dt * 16) = rows.o[qt][dt];
+            } else {
+                const float inv = rows.l[qt] == 0.0f ? 0.0f : 1.0f / rows.l[qt];
+                uint16_t *row = static_cast<uint16_t *>(z.out) + row_of_q(z, w) * D + 4 * g;
+#pragma unroll
+                for (int dt = 0; dt < D / 16; dt++)
+                    *reinterpret_cast<uint2 *>(row + dt * 16) =
+                        make_uint2(pack_bf16(rows.o[qt][dt][0] * inv, rows.o[qt][dt][1] * inv), pack_bf16(rows.o[qt][dt][2] * inv, rows.o[qt][dt][3] * inv));
+            }
         }
+        if (!more)
+            return;
+        skip += z.list_size;
+        list.ask(args_again(), u, tid * list.EACH);
     }
+    // a sum is not finite: all of the keys again, row by row
+    __syncthreads();
+    attend_rows_singly<uint16_t, D, G::THREADS, SPARSE>(args_again(), u, G::CAP, KEYS, KEYS, smem);
 }
 
 // ---- the parts of a row, in their order: D / 4 lanes a row, AT parts at a time ------------------------------------------
@@ -1609,6 +1657,14 @@ int64_t listed_pages(const dream_page_desc *pages, int32_t n_tree, int64_t max_k
     return most + n_tree / pages->page_size + 2;
 }
 
+// Entries of a list, for so many pages: whole tiles of all waves (16 entries, 256 rows), and not so few that calls in which more pages are seen than was said take many lists (64 are 1 KB, and change no
+// number of workgroups on a CU).
+int list_size_of(int64_t pages, int32_t n_tree)
+{
+    const int64_t most = n_tree > 64 ? SPARSE_LIST / 2 : SPARSE_LIST, size = pages < 64 ? 64 : (pages + 15) / 16 * 16;
+    return (int)(size < most ? size : most);
+}
+
 // most_slots: parts that there is room for, 2 at least where there are groups
 PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32_t n_tree, int64_t max_kv, int32_t n_groups, int64_t max_shared, bool sparse, int64_t seen_pages, int most_slots = MOST_SPLITS)
 {
@@ -1648,9 +1704,10 @@ PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32
         choose(D, f32, own, false, most_slots, p.own);
     }
     finish(p.own, heads, sparse ? ceil_div(listed, n_tree > 64 ? SPARSE_LIST / 2 : SPARSE_LIST) : 1);
-    p.list_size = sparse ? ceil_div(listed, p.own.part.splits) : 0;
+    p.list_size = sparse ? list_size_of(ceil_div(listed, p.own.part.splits), n_tree) : 0;
     p.all_rows = heads * rows;
-    p.bytes = p.n_slots > 1 ? (size_t)p.n_slots * p.all_rows * (D + 2) * 4 : 0;
+    const bool several = sparse && !f32 && (int64_t)p.list_size * p.own.part.splits <= pages->max_pages;      // a workgroup may need several lists, and a slot for what they give (the page that the prefix ends in may be listed for the tree as well)
+    p.bytes = p.n_slots > 1 || several ? (size_t)p.n_slots * p.all_rows * (D + 2) * 4 : 0;
     return p;
 }
 
