@@ -466,7 +466,8 @@ int dream_mx_verify_attn(const dream_attn_desc *desc, const void *q, const void 
  *                sees shared positions below its own prefix length only; one in front of the first group or behind the last shares nothing.  n_groups at most B
  *   max_shared_len, max_kv_len   host-known upper bounds of shared_len and of prefix_len + n_tree; only used to choose the launch shape
  *   workspace    what ..._workspace gives is what the fastest launch needs; that of another call of the same sequences and nodes does too, if
- *                it holds one part of the rows (two, with groups): fewer parts are made then, and sums are added in another order.  DREAM_ERR_WORKSPACE below that
+ *                it holds one part of the rows (two, with groups, or where more than 1024 selected pages, 512 above 64 nodes, may be seen): fewer parts are
+ *                made then, and sums are added in another order.  A part is batch * n_q_heads * n_tree * (D + 2) * 4 bytes.  DREAM_ERR_WORKSPACE below that
  *   A node that sees nothing yields a zero row and lse = -inf.  What a node does not see does not change its row, whatever it holds:
  *   NaN and infinities too.  Values and scores that are not finite: as in dream_window_verify_attn.  batch * n_q_heads at most 2^20, q and out 16-byte aligned.
  *

@@ -1703,7 +1703,7 @@ PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32
     } else {
         choose(D, f32, own, false, most_slots, p.own);
     }
-    finish(p.own, heads, sparse ? ceil_div(listed, n_tree > 64 ? SPARSE_LIST / 2 : SPARSE_LIST) : 1);
+    finish(p.own, heads, sparse && listed > (n_tree > 64 ? SPARSE_LIST / 2 : SPARSE_LIST) ? 2 : 1);      // (pages that no list holds: two workgroups at least, each list by list)
     p.list_size = sparse ? list_size_of(ceil_div(listed, p.own.part.splits), n_tree) : 0;
     p.all_rows = heads * rows;
     const bool several = sparse && !f32 && (int64_t)p.list_size * p.own.part.splits <= pages->max_pages;      // a workgroup may need several lists, and a slot for what they give (the page that the prefix ends in may be listed for the tree as well)

@@ -155,3 +155,12 @@ def test_a_page_more_than_was_said_does_not_change_the_pace(T, splits):
         return best
     said, less = time_of(180), time_of(1)
     assert less < 3.0 * said, (said, less)
+
+
+@pytest.mark.parametrize("T,splits", [(1, 2), (1, 0), (9, 2), (70, 2)])
+def test_more_pages_than_any_list_holds(T, splits):
+    """Without a hint, in the smallest workspace: two parts, several full lists each."""
+    dream.dream_set_kv_splits(splits)
+    p = Hinted(2, 1, 64, T, [50000 if T == 1 else 30000 if T == 9 else 23000], 16, sparse=0.95, seed=T)
+    p.call(p.workspace() if not splits else dream.alloc_workspace(2 * 2 * T * 66 * 4).fill_(0xFF))
+    p.check()
