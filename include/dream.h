@@ -470,6 +470,7 @@ int dream_mx_verify_attn(const dream_attn_desc *desc, const void *q, const void 
  *                made then, and sums are added in another order.  A part is batch * n_q_heads * n_tree * (D + 2) * 4 bytes.  DREAM_ERR_WORKSPACE below that
  *   A node that sees nothing yields a zero row and lse = -inf.  What a node does not see does not change its row, whatever it holds:
  *   NaN and infinities too.  Values and scores that are not finite: as in dream_window_verify_attn.  batch * n_q_heads at most 2^20, q and out 16-byte aligned.
+ *   Calls whose launch would have 2^32 threads are DREAM_ERR_UNSUPPORTED; with batch * n_q_heads * n_tree at most 2^23 none has.
  *
  * dream_page_bounds: of every page that rows from_len[b] .. to_len[b] - 1 (from_len NULL: 0) lie in, the largest and the
  *   smallest of its keys' values in every channel, over the page's rows below to_len[b]:

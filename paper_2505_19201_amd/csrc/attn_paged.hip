@@ -1511,6 +1511,7 @@ enum Form { SINGLY, KEYS, ROWS };
 struct Shape {                            // of a launch's workgroups
     Form form;
     int qt, waves;                        // query tiles of a wave
+    int threads() const { return 64 * waves; }
     int cap() const { return form == SINGLY ? SINGLE_ROWS : form == KEYS ? 16 * qt : 16 * qt * waves; }
     int keys(int D) const { return form == SINGLY ? SINGLE_RUN : form == KEYS ? 32 * waves : D == 256 ? 32 : 64; }      // that a step of a workgroup takes
     bool operator==(const Shape &o) const { return form == o.form && qt == o.qt && waves == o.waves; }
@@ -1522,7 +1523,7 @@ struct Segment {
 struct PagedPlan {
     Segment shared, own;
     int n_slots, shared_slots, list_size;
-    int64_t all_rows;
+    int64_t all_rows, threads;            // threads: of the largest launch
     size_t bytes;
 };
 
@@ -1677,7 +1678,9 @@ PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32
     auto finish = [&](Segment &s, int64_t n_heads, int least) {
         s.part.splits = s.part.splits > least ? s.part.splits : least;
         s.part.streams = (int)(n_heads * s.part.splits);
-        s.part.blocks = ceil_div(s.part.streams, 8) * 8 * s.part.row_groups;
+        const int64_t blocks = (int64_t)ceil_div(s.part.streams, 8) * 8 * s.part.row_groups, threads = blocks * s.shape.threads();
+        s.part.blocks = (int)blocks;      // (where it does not fit, `threads` is refused)
+        p.threads += threads;             // (both parts' in one launch, or more than either's)
         s.part.row_groups_magic = magic_for(s.part.row_groups);
         s.part.splits_magic = magic_for(s.part.splits);
         s.part.slot = p.n_slots;
@@ -1707,6 +1710,8 @@ PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32
     p.list_size = sparse ? list_size_of(ceil_div(listed, p.own.part.splits), n_tree) : 0;
     p.all_rows = heads * rows;
     const bool several = sparse && !f32 && (int64_t)p.list_size * p.own.part.splits <= pages->max_pages;      // a workgroup may need several lists, and a slot for what they give (the page that the prefix ends in may be listed for the tree as well)
+    if (p.n_slots > 1 && p.threads < p.all_rows * (D / 4))
+        p.threads = p.all_rows * (D / 4);
     p.bytes = p.n_slots > 1 || several ? (size_t)p.n_slots * p.all_rows * (D + 2) * 4 : 0;
     return p;
 }
@@ -1843,6 +1848,8 @@ int run(const char *who, const dream_attn_desc *d, const dream_page_desc *pages,
         if (ws_bytes < p.bytes)
             return fail(DREAM_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, ws_bytes, needed);
     }
+    if (p.threads >= (1ll << 32) - 1024)      // (the join's last workgroup may be whole)
+        return fail(DREAM_ERR_UNSUPPORTED, "%s: a launch of %lld threads, 2^32 or more", who, (long long)p.threads);
     a.part_o = static_cast<float *>(ws);
     a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)p.n_slots * p.all_rows * d->head_dim);
     a.batch = d->batch; a.hq = d->n_q_heads; a.hkv = d->n_kv_heads; a.group = a.hq / a.hkv; a.rows = a.n_tree * a.group; a.words = (a.n_tree + 63) / 64;
