@@ -162,27 +162,26 @@ __global__ __launch_bounds__(256) void append_kernel(const int32_t *row_base, co
         return src + ((int64_t)blockIdx.x * (idx < a.end_q ? here(hq) : here(hkv)) + h) * D;
     };
     auto channel = [&](int it) { return PAIRED || it < turned ? it * N : it * N + half; };
-    auto request = [&](int first) {
+    // all of a thread's pieces are on their way before the position is known; BATCH of them are all there are (launch_append)
+    const int first = blockIdx.y * 256;
 #pragma unroll
-        for (int u = 0; u < BATCH; u++) {
-            const int idx = first + u * stride + tid;
-            if (idx < a.end_v) {
-                bool value;
-                int h, it;
-                const T *src = source(idx, value, h, it);
-                if constexpr (N == NV) {              // a value's piece is one that does not turn
-                    x[u].load(src + (value ? it * N : channel(it)));
-                } else if (value) {
-                    w[u].load(src + it * NV);
-                } else {
-                    x[u].load(src + channel(it));
-                }
-                if (!PAIRED && !value && it < turned)
-                    y[u].load(src + channel(it) + half);
+    for (int u = 0; u < BATCH; u++) {
+        const int idx = first + u * stride + tid;
+        if (idx < a.end_v) {
+            bool value;
+            int h, it;
+            const T *src = source(idx, value, h, it);
+            if constexpr (N == NV) {              // a value's piece is one that does not turn
+                x[u].load(src + (value ? it * N : channel(it)));
+            } else if (value) {
+                w[u].load(src + it * NV);
+            } else {
+                x[u].load(src + channel(it));
             }
+            if (!PAIRED && !value && it < turned)
+                y[u].load(src + channel(it) + half);
         }
-    };
-    request(blockIdx.y * 256);
+    }
     int64_t pos = start;
     if (walk) {
         int p = r;
@@ -210,45 +209,41 @@ __global__ __launch_bounds__(256) void append_kernel(const int32_t *row_base, co
     __syncthreads();
     const bool kept = page >= 0 && page < a.n_pages;
     const int64_t in_pool = (((int64_t)(kept ? page : 0) * hkv << lg_page) + (row & ((1 << lg_page) - 1))) * D;      // of head 0
-    for (int first = blockIdx.y * 256; first < a.end_v; first += stride * BATCH) {
-        if (first >= stride)
-            request(first);
 #pragma unroll
-        for (int u = 0; u < BATCH; u++) {
-            const int idx = first + u * stride + tid;
-            if (idx >= a.end_v || (idx >= a.end_q && !kept))
-                continue;
-            bool value;
-            int h, it;
-            source(idx, value, h, it);
-            T *dst = idx < a.end_q ? here(q_out) + ((int64_t)blockIdx.x * here(hq) + h) * D
-                                   : (value ? here(v_pages) : here(k_pages)) + in_pool + ((int64_t)h << lg_page) * D;
-            if (N != NV && value) {
-                w[u].store(dst + it * NV);
-                continue;
-            }
-            if (!value && it < turned) {
-                if constexpr (PAIRED) {
-#pragma unroll
-                    for (int i = 0; i < N; i += 2) {
-                        const float2 t = s_turn[it * (N / 2) + i / 2];
-                        const float p = x[u][i], q = x[u][i + 1];
-                        x[u].set(i, p * t.x - q * t.y, p * t.y + q * t.x);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < N; i += 2) {
-                        constexpr int SECOND = N > 1;
-                        const float2 t0 = s_turn[it * N + i], t1 = s_turn[it * N + i + SECOND];
-                        const float p0 = x[u][i], q0 = y[u][i], p1 = x[u][i + SECOND], q1 = y[u][i + SECOND];
-                        x[u].set(i, p0 * t0.x - q0 * t0.y, p1 * t1.x - q1 * t1.y);
-                        y[u].set(i, p0 * t0.y + q0 * t0.x, p1 * t1.y + q1 * t1.x);
-                    }
-                    y[u].store(dst + channel(it) + half);
-                }
-            }
-            x[u].store(dst + (value ? it * N : channel(it)));
+    for (int u = 0; u < BATCH; u++) {
+        const int idx = first + u * stride + tid;
+        if (idx >= a.end_v || (idx >= a.end_q && !kept))
+            continue;
+        bool value;
+        int h, it;
+        source(idx, value, h, it);
+        T *dst = idx < a.end_q ? here(q_out) + ((int64_t)blockIdx.x * here(hq) + h) * D
+                               : (value ? here(v_pages) : here(k_pages)) + in_pool + ((int64_t)h << lg_page) * D;
+        if (N != NV && value) {
+            w[u].store(dst + it * NV);
+            continue;
         }
+        if (!value && it < turned) {
+            if constexpr (PAIRED) {
+#pragma unroll
+                for (int i = 0; i < N; i += 2) {
+                    const float2 t = s_turn[it * (N / 2) + i / 2];
+                    const float p = x[u][i], q = x[u][i + 1];
+                    x[u].set(i, p * t.x - q * t.y, p * t.y + q * t.x);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; i += 2) {
+                    constexpr int SECOND = N > 1;
+                    const float2 t0 = s_turn[it * N + i], t1 = s_turn[it * N + i + SECOND];
+                    const float p0 = x[u][i], q0 = y[u][i], p1 = x[u][i + SECOND], q1 = y[u][i + SECOND];
+                    x[u].set(i, p0 * t0.x - q0 * t0.y, p1 * t1.x - q1 * t1.y);
+                    y[u].set(i, p0 * t0.y + q0 * t0.x, p1 * t1.y + q1 * t1.x);
+                }
+                y[u].store(dst + channel(it) + half);
+            }
+        }
+        x[u].store(dst + (value ? it * N : channel(it)));
     }
 }
 
@@ -257,7 +252,8 @@ int launch_append(const AppendArgs &a, bool paired, bool wide, int64_t rows, hip
 {
     constexpr int N = 16 / sizeof(T);
     auto *kernel = paired ? (wide ? &append_kernel<T, true, N> : &append_kernel<T, true, 2>) : wide ? &append_kernel<T, false, N> : &append_kernel<T, false, 1>;
-    const int64_t most = (a.end_v + 255) / 256, least = (a.end_v + 256 * BATCH - 1) / (256 * BATCH), parts = 1024 / rows > least ? 1024 / rows : least;      // no more than a thread has in flight (685 rows of 96 float32 heads of 128 18.2 -> 15.4 us)
+    // workgroups of a row: at least so many that a thread has all of its pieces in flight, parts * 256 * BATCH >= end_v, which append_kernel relies on (685 rows of 96 float32 heads of 128 18.2 -> 15.4 us)
+    const int64_t most = (a.end_v + 255) / 256, least = (a.end_v + 256 * BATCH - 1) / (256 * BATCH), parts = 1024 / rows > least ? 1024 / rows : least;
     hipLaunchKernelGGL(kernel, dim3((unsigned)rows, (unsigned)(parts < 1 ? 1 : parts < most ? parts : most)), dim3(256), 0, st, a.row_base, a.table,
                        a.pos_base, static_cast<const T *>(a.q), static_cast<const T *>(a.k), static_cast<const T *>(a.v), a.n_rows, a.rows_magic, a.max_pages, a.lg_page, a.hq, a.hkv, a.pieces_magic,
                        a.vpieces_magic, static_cast<T *>(a.q_out), static_cast<T *>(a.k_pages), static_cast<T *>(a.v_pages), a);
