@@ -456,7 +456,7 @@ int dream_mx_verify_attn(const dream_attn_desc *desc, const void *q, const void 
  *
  * dream_paged_commit: dream_kv_commit for pools, with its arguments and its result: row prefix_len[b] + j receives the old row
  *   prefix_len[b] + accept_path[b][j] for j = 0 .. accept_len[b], in every pool of pools_host (HOST array of n_pools DEVICE
- *   pointers).  DREAM_ERR_UNSUPPORTED if min(path_stride, n_tree) rows exceed 64 KB.
+ *   pointers, each pool once: they must not overlap).  DREAM_ERR_UNSUPPORTED if min(path_stride, n_tree) rows exceed 64 KB.
  *
  * dream_paged_verify_attn: dream_tree_verify_attn over pages (n_tree = 1 is plain decoding), where a prefix that sequences
  *   share is read once for all of them.
@@ -478,7 +478,7 @@ int dream_mx_verify_attn(const dream_attn_desc *desc, const void *q, const void 
  *                and -inf.  Other pages' bounds keep their content.  Sequences whose runs meet in a page must agree on its rows
  *   max_new      host-known upper bound of to_len - from_len; only used to choose the launch shape
  *
- * dream_page_select: which pages of its prefix each node is to see, for every KV head, by an upper bound of its scores there.
+ * dream_page_select: which pages of its prefix each node is to see, for every KV head, by a bound of what its queries, as they are rounded here, score there.
  *   With the queries of the Hq / Hkv heads of a KV head held as whole numbers c = rint(q / 2^f), f in [-100, 122] the least
  *   exponent at which none exceeds 127 (one for all the heads and channels), and the bounds of a page as u = ceil(largest / 2^e),
  *   w = floor(smallest / 2^e), e likewise (one for all the channels),

@@ -632,8 +632,9 @@ __device__ __forceinline__ float largest(f32x4 a) { return fmaxf(fmaxf(fmaxf(a[0
 // A weight goes into the second product as PIECES bf16 numbers, its value rounded and what that leaves: with two of them what is lost is 2^-16 of it, with one 2^-8, as much as the row's own rounding
 // (against 64 bits rows are off by 0.0017 and by 0.0023 of their size, root mean square).  Two where that costs little: bf16 weights in one part and in two, us a layer,
 //   keys, 128: one sequence, 60 nodes x 764 keys 12.2 and 12.4; 8 sequences, one node x 16 100 keys 86.1 and 86.1
-//   rows, 256: 16 sequences, one node x 8011 shared keys 31.2 and 32.0; selected pages, 4 x 33 nodes 66.9 and 70.0 (attention 44 of them)
-//   rows, 128: 8 x 60 nodes x 4096 shared keys 60.8 and 90.3 (the registers do not hold both), selected pages 86.5 and 94.3; 64: 32 x 33 nodes x 1600 shared keys 45.3 and 53.5; so one there
+//   rows, 256: 16 sequences, one node x 8011 shared keys 31.2 and 31.7; selected pages, 4 x 33 nodes 66.9 and 70.0 (attention 44 of them); 16 x 60 nodes x 2000 keys 72.8 and 78.0
+//   rows, 128: 64 rows a workgroup, 8 x 60 nodes x 1343 keys 30.8 and 35.5, selected pages 88.0 and 95.7; 128 rows, 8 x 60 nodes x 4096 shared keys 60.8 and 90.3 (the registers do not hold both)
+//   rows, 64: 32 x 33 nodes x 1600 shared keys 45.3 and 53.5; so one in the rows kernel below 256
 template <int D, int QT, int NC, bool SPARSE, int PIECES>
 struct QueryRows {
     static constexpr int ROW = 2 * D, NKS = D / 32, NDT = D / 16;
@@ -961,7 +962,7 @@ struct KeysGeom {
 
 // Few rows: the waves take the key tiles in turn, each for all of the rows, and never meet until the end.  A wave asks for its next keys as soon as a tile's scores are there, and for its next
 // values as soon as they are added up.  What bounds it: memory where caches are long (8 sequences of up to 16 100 rows, 8 KV heads of 128, one node: 439 MB in 84 us, 5.2 TB/s); where they are short, what a CU
-// pulls (75 to 87 KB a us) and the trips to memory ahead of the first scores and behind the last (one sequence, 60 nodes, 764 rows, 32 KV heads of 128: 12.3 us, of which a wave is in its tiles for 5).
+// pulls (75 to 87 KB a us) and the trips to memory ahead of the first scores and behind the last (one sequence, 60 nodes, 764 rows, 32 KV heads of 128: 12.4 us, of which a wave is in its tiles for 5).
 template <int D, int QT, int NW, bool SPARSE>
 __global__ __launch_bounds__(64 * NW) void paged_keys_kernel(PLAIN, PagedAttnArgs first)
 {
@@ -1534,6 +1535,8 @@ struct PagedPlan {
 // fastest in the geometric mean, 8 % at the 95th percentile, 39 % at most, on the data that they were fitted to.  What a shape is worth over these problems (mean and most that the fastest would take
 // longer without it): 16 rows 3.1 % and 24 %, 32 rows 0.5 % and 17 %, 64 rows 2.9 % and 54 %, 128 rows 0.9 % and 25 %, 128 rows of 256 on eight waves 0.1 % and 5 %; eight waves at
 // smaller head_dim (0.2 %) and four query tiles a wave are left out.
+// Two parts by the same constants, and calls over selected pages, measured afterwards: 27 problems with groups, every shape and split of both parts: 5.5 % behind the fastest in the geometric mean, 34 % at most
+// (12 % but for two problems of two KV heads of 256); 17 of selected pages: 2.2 % and 10 %.
 struct Kind {
     Shape shape;
     float base, per_group, latency, issue;
@@ -1567,7 +1570,7 @@ Load load_of(int D, const Problem &p, const Kind &k)
     const Shape &s = k.shape;
     const int64_t groups = row_groups_of(p, s), units = p.heads * (p.groups ? p.rows / s.cap() + 1 : groups);
     float keys = (float)p.keys;
-    if (p.nodes_of) {                     // nodes that ask alike see more pages together: measured about the 0.4th power of their number
+    if (p.nodes_of) {                     // nodes that ask alike see more pages together: two 1.26 to 1.42 times as many as one, 60 2.3 to 3.9 (2^0.33 to 2^0.51, 60^0.2 to 60^0.33)
         const float nodes = (float)(p.rows < s.cap() ? p.rows : s.cap()) / (float)p.nodes_of;
         keys *= nodes > 1.0f ? powf(nodes, 0.4f) : 1.0f;
         keys = keys < (float)p.all_keys ? keys : (float)p.all_keys;
@@ -1797,7 +1800,7 @@ int launch_all(PagedAttnArgs &a, const PagedPlan &p, bool f32, hipStream_t st)
     if (p.n_slots == 1)
         return DREAM_OK;
     auto join = [&](auto kernel) {
-        const int threads = p.all_rows * (D / 4) <= 64 * 1024 ? 64 : 256;      // few rows over all CUs (256 rows of 256, 24 parts: 7.2 -> 6.4 us; fewer parts: no difference)
+        const int threads = p.all_rows * (D / 4) <= 64 * 1024 ? 64 : 256;      // few rows over all CUs (256 rows of 256, 33 parts: 7.2 -> 6.5 us; fewer parts: no difference)
         hipLaunchKernelGGL(kernel, dim3(ceil_div(p.all_rows, threads / (D / 4))), dim3(threads), 0, st, a.part_o, a.part_ml, a.out, a.lse, (uint32_t)p.all_rows, p.n_slots, a.rows, a.rows_magic, a.hkv,
                            a.hkv_magic, a.group, a.group_magic, a.hq, a.n_tree);
     };

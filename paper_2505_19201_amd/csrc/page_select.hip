@@ -1,7 +1,7 @@
-// dream_page_select: which pages of its prefix each node sees, by an upper bound of its scores there.
+// dream_page_select: which pages of its prefix each node sees, by a bound of what its queries, as they are rounded here, score there.
 //
 // With a page's largest value U_d and smallest W_d in every channel, q . k <= sum_d max(q_d, 0) U_d + min(q_d, 0) W_d for each of its keys; summed over the query heads of a KV head that is one
-// number for a node, a KV head and a page.  Queries and bounds are held as whole numbers up to 127 times a power of two (queries to nearest, bounds rounded outwards, so that they stay bounds).
+// number for a node, a KV head and a page.  Queries and bounds are held as whole numbers up to 127 times a power of two (queries to nearest, bounds rounded outwards: the score bounds the products of the rounded queries).
 // Two reasons: the sums are whole numbers, so no order of adding them changes which page comes first, and the matrix instruction takes 8-bit numbers at four times the rate.  What is lost is a
 // step of 2^-7 of the largest value, of numbers that only rank pages.
 //

@@ -5,7 +5,7 @@
 // once and written once.
 // Commit.  The accepted path's rows move up, in all layers' pools by one launch: everything a workgroup moves is in registers before it writes any of it.  (40 pools of 8 heads of 128: 3.7 us, four
 // trips to memory.)
-// Bounds.  The largest and smallest value of each channel of a page: a page and head is one contiguous run of page_size * D values.  (A prompt's 39 MB in 10.3 us, 3.8 TB/s; a round's pages in 3.5.)
+// Bounds.  The largest and smallest value of each channel of a page: a page and head is one contiguous run of page_size * D values.  (A prompt's 39 MB in 10.2 us, 3.8 TB/s; a round's pages in 3.5.)
 #include <float.h>
 #include <type_traits>
 #include "paged.h"
