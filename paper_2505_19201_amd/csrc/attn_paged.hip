@@ -1683,7 +1683,8 @@ PagedPlan plan_for(const dream_attn_desc *d, const dream_page_desc *pages, int32
         s.part.streams = (int)(n_heads * s.part.splits);
         const int64_t blocks = (int64_t)ceil_div(s.part.streams, 8) * 8 * s.part.row_groups, threads = blocks * s.shape.threads();
         s.part.blocks = (int)blocks;      // (where it does not fit, `threads` is refused)
-        p.threads += threads;             // (both parts' in one launch, or more than either's)
+        const bool together = p.n_slots && p.shared.shape == s.shape;      // (one launch for the shared and the own part)
+        p.threads = together ? p.threads + threads : p.threads > threads ? p.threads : threads;
         s.part.row_groups_magic = magic_for(s.part.row_groups);
         s.part.splits_magic = magic_for(s.part.splits);
         s.part.slot = p.n_slots;
